@@ -443,7 +443,7 @@ def _handle(s, lib):
         if "q" in s:
             size = lib.cache_attention_workspace_bytes(s["cache"], s["n"], s["tokens"], s["hq"], s["max_len"])
         elif "max_keep" in s:
-            size = lib.cache_compact_workspace_bytes(s["cache"], s["n"], s["max_keep"])
+            size = lib.cache_compact_workspace_bytes(s["cache"], s["n"])
         s["ws_bytes"], s["ws"] = size, torch.empty(max(size, 1), dtype=torch.uint8, device="cuda")
     return s["cache"]
 
