@@ -303,6 +303,147 @@ PYR_API int pyr_decode_update(const void* q_win, const void* k, const void* v,
                       void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * A cache held in 4 bits, for the generation phase of many sequences: pages in device memory that the slots of a table share.
+ * K and V of a token are stored as 4-bit floating-point numbers (e2m1: a sign and 0, 0.5, 1, 1.5, 2, 3, 4 or 6) times a power of two per 32
+ * channels of a head (one byte, 2^(byte - 127); 255: not a number) - 34 bytes for 32 channels of K and V, 4.25 bits a number against
+ * bf16's 16.  A block's power of two is the smallest that brings its largest magnitude to 7 or less (7 is rounded to 6), between 2^-126 and 2^125; numbers are
+ * rounded to the nearest, ties to the even code; a block with an infinity or a NaN is stored as NaN as a whole.
+ *
+ * A slot is a sequence: lens[slot] tokens, in pages table[slot][0 .. ceil(lens / page_tokens) - 1], the last one filled in part.  refs[page] says how
+ * many slots hold a page; 0 is a free one.  Full pages may be shared (pyr_cache_fork), a page filled in part never is, so storing behind the last
+ * token touches no other slot.  An empty cache: refs and lens 0 (the table and the pages may hold anything).
+ * All of it lives in device memory that the caller owns and may be read between calls; no call waits for the device, and every call
+ * can be captured into a graph and replayed, the sequences growing from replay to replay.  Calls that change one cache, and calls that read it,
+ * are ordered by the caller (one stream, or events).
+ *
+ * What is on the device is checked there: a slot of -1 is a row of a padded batch and skipped; pages outside the pool and slots outside the table are never
+ * followed (what each call does then is said there).  The calls that hand out or share pages write a status to device memory:
+ *   0   done
+ *   n > 0   n pages are lacking: nothing was changed
+ *   PYR_CACHE_BAD_SLOT    a slot outside the table (other than -1) or named twice, a child that holds tokens or is a parent: nothing was changed
+ *   PYR_CACHE_BAD_COUNT   a count below 0, or more tokens than a row of the table or the call's limit holds: nothing was changed
+ * (the lower one if both apply).  Pages are handed out from the lowest, in the order of the rows.
+ *
+ * Layout, for programs that read or write pages themselves: a page is [n_kv_heads][page_tokens / 32] tiles of 34 * d bytes, a tile
+ * being 32 tokens of one head; with nb = d / 32, in this order
+ *   16 d bytes  K's codes   [half 2][block nb][token 16][byte 16]: token 16 * half + token, channel 32 * block + 2 * byte (low four bits) and the next
+ *   16 d bytes  V's codes   [h d/64][j 4][r 16][p 2][q 2][byte 4]: channel 64 h + 32 p + 2 r + q, token 16 * (byte / 2) + 4 j + 2 * (byte % 2) and the next
+ *      d bytes  K's scales  [block nb][token 16][half 2]
+ *      d bytes  V's scales  [j 4][block nb][half 2][s 4]: token 16 * half + 4 j + s
+ *
+ * Host checks of every call: PYR_ERR_NULL; PYR_ERR_SHAPE (negative sizes; n_slots > PYR_CACHE_MAX_SLOTS; n > PYR_CACHE_MAX_ROWS where pages are handed out or shared);
+ * PYR_ERR_UNSUPPORTED (head_dim not 64 or 128, page_tokens not a power of two from 32 to 1024, pages not 256-byte aligned, rows not 16-byte aligned,
+ * 2^31 or more tokens in the pool, a row of the table or a batch); PYR_ERR_WORKSPACE; PYR_ERR_LAUNCH.
+ */
+#define PYR_CACHE_MAX_ROWS 4096
+#define PYR_CACHE_MAX_SLOTS 262144
+#define PYR_CACHE_BAD_SLOT (-1)
+#define PYR_CACHE_BAD_COUNT (-2)
+
+typedef struct pyr_cache {
+    void* pages;          /* dev [n_pages] pages of pyr_cache_page_bytes() bytes, 256-byte aligned   */
+    int32_t* refs;        /* dev int32 [n_pages]                                                     */
+    int32_t* table;       /* dev int32 [n_slots, max_pages]                                          */
+    int32_t* lens;        /* dev int32 [n_slots]                                                     */
+    int32_t n_pages;
+    int32_t page_tokens;  /* 32, 64, ... 1024                                                        */
+    int32_t n_slots;
+    int32_t max_pages;    /* of a slot                                                               */
+    int32_t n_kv_heads;
+    int32_t head_dim;
+} pyr_cache;
+
+/* Host only.  Bytes of a page; reads page_tokens, n_kv_heads and head_dim of the cache. */
+PYR_API int pyr_cache_page_bytes(const pyr_cache* cache, size_t* bytes_out);
+
+/*
+ * Room for n_new[i] more tokens in slots[i] (i < n), and their place: start[i] = lens[slots[i]], lens[slots[i]] += n_new[i], pages as needed.
+ *   slots, n_new       dev int32 [n]
+ *   start              dev int32 [n], written: the place of the first new token, what pyr_cache_store takes; -1 for a
+ *                      skipped row, and for all rows if the status is not 0
+ *   status             dev int32 [1], written
+ */
+PYR_API int pyr_cache_reserve(const pyr_cache* cache, const int32_t* slots, const int32_t* n_new, int32_t n,
+                      int32_t* start, int32_t* status, void* stream);
+
+/*
+ * children[i] becomes a copy of parents[i]: full pages are shared, of a page filled in part the tokens are copied into a fresh one.  Several children
+ * may have one parent.  A row is skipped if both are -1.
+ *   parents, children  dev int32 [n]; children are empty slots
+ *   status             dev int32 [1], written
+ */
+PYR_API int pyr_cache_fork(const pyr_cache* cache, const int32_t* parents, const int32_t* children, int32_t n,
+                   int32_t* status, void* stream);
+
+/*
+ * Slots are emptied: their pages' counts go down (0: free), their entries of the table become -1, lens 0.  A slot named twice is
+ * emptied once; slots outside the table are skipped.
+ *   slots              dev int32 [n]
+ */
+PYR_API int pyr_cache_release(const pyr_cache* cache, const int32_t* slots, int32_t n, void* stream);
+
+/*
+ * Slots are cut to the tokens that a selection kept (Gather(KV, index) without leaving 4 bits): token j of slots[i] becomes its token
+ * kept_idx[out_offsets[i] + j] - seq_offsets[i], j < out_offsets[i+1] - out_offsets[i], its bits unchanged.  Indexes as pyr_select and pyr_decode_update write
+ * them, seq_offsets as the batch they ran on (lens[slots[i]] rows each); any order and repetitions are fine.
+ * The tokens go into fresh pages, then the old ones are given back: the pool needs room for both.  A slot that shares pages leaves the others as they are.
+ *   slots              dev int32 [n]
+ *   kept_idx           dev int32 [n_kept]; an index outside the slot's tokens gives a token of NaN
+ *   seq_offsets        dev int32 [n] or more;  out_offsets  dev int32 [n+1], within 0 .. n_kept
+ *   max_keep           no out_offsets[i+1] - out_offsets[i] is larger
+ *   status             dev int32 [1], written
+ *   workspace          dev, >= pyr_cache_compact_workspace_bytes(), 256-byte aligned
+ */
+PYR_API int pyr_cache_compact_workspace_bytes(const pyr_cache* cache, int32_t n, size_t* bytes_out);
+PYR_API int pyr_cache_compact(const pyr_cache* cache, const int32_t* slots, int32_t n, const int32_t* kept_idx, int32_t n_kept,
+                      const int32_t* seq_offsets, const int32_t* out_offsets, int32_t max_keep, int32_t* status,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Rows of K and V into the cache: token start[i] + j of slots[i] becomes row offsets[i] + j, or row row_idx[offsets[i] + j],
+ * j < offsets[i+1] - offsets[i].  Rows of a prompt's selection go in straight from the layer's K and V: row_idx = kept_idx, offsets = out_offsets.
+ *   k, v               dev bf16 [n_rows, Hkv, d]
+ *   row_idx            dev int32 [n_list] or NULL (then n_list = n_rows)
+ *   offsets            dev int32 [n+1];  slots, start  dev int32 [n]
+ *   max_new            no offsets[i+1] - offsets[i] is larger (tokens beyond it are not stored, or some of them)
+ * Tokens that have no page, a start of -1 (pyr_cache_reserve found no room) and rows outside k and v are not stored; nothing else in the pages
+ * changes.  Two rows of a call must not store the same tokens.
+ */
+PYR_API int pyr_cache_store(const pyr_cache* cache, const void* k, const void* v, int32_t n_rows, const int32_t* row_idx, int32_t n_list,
+                    const int32_t* offsets, const int32_t* slots, const int32_t* start, int32_t n, int32_t max_new, void* stream);
+
+/*
+ * The cache as bf16 rows (exactly: every number of the cache is one of bf16's), packed as pyr_decode_update and pyr_score read them: row
+ * offsets[i] + j is token j of slots[i], j < min(lens[slots[i]], offsets[i+1] - offsets[i], max_len).  Rows that no token goes to stay as they were.
+ *   offsets            dev int32 [n+1];  slots  dev int32 [n]
+ *   k_out, v_out       dev bf16 [n_rows, Hkv, d]; one of them may be NULL; rows from n_rows on are not written
+ */
+PYR_API int pyr_cache_load(const pyr_cache* cache, const int32_t* slots, const int32_t* offsets, int32_t n, int32_t max_len,
+                   void* k_out, void* v_out, int32_t n_rows, void* stream);
+
+/*
+ * Attention of each sequence's newest n_tokens tokens over its cache, theirs included (store them first): token i of slots[b] sees the tokens
+ * 0 .. lens[slots[b]] - n_tokens + i.
+ *   out[b,i,h,:] = sum_t softmax_t(scale * q[b,i,h,:].k[t,h/g,:]) v[t,h/g,:]
+ * bf16 MFMA products on the cache's exact values (P times V's power of two is rounded to bf16), fp32 accumulation and softmax.
+ *   q                  dev bf16 [n, n_tokens, Hq, d]
+ *   slots              dev int32 [n]
+ *   max_len            about the longest sequence (it decides how the work is cut up and how large the workspace is, not the result: longer
+ *                      ones are right as well); a captured graph takes one for the lengths to come
+ *   softmax_scale      <= 0 selects 1/sqrt(d)
+ *   out                dev bf16 [n, n_tokens, Hq, d], written
+ *   lse                dev fp32 [n, n_tokens, Hq], written, as pyr_attention's; may be NULL
+ *   workspace          dev, >= pyr_cache_attention_workspace_bytes(), 256-byte aligned; not read where that is 0
+ * A token that sees nothing (an empty slot, a skipped row, fewer tokens in the cache than n_tokens): zeros in out, -inf in lse.  A page outside the pool: NaN.
+ * One launch, and one that adds up partial results where few long sequences are split.
+ */
+PYR_API int pyr_cache_attention_workspace_bytes(const pyr_cache* cache, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len,
+                                        size_t* bytes_out);
+PYR_API int pyr_cache_attention(const pyr_cache* cache, const void* q, const int32_t* slots, int32_t n, int32_t n_tokens, int32_t n_q_heads,
+                        int32_t max_len, float softmax_scale, void* out, float* lse,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Diagnostic for the benchmark report, not part of the method: a launch of nothing but bf16 MFMAs
  * (v_mfma_f32_32x32x16_bf16 back to back, two wavefronts per SIMD, every compute unit), so that the
  * rate this very GPU sustains can be printed beside the published peak.

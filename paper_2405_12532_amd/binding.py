@@ -30,6 +30,11 @@ class PyrLaunches(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("attention_chunk", "attention_units", "stats_order", "window_order", "sums", "select_split")]
 
 
+class PyrCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("pages", "refs", "table", "lens")] + [(n, ctypes.c_int32) for n in (
+        "n_pages", "page_tokens", "n_slots", "max_pages", "n_kv_heads", "head_dim")]
+
+
 class PyrError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -68,6 +73,16 @@ _SIGNATURES = {
     "pyr_diag_launches": (ctypes.c_int, [ctypes.POINTER(PyrShape), _VP, _I32, _I32, _VP, _I64, _I32, _I32, ctypes.POINTER(PyrLaunches)]),
     "pyr_diag_layer": (ctypes.c_int, [ctypes.POINTER(PyrShape), _VP, _I32, _I32, _I32, ctypes.POINTER(_I32)]),
     "pyr_diag_update": (ctypes.c_int, [ctypes.POINTER(PyrShape), _VP, _I32, _I32, _I32, ctypes.POINTER(_I32)]),
+    "pyr_cache_page_bytes": (ctypes.c_int, [ctypes.POINTER(PyrCache), ctypes.POINTER(_SZ)]),
+    "pyr_cache_reserve": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _VP, _VP, _VP]),
+    "pyr_cache_fork": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _VP, _VP]),
+    "pyr_cache_release": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _I32, _VP]),
+    "pyr_cache_compact_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(PyrCache), _I32, ctypes.POINTER(_SZ)]),
+    "pyr_cache_compact": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _I32, _VP, _I32, _VP, _VP, _I32, _VP, _VP, _SZ, _VP]),
+    "pyr_cache_store": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _VP, _I32, _VP, _VP, _VP, _I32, _I32, _VP]),
+    "pyr_cache_load": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _I32, _VP, _VP, _I32, _VP]),
+    "pyr_cache_attention_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(PyrCache), _I32, _I32, _I32, _I32, ctypes.POINTER(_SZ)]),
+    "pyr_cache_attention": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _I32, _I32, _I32, _F32, _VP, _VP, _VP, _SZ, _VP]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -295,6 +310,69 @@ def decode_update(q_win, k, v, seq_offsets_dev, seq_offsets_host, shape, w, soft
                                     _ptr(keep_len_host), _ptr(row_weights_dev), _ptr(pos), _ptr(scores), _ptr(kept_idx),
                                     _ptr(out_offsets_dev), _ptr(k_out), _ptr(v_out), _ptr(pos_out), _ptr(workspace),
                                     int(workspace_bytes_), _stream(stream)), "pyr_decode_update")
+
+
+# ----------------------------------------------------------------------------- the cache held in 4 bits
+def make_cache(pages, refs, table, lens, page_tokens: int, n_kv_heads: int, head_dim: int) -> PyrCache:
+    """The description of a cache that the calls below take.  pages: uint8, whole pages (cache_page_bytes); refs int32 [n_pages], table int32
+    [n_slots, max_pages], lens int32 [n_slots].  It keeps the tensors alive."""
+    cache = PyrCache(_ptr(pages), _ptr(refs), _ptr(table), _ptr(lens), refs.shape[0], int(page_tokens), table.shape[0], table.shape[1],
+                     int(n_kv_heads), int(head_dim))
+    cache.tensors = (pages, refs, table, lens)
+    return cache
+
+
+def cache_page_bytes(page_tokens: int, n_kv_heads: int, head_dim: int) -> int:
+    out, cache = _SZ(0), PyrCache(page_tokens=int(page_tokens), n_kv_heads=int(n_kv_heads), head_dim=int(head_dim))
+    _check(load().pyr_cache_page_bytes(ctypes.byref(cache), ctypes.byref(out)), "pyr_cache_page_bytes")
+    return int(out.value)
+
+
+def cache_reserve(cache, slots, n_new, n, start, status, stream=None):
+    _check(load().pyr_cache_reserve(ctypes.byref(cache), _ptr(slots), _ptr(n_new), int(n), _ptr(start), _ptr(status), _stream(stream)),
+           "pyr_cache_reserve")
+
+
+def cache_fork(cache, parents, children, n, status, stream=None):
+    _check(load().pyr_cache_fork(ctypes.byref(cache), _ptr(parents), _ptr(children), int(n), _ptr(status), _stream(stream)), "pyr_cache_fork")
+
+
+def cache_release(cache, slots, n, stream=None):
+    _check(load().pyr_cache_release(ctypes.byref(cache), _ptr(slots), int(n), _stream(stream)), "pyr_cache_release")
+
+
+def cache_compact_workspace_bytes(cache, n) -> int:
+    out = _SZ(0)
+    _check(load().pyr_cache_compact_workspace_bytes(ctypes.byref(cache), int(n), ctypes.byref(out)), "pyr_cache_compact_workspace_bytes")
+    return int(out.value)
+
+
+def cache_compact(cache, slots, n, kept_idx, n_kept, seq_offsets, out_offsets, max_keep, status, workspace, workspace_bytes_, stream=None):
+    _check(load().pyr_cache_compact(ctypes.byref(cache), _ptr(slots), int(n), _ptr(kept_idx), int(n_kept), _ptr(seq_offsets), _ptr(out_offsets),
+                                    int(max_keep), _ptr(status), _ptr(workspace), int(workspace_bytes_), _stream(stream)), "pyr_cache_compact")
+
+
+def cache_store(cache, k, v, n_rows, row_idx, n_list, offsets, slots, start, n, max_new, stream=None):
+    _check(load().pyr_cache_store(ctypes.byref(cache), _ptr(k), _ptr(v), int(n_rows), _ptr(row_idx), int(n_list), _ptr(offsets), _ptr(slots),
+                                  _ptr(start), int(n), int(max_new), _stream(stream)), "pyr_cache_store")
+
+
+def cache_load(cache, slots, offsets, n, max_len, k_out, v_out, n_rows, stream=None):
+    _check(load().pyr_cache_load(ctypes.byref(cache), _ptr(slots), _ptr(offsets), int(n), int(max_len), _ptr(k_out), _ptr(v_out), int(n_rows),
+                                 _stream(stream)), "pyr_cache_load")
+
+
+def cache_attention_workspace_bytes(cache, n, n_tokens, n_q_heads, max_len) -> int:
+    out = _SZ(0)
+    _check(load().pyr_cache_attention_workspace_bytes(ctypes.byref(cache), int(n), int(n_tokens), int(n_q_heads), int(max_len), ctypes.byref(out)),
+           "pyr_cache_attention_workspace_bytes")
+    return int(out.value)
+
+
+def cache_attention(cache, q, slots, n, n_tokens, n_q_heads, max_len, softmax_scale, out, lse, workspace, workspace_bytes_, stream=None):
+    _check(load().pyr_cache_attention(ctypes.byref(cache), _ptr(q), _ptr(slots), int(n), int(n_tokens), int(n_q_heads), int(max_len),
+                                      float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace), int(workspace_bytes_), _stream(stream)),
+           "pyr_cache_attention")
 
 
 # ----------------------------------------------------------------------------- convenience for tests / smoke

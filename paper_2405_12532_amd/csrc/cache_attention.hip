@@ -1,0 +1,370 @@
+// Attention of a sequence's newest tokens over its cache held in 4 bits (Section 4.1, generation phase: the step that every generated token
+// takes between two updates of the cache):
+//   out[b,i,h,:] = sum_t softmax_t(scale * q[b,i,h,:] . k[t,h/g,:]) v[t,h/g,:],   t < len_b - n + 1 + i,  n tokens a sequence.
+//
+// One pass over the cache with the running reference and sum of a softmax.  A wavefront takes tiles of 32 tokens of one KV head and up to 16 * NT
+// query rows (tokens x query heads of the group) as the columns of the products
+//   S^T = K Q^T      16 tokens x 16 rows, contracted over 32 channels a step, K converted to bf16 (exactly) with its scale
+//   O^T = V^T P^T    16 channels x 16 rows, contracted over the 32 tokens.  V's codes are converted without their scale, which depends on the
+//                    token and the block of 32 channels: it is a factor of P instead, P' = P * 2^e per block, rounded to bf16 (as P is in pyr_attention)
+// and the layout of the tile makes every operand what a lane loads or has computed: nothing passes through LDS but the wavefronts' results at
+// the end.  The reference of a row is the largest logit when it was last moved; it is moved when a logit outgrows it by 2^12, so that most tiles
+// neither look for the maximum across lanes nor rescale.  P, its sum and O are fp32.
+//
+// Bound: reading the cache.
+#include <float.h>
+#include <math.h>
+
+#include "cache_device.h"
+
+namespace pyr {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr float kGrowth = 12.f;                   // how far (log2) a row may outgrow its reference
+
+struct AttendArgs {
+    CacheView c;
+    const uint16_t* q;
+    const int32_t* slots;
+    void* out;                                    // splits == 1: bf16 [n, tokens, Hq, D]; else fp32 [splits, rows, D], not normalised
+    float* lse;                                   // splits == 1: [rows] or NULL; else [splits, rows, 2]: reference and sum
+    int32_t n_seqs, n_tokens, n_q_heads;
+    int32_t chunk;                                // tiles of a split (the last one takes what is left)
+    int32_t splits;
+    float scale;                                  // softmax scale * log2(e)
+};
+static_assert(sizeof(AttendArgs) <= 112, "short arguments");
+
+// What a wavefront holds of a tile.
+template <int D>
+struct Tile {
+    u32x4 k[D / 64], v[D / 64], vs[D / 64];
+    uint32_t ks;
+};
+
+template <int D>
+__device__ __forceinline__ void load_tile(Tile<D>& t, const uint8_t* tile, int lane) {
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) t.k[h] = *(const u32x4*)(tile + h * 1024 + lane * 16);
+    if (D == 128) t.ks = *(const uint16_t*)(tile + 32 * D + lane * 2);
+    else t.ks = tile[32 * D + (lane & 31) * 2 + (lane >> 5)];
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) t.v[h] = *(const u32x4*)(tile + 16 * D + h * 1024 + lane * 16);
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) t.vs[h] = *(const u32x4*)(tile + 33 * D + (lane >> 4) * (D / 4) + h * 16);
+}
+
+__device__ __forceinline__ float max_of_groups(float x) {      // over the lanes with the same lane & 15
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_of_groups(float x) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+template <int D, int NT>
+struct Rows {
+    bf16x8 q[NT][D / 32];                         // operand of step s: lane 16 j + col, see load_rows
+    f32x4 o[NT][D / 16];
+    float m[NT], l[NT];                           // reference; sum over the tokens that this lane sees
+    int32_t seen[NT];                             // tokens that the row of this lane's column sees
+};
+
+// One tile's products.  kMasked: some row does not see all of its tokens.
+template <int D, int NT, bool kMasked>
+__device__ __forceinline__ void attend_tile(Rows<D, NT>& w, const Tile<D>& t, int first_token, float scale, int lane) {
+    constexpr int kSteps = D / 32;
+    const int j = lane >> 4;
+    f32x4 s[NT][2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        uint32_t codes[kSteps];
+        float ks;
+        if constexpr (D == 128) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) codes[i] = t.k[half][i];
+            ks = scale_of(half == 0 ? t.ks & 255 : t.ks >> 8);
+        } else {
+            // (a lane of the lower half holds 32 channels of token t, one of the upper half of token 16 + t: the upper lanes take over 16 channels
+            //  of the lower ones' blocks, and the other way round)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) codes[i] = __builtin_amdgcn_permlane32_swap(t.k[0][i], t.k[0][i + 2], false, false)[half];
+            ks = scale_of(__builtin_amdgcn_permlane32_swap(t.ks, t.ks, false, false)[half]);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s[n][half] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const bf16x8 k = values_of(codes[i], ks);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) s[n][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, w.q[n][i], s[n][half], 0, 0, 0);
+        }
+    }
+    float p[NT][8];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            p[n][e] = s[n][e >> 2][e & 3];
+            if (kMasked && first_token + 16 * (e >> 2) + 4 * j + (e & 3) >= w.seen[n]) p[n][e] = -INFINITY;
+        }
+        float top = p[n][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, p[n][e]);
+        top *= scale;
+        if (__builtin_amdgcn_ballot_w64(top > w.m[n] + kGrowth) != 0) {
+            const float m = fmaxf(w.m[n], max_of_groups(top));
+            const float f = __builtin_amdgcn_exp2f(w.m[n] - m);
+            w.m[n] = m;
+            w.l[n] *= f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) w.o[n][i] *= f;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            p[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][e], scale, -w.m[n]));
+            w.l[n] += p[n][e];
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b) {
+        float vs[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vs[e] = scale_of((t.vs[b >> 1][(b & 1) * 2 + (e >> 2)] >> (8 * (e & 3))) & 255);
+        const bf16x8 v0 = values_of(t.v[b >> 1][(b & 1) * 2], 1.f), v1 = values_of(t.v[b >> 1][(b & 1) * 2 + 1], 1.f);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            bf16x8 ps;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float x = p[n][e] * vs[e];
+                // (a token that a row does not see may have any scale byte, NaN among them)
+                if (kMasked && first_token + 16 * (e >> 2) + 4 * j + (e & 3) >= w.seen[n]) x = 0.f;
+                ps[e] = (__bf16)x;
+            }
+            w.o[n][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, ps, w.o[n][2 * b], 0, 0, 0);
+            w.o[n][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, ps, w.o[n][2 * b + 1], 0, 0, 0);
+        }
+    }
+}
+
+template <int D, int NT>
+__global__ __launch_bounds__(64 * kWaves) void cache_attention_kernel(AttendArgs a) {
+    constexpr int kRow = D + 4;                   // floats of a row in LDS
+    __shared__ __align__(16) float results[kWaves][16][kRow];
+    __shared__ float stats[kWaves][NT][16][2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane >> 4;
+    const int hkv = a.c.n_kv_heads, g = a.n_q_heads / hkv, cols = a.n_tokens * g;
+    // workgroup -> (sequence, split, column group, head): neighbours read neighbouring heads of the same pages
+    const int col_groups = (cols + 16 * NT - 1) / (16 * NT);
+    int id = blockIdx.x;
+    const int head = id % hkv;
+    id /= hkv;
+    const int first_col = (id % col_groups) * (16 * NT);
+    id /= col_groups;
+    const int split = id % a.splits, b = id / a.splits;
+
+    const int slot = cache_slot(a.c, a.slots, b);
+    const int len = slot < 0 ? 0 : cache_len(a.c, slot);
+    const int tiles = (len + 31) >> 5;
+    const int begin = split * a.chunk;
+    const int end = split == a.splits - 1 ? tiles : min(tiles, begin + a.chunk);
+    if (a.splits > 1 && begin >= end && split > 0) return;           // (the join does not look at it)
+
+    Rows<D, NT> w;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int col = first_col + 16 * n + (lane & 15);
+        const int token = col / g;
+        w.seen[n] = len - a.n_tokens + 1 + token;
+        w.m[n] = -FLT_MAX;
+        w.l[n] = 0.f;
+        const uint16_t* row = a.q + (((int64_t)b * a.n_tokens + token) * a.n_q_heads + head * g + (col - token * g)) * D;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            const int channel = D == 128 ? 32 * j + 8 * i : 32 * (j & 1) + 8 * (i + 2 * (j >> 1));
+            w.q[n][i] = col < cols ? *(const bf16x8*)(row + channel) : bf16x8{};
+        }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) w.o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int all_see = len - a.n_tokens + 1;                        // tokens below it are seen by every row
+
+    // the wavefront's tiles: begin + wave, + kWaves, ...; lane l holds the page of the l-th of 64
+    const int32_t* row_pages = a.c.table + (int64_t)max(slot, 0) * a.c.max_pages;
+    const int tile_shift = a.c.shift - 5;
+    bool bad = false;
+    int pages = 0;
+    const int count = max(0, (end - begin - wave + kWaves - 1) / kWaves);
+    auto fetch = [&](Tile<D>& t, int i) {                            // (i goes up by one from call to call)
+        if (i >= count) return;
+        if ((i & 63) == 0) {
+            const int mine = begin + wave + (i + lane) * kWaves;
+            pages = mine < end ? row_pages[mine >> tile_shift] : 0;
+            bad |= __builtin_amdgcn_ballot_w64(pages < 0 || pages >= a.c.n_pages) != 0;
+            if (pages < 0 || pages >= a.c.n_pages) pages = 0;
+        }
+        const int page = __builtin_amdgcn_readlane(pages, i & 63);
+        const int tile = begin + wave + i * kWaves;
+        load_tile<D>(t, cache_tile<D>(a.c, page, head, tile & ((1 << tile_shift) - 1)), lane);
+    };
+    auto attend = [&](const Tile<D>& t, int i) {
+        const int token = (begin + wave + i * kWaves) * 32;
+        if (token + 32 <= all_see) attend_tile<D, NT, false>(w, t, token, a.scale, lane);
+        else attend_tile<D, NT, true>(w, t, token, a.scale, lane);
+    };
+    Tile<D> t0, t1;
+    fetch(t0, 0);
+    fetch(t1, 1);
+    for (int i = 0; i < count; i += 2) {
+        attend(t0, i);
+        fetch(t0, i + 2);
+        if (i + 1 < count) {
+            attend(t1, i + 1);
+            fetch(t1, i + 3);
+        }
+    }
+
+    // the wavefronts' results: references and sums first, then the rows, weighted by 2^(reference - largest)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        w.l[n] = bad ? NAN : sum_of_groups(w.l[n]);
+        if (j == 0) {
+            stats[wave][n][lane & 15][0] = w.m[n];
+            stats[wave][n][lane & 15][1] = w.l[n];
+        }
+    }
+    const int64_t rows = (int64_t)a.n_seqs * a.n_tokens * a.n_q_heads;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int p = 0; p < D / 32; ++p) {
+            // rows 4 j + r of products 2 p and 2 p + 1 are channels 32 p + 2 (4 j + r) and the next
+            float* to = &results[wave][lane & 15][32 * p + 8 * j];
+            const f32x4 x = w.o[n][2 * p], y = w.o[n][2 * p + 1];
+            *(f32x4*)to = f32x4{x[0], y[0], x[1], y[1]};
+            *(f32x4*)(to + 4) = f32x4{x[2], y[2], x[3], y[3]};
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 16 * (D / 4); i += 64 * kWaves) {
+            const int r = i / (D / 4), c4 = i % (D / 4);
+            const int col = first_col + 16 * n + r;
+            if (col >= cols) continue;
+            float top = stats[0][n][r][0], sum = 0.f;
+#pragma unroll
+            for (int v = 1; v < kWaves; ++v) top = fmaxf(top, stats[v][n][r][0]);
+            f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int v = 0; v < kWaves; ++v) {
+                const float f = __builtin_amdgcn_exp2f(stats[v][n][r][0] - top);
+                sum += f * stats[v][n][r][1];
+                o += f * *(const f32x4*)&results[v][r][4 * c4];
+            }
+            const int token = col / g;
+            const int64_t at = ((int64_t)b * a.n_tokens + token) * a.n_q_heads + head * g + (col - token * g);
+            if (a.splits == 1) {
+                const float f = sum == 0.f ? 0.f : 1.f / sum;
+                bf16x4 y;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) y[x] = (__bf16)(o[x] * f);
+                *(bf16x4*)((uint16_t*)a.out + at * D + 4 * c4) = y;
+                if (a.lse != nullptr && c4 == 0) a.lse[at] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+            } else {
+                const int64_t part = split * rows + at;
+                *(f32x4*)((float*)a.out + part * D + 4 * c4) = o;
+                if (c4 == 0) {
+                    a.lse[2 * part] = top;
+                    a.lse[2 * part + 1] = sum;
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// The splits of a row, weighted by 2^(reference - largest) and added up: one wavefront a row.
+template <int D>
+__global__ __launch_bounds__(256) void cache_join_kernel(CacheView c, const int32_t* __restrict__ slots, const float* __restrict__ parts,
+                                                         const float* __restrict__ stats, uint16_t* __restrict__ out, float* __restrict__ lse,
+                                                         int64_t rows, int rows_of_seq, int chunk, int splits) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    const int slot = cache_slot(c, slots, (int)(row / rows_of_seq));
+    const int tiles = slot < 0 ? 0 : (cache_len(c, slot) + 31) >> 5;
+    const int live = min(splits, max(1, (tiles + chunk - 1) / chunk));
+    float top = -FLT_MAX;
+    for (int s = lane; s < live; s += 64) top = fmaxf(top, stats[2 * (s * rows + row)]);
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    float sum = 0.f;
+    float o[D / 64] = {};
+    for (int s = 0; s < live; ++s) {
+        const int64_t at = s * rows + row;
+        const float f = __builtin_amdgcn_exp2f(stats[2 * at] - top);
+        sum += f * stats[2 * at + 1];
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) o[x] += f * parts[at * D + (D / 64) * lane + x];
+    }
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    if (D == 128) *(bf16x2*)(out + row * D + 2 * lane) = bf16x2{(__bf16)(o[0] * f), (__bf16)(o[D / 64 - 1] * f)};
+    else *(__bf16*)(out + row * D + lane) = (__bf16)(o[0] * f);
+    if (lse != nullptr && lane == 0) lse[row] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+}
+
+template <int D>
+int launch(const CacheAttention& x, const CacheView& c, const AttendArgs& a, void* out, float* lse, hipStream_t stream) {
+    const int64_t grid = (int64_t)a.n_seqs * a.splits * x.col_groups * c.n_kv_heads;
+    if (x.col_tiles == 1) hipLaunchKernelGGL((cache_attention_kernel<D, 1>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
+    else if (x.col_tiles == 2) hipLaunchKernelGGL((cache_attention_kernel<D, 2>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
+    else hipLaunchKernelGGL((cache_attention_kernel<D, 4>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
+    int rc = check_launch();
+    if (rc != PYR_OK || a.splits == 1) return rc;
+    const int rows_of_seq = a.n_tokens * a.n_q_heads;
+    const int64_t rows = (int64_t)a.n_seqs * rows_of_seq;
+    hipLaunchKernelGGL(cache_join_kernel<D>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, c, a.slots, (const float*)a.out, (const float*)a.lse,
+                       (uint16_t*)out, lse, rows, rows_of_seq, a.chunk, a.splits);
+    return check_launch();
+}
+
+}  // namespace
+
+CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_len) {
+    CacheAttention x{};
+    const int cols = n_tokens * (n_q_heads / n_kv_heads);
+    const int tiles = (cols + 15) / 16;
+    x.col_tiles = tiles == 1 ? 1 : tiles == 2 ? 2 : 4;
+    x.col_groups = (tiles + x.col_tiles - 1) / x.col_tiles;
+    const int64_t units = (int64_t)n_seqs * n_kv_heads * x.col_groups, key_tiles = (max_len + 31) / 32;
+    constexpr int64_t kWorkgroups = 1024, kShortest = 8;
+    int64_t splits = units > 0 ? (kWorkgroups + units - 1) / units : 1;
+    int64_t chunk = splits > 0 ? (key_tiles + splits - 1) / splits : key_tiles;
+    if (chunk < kShortest) chunk = kShortest;
+    chunk = (chunk + kWaves - 1) / kWaves * kWaves;
+    splits = (key_tiles + chunk - 1) / chunk;
+    x.chunk = (int32_t)chunk;
+    x.splits = splits < 1 ? 1 : (int32_t)splits;
+    const int64_t rows = (int64_t)n_seqs * n_tokens * n_q_heads;
+    x.part_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * head_dim * sizeof(float);
+    x.stat_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * 2 * sizeof(float);
+    return x;
+}
+
+int launch_cache_attention(const CacheAttention& x, const CacheView& c, int32_t head_dim, const void* q, const int32_t* slots, int32_t n_seqs,
+                           int32_t n_tokens, int32_t n_q_heads, float scale_log2, void* out, float* lse, void* parts, float* stats, hipStream_t stream) {
+    if (n_seqs == 0) return PYR_OK;
+    AttendArgs a{c, (const uint16_t*)q, slots, out, lse, n_seqs, n_tokens, n_q_heads, x.chunk, x.splits, scale_log2};
+    if (x.splits > 1) {
+        a.out = parts;
+        a.lse = stats;
+    }
+    return head_dim == 128 ? launch<128>(x, c, a, out, lse, stream) : launch<64>(x, c, a, out, lse, stream);
+}
+
+}  // namespace pyr

@@ -152,6 +152,32 @@ int launch_sum_parts(const float* parts, int groups, int32_t total_tokens, float
 int launch_gather_positions(const int32_t* pos, const int32_t* kept_idx, int64_t n_kept, int32_t* pos_out,
                             hipStream_t stream);
 
+// The cache held in 4 bits (cache_device.h says how it lies in memory; cache_api.hip checks the arguments).
+struct CacheView;
+constexpr int kMaxCacheRows = PYR_CACHE_MAX_ROWS, kMaxCacheSlots = PYR_CACHE_MAX_SLOTS;
+
+// How an attention over the cache is cut up: 16-row column tiles of a workgroup, workgroups per head and split; 32-token tiles of a split; splits and
+// what their partial results take.
+struct CacheAttention {
+    int32_t col_tiles, col_groups, chunk, splits;
+    size_t part_bytes, stat_bytes;
+};
+CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_len);
+int launch_cache_attention(const CacheAttention& plan, const CacheView& c, int32_t head_dim, const void* q, const int32_t* slots, int32_t n_seqs,
+                           int32_t n_tokens, int32_t n_q_heads, float scale_log2, void* out, float* lse, void* parts, float* stats, hipStream_t stream);
+int launch_cache_store(const CacheView& c, int32_t head_dim, const void* k, const void* v, int32_t n_rows, const int32_t* row_idx, int32_t n_list,
+                       const int32_t* offsets, const int32_t* slots, const int32_t* start, int32_t n_seqs, int32_t max_new, hipStream_t stream);
+int launch_cache_load(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* offsets, int32_t n_seqs, int32_t max_len,
+                      void* k, void* v, int32_t n_rows, hipStream_t stream);
+int launch_cache_reserve(const CacheView& c, const int32_t* slots, const int32_t* n_new, int32_t n, int32_t* start, int32_t* status, hipStream_t stream);
+int launch_cache_fork(const CacheView& c, int32_t head_dim, const int32_t* parents, const int32_t* children, int32_t n, int32_t* status, hipStream_t stream);
+int launch_cache_release(const CacheView& c, const int32_t* slots, int32_t n, hipStream_t stream);
+// A cut is two launches: the rows of the table, which leaves the old ones in old_rows [n, 1 + max_pages], and the tokens.
+int launch_cache_cut(const CacheView& c, const int32_t* slots, const int32_t* out_offsets, int32_t n, int32_t n_list, int32_t max_keep, int32_t* old_rows,
+                     int32_t* status, hipStream_t stream);
+int launch_cache_move(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* kept_idx, int32_t n_list, const int32_t* seq_offsets,
+                      const int32_t* out_offsets, const int32_t* old_rows, const int32_t* status, int32_t n_seqs, int32_t max_keep, hipStream_t stream);
+
 // Raise a kernel's dynamic LDS limit to `bytes`, once per device (done_mask: one bit per device id).
 int ensure_dynamic_lds(const void* kernel, int bytes, std::atomic<uint64_t>* done_mask);
 

@@ -1,0 +1,395 @@
+"""The operators on a cache held in 4 bits against the float64 oracle: pages and codes bit for bit, attention within the bounds its roundings give."""
+import numpy as np
+import pytest
+
+from oracle import cache_oracle as orc
+from paper_2405_12532_amd import synth
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+from tests.caches import Pair, attend, bf16, check_attention, dev  # noqa: E402
+
+
+# ------------------------------------------------------------------------------------------------ rows in and out
+def special_rows(rng, rows, hkv, d):
+    """Rows whose blocks hold what a conversion can trip over: ties, borders of the power of two, the ends of bf16's range, numbers that are none."""
+    x = rng.normal(size=(rows, hkv, d)) * 2.0 ** rng.integers(-30, 30, (rows, hkv, 1))
+    flat = x.reshape(-1, 32)
+    n = len(flat)
+    ties = np.array([6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, -0.25, -0.75, -1.25, -1.75, -2.5, -3.5, -5, -0.0, 0.0, 5.96875, 6.0])
+    for i in range(0, n, 7):
+        flat[i, :19] = ties * 2.0 ** float(rng.integers(-100, 100))
+    for i, top in zip(range(1, n, 5), [7.0, 7.03125, 3.5, 3.515625, 2.0 ** -126, 2.0 ** -130, 2.0 ** -133, 3.38e38, 1.7e38, 0.0] * n):
+        flat[i] = rng.choice([-1, 1, 0.5, 0.25, 0], 32) * top
+    for i, bad in zip(range(3, n, 23), [np.inf, -np.inf, np.nan] * n):
+        flat[i, rng.integers(32)] = bad
+    return flat.reshape(rows, hkv, d)
+
+
+@pytest.mark.parametrize("hkv,d,page", [(1, 128, 32), (3, 64, 64), (5, 128, 256), (8, 64, 32)])
+def test_store_writes_the_nearest_numbers_and_nothing_else(lib, hkv, d, page):
+    # pieces that begin and end inside a tile, one token, none, whole tiles, across pages; one in a padded row, one without room
+    lens = [100, 70, 64, 33, 200, 40, 40]
+    start, count, slots = [37, 69, 0, 31, 5, 3, -1], [50, 1, 64, 0, 190, 7, 9], [0, 1, 2, 3, 4, -1, 6]
+    pair = Pair(lib, lens, hkv, d, page, seed=d + hkv)
+    rows = sum(count)
+    kt, k = bf16(special_rows(pair.rng, rows, hkv, d))
+    vt, v = bf16(special_rows(pair.rng, rows, hkv, d))
+    offsets = np.concatenate([[0], np.cumsum(count)])
+    lib.cache_store(pair.cache, kt, vt, rows, None, rows, dev(offsets), dev(slots), dev(start), 7, max(count))
+    pair.o.store(k, v, None, offsets, slots, start)
+    pair.check()
+    assert np.array_equal(pair.pages.cpu().numpy(), pair.o.pages)                       # not a byte beside them
+
+
+def test_store_through_an_index_list(lib):
+    pair = Pair(lib, [90, 64], 4, 128, 32)
+    kt, k = bf16(pair.rng.normal(size=(200, 4, 128)))
+    vt, v = bf16(pair.rng.normal(size=(200, 4, 128)))
+    idx = pair.rng.integers(0, 200, 60).astype(np.int32)
+    idx[[5, 41]], idx[17] = 200, -1                                                      # rows that k and v do not have
+    lib.cache_store(pair.cache, kt, vt, 200, dev(idx), 60, dev([0, 40, 60]), dev([0, 1]), dev([50, 44]), 2, 40)
+    pair.o.store(k, v, idx, [0, 40, 60], [0, 1], [50, 44])
+    assert np.array_equal(pair.pages.cpu().numpy(), pair.o.pages)
+
+
+def test_store_leaves_out_tokens_without_a_page(lib):
+    pair = Pair(lib, [64, 64], 2, 64, 32)
+    pair.o.table[0, 1], pair.o.table[1, 0] = -1, len(pair.o.refs)                        # a page that is not there, one outside the pool
+    pair.up()
+    kt, k = bf16(pair.rng.normal(size=(140, 2, 64)))
+    lib.cache_store(pair.cache, kt, kt, 140, None, 140, dev([0, 70, 140]), dev([0, 1]), dev([0, 0]), 2, 70)      # (and 6 tokens behind a row's end)
+    pair.o.store(k, k, None, [0, 70, 140], [0, 1], [0, 0])
+    assert np.array_equal(pair.pages.cpu().numpy(), pair.o.pages)
+
+
+@pytest.mark.parametrize("hkv,d,page", [(1, 128, 32), (6, 64, 128), (5, 128, 64), (8, 64, 32)])
+def test_load_gives_the_exact_values(lib, hkv, d, page):
+    lens = [0, 1, 33, 64, 200, 31, 9]
+    pair = Pair(lib, lens, hkv, d, page, scales=(1, 253))
+    pair.o.pages[pair.o.table[4, 0], 0, 0, 32 * d] = 255                                 # a block that is no number
+    pair.up()
+    room = [3, 1, 33, 70, 150, 31, 9]                                                    # rows for them: more than there are, fewer than there are
+    slots = [0, 1, 2, 3, 4, -1, 6]
+    offsets = np.concatenate([[0], np.cumsum(room)])
+    n_rows = int(offsets[-1]) - 2                                                        # the last two have no rows
+    out = [torch.full((n_rows + 5, hkv, d), 77.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    lib.cache_load(pair.cache, dev(slots), dev(offsets), 7, 200, out[0], out[1], n_rows)
+    want = [np.full((n_rows + 5, hkv, d), 77.0) for _ in range(2)]
+    for b, s in enumerate(slots):
+        if s < 0:
+            continue
+        for o, x in zip(want, pair.o.read(s)):
+            n = min(lens[s], room[b], n_rows - int(offsets[b]))
+            o[offsets[b]:offsets[b] + n] = x[:n]
+    for o, x in zip(out, want):
+        with np.errstate(over="ignore"):
+            assert np.array_equal(o.double().cpu().numpy(), x, equal_nan=True)
+    only = torch.full_like(out[1], 77.0)
+    lib.cache_load(pair.cache, dev(slots), dev(offsets), 7, 200, None, only, n_rows)
+    assert torch.equal(only.view(torch.int16), out[1].view(torch.int16))
+
+
+# ------------------------------------------------------------------------------------------------ attention
+ATTEND = [  # lens, hq, hkv, d, page, tokens
+    ([0, 1, 2, 31, 32, 33, 64, 65, 127, 300], 4, 4, 128, 64, 1),
+    ([0, 1, 2, 31, 32, 33, 64, 65, 127, 300], 8, 2, 64, 32, 1),
+    ([0, 1, 2, 5, 33, 129, 260], 8, 2, 128, 256, 5),            # rows that see nothing, 20 of them on a head
+    ([0, 3, 4, 31, 128, 290], 8, 8, 64, 128, 4),
+    ([257, 64, 9], 16, 1, 128, 32, 9),                          # 144 rows on a head
+    ([200, 40, 95], 12, 3, 64, 1024, 12),                       # 48
+    ([150, 96], 5, 5, 128, 32, 3),
+    ([70, 1], 71, 1, 64, 64, 1),                                # a group that is no power of two
+]
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d,page,tokens", ATTEND)
+def test_attention(lib, lens, hq, hkv, d, page, tokens):
+    pair = Pair(lib, lens, hkv, d, page, seed=hq)
+    qt, q = bf16(pair.rng.normal(size=(len(lens) + 2, tokens, hq, d)) * 0.2)
+    slots = [int(s) for s in pair.rng.permutation(len(lens))] + [-1, 0]
+    out, lse = attend(pair, qt, slots, tokens, max(lens))
+    check_attention(pair, q, slots, out, lse)
+    alone, _ = attend(pair, qt, slots, tokens, max(lens), want_lse=False)
+    assert torch.equal(alone.view(torch.int16), out.view(torch.int16))
+    # how the work is cut up does not depend on the lengths that are there
+    for bound in (0, 64, 1 << 20):
+        out, lse = attend(pair, qt, slots, tokens, bound)
+        check_attention(pair, q, slots, out, lse)
+
+
+@pytest.mark.parametrize("lens,hq,hkv,d,tokens", [([5000, 1, 700, 0], 4, 2, 128, 1), ([4097, 4096], 8, 1, 64, 3), ([9000], 2, 1, 64, 1)])
+def test_attention_split_along_the_cache(lib, lens, hq, hkv, d, tokens):
+    pair = Pair(lib, lens, hkv, d, 64)
+    assert lib.cache_attention_workspace_bytes(pair.cache, len(lens), tokens, hq, max(lens)) > 0
+    qt, q = bf16(pair.rng.normal(size=(len(lens), tokens, hq, d)) * 0.2)
+    slots = list(range(len(lens)))
+    reads = {s: pair.o.read(s) for s in slots}
+    out, lse = attend(pair, qt, slots, tokens, max(lens))
+    check_attention(pair, q, slots, out, lse, reads=reads)
+    again, lse2 = attend(pair, qt, slots, tokens, max(lens))
+    assert torch.equal(again.view(torch.int16), out.view(torch.int16)) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_with_large_and_growing_logits(lib, d):
+    """References that move: logits that grow along the cache by far more than 2^12, and that fall; a scale of 1."""
+    pair = Pair(lib, [0, 0], 2, d, 64, n_slots=2, max_pages=8, spare=16)
+    k = pair.rng.normal(size=(1000, 2, d))
+    k[:500] *= np.linspace(0.01, 8, 500)[:, None, None]
+    k[500:] *= np.linspace(8, 0.01, 500)[:, None, None]
+    kt, k = bf16(k)
+    vt, v = bf16(pair.rng.normal(size=(1000, 2, d)))
+    start = torch.empty(2, dtype=torch.int32, device="cuda")
+    lib.cache_reserve(pair.cache, dev([0, 1]), dev([500, 500]), 2, start, pair.status)
+    lib.cache_store(pair.cache, kt, vt, 1000, None, 1000, dev([0, 500, 1000]), dev([0, 1]), start, 2, 500)
+    pair.o.reserve([0, 1], [500, 500])
+    pair.o.store(k, v, None, [0, 500, 1000], [0, 1], [0, 0])
+    pair.check()
+    qt, q = bf16(pair.rng.normal(size=(2, 2, 4, d)))
+    out, lse = attend(pair, qt, [0, 1], 2, 500, scale=1.0)
+    check_attention(pair, q, [0, 1], out, lse, scale=1.0)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_blocks_that_are_no_number_reach_the_rows_that_see_them_alone(lib, d):
+    pair = Pair(lib, [80, 80, 80], 2, d, 32)
+    place = orc.tile_places(d)
+    for slot, token, kind in ((0, 79, 2), (1, 78, 3), (2, 10, 2)):       # K of the newest token, V of the one before, K of an old one; head 1
+        tile = pair.o.pages[pair.o.table[slot, token // 32], 1, 0]
+        tile[place[kind][token % 32, 1]] = 255
+        codes = place[kind - 2][token % 32, 32:64]
+        for byte, high in codes:
+            tile[byte] &= 0x0F if high else 0xF0
+    pair.up()
+    qt, q = bf16(pair.rng.normal(size=(3, 3, 4, d)) * 0.2)
+    out, lse = attend(pair, qt, [0, 1, 2], 3, 80)
+    check_attention(pair, q, [0, 1, 2], out, lse)
+    o = out.double().cpu().numpy()
+    assert not np.isnan(o[:, :, :2]).any() and np.isnan(o[0, 2, 2:]).all() and not np.isnan(o[0, :2]).any() and np.isnan(o[2, :, 2:]).all()
+
+
+def test_a_page_outside_the_pool_gives_nan(lib):
+    pair = Pair(lib, [100, 100], 2, 128, 32)
+    pair.o.table[0, 2] = len(pair.o.refs)
+    pair.up()
+    qt, q = bf16(pair.rng.normal(size=(2, 1, 4, 128)))
+    out, lse = attend(pair, qt, [0, 1], 1, 100)
+    assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
+    check_attention(pair, q[1:], [1], out[1:], lse[1:])
+
+
+# ------------------------------------------------------------------------------------------------ pages
+def compact(pair, slots, kept, seq_offsets, out_offsets, max_keep):
+    size = pair.lib.cache_compact_workspace_bytes(pair.cache, len(slots))
+    ws = torch.full((max(size, 256),), 0xFF, dtype=torch.uint8, device="cuda")
+    pair.lib.cache_compact(pair.cache, dev(slots), len(slots), dev(kept), len(kept), dev(seq_offsets), dev(out_offsets), max_keep, pair.status, ws, size)
+    return int(pair.status)
+
+
+def reserve(pair, slots, n_new):
+    start = torch.full((len(slots),), 99, dtype=torch.int32, device="cuda")
+    pair.lib.cache_reserve(pair.cache, dev(slots), dev(n_new), len(slots), start, pair.status)
+    return start.cpu().tolist(), int(pair.status)
+
+
+def both_reserve(pair, slots, n_new):
+    start, status = pair.o.reserve(slots, n_new)
+    assert reserve(pair, slots, n_new) == (start.tolist(), status)
+    pair.check()
+    return status
+
+
+def both_fork(pair, parents, children):
+    status = pair.o.fork(parents, children)
+    pair.lib.cache_fork(pair.cache, dev(parents), dev(children), len(parents), pair.status)
+    assert int(pair.status) == status
+    pair.check()
+    return status
+
+
+def both_release(pair, slots):
+    pair.o.release(slots)
+    pair.lib.cache_release(pair.cache, dev(slots), len(slots))
+    pair.check()
+
+
+def both_compact(pair, slots, kept, seq_offsets, out_offsets, max_keep):
+    status = pair.o.compact(slots, np.asarray(kept), seq_offsets, out_offsets, max_keep)
+    assert compact(pair, slots, kept, seq_offsets, out_offsets, max_keep) == status
+    pair.check()
+    return status
+
+
+@pytest.mark.parametrize("hkv,d,page", [(1, 64, 32), (3, 128, 64), (9, 64, 256)])
+def test_pages_through_a_life(lib, hkv, d, page):
+    pair = Pair(lib, [100, 0, page, 2 * page + 1, 31], hkv, d, page, n_slots=12, max_pages=12, spare=20)
+    assert both_reserve(pair, [1, -1, 0, 4], [1, 7, page, 0]) == 0
+    assert both_fork(pair, [0, 0, 3, -1, 2], [5, 6, 7, -1, 8]) == 0
+    assert both_reserve(pair, [5, 0, 8], [page + 3, 1, 1]) == 0                          # a branch and its parent go apart
+    k, v = (bf16(pair.rng.normal(size=(page + 5, hkv, d))) for _ in range(2))
+    offsets, slots, start = [0, page + 3, page + 4, page + 5], [5, 0, 8], [int(pair.o.lens[5]) - page - 3, int(pair.o.lens[0]) - 1, int(pair.o.lens[8]) - 1]
+    lib.cache_store(pair.cache, k[0], v[0], page + 5, None, page + 5, dev(offsets), dev(slots), dev(start), 3, page + 3)
+    pair.o.store(k[1], v[1], None, offsets, slots, start)
+    pair.check()
+    both_release(pair, [0, 0, 99, -1, -7])
+    # branches are cut: every third token, all of them, none, repeated and in any order
+    lens = [int(pair.o.lens[s]) for s in (5, 6, 7, 8)]
+    off = np.concatenate([[0], np.cumsum(lens)])
+    kept = [np.arange(0, lens[0], 3), np.arange(lens[1]), np.arange(0), np.array([lens[3] - 1, 0, 0])]
+    koff = np.concatenate([[0], np.cumsum([len(x) for x in kept])])
+    flat = np.concatenate([x + o for x, o in zip(kept, off)]).astype(np.int32)
+    assert both_compact(pair, [5, 6, 7, 8], flat, off, koff, max(len(x) for x in kept)) == 0
+    both_release(pair, list(range(12)))
+    assert not pair.refs.any() and not pair.lens.any()
+
+
+def test_pages_that_run_out_change_nothing(lib):
+    pair = Pair(lib, [64, 40], 2, 64, 32, n_slots=4, max_pages=6, spare=3)
+    assert both_reserve(pair, [0, 1], [64, 90]) == 2
+    assert both_reserve(pair, [0, 1], [64, 24]) == 0                                     # two pages, and none for the 24
+    assert both_fork(pair, [0], [2]) == 0                                                # full pages only: none is needed
+    assert both_reserve(pair, [1], [2]) == 0                                             # the last page
+    assert both_fork(pair, [1], [3]) == 1
+    assert both_compact(pair, [0], np.arange(64), [0], [0, 64], 64) == 2
+
+
+def test_pages_of_a_large_pool_are_handed_out_from_the_lowest(lib):
+    """More counts than one look of the workgroup takes, more rows than it has threads."""
+    n, page = 1500, 32
+    pair = Pair(lib, [], 1, 64, page, n_slots=n, max_pages=16, spare=40003)
+    used = pair.rng.random(40003) < 0.6
+    pair.o.refs[used] = 1
+    pair.up()
+    n_new = pair.rng.integers(0, 16 * page + 1, n).tolist()
+    slots = [int(s) for s in pair.rng.permutation(n)]
+    start, status = pair.o.reserve(slots, n_new)
+    assert status == 0 and reserve(pair, slots, n_new) == (start.tolist(), 0)
+    assert np.array_equal(pair.table.cpu().numpy(), pair.o.table) and pair.refs.cpu().tolist() == pair.o.refs.tolist()
+    assert reserve(pair, slots, [16 * page - int(x) for x in pair.o.lens[slots]])[1] == pair.o.reserve(slots, [16 * page - int(x) for x in pair.o.lens[slots]])[1] > 0
+    assert np.array_equal(pair.table.cpu().numpy(), pair.o.table) and pair.refs.cpu().tolist() == pair.o.refs.tolist()
+    pair.lib.cache_release(pair.cache, dev(slots), n)
+    assert pair.refs.cpu().tolist() == used.astype(int).tolist() and not pair.lens.any() and (pair.table == -1).all()
+
+
+def test_rows_that_cannot_be_are_refused_on_the_device(lib):
+    pair = Pair(lib, [40, 50, 0], 1, 64, 32, n_slots=3, max_pages=3, spare=6)
+    for slots, n_new, status in (([0, 0], [1, 1], -1), ([3], [1], -1), ([-2], [1], -1), ([0], [-1], -2), ([0], [57], -2), ([1, 1], [1, 100], -2),
+                                 ([0, 5, 1], [57, 1, 1], -2)):
+        assert both_reserve(pair, slots, n_new) == status, (slots, n_new)
+    for parents, children in (([0], [1]), ([0], [0]), ([0, 1], [2, 2]), ([0], [3]), ([3], [2]), ([-1], [2]), ([0], [-1]), ([2], [2]), ([0, 2], [2, 2])):
+        assert both_fork(pair, parents, children) == -1, (parents, children)
+    for slots, kept, koff, most, status in (([0, 0], [0, 1], [0, 1, 2], 1, -1), ([3], [0], [0, 1], 1, -1), ([0], [0, 1], [0, 2], 1, -2),
+                                            ([0], [0, 1], [0, 3], 3, -2), ([0, 1], [0, 1], [2, 1, 2], 2, -2), ([0], [0], [-1, 1], 2, -2)):
+        assert both_compact(pair, slots, kept, [0, 0], koff, most) == status, (slots, koff)
+    # indexes outside a slot's tokens give tokens of NaN, the others stand
+    kept = np.array([3, 40, -1, 39, 1 << 30])
+    assert both_compact(pair, [0], kept, [0], [0, 5], 5) == 0
+    k, v = pair.o.read(0)
+    assert [bool(np.isnan(x).all()) for x in k] == [False, True, True, False, True]
+
+
+# ------------------------------------------------------------------------------------------------ streams, graphs, together
+def test_another_stream_than_the_current_one(lib):
+    pair = Pair(lib, [90, 33], 4, 128, 32, n_slots=4, max_pages=4, spare=8)
+    qt, q = bf16(pair.rng.normal(size=(2, 1, 8, 128)) * 0.2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    parents, children = dev([0, 1]), dev([2, 3])
+    torch.cuda.synchronize()
+    lib.cache_fork(pair.cache, parents, children, 2, pair.status, stream=side)
+    out, lse = attend(pair, qt, [2, 3], 1, 90, stream=side)
+    side.synchronize()
+    pair.o.fork([0, 1], [2, 3])
+    pair.check()
+    check_attention(pair, q, [2, 3], out, lse)
+
+
+def test_captured_steps_grow_the_sequences_on_every_replay(lib):
+    """reserve, store and attention in a graph: every replay is a step, and what it leaves is what eager calls leave.  The program's own work goes on between
+    replays; two graphs share a workspace."""
+    lens, hq, hkv, d, page, steps = [30, 500, 63, 0], 8, 2, 128, 64, 6
+    pairs = [Pair(lib, lens, hkv, d, page, n_slots=5, max_pages=12, spare=30, seed=4) for _ in range(2)]
+    rows = [bf16(pairs[0].rng.normal(size=(4, hkv, d))) for _ in range(2 * steps)]
+    qs = [bf16(pairs[0].rng.normal(size=(5, 1, hq, d)) * 0.2) for _ in range(steps)]
+    slots, n_new, offsets = dev([2, 0, 1, 3, -1]), dev([1, 1, 1, 1, 1]), dev([0, 1, 2, 3, 4, 4])
+    bufs = []
+    size = lib.cache_attention_workspace_bytes(pairs[0].cache, 5, 1, hq, page * 12)
+    ws = torch.empty(max(size, 256), dtype=torch.uint8, device="cuda")
+    for pair in pairs:
+        bufs.append(dict(k=torch.empty_like(rows[0][0]), v=torch.empty_like(rows[0][0]), q=torch.empty_like(qs[0][0]), out=torch.empty_like(qs[0][0]),
+                         lse=torch.empty(5, 1, hq, dtype=torch.float32, device="cuda"), start=torch.empty(5, dtype=torch.int32, device="cuda")))
+
+    def step(pair, b):
+        lib.cache_reserve(pair.cache, slots, n_new, 5, b["start"], pair.status)
+        lib.cache_store(pair.cache, b["k"], b["v"], 4, None, 4, offsets, slots, b["start"], 5, 1)
+        lib.cache_attention(pair.cache, b["q"], slots, 5, 1, hq, page * 12, 0.0, b["out"], b["lse"], ws, size)
+
+    graphs = []
+    for pair, b in list(zip(pairs, bufs))[:1] * 2:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step(pair, b)
+        graphs.append(g)
+    torch.cuda.synchronize()
+    for i in range(steps):
+        for b in bufs:
+            b["k"].copy_(rows[2 * i][0])
+            b["v"].copy_(rows[2 * i + 1][0])
+            b["q"].copy_(qs[i][0])
+        graphs[i % 2].replay()
+        step(pairs[1], bufs[1])
+        torch.cuda.synchronize()
+        start, status = pairs[0].o.reserve([2, 0, 1, 3, -1], [1] * 5)
+        pairs[0].o.store(rows[2 * i][1], rows[2 * i + 1][1], None, [0, 1, 2, 3, 4, 4], [2, 0, 1, 3, -1], start)
+        assert status == 0 and int(pairs[0].status) == 0 and bufs[0]["start"].cpu().tolist() == start.tolist()
+        for name in ("out", "lse", "start"):
+            assert torch.equal(bufs[0][name], bufs[1][name]), (i, name)
+        for name in ("pages", "table", "refs", "lens"):
+            assert torch.equal(getattr(pairs[0], name), getattr(pairs[1], name)), (i, name)
+        check_attention(pairs[0], qs[i][1], [2, 0, 1, 3, -1], bufs[0]["out"], bufs[0]["lse"])
+    pairs[0].check()
+
+
+def test_from_a_prompt_to_the_cache_and_through_its_updates(lib):
+    """What a serving program does with the whole of it: a layer's prefill step chooses rows, they go into the cache in 4 bits, a branch takes new tokens and attends,
+    the cache is read back for the generation-phase update, and its choice cuts the branch."""
+    wl = synth.shrunk(synth.workload("cfg2"), (150, 97), n_q_heads=8, n_kv_heads=2, head_dim=128, w=16, hidden_dim=0)
+    x = synth.make_inputs(wl)
+    keep = np.array([90, 60], dtype=np.int32)
+    x["keep_len"] = keep
+    res = lib.prefill_layer_from_numpy(x, wl.w)
+    F = synth.bf16_bits_to_f64
+    pair = Pair(lib, [0, 0], 2, 128, 32, n_slots=4, max_pages=6, spare=20, fill=0x5A)
+    k, v = lib.to_device_bf16(x["k"]), lib.to_device_bf16(x["v"])
+    start = torch.empty(2, dtype=torch.int32, device="cuda")
+    koff = np.array([0, 90, 150])
+    lib.cache_reserve(pair.cache, dev([0, 1]), dev(keep), 2, start, pair.status)
+    lib.cache_store(pair.cache, k, v, k.shape[0], dev(res["kept_idx"]), 150, dev(koff), dev([0, 1]), start, 2, 90)
+    pair.o.reserve([0, 1], keep)
+    pair.o.store(F(x["k"]), F(x["v"]), res["kept_idx"], koff, [0, 1], [0, 0])
+    pair.check()
+    # a branch of both grows by two tokens
+    both_fork(pair, [0, 1], [2, 3])
+    both_reserve(pair, [2, 3], [2, 2])
+    newk, newv = (bf16(pair.rng.normal(size=(4, 2, 128))) for _ in range(2))
+    lib.cache_store(pair.cache, newk[0], newv[0], 4, None, 4, dev([0, 2, 4]), dev([2, 3]), dev(keep), 2, 2)
+    pair.o.store(newk[1], newv[1], None, [0, 2, 4], [2, 3], keep)
+    qt, q = bf16(pair.rng.normal(size=(2, 2, 8, 128)) * 0.3)
+    out, lse = attend(pair, qt, [2, 3], 2, 92)
+    check_attention(pair, q, [2, 3], out, lse)
+    # read back, updated, cut
+    off = np.array([0, 92, 154], dtype=np.int32)
+    kb, vb = (torch.empty((154, 2, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    lib.cache_load(pair.cache, dev([2, 3]), dev(off), 2, 92, kb, vb, 154)
+    q_win = pair.rng.normal(size=(2, 16, 8, 128)).astype(np.float32)
+    q_bits = torch.from_numpy(q_win).to(torch.bfloat16).view(torch.int16).numpy().view(np.uint16)
+    upd = lib.decode_update_from_numpy(q_bits, lib.to_host_bits(kb), lib.to_host_bits(vb), off, [70, 40], 16)
+    assert both_compact(pair, [2, 3], upd["kept_idx"], off[:2], upd["out_offsets"], 70) == 0
+    out_k = torch.empty((110, 2, 128), dtype=torch.bfloat16, device="cuda")
+    lib.cache_load(pair.cache, dev([2, 3]), dev([0, 70, 110]), 2, 70, out_k, None, 110)
+    assert np.array_equal(lib.to_host_bits(out_k) & 0x7FFF, upd["k_out"] & 0x7FFF)      # the update's own gather, from the bf16 rows
+    out, lse = attend(pair, qt, [2, 3], 2, 70)
+    check_attention(pair, q, [2, 3], out, lse)
+    both_release(pair, [0, 1, 2, 3])
+    assert not pair.refs.any()
