@@ -333,7 +333,7 @@ PYR_API int pyr_decode_update(const void* q_win, const void* k, const void* v,
  *
  * Host checks of every call: PYR_ERR_NULL; PYR_ERR_SHAPE (negative sizes; n_slots > PYR_CACHE_MAX_SLOTS; n > PYR_CACHE_MAX_ROWS where pages are handed out or shared);
  * PYR_ERR_UNSUPPORTED (head_dim not 64 or 128, page_tokens not a power of two from 32 to 1024, pages not 256-byte aligned, rows not 16-byte aligned,
- * 2^31 or more tokens in the pool, a row of the table or a batch); PYR_ERR_WORKSPACE; PYR_ERR_LAUNCH.
+ * 2^31 or more tokens in the pool, a row of the table or a batch, or entries of the table); PYR_ERR_WORKSPACE; PYR_ERR_LAUNCH.
  */
 #define PYR_CACHE_MAX_ROWS 4096
 #define PYR_CACHE_MAX_SLOTS 262144

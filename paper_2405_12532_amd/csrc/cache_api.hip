@@ -9,7 +9,7 @@ constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 constexpr int64_t kMost = (int64_t)1 << 31;
-constexpr int64_t kMaxGridY = 65535;
+int64_t head_groups(const pyr_cache* c) { return (c->n_kv_heads + 3) / 4; }      // (workgroups of a tile, at most)
 
 int check_layout(const pyr_cache* c) {
     if (c == nullptr) return PYR_ERR_NULL;
@@ -24,7 +24,7 @@ int check_sizes(const pyr_cache* c) {
     const int rc = check_layout(c);
     if (rc != PYR_OK) return rc;
     if (c->n_pages < 1 || c->n_slots < 1 || c->max_pages < 1 || c->n_slots > PYR_CACHE_MAX_SLOTS) return PYR_ERR_SHAPE;
-    if ((int64_t)c->n_pages * c->page_tokens >= kMost || (int64_t)c->max_pages * c->page_tokens >= kMost) return PYR_ERR_UNSUPPORTED;
+    if ((int64_t)c->n_slots * c->max_pages >= kMost || (int64_t)c->n_pages * c->page_tokens >= kMost || (int64_t)c->max_pages * c->page_tokens >= kMost) return PYR_ERR_UNSUPPORTED;
     return PYR_OK;
 }
 
@@ -117,7 +117,7 @@ int pyr_cache_compact(const pyr_cache* cache, const int32_t* slots, int32_t n, c
     size_t need = 0;
     pyr_cache_compact_workspace_bytes(cache, n, &need);
     if (!workspace_ok(workspace, workspace_bytes, need)) return PYR_ERR_WORKSPACE;
-    if ((int64_t)n * (((int64_t)max_keep + 31) / 32) >= kMost) return PYR_ERR_UNSUPPORTED;
+    if ((int64_t)n * (((int64_t)max_keep + 31) / 32) * head_groups(cache) >= kMost) return PYR_ERR_UNSUPPORTED;
     const pyr::CacheView c = view(cache);
     rc = pyr::launch_cache_cut(c, slots, out_offsets, n, n_kept, max_keep, (int32_t*)workspace, status, (hipStream_t)stream);
     if (rc != PYR_OK) return rc;
@@ -133,7 +133,7 @@ int pyr_cache_store(const pyr_cache* cache, const void* k, const void* v, int32_
     if (n == 0 || n_rows == 0 || n_list == 0 || max_new == 0) return PYR_OK;
     if (!k || !v || !offsets || !slots || !start) return PYR_ERR_NULL;
     if (!aligned16(k) || !aligned16(v)) return PYR_ERR_UNSUPPORTED;
-    if ((int64_t)n * (((int64_t)max_new + 30) / 32 + 1) >= kMost) return PYR_ERR_UNSUPPORTED;
+    if ((int64_t)n * (((int64_t)max_new + 30) / 32 + 1) * head_groups(cache) >= kMost) return PYR_ERR_UNSUPPORTED;
     return pyr::launch_cache_store(view(cache), cache->head_dim, k, v, n_rows, row_idx, n_list, offsets, slots, start, n, max_new, (hipStream_t)stream);
 }
 
@@ -147,7 +147,7 @@ int pyr_cache_load(const pyr_cache* cache, const int32_t* slots, const int32_t* 
     if (!aligned16(k_out) || !aligned16(v_out)) return PYR_ERR_UNSUPPORTED;
     const int64_t capacity = (int64_t)cache->max_pages * cache->page_tokens;
     if (max_len > capacity) max_len = (int32_t)capacity;
-    if ((int64_t)n * (((int64_t)max_len + 31) / 32) >= kMost) return PYR_ERR_UNSUPPORTED;
+    if ((int64_t)n * (((int64_t)max_len + 31) / 32) * head_groups(cache) >= kMost) return PYR_ERR_UNSUPPORTED;
     return pyr::launch_cache_load(view(cache), cache->head_dim, slots, offsets, n, max_len, k_out, v_out, n_rows, (hipStream_t)stream);
 }
 

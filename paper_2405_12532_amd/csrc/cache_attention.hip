@@ -28,7 +28,7 @@ struct AttendArgs {
     const uint16_t* q;
     const int32_t* slots;
     void* out;                                    // splits == 1: bf16 [n, tokens, Hq, D]; else fp32 [splits, rows, D], not normalised
-    float* lse;                                   // splits == 1: [rows] or NULL; else [splits, rows, 2]: reference and sum
+    float* lse;                                   // splits == 1: [rows] or NULL; else [splits, rows, 4]: reference, sum, sum of the rounded
     int32_t n_seqs, n_tokens, n_q_heads;
     int32_t chunk;                                // tiles of a split (the last one takes what is left)
     int32_t splits;
@@ -72,15 +72,15 @@ template <int D, int NT>
 struct Rows {
     bf16x8 q[NT][D / 32];                         // operand of step s: lane 16 j + col, see load_rows
     f32x4 o[NT][D / 16];
-    float m[NT], l[NT];                           // reference; sum over the tokens that this lane sees
+    f32x4 weight[NT];                             // sum of the rounded P, in every element
+    float m[NT], l[NT];                           // reference; sum of P over the tokens that this lane sees
     int32_t seen[NT];                             // tokens that the row of this lane's column sees
 };
 
-// One tile's products.  kMasked: some row does not see all of its tokens.
-template <int D, int NT, bool kMasked>
-__device__ __forceinline__ void attend_tile(Rows<D, NT>& w, const Tile<D>& t, int first_token, float scale, int lane) {
+// One tile's products.  masked: some row does not see all of its tokens.
+template <int D, int NT>
+__device__ __forceinline__ void attend_tile(Rows<D, NT>& w, const Tile<D>& t, int first_token, bool masked, float scale, int lane) {
     constexpr int kSteps = D / 32;
-    const int j = lane >> 4;
     f32x4 s[NT][2];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -106,31 +106,42 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT>& w, const Tile<D>& t, in
             for (int n = 0; n < NT; ++n) s[n][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, w.q[n][i], s[n][half], 0, 0, 0);
         }
     }
+    bf16x8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
     float p[NT][8];
+    uint32_t hidden[NT];                          // bit e: the row does not see the lane's e-th token
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+        hidden[n] = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            p[n][e] = s[n][e >> 2][e & 3];
-            if (kMasked && first_token + 16 * (e >> 2) + 4 * j + (e & 3) >= w.seen[n]) p[n][e] = -INFINITY;
+        for (int e = 0; e < 8; ++e) p[n][e] = s[n][e >> 2][e & 3];
+        if (masked) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (first_token + 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3) >= w.seen[n]) {
+                    p[n][e] = -INFINITY;
+                    hidden[n] |= 1u << e;
+                }
         }
-        float top = p[n][0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) top = fmaxf(top, p[n][e]);
-        top *= scale;
+        float top = fmaxf(fmaxf(fmaxf(p[n][0], p[n][1]), fmaxf(p[n][2], p[n][3])), fmaxf(fmaxf(p[n][4], p[n][5]), fmaxf(p[n][6], p[n][7]))) * scale;
         if (__builtin_amdgcn_ballot_w64(top > w.m[n] + kGrowth) != 0) {
             const float m = fmaxf(w.m[n], max_of_groups(top));
             const float f = __builtin_amdgcn_exp2f(w.m[n] - m);
             w.m[n] = m;
             w.l[n] *= f;
+            w.weight[n] *= f;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) w.o[n][i] *= f;
         }
+        bf16x8 rounded;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             p[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][e], scale, -w.m[n]));
             w.l[n] += p[n][e];
+            rounded[e] = (__bf16)p[n][e];
         }
+        w.weight[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, rounded, w.weight[n], 0, 0, 0);
     }
 #pragma unroll
     for (int b = 0; b < D / 32; ++b) {
@@ -142,11 +153,12 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT>& w, const Tile<D>& t, in
         for (int n = 0; n < NT; ++n) {
             bf16x8 ps;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float x = p[n][e] * vs[e];
+            for (int e = 0; e < 8; ++e) ps[e] = (__bf16)(p[n][e] * vs[e]);
+            if (masked) {
                 // (a token that a row does not see may have any scale byte, NaN among them)
-                if (kMasked && first_token + 16 * (e >> 2) + 4 * j + (e & 3) >= w.seen[n]) x = 0.f;
-                ps[e] = (__bf16)x;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (hidden[n] >> e & 1) ps[e] = (__bf16)0.f;
             }
             w.o[n][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, ps, w.o[n][2 * b], 0, 0, 0);
             w.o[n][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, ps, w.o[n][2 * b + 1], 0, 0, 0);
@@ -155,10 +167,10 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT>& w, const Tile<D>& t, in
 }
 
 template <int D, int NT>
-__global__ __launch_bounds__(64 * kWaves) void cache_attention_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : 2) void cache_attention_kernel(AttendArgs a) {
     constexpr int kRow = D + 4;                   // floats of a row in LDS
     __shared__ __align__(16) float results[kWaves][16][kRow];
-    __shared__ float stats[kWaves][NT][16][2];
+    __shared__ float stats[kWaves][NT][16][4];    // reference, sum, sum of the rounded
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane >> 4;
     const int hkv = a.c.n_kv_heads, g = a.n_q_heads / hkv, cols = a.n_tokens * g;
     // workgroup -> (sequence, split, column group, head): neighbours read neighbouring heads of the same pages
@@ -169,11 +181,16 @@ __global__ __launch_bounds__(64 * kWaves) void cache_attention_kernel(AttendArgs
     const int first_col = (id % col_groups) * (16 * NT);
     id /= col_groups;
     const int split = id % a.splits, b = id / a.splits;
+    const int begin = split * a.chunk;
 
+    // the wavefront's tiles: begin + wave, + kWaves, ...; lane l holds the page of the l-th of 64 (asked for together with the length)
     const int slot = cache_slot(a.c, a.slots, b);
+    const int32_t* row_pages = a.c.table + (int64_t)max(slot, 0) * a.c.max_pages;
+    const int tile_shift = a.c.shift - 5;
+    auto page_of = [&](int i) { return row_pages[min((begin + wave + (i + lane) * kWaves) >> tile_shift, a.c.max_pages - 1)]; };
+    int pages = page_of(0);
     const int len = slot < 0 ? 0 : cache_len(a.c, slot);
     const int tiles = (len + 31) >> 5;
-    const int begin = split * a.chunk;
     const int end = split == a.splits - 1 ? tiles : min(tiles, begin + a.chunk);
     if (a.splits > 1 && begin >= end && split > 0) return;           // (the join does not look at it)
 
@@ -185,6 +202,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_attention_kernel(AttendArgs
         w.seen[n] = len - a.n_tokens + 1 + token;
         w.m[n] = -FLT_MAX;
         w.l[n] = 0.f;
+        w.weight[n] = f32x4{0.f, 0.f, 0.f, 0.f};
         const uint16_t* row = a.q + (((int64_t)b * a.n_tokens + token) * a.n_q_heads + head * g + (col - token * g)) * D;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
@@ -196,19 +214,15 @@ __global__ __launch_bounds__(64 * kWaves) void cache_attention_kernel(AttendArgs
     }
     const int all_see = len - a.n_tokens + 1;                        // tokens below it are seen by every row
 
-    // the wavefront's tiles: begin + wave, + kWaves, ...; lane l holds the page of the l-th of 64
-    const int32_t* row_pages = a.c.table + (int64_t)max(slot, 0) * a.c.max_pages;
-    const int tile_shift = a.c.shift - 5;
     bool bad = false;
-    int pages = 0;
     const int count = max(0, (end - begin - wave + kWaves - 1) / kWaves);
     auto fetch = [&](Tile<D>& t, int i) {                            // (i goes up by one from call to call)
         if (i >= count) return;
         if ((i & 63) == 0) {
-            const int mine = begin + wave + (i + lane) * kWaves;
-            pages = mine < end ? row_pages[mine >> tile_shift] : 0;
-            bad |= __builtin_amdgcn_ballot_w64(pages < 0 || pages >= a.c.n_pages) != 0;
-            if (pages < 0 || pages >= a.c.n_pages) pages = 0;
+            if (i > 0) pages = page_of(i);
+            const bool outside = i + lane < count && (pages < 0 || pages >= a.c.n_pages);
+            bad |= __builtin_amdgcn_ballot_w64(outside) != 0;
+            if (outside) pages = 0;
         }
         const int page = __builtin_amdgcn_readlane(pages, i & 63);
         const int tile = begin + wave + i * kWaves;
@@ -216,8 +230,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_attention_kernel(AttendArgs
     };
     auto attend = [&](const Tile<D>& t, int i) {
         const int token = (begin + wave + i * kWaves) * 32;
-        if (token + 32 <= all_see) attend_tile<D, NT, false>(w, t, token, a.scale, lane);
-        else attend_tile<D, NT, true>(w, t, token, a.scale, lane);
+        attend_tile<D, NT>(w, t, token, token + 32 > all_see, a.scale, lane);
     };
     Tile<D> t0, t1;
     fetch(t0, 0);
@@ -235,10 +248,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_attention_kernel(AttendArgs
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         w.l[n] = bad ? NAN : sum_of_groups(w.l[n]);
-        if (j == 0) {
-            stats[wave][n][lane & 15][0] = w.m[n];
-            stats[wave][n][lane & 15][1] = w.l[n];
-        }
+        if (j == 0) *(f32x4*)stats[wave][n][lane & 15] = f32x4{w.m[n], w.l[n], bad ? NAN : w.weight[n][0], 0.f};
     }
     const int64_t rows = (int64_t)a.n_seqs * a.n_tokens * a.n_q_heads;
 #pragma unroll
@@ -256,20 +266,24 @@ __global__ __launch_bounds__(64 * kWaves) void cache_attention_kernel(AttendArgs
             const int r = i / (D / 4), c4 = i % (D / 4);
             const int col = first_col + 16 * n + r;
             if (col >= cols) continue;
-            float top = stats[0][n][r][0], sum = 0.f;
+            f32x4 st[kWaves];
 #pragma unroll
-            for (int v = 1; v < kWaves; ++v) top = fmaxf(top, stats[v][n][r][0]);
+            for (int v = 0; v < kWaves; ++v) st[v] = *(const f32x4*)stats[v][n][r];
+            float top = st[0][0], sum = 0.f, weight = 0.f;
+#pragma unroll
+            for (int v = 1; v < kWaves; ++v) top = fmaxf(top, st[v][0]);
             f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int v = 0; v < kWaves; ++v) {
-                const float f = __builtin_amdgcn_exp2f(stats[v][n][r][0] - top);
-                sum += f * stats[v][n][r][1];
+                const float f = __builtin_amdgcn_exp2f(st[v][0] - top);
+                sum += f * st[v][1];
+                weight += f * st[v][2];
                 o += f * *(const f32x4*)&results[v][r][4 * c4];
             }
             const int token = col / g;
             const int64_t at = ((int64_t)b * a.n_tokens + token) * a.n_q_heads + head * g + (col - token * g);
             if (a.splits == 1) {
-                const float f = sum == 0.f ? 0.f : 1.f / sum;
+                const float f = weight == 0.f ? 0.f : 1.f / weight;
                 bf16x4 y;
 #pragma unroll
                 for (int x = 0; x < 4; ++x) y[x] = (__bf16)(o[x] * f);
@@ -278,58 +292,84 @@ __global__ __launch_bounds__(64 * kWaves) void cache_attention_kernel(AttendArgs
             } else {
                 const int64_t part = split * rows + at;
                 *(f32x4*)((float*)a.out + part * D + 4 * c4) = o;
-                if (c4 == 0) {
-                    a.lse[2 * part] = top;
-                    a.lse[2 * part + 1] = sum;
-                }
+                if (c4 == 0) *(f32x4*)(a.lse + 4 * part) = f32x4{top, sum, weight, 0.f};
             }
         }
         __syncthreads();
     }
 }
 
-// The splits of a row, weighted by 2^(reference - largest) and added up: one wavefront a row.
+// The splits of a row, weighted by 2^(reference - largest) and added up: one workgroup a row, D / 4 threads a split.
+struct JoinArgs {
+    CacheView c;
+    const int32_t* slots;
+    const float* parts;
+    const f32x4* stats;
+    uint16_t* out;
+    float* lse;
+    int32_t rows, rows_of_seq, chunk, splits;
+};
+static_assert(sizeof(JoinArgs) <= 112, "short arguments");
+
 template <int D>
-__global__ __launch_bounds__(256) void cache_join_kernel(CacheView c, const int32_t* __restrict__ slots, const float* __restrict__ parts,
-                                                         const float* __restrict__ stats, uint16_t* __restrict__ out, float* __restrict__ lse,
-                                                         int64_t rows, int rows_of_seq, int chunk, int splits) {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const int slot = cache_slot(c, slots, (int)(row / rows_of_seq));
-    const int tiles = slot < 0 ? 0 : (cache_len(c, slot) + 31) >> 5;
-    const int live = min(splits, max(1, (tiles + chunk - 1) / chunk));
+__global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs a) {
+    constexpr int kQuads = D / 4, kSets = 256 / kQuads;
+    __shared__ float tops[4];
+    __shared__ f32x4 sums[kSets][kQuads];
+    __shared__ float weights[kSets][2];
+    const int row = blockIdx.x, set = threadIdx.x / kQuads, quad = threadIdx.x % kQuads;
+    const int slot = cache_slot(a.c, a.slots, row / a.rows_of_seq);
+    const int tiles = slot < 0 ? 0 : (cache_len(a.c, slot) + 31) >> 5;
+    const int live = min(a.splits, max(1, (tiles + a.chunk - 1) / a.chunk));
     float top = -FLT_MAX;
-    for (int s = lane; s < live; s += 64) top = fmaxf(top, stats[2 * (s * rows + row)]);
+    for (int s = threadIdx.x; s < live; s += 256) top = fmaxf(top, a.stats[(int64_t)s * a.rows + row][0]);
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-    float sum = 0.f;
-    float o[D / 64] = {};
-    for (int s = 0; s < live; ++s) {
-        const int64_t at = s * rows + row;
-        const float f = __builtin_amdgcn_exp2f(stats[2 * at] - top);
-        sum += f * stats[2 * at + 1];
-#pragma unroll
-        for (int x = 0; x < D / 64; ++x) o[x] += f * parts[at * D + (D / 64) * lane + x];
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    float sum = 0.f, weight = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = set; s < live; s += kSets) {
+        const int64_t at = (int64_t)s * a.rows + row;
+        const f32x4 st = a.stats[at];
+        const float f = __builtin_amdgcn_exp2f(st[0] - top);
+        sum += f * st[1];
+        weight += f * st[2];
+        o += f * *(const f32x4*)(a.parts + at * D + 4 * quad);
     }
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
-    if (D == 128) *(bf16x2*)(out + row * D + 2 * lane) = bf16x2{(__bf16)(o[0] * f), (__bf16)(o[D / 64 - 1] * f)};
-    else *(__bf16*)(out + row * D + lane) = (__bf16)(o[0] * f);
-    if (lse != nullptr && lane == 0) lse[row] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+    sums[set][quad] = o;
+    if (quad == 0) {
+        weights[set][0] = sum;
+        weights[set][1] = weight;
+    }
+    __syncthreads();
+    if (set != 0) return;
+#pragma unroll
+    for (int x = 1; x < kSets; ++x) {
+        o += sums[x][quad];
+        sum += weights[x][0];
+        weight += weights[x][1];
+    }
+    const float f = weight == 0.f ? 0.f : 1.f / weight;
+    bf16x4 y;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) y[x] = (__bf16)(o[x] * f);
+    *(bf16x4*)(a.out + (int64_t)row * D + 4 * quad) = y;
+    if (a.lse != nullptr && quad == 0) a.lse[row] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
 }
 
 template <int D>
 int launch(const CacheAttention& x, const CacheView& c, const AttendArgs& a, void* out, float* lse, hipStream_t stream) {
     const int64_t grid = (int64_t)a.n_seqs * a.splits * x.col_groups * c.n_kv_heads;
     if (x.col_tiles == 1) hipLaunchKernelGGL((cache_attention_kernel<D, 1>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
-    else if (x.col_tiles == 2) hipLaunchKernelGGL((cache_attention_kernel<D, 2>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
-    else hipLaunchKernelGGL((cache_attention_kernel<D, 4>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
-    int rc = check_launch();
+    else hipLaunchKernelGGL((cache_attention_kernel<D, 2>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
+    const int rc = check_launch();
     if (rc != PYR_OK || a.splits == 1) return rc;
-    const int rows_of_seq = a.n_tokens * a.n_q_heads;
-    const int64_t rows = (int64_t)a.n_seqs * rows_of_seq;
-    hipLaunchKernelGGL(cache_join_kernel<D>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, c, a.slots, (const float*)a.out, (const float*)a.lse,
-                       (uint16_t*)out, lse, rows, rows_of_seq, a.chunk, a.splits);
+    const int32_t rows_of_seq = a.n_tokens * a.n_q_heads, rows = a.n_seqs * rows_of_seq;
+    const JoinArgs j{c, a.slots, (const float*)a.out, (const f32x4*)a.lse, (uint16_t*)out, lse, rows, rows_of_seq, a.chunk, a.splits};
+    hipLaunchKernelGGL(cache_join_kernel<D>, dim3((unsigned)rows), dim3(256), 0, stream, j);
     return check_launch();
 }
 
@@ -339,10 +379,10 @@ CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_
     CacheAttention x{};
     const int cols = n_tokens * (n_q_heads / n_kv_heads);
     const int tiles = (cols + 15) / 16;
-    x.col_tiles = tiles == 1 ? 1 : tiles == 2 ? 2 : 4;
+    x.col_tiles = tiles == 1 ? 1 : 2;
     x.col_groups = (tiles + x.col_tiles - 1) / x.col_tiles;
     const int64_t units = (int64_t)n_seqs * n_kv_heads * x.col_groups, key_tiles = (max_len + 31) / 32;
-    constexpr int64_t kWorkgroups = 1024, kShortest = 8;
+    constexpr int64_t kWorkgroups = 512, kShortest = 16;
     int64_t splits = units > 0 ? (kWorkgroups + units - 1) / units : 1;
     int64_t chunk = splits > 0 ? (key_tiles + splits - 1) / splits : key_tiles;
     if (chunk < kShortest) chunk = kShortest;
@@ -352,7 +392,7 @@ CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_
     x.splits = splits < 1 ? 1 : (int32_t)splits;
     const int64_t rows = (int64_t)n_seqs * n_tokens * n_q_heads;
     x.part_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * head_dim * sizeof(float);
-    x.stat_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * 2 * sizeof(float);
+    x.stat_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * 4 * sizeof(float);
     return x;
 }
 

@@ -13,6 +13,7 @@ constexpr int kMaxRows = kMaxCacheRows, kMaxSlots = kMaxCacheSlots;
 
 struct Shared {
     int32_t first[kMaxRows + 1];          // pages that the rows before a row ask for
+    int32_t entry[kMaxRows];              // where a row's next page goes, as an entry of the table
     uint32_t seen[kMaxSlots / 32];        // slots that a row names
     int32_t waves[kWaves];
     int32_t status;
@@ -51,15 +52,19 @@ __device__ __forceinline__ void clear(Shared& s, const CacheView& c) {
 
 __device__ __forceinline__ void refuse(Shared& s, int status) { atomicMin(&s.status, status); }      // (the lowest of a call's codes is kept)
 
-// need(i) -> pages that row i asks for (their sum fits an int: n * max_pages does); fills s.first.  Returns the sum.
+// need(i, entry) -> pages that row i asks for (their sum fits an int: n * max_pages does), the first of them to become that entry of the table.
+// Returns the sum.
 template <typename Need>
 __device__ __forceinline__ int sum_needs(Shared& s, int n, Need need) {
     int all = 0;
     for (int base = 0; base < n; base += kThreads) {
         const int i = base + threadIdx.x;
-        int total;
-        const int before = scan(s, i < n ? need(i) : 0, &total);
-        if (i < n) s.first[i] = all + before;
+        int total, entry = 0;
+        const int before = scan(s, i < n ? need(i, &entry) : 0, &total);
+        if (i < n) {
+            s.first[i] = all + before;
+            s.entry[i] = entry;
+        }
         all += total;
     }
     if (threadIdx.x == 0) s.first[n] = all;
@@ -77,9 +82,8 @@ __device__ __forceinline__ int row_of_rank(const Shared& s, int n, int rank) {  
     return lo;
 }
 
-// The lowest `need` free pages become pages place(rank) of the table, with a count of one.  Returns how many are lacking; then none is taken.
-template <typename Place>
-__device__ __forceinline__ int hand_out(Shared& s, const CacheView& c, int need, Place place) {
+// The lowest `need` free pages go to the rows, with a count of one.  Returns how many are lacking; then none is taken.
+__device__ __forceinline__ int hand_out(Shared& s, const CacheView& c, int n, int need) {
     constexpr int kEach = 16;
     int found = 0;
     for (int base = 0; base < c.n_pages && found < need; base += kThreads * kEach) {
@@ -98,17 +102,22 @@ __device__ __forceinline__ int hand_out(Shared& s, const CacheView& c, int need,
         }
         int total;
         int rank = found + scan(s, __popc(free), &total);
-        for (; free != 0 && rank < need; free &= free - 1, ++rank) {
-            const int page = p0 + __ffs(free) - 1;
-            *place(rank) = page;
-            c.refs[page] = 1;
+        if (free != 0 && rank < need) {
+            int row = row_of_rank(s, n, rank);
+            for (; free != 0 && rank < need; free &= free - 1, ++rank) {
+                while (s.first[row + 1] <= rank) ++row;
+                const int page = p0 + __ffs(free) - 1;
+                c.table[s.entry[row] + (rank - s.first[row])] = page;
+                c.refs[page] = 1;
+            }
         }
         found += total;
     }
     if (found >= need) return 0;
     __syncthreads();
     for (int rank = threadIdx.x; rank < found; rank += kThreads) {
-        int32_t* at = place(rank);
+        const int row = row_of_rank(s, n, rank);
+        int32_t* at = &c.table[s.entry[row] + (rank - s.first[row])];
         c.refs[*at] = 0;
         *at = -1;
     }
@@ -123,7 +132,7 @@ __global__ __launch_bounds__(kThreads) void cache_reserve_kernel(CacheView c, co
     __shared__ Shared s;
     clear(s, c);
     const int64_t most = (int64_t)c.max_pages << c.shift;
-    auto need = [&](int i) -> int {
+    auto need = [&](int i, int* entry) -> int {
         const int slot = slots[i];
         if (slot == -1) return 0;
         if (slot < 0 || slot >= c.n_slots) {
@@ -136,15 +145,12 @@ __global__ __launch_bounds__(kThreads) void cache_reserve_kernel(CacheView c, co
             refuse(s, PYR_CACHE_BAD_COUNT);
             return 0;
         }
+        *entry = slot * c.max_pages + pages_of(c, old);
         return pages_of(c, old + more) - pages_of(c, old);
     };
     const int all = sum_needs(s, n, need);
     int state = s.status;
-    if (state == 0)
-        state = hand_out(s, c, all, [&](int rank) -> int32_t* {
-            const int i = row_of_rank(s, n, rank), slot = slots[i];
-            return c.table + (int64_t)slot * c.max_pages + pages_of(c, cache_len(c, slot)) + (rank - s.first[i]);
-        });
+    if (state == 0) state = hand_out(s, c, n, all);
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const int slot = slots[i];
@@ -161,25 +167,23 @@ __global__ __launch_bounds__(kThreads) void cache_fork_kernel(CacheView c, const
     __shared__ Shared s;
     clear(s, c);
     const int part = (1 << c.shift) - 1;
-    auto need = [&](int i) -> int {
+    auto need = [&](int i, int* entry) -> int {
         const int parent = parents[i], child = children[i];
         if (parent == -1 && child == -1) return 0;
         if (parent < 0 || parent >= c.n_slots || child < 0 || child >= c.n_slots || c.lens[child] != 0 || !claim(s, child)) {
             refuse(s, PYR_CACHE_BAD_SLOT);
             return 0;
         }
-        return (cache_len(c, parent) & part) != 0 ? 1 : 0;
+        const int len = cache_len(c, parent);
+        *entry = child * c.max_pages + (len >> c.shift);
+        return (len & part) != 0 ? 1 : 0;
     };
     const int all = sum_needs(s, n, need);
     for (int i = threadIdx.x; i < n; i += kThreads)
         if (parents[i] >= 0 && parents[i] < c.n_slots && (s.seen[parents[i] >> 5] >> (parents[i] & 31) & 1) != 0) refuse(s, PYR_CACHE_BAD_SLOT);
     __syncthreads();
     int state = s.status;
-    if (state == 0)
-        state = hand_out(s, c, all, [&](int rank) -> int32_t* {
-            const int i = row_of_rank(s, n, rank);
-            return c.table + (int64_t)children[i] * c.max_pages + (cache_len(c, parents[i]) >> c.shift);
-        });
+    if (state == 0) state = hand_out(s, c, n, all);
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kThreads)
         if (state == 0 && children[i] >= 0) c.lens[children[i]] = cache_len(c, parents[i]);
@@ -236,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void cache_cut_kernel(CacheView c, const 
     __shared__ Shared s;
     clear(s, c);
     const int64_t most = min((int64_t)max_keep, (int64_t)c.max_pages << c.shift);
-    auto need = [&](int i) -> int {
+    auto need = [&](int i, int* entry) -> int {
         const int slot = slots[i];
         if (slot == -1) return 0;
         if (slot < 0 || slot >= c.n_slots) {
@@ -249,6 +253,7 @@ __global__ __launch_bounds__(kThreads) void cache_cut_kernel(CacheView c, const 
             refuse(s, PYR_CACHE_BAD_COUNT);
             return 0;
         }
+        *entry = slot * c.max_pages;
         return pages_of(c, to - at);
     };
     const int all = sum_needs(s, n, need);
@@ -263,10 +268,7 @@ __global__ __launch_bounds__(kThreads) void cache_cut_kernel(CacheView c, const 
             old_rows[x] = at == 0 ? len : at <= pages_of(c, len) ? c.table[(int64_t)slot * c.max_pages + at - 1] : -1;
         }
         __syncthreads();
-        state = hand_out(s, c, all, [&](int rank) -> int32_t* {
-            const int i = row_of_rank(s, n, rank);
-            return c.table + (int64_t)slots[i] * c.max_pages + (rank - s.first[i]);
-        });
+        state = hand_out(s, c, n, all);
         __syncthreads();
         for (int x = threadIdx.x; x < entries; x += kThreads) {
             const int i = x / stride, at = x - i * stride, slot = slots[i];
