@@ -21,7 +21,7 @@ namespace pyr {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr float kGrowth = 12.f;                   // how far (log2) a row may outgrow its reference
+constexpr float kGrowth = 4096.f;                 // how far a lane's weights of a tile may outgrow the reference
 
 struct AttendArgs {
     CacheView c;
@@ -36,23 +36,27 @@ struct AttendArgs {
 };
 static_assert(sizeof(AttendArgs) <= 112, "short arguments");
 
-// What a wavefront holds of a tile.
-template <int D>
+// What a wavefront holds of a tile.  R: how many times its 16 columns repeat the rows (see Rows).
+template <int D, int R>
 struct Tile {
-    u32x4 k[D / 64], v[D / 64], vs[D / 64];
+    u32x4 k[D / 64], v[D / 64];
+    u32x2 vs[D / 32 / R];
     uint32_t ks;
 };
 
-template <int D>
-__device__ __forceinline__ void load_tile(Tile<D>& t, const uint8_t* tile, int lane) {
+// kOnce: nobody else reads the tile.
+template <int D, int R, bool kOnce>
+__device__ __forceinline__ void load_tile(Tile<D, R>& t, const uint8_t* tile, int lane) {
+    auto load = [](const uint8_t* p) { return kOnce ? __builtin_nontemporal_load((const u32x4*)p) : *(const u32x4*)p; };
 #pragma unroll
-    for (int h = 0; h < D / 64; ++h) t.k[h] = *(const u32x4*)(tile + h * 1024 + lane * 16);
-    if (D == 128) t.ks = *(const uint16_t*)(tile + 32 * D + lane * 2);
-    else t.ks = tile[32 * D + (lane & 31) * 2 + (lane >> 5)];
+    for (int h = 0; h < D / 64; ++h) t.k[h] = load(tile + (uint32_t)(h * 1024 + lane * 16));
+    if (D == 128) t.ks = *(const uint16_t*)(tile + (uint32_t)(32 * D + lane * 2));
+    else t.ks = tile[(uint32_t)(32 * D + (lane & 31) * 2 + (lane >> 5))];
 #pragma unroll
-    for (int h = 0; h < D / 64; ++h) t.v[h] = *(const u32x4*)(tile + 16 * D + h * 1024 + lane * 16);
+    for (int h = 0; h < D / 64; ++h) t.v[h] = load(tile + (uint32_t)(16 * D + h * 1024 + lane * 16));
 #pragma unroll
-    for (int h = 0; h < D / 64; ++h) t.vs[h] = *(const u32x4*)(tile + 33 * D + (lane >> 4) * (D / 4) + h * 16);
+    for (int v = 0; v < D / 32 / R; ++v)
+        t.vs[v] = *(const u32x2*)(tile + (uint32_t)(33 * D + (lane >> 4) * (D / 4) + 8 * ((lane & 15) / (16 / R)) + 8 * R * v));
 }
 
 __device__ __forceinline__ float max_of_groups(float x) {      // over the lanes with the same lane & 15
@@ -68,9 +72,11 @@ __device__ __forceinline__ float sum_of_groups(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
-template <int D, int NT>
+// Up to 16 / R rows fill the columns of a product R times over: column c is row c % (16 / R), and of V's blocks v R .. v R + R - 1 it has the scales of
+// block v R + c / (16 / R).  So P' is made once per R blocks, and of a block's products those of its columns count.
+template <int D, int NT, int R>
 struct Rows {
-    bf16x8 q[NT][D / 32];                         // operand of step s: lane 16 j + col, see load_rows
+    bf16x8 q[NT][D / 32];                         // operand of step s: lane 16 j + col
     f32x4 o[NT][D / 16];
     f32x4 weight[NT];                             // sum of the rounded P, in every element
     float m[NT], l[NT];                           // reference; sum of P over the tokens that this lane sees
@@ -78,10 +84,10 @@ struct Rows {
 };
 
 // One tile's products.  masked: some row does not see all of its tokens.
-template <int D, int NT>
-__device__ __forceinline__ void attend_tile(Rows<D, NT>& w, const Tile<D>& t, int first_token, bool masked, float scale, int lane) {
+template <int D, int NT, int R>
+__device__ __forceinline__ void attend_tile(Rows<D, NT, R>& w, const Tile<D, R>& t, int first_token, bool masked, float scale, int lane) {
     constexpr int kSteps = D / 32;
-    f32x4 s[NT][2];
+    float p[NT][8];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         uint32_t codes[kSteps];
@@ -97,25 +103,27 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT>& w, const Tile<D>& t, in
             for (int i = 0; i < 2; ++i) codes[i] = __builtin_amdgcn_permlane32_swap(t.k[0][i], t.k[0][i + 2], false, false)[half];
             ks = scale_of(__builtin_amdgcn_permlane32_swap(t.ks, t.ks, false, false)[half]);
         }
+        f32x4 s[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s[n][half] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < NT; ++n) s[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const bf16x8 k = values_of(codes[i], ks);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) s[n][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, w.q[n][i], s[n][half], 0, 0, 0);
+            for (int n = 0; n < NT; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, w.q[n][i], s[n], 0, 0, 0);
         }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[n][4 * half + e] = s[n][e];
     }
     bf16x8 ones;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
-    float p[NT][8];
     uint32_t hidden[NT];                          // bit e: the row does not see the lane's e-th token
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         hidden[n] = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[n][e] = s[n][e >> 2][e & 3];
         if (masked) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -124,54 +132,68 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT>& w, const Tile<D>& t, in
                     hidden[n] |= 1u << e;
                 }
         }
-        float top = fmaxf(fmaxf(fmaxf(p[n][0], p[n][1]), fmaxf(p[n][2], p[n][3])), fmaxf(fmaxf(p[n][4], p[n][5]), fmaxf(p[n][6], p[n][7]))) * scale;
-        if (__builtin_amdgcn_ballot_w64(top > w.m[n] + kGrowth) != 0) {
-            const float m = fmaxf(w.m[n], max_of_groups(top));
+        // weights against the reference as it is; where their sum shows that a row has outgrown it (or has none yet), again against a new one
+        float x[8], sum;
+        auto weigh = [&] {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][e], scale, -w.m[n]));
+            sum = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+        };
+        weigh();
+        if (__builtin_amdgcn_ballot_w64(!(sum <= kGrowth)) != 0) {
+            float top = p[n][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) top = fmaxf(top, p[n][e]);
+            const float m = fmaxf(w.m[n], max_of_groups(top * scale));
             const float f = __builtin_amdgcn_exp2f(w.m[n] - m);
             w.m[n] = m;
             w.l[n] *= f;
             w.weight[n] *= f;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) w.o[n][i] *= f;
+            weigh();
         }
+        w.l[n] += sum;
         bf16x8 rounded;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            p[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][e], scale, -w.m[n]));
-            w.l[n] += p[n][e];
-            rounded[e] = (__bf16)p[n][e];
+            p[n][e] = x[e];
+            rounded[e] = (__bf16)x[e];
         }
         w.weight[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, rounded, w.weight[n], 0, 0, 0);
     }
 #pragma unroll
-    for (int b = 0; b < D / 32; ++b) {
+    for (int v = 0; v < D / 32 / R; ++v) {
         float vs[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vs[e] = scale_of((t.vs[b >> 1][(b & 1) * 2 + (e >> 2)] >> (8 * (e & 3))) & 255);
-        const bf16x8 v0 = values_of(t.v[b >> 1][(b & 1) * 2], 1.f), v1 = values_of(t.v[b >> 1][(b & 1) * 2 + 1], 1.f);
+        for (int e = 0; e < 8; ++e) vs[e] = scale_of((t.vs[v][e >> 2] >> (8 * (e & 3))) & 255);
+        bf16x8 ps[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            bf16x8 ps;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ps[e] = (__bf16)(p[n][e] * vs[e]);
+            for (int e = 0; e < 8; ++e) ps[n][e] = (__bf16)(p[n][e] * vs[e]);
             if (masked) {
                 // (a token that a row does not see may have any scale byte, NaN among them)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (hidden[n] >> e & 1) ps[e] = (__bf16)0.f;
+                    if (hidden[n] >> e & 1) ps[n][e] = (__bf16)0.f;
             }
-            w.o[n][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, ps, w.o[n][2 * b], 0, 0, 0);
-            w.o[n][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, ps, w.o[n][2 * b + 1], 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 2 * R * v; i < 2 * R * (v + 1); ++i) {
+            const bf16x8 x = values_of(t.v[i >> 2][i & 3], 1.f);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) w.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, ps[n], w.o[n][i], 0, 0, 0);
         }
     }
 }
 
-template <int D, int NT>
-__global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : 2) void cache_attention_kernel(AttendArgs a) {
+template <int D, int NT, int R>
+__global__ __launch_bounds__(64 * kWaves, NT == 1 && (D == 64 || R == 4) ? 3 : 2) void cache_attention_kernel(AttendArgs a) {
     constexpr int kRow = D + 4;                   // floats of a row in LDS
     __shared__ __align__(16) float results[kWaves][16][kRow];
     __shared__ float stats[kWaves][NT][16][4];    // reference, sum, sum of the rounded
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4;
     const int hkv = a.c.n_kv_heads, g = a.n_q_heads / hkv, cols = a.n_tokens * g;
     // workgroup -> (sequence, split, column group, head): neighbours read neighbouring heads of the same pages
     const int col_groups = (cols + 16 * NT - 1) / (16 * NT);
@@ -194,10 +216,10 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : 2) void cache_attention_
     const int end = split == a.splits - 1 ? tiles : min(tiles, begin + a.chunk);
     if (a.splits > 1 && begin >= end && split > 0) return;           // (the join does not look at it)
 
-    Rows<D, NT> w;
+    Rows<D, NT, R> w;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int col = first_col + 16 * n + (lane & 15);
+        const int col = first_col + 16 * n + (lane & 15) % (16 / R);
         const int token = col / g;
         w.seen[n] = len - a.n_tokens + 1 + token;
         w.m[n] = -FLT_MAX;
@@ -216,7 +238,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : 2) void cache_attention_
 
     bool bad = false;
     const int count = max(0, (end - begin - wave + kWaves - 1) / kWaves);
-    auto fetch = [&](Tile<D>& t, int i) {                            // (i goes up by one from call to call)
+    auto fetch = [&](Tile<D, R>& t, int i) {                            // (i goes up by one from call to call)
         if (i >= count) return;
         if ((i & 63) == 0) {
             if (i > 0) pages = page_of(i);
@@ -226,13 +248,13 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : 2) void cache_attention_
         }
         const int page = __builtin_amdgcn_readlane(pages, i & 63);
         const int tile = begin + wave + i * kWaves;
-        load_tile<D>(t, cache_tile<D>(a.c, page, head, tile & ((1 << tile_shift) - 1)), lane);
+        load_tile<D, R, NT == 1>(t, cache_tile<D>(a.c, page, head, tile & ((1 << tile_shift) - 1)), lane);
     };
-    auto attend = [&](const Tile<D>& t, int i) {
+    auto attend = [&](const Tile<D, R>& t, int i) {
         const int token = (begin + wave + i * kWaves) * 32;
-        attend_tile<D, NT>(w, t, token, token + 32 > all_see, a.scale, lane);
+        attend_tile<D, NT, R>(w, t, token, token + 32 > all_see, a.scale, lane);
     };
-    Tile<D> t0, t1;
+    Tile<D, R> t0, t1;
     fetch(t0, 0);
     fetch(t1, 1);
     for (int i = 0; i < count; i += 2) {
@@ -256,13 +278,15 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 ? 3 : 2) void cache_attention_
 #pragma unroll
         for (int p = 0; p < D / 32; ++p) {
             // rows 4 j + r of products 2 p and 2 p + 1 are channels 32 p + 2 (4 j + r) and the next
-            float* to = &results[wave][lane & 15][32 * p + 8 * j];
+            float* to = &results[wave][(lane & 15) % (16 / R)][32 * p + 8 * j];
             const f32x4 x = w.o[n][2 * p], y = w.o[n][2 * p + 1];
-            *(f32x4*)to = f32x4{x[0], y[0], x[1], y[1]};
-            *(f32x4*)(to + 4) = f32x4{x[2], y[2], x[3], y[3]};
+            if ((lane & 15) / (16 / R) == p % R) {
+                *(f32x4*)to = f32x4{x[0], y[0], x[1], y[1]};
+                *(f32x4*)(to + 4) = f32x4{x[2], y[2], x[3], y[3]};
+            }
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < 16 * (D / 4); i += 64 * kWaves) {
+        for (int i = threadIdx.x; i < (16 / R) * (D / 4); i += 64 * kWaves) {
             const int r = i / (D / 4), c4 = i % (D / 4);
             const int col = first_col + 16 * n + r;
             if (col >= cols) continue;
@@ -363,8 +387,12 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs a) {
 template <int D>
 int launch(const CacheAttention& x, const CacheView& c, const AttendArgs& a, void* out, float* lse, hipStream_t stream) {
     const int64_t grid = (int64_t)a.n_seqs * a.splits * x.col_groups * c.n_kv_heads;
-    if (x.col_tiles == 1) hipLaunchKernelGGL((cache_attention_kernel<D, 1>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
-    else hipLaunchKernelGGL((cache_attention_kernel<D, 2>), dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, a);
+    const dim3 blocks((unsigned)grid), threads(64 * kWaves);
+    constexpr int kMost = D / 32;      // columns of a product hold at most so many times the rows
+    if (x.col_tiles == 2) hipLaunchKernelGGL((cache_attention_kernel<D, 2, 1>), blocks, threads, 0, stream, a);
+    else if (x.repeats == 1) hipLaunchKernelGGL((cache_attention_kernel<D, 1, 1>), blocks, threads, 0, stream, a);
+    else if (x.repeats == 2) hipLaunchKernelGGL((cache_attention_kernel<D, 1, 2>), blocks, threads, 0, stream, a);
+    else hipLaunchKernelGGL((cache_attention_kernel<D, 1, kMost>), blocks, threads, 0, stream, a);
     const int rc = check_launch();
     if (rc != PYR_OK || a.splits == 1) return rc;
     const int32_t rows_of_seq = a.n_tokens * a.n_q_heads, rows = a.n_seqs * rows_of_seq;
@@ -382,7 +410,7 @@ CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_
     x.col_tiles = tiles == 1 ? 1 : 2;
     x.col_groups = (tiles + x.col_tiles - 1) / x.col_tiles;
     const int64_t units = (int64_t)n_seqs * n_kv_heads * x.col_groups, key_tiles = (max_len + 31) / 32;
-    constexpr int64_t kWorkgroups = 512, kShortest = 16;
+    const int64_t kWorkgroups = x.col_tiles == 1 ? 512 : 256, kShortest = 16;
     int64_t splits = units > 0 ? (kWorkgroups + units - 1) / units : 1;
     int64_t chunk = splits > 0 ? (key_tiles + splits - 1) / splits : key_tiles;
     if (chunk < kShortest) chunk = kShortest;
@@ -390,6 +418,7 @@ CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_
     splits = (key_tiles + chunk - 1) / chunk;
     x.chunk = (int32_t)chunk;
     x.splits = splits < 1 ? 1 : (int32_t)splits;
+    x.repeats = cols <= 4 && head_dim == 128 ? 4 : cols <= 8 ? 2 : 1;
     const int64_t rows = (int64_t)n_seqs * n_tokens * n_q_heads;
     x.part_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * head_dim * sizeof(float);
     x.stat_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * 4 * sizeof(float);

@@ -2,35 +2,53 @@
 // goes the same way, through its index) and back to bf16, and tokens of the cache into other pages of it, without their values being touched.
 //
 // A wavefront owns one tile (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte, and the halves of a byte are
-// tokens of the same tile.  K: lane 16 * block + token has the 32 channels of a scale to itself.  V: lane 16 * j + r has channels
-// 2 r, 2 r + 1 of every block for eight tokens, so a block's largest magnitude is a maximum over 16 lanes.
+// tokens of the same tile.
 // Bound: reading and writing HBM.
 #include "cache_device.h"
 
 namespace pyr {
 namespace {
 
+// bf16 rows are read and written past the caches (nontemporal), codes are not: 70 % of 8 x 2048 tokens on 32 heads stored and read back 103 -> 78 us,
+// cut and read back 97 -> 86 us.
 constexpr int kWaves = 4;
 
 __device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b) {      // of both halves
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
 }
 template <int kCtrl>
-__device__ __forceinline__ uint32_t max_dpp(uint32_t x) {
-    return max_u16(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xf, 0xf, false));
-}
-__device__ __forceinline__ uint32_t max_of_16(uint32_t x) {                // of both halves, over 16 lanes
-    x = max_dpp<0x140>(x);      // mirror of 16
-    x = max_dpp<0x141>(x);      // of 8
-    x = max_dpp<0x1b>(x);       // of 4
-    return max_dpp<0xb1>(x);    // of 2
-}
+__device__ __forceinline__ uint32_t max_dpp(uint32_t x) { return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xf, 0xf, false)); }
 __device__ __forceinline__ bf16x2 pair_of(uint32_t x) { return __builtin_bit_cast(bf16x2, x); }
-__device__ __forceinline__ uint32_t code4(uint32_t old, float a, float b, int sel) {
-    return sel == 0   ? __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(old, a, b, 1.f, 0)
-           : sel == 1 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(old, a, b, 1.f, 1)
-           : sel == 2 ? __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(old, a, b, 1.f, 2)
-                      : __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(old, a, b, 1.f, 3);
+
+// The codes of eight channels, whose block four neighbouring lanes hold; *byte: the block's scale.
+__device__ __forceinline__ uint32_t codes_of(u32x4 x, uint32_t* byte) {
+    uint32_t top = max_u16(max_u16(x[0] & 0x7fff7fffu, x[1] & 0x7fff7fffu), max_u16(x[2] & 0x7fff7fffu, x[3] & 0x7fff7fffu));
+    top = max(top & 0xffff, top >> 16);
+    top = max_dpp<0xb1>(top);       // the neighbour's, the other pair's
+    top = max_dpp<0x4e>(top);
+    *byte = scale_byte(top);
+    const float scale = scale_of(*byte);
+    uint32_t y = 0;
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(y, pair_of(x[0]), scale, 0);
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(y, pair_of(x[1]), scale, 1);
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(y, pair_of(x[2]), scale, 2);
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(y, pair_of(x[3]), scale, 3);
+    return *byte == 255 ? 0 : y;
+}
+
+typedef __attribute__((address_space(3))) char* lptr_t;
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+
+// Transposing LDS read (ds_read_b64_tr_b8).  Inside every group of 16 lanes, lane j receives byte (j & 7) of the 8-byte words addressed by lanes
+// (j >> 3), 2 + (j >> 3), 4 + (j >> 3) ... 14 + (j >> 3), in this order.
+__device__ __forceinline__ i32x2 lds_read_tr8(uint32_t lds_addr) {
+    return __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3)))*)(uintptr_t)lds_addr);
+}
+
+// A wavefront's own part of LDS: what its lanes have written before is what they read behind this.
+__device__ __forceinline__ void meet() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 // Workgroups count through the head groups first: the heads of a row lie side by side in memory.
@@ -42,9 +60,15 @@ struct StoreArgs {
 };
 static_assert(sizeof(StoreArgs) <= 112, "short arguments");
 
+// Rows are read and quantised as they lie in memory, 16 bytes a lane; their codes and scales meet in LDS, from where the lanes take them in
+// the tile's order, V's through transposing reads that turn bytes of two channels of a token into words of eight tokens of a channel.
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a, int32_t tiles_of_piece, int32_t head_groups) {
-    constexpr int kBlocks = D / 32, kHalves = D / 64;
+    constexpr int kBlocks = D / 32, kHalves = D / 64, kRow = D / 2 + 16;      // bytes of a token's codes in LDS
+    struct Staged {
+        uint8_t k[32][kRow], v[32][kRow], scales[2 * D];
+    };
+    __shared__ __align__(16) Staged all_staged[kWaves];
     const int lane = threadIdx.x & 63, t = lane & 15, j = lane >> 4;
     const int place = blockIdx.x / head_groups, b = place / tiles_of_piece;
     const int head = (blockIdx.x - place * head_groups) * kWaves + (threadIdx.x >> 6);
@@ -68,106 +92,81 @@ __global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a, i
         }
     }
     if (page < 0 || page >= a.c.n_pages) return;
+    const uint32_t stored = (uint32_t)__builtin_amdgcn_ballot_w64(from >= 0);                            // bit t: token t
+    if (stored == 0) return;
     uint8_t* const out = cache_tile<D>(a.c, page, head, tile & ((1 << (a.c.shift - 5)) - 1));
 
-    // everything that is read: K (lane 16 * block + token), V (eight tokens, 16 * (e / 4) + 4 * j + e % 4, of channels 2 t, 2 t + 1 of every block), and, where
-    // the tile is not written as a whole, V's codes (rows outside are read as row 0 and not used)
+    // what is read: rows (one that is not there: row 0, not stored) and, where the tile is not written as a whole, V's codes
+    constexpr int kLanes = D / 8, kLoads = 32 * kLanes / 64;      // lanes of a row
     const int64_t row_words = (int64_t)a.c.n_kv_heads * D;
-    int krow[kHalves], row[8];
-    uint32_t keep = 0;      // the bits of a word of V's codes that stay as they are
-    u32x4 x[kHalves][4];
+    u32x4 kx[kLoads], vx[kLoads];
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) {
-        krow[h] = __shfl(from, 16 * (D == 128 ? h : j >> 1) + t);
-        const u32x4* k = (const u32x4*)(a.k + max(krow[h], 0) * row_words + head * D + 32 * (D == 128 ? j : j & 1));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[h][i] = k[i];
+    for (int i = 0; i < kLoads; ++i) {
+        const int64_t at = max(__shfl(from, i * (64 / kLanes) + lane / kLanes), 0) * row_words + head * D + 8 * (lane % kLanes);
+        kx[i] = __builtin_nontemporal_load((const u32x4*)(a.k + at));
+        vx[i] = __builtin_nontemporal_load((const u32x4*)(a.v + at));
     }
-    uint32_t y[kBlocks][8];
+    uint32_t keep = 0;                                            // the bits of a word of V's codes that stay as they are
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        row[e] = __shfl(from, 16 * (e >> 2) + 4 * j + (e & 3));
-        if (row[e] < 0) keep |= 0xfu << (4 * e);
-        const uint32_t* v = (const uint32_t*)(a.v + max(row[e], 0) * row_words + head * D) + t;
-#pragma unroll
-        for (int p = 0; p < kBlocks; ++p) y[p][e] = v[16 * p];
-    }
+    for (int e = 0; e < 8; ++e)
+        if ((stored >> (16 * (e >> 2) + 4 * j + (e & 3)) & 1) == 0) keep |= 0xfu << (4 * e);
     u32x4* const codes = (u32x4*)(out + 16 * D) + lane;
-    uint8_t* const scales = out + 33 * D + j * (8 * kBlocks);
     u32x4 old[kHalves] = {};
-    if (keep != 0 && keep != 0xffffffffu) {
+    if (stored != 0xffffffffu) {
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) old[h] = codes[64 * h];
     }
 
-    // K
+    Staged& staged = all_staged[threadIdx.x >> 6];
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) {
-        const int half = D == 128 ? h : j >> 1, block = D == 128 ? j : j & 1;
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = max_u16(top, x[h][i >> 2][i & 3] & 0x7fff7fffu);
-        const uint32_t byte = scale_byte(max(top & 0xffff, top >> 16));
-        const float scale = scale_of(byte);
-        u32x4 word;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t w = 0;
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, pair_of(x[h][i][0]), scale, 0);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, pair_of(x[h][i][1]), scale, 1);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, pair_of(x[h][i][2]), scale, 2);
-            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, pair_of(x[h][i][3]), scale, 3);
-            word[i] = byte == 255 ? 0 : w;
-        }
-        if (krow[h] >= 0) {
-            *(u32x4*)(out + h * 1024 + lane * 16) = word;
-            out[32 * D + (block * 16 + t) * 2 + half] = (uint8_t)byte;
+    for (int i = 0; i < kLoads; ++i) {
+        const int token = i * (64 / kLanes) + lane / kLanes, piece = lane % kLanes, block = piece >> 2;
+        uint32_t ks, vs;
+        *(uint32_t*)&staged.k[token][4 * piece] = codes_of(kx[i], &ks);
+        *(uint32_t*)&staged.v[token][4 * piece] = codes_of(vx[i], &vs);
+        if ((lane & 3) == 0) {
+            const int half = token >> 4, low = token & 15;
+            staged.scales[(block * 16 + low) * 2 + half] = (uint8_t)ks;
+            staged.scales[D + (((low >> 2) * kBlocks + block) * 2 + half) * 4 + (low & 3)] = (uint8_t)vs;
         }
     }
-
-    // V
-    if (keep == 0xffffffffu) return;
+    meet();
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
-        u32x4 word{0, 0, 0, 0};
+        const int token = 16 * (D == 128 ? h : j >> 1) + t, block = D == 128 ? j : j & 1;
+        const u32x4 x = *(const u32x4*)&staged.k[token][16 * block];
+        if (stored >> token & 1) *(u32x4*)(out + h * 1024 + lane * 16) = x;
+    }
+    // rows of the transposing reads: tokens 0, 2, 4, 6, 1, 3, 5, 7 of the lanes' eight, 16 * (e / 4) + 4 * j + e % 4; columns: 16 bytes, a block's
+    const int e = (t >> 1 & 3) * 2 + (t >> 3);
+    const uint32_t rows = (uint32_t)(uintptr_t)(lptr_t)&staged.v[16 * (e >> 2) + 4 * j + (e & 3)][8 * (t & 1)];
 #pragma unroll
-        for (int p2 = 0; p2 < 2; ++p2) {
-            const int p = 2 * h + p2;
-            float f[8];
-            u32x2 bytes{0, 0};
-            uint32_t bad = 0;
+    for (int h = 0; h < kHalves; ++h) {
+        u32x4 word;
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const uint32_t a0 = y[p][e] & 0x7fff7fffu, a1 = y[p][e + 1] & 0x7fff7fffu;
-                const uint32_t top = max_of_16(max(a0 & 0xffff, a0 >> 16) | max(a1 & 0xffff, a1 >> 16) << 16);
-                const uint32_t s0 = scale_byte(top & 0xffff), s1 = scale_byte(top >> 16);
-                if (s0 == 255) bad |= 0xfu << (4 * e);
-                if (s1 == 255) bad |= 0xf0u << (4 * e);
-                bytes[e >> 2] |= (s0 | s1 << 8) << (8 * (e & 3));
-                f[e] = scale_of(254 - min(s0, 253u));
-                f[e + 1] = scale_of(254 - min(s1, 253u));
-            }
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                uint32_t w = 0;
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float v0 = __uint_as_float(q == 0 ? y[p][e] << 16 : y[p][e] & 0xffff0000u);
-                    const float v1 = __uint_as_float(q == 0 ? y[p][e + 1] << 16 : y[p][e + 1] & 0xffff0000u);
-                    w = code4(w, v0 * f[e], v1 * f[e + 1], e >> 1);
-                }
-                word[2 * p2 + q] = w & ~bad;
-            }
-            if (keep == 0) {
-                if (t == 0) *(u32x2*)(scales + 8 * p) = bytes;
-            } else if (t < 8) {
-                const uint32_t byte = (t < 4 ? bytes[0] : bytes[1]) >> (8 * (t & 3));
-                if ((keep >> (4 * t) & 1) == 0) scales[8 * p + t] = (uint8_t)byte;
-            }
+        for (int p = 0; p < 2; ++p) {
+            const i32x2 x = lds_read_tr8(rows + 16 * (2 * h + p));
+            const uint32_t even = x[0], odd = x[1];
+            word[2 * p] = (even & 0x0f0f0f0fu) | (odd & 0x0f0f0f0fu) << 4;
+            word[2 * p + 1] = (even >> 4 & 0x0f0f0f0fu) | (odd & 0xf0f0f0f0u);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) word[i] = (word[i] & ~keep) | (old[h][i] & keep);
-        codes[64 * h] = word;
+        if (keep != 0xffffffffu) codes[64 * h] = word;
+    }
+    if (lane < 2 * D / 4) {
+        const uint32_t x = *(const uint32_t*)&staged.scales[4 * lane];
+        uint8_t* to = out + 32 * D + 4 * lane;
+        if (stored == 0xffffffffu) *(uint32_t*)to = x;
+        else {
+            const bool is_k = lane < D / 4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // K: [block][token 16][half], V: [j][block][half][s]
+                const int token = is_k ? 16 * (i & 1) + (2 * lane + (i >> 1) & 15) : 16 * (lane & 1) + 4 * ((lane - D / 4) / (2 * kBlocks)) + i;
+                if (stored >> token & 1) to[i] = (uint8_t)(x >> (8 * i));
+            }
+        }
     }
 }
 
@@ -205,10 +204,6 @@ __global__ __launch_bounds__(64 * kWaves) void cache_load_kernel(LoadArgs a) {
         vc[h] = *(const u32x4*)(in + 16 * D + h * 1024 + lane * 16);
         vs[h] = *(const u32x4*)(in + 33 * D + j * (8 * kBlocks) + 16 * h);
     }
-    auto meet = [] {                                          // (the wavefront's own part of LDS: its accesses keep their order)
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    };
     auto write_rows = [&](uint16_t* out) {
         constexpr int kLanes = D / 8;                         // of a row
         meet();
@@ -216,7 +211,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_load_kernel(LoadArgs a) {
         for (int i = 0; i < 32 * kLanes / 64; ++i) {
             const int token = i * (64 / kLanes) + lane / kLanes, channel = 8 * (lane % kLanes);
             const u32x4 x = *(const u32x4*)&rows[token][channel];
-            if (token < count) *(u32x4*)(out + to + token * row_words + channel) = x;
+            if (token < count) __builtin_nontemporal_store(x, (u32x4*)(out + to + token * row_words + channel));
         }
         meet();
     };
@@ -259,9 +254,15 @@ static_assert(sizeof(MoveArgs) <= 112, "short arguments");
 // Token t of a slot becomes what was its token kept_idx[out_offsets[b] + t] - seq_offsets[b]: old_rows [n, 1 + max_pages] holds the length and
 // the pages that the slot had (cache_pages.hip has changed its row of the table already; nothing else has written to the old pages since).
 // A wavefront takes every head_step-th head of a tile: finding the tile's sources is four loads that wait for one another.
+// K's codes are gathered by 16 bytes.  V's are taken a source tile at a time (kept tokens come in order, so that there are two or three; any order
+// works): read as they lie, turned in LDS to a row of bytes per token, the kept rows copied, and turned back into words of eight tokens.
 template <int D>
 __global__ __launch_bounds__(64 * kWaves) void cache_move_kernel(MoveArgs a, int32_t head_groups) {
-    constexpr int kBlocks = D / 32, kHalves = D / 64;
+    constexpr int kBlocks = D / 32, kHalves = D / 64, kRow = D / 2 + 16;
+    struct Staged {
+        uint8_t words[kBlocks][4][16][8], source[32][kRow], kept[32][kRow];
+    };
+    __shared__ __align__(16) Staged all_staged[kWaves];
     const int lane = threadIdx.x & 63, t = lane & 15, j = lane >> 4;
     const int place = blockIdx.x / head_groups, b = place / a.tiles_of_seq, tile = place - b * a.tiles_of_seq;
     const int first_head = (blockIdx.x - place * head_groups) * kWaves + (threadIdx.x >> 6), head_step = head_groups * kWaves;
@@ -280,58 +281,96 @@ __global__ __launch_bounds__(64 * kWaves) void cache_move_kernel(MoveArgs a, int
         const int p = old_row[1 + (kept >> a.c.shift)];
         if (p >= 0 && p < a.c.n_pages) from = (p << a.c.shift) + (kept & ((1 << a.c.shift) - 1));
     }
-    int kfrom[kHalves], vfrom[8];
-#pragma unroll
-    for (int h = 0; h < kHalves; ++h) kfrom[h] = __shfl(from, 16 * (D == 128 ? h : j >> 1) + t);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) vfrom[e] = __shfl(from, 16 * (e >> 2) + 4 * j + (e & 3));
-    // scale bytes of V: lane t of a group takes slot t / 2, every second block
-    const int se = t >> 1, stoken = 16 * (se >> 2) + 4 * j + (se & 3), sfrom = __shfl(from, stoken);
-    auto source = [&](int token, int head) -> const uint8_t* {      // (a token that comes from nowhere: any, and what is read is not used)
+    const uint32_t all = (uint32_t)__builtin_amdgcn_ballot_w64(from >= 0);
+    auto source_of = [&](int token, int head) -> const uint8_t* {      // (a token that comes from nowhere: any, and what is read is not used)
         token = max(token, 0);
         return cache_tile<D>(a.c, token >> a.c.shift, head, (token >> 5) & tile_mask);
     };
+    Staged& staged = all_staged[threadIdx.x >> 6];
+    // scale bytes of V: lane t of a group takes slot t / 2, every second block
+    const int se = t >> 1, stoken = 16 * (se >> 2) + 4 * j + (se & 3), sfrom = __shfl(from, stoken);
+    // rows of the transposing reads.  Words: 8 lanes' columns r of two groups of eight tokens; kept: tokens 0, 2, 4, 6, 1, 3, 5, 7 of the lanes' eight
+    const int e = (t >> 1 & 3) * 2 + (t >> 3), column = 8 * (j & 1);
+    const uint32_t words = (uint32_t)(uintptr_t)(lptr_t)&staged.words[0][2 * (j >> 1) + (t & 1)][column + (t >> 1)][0];
+    const uint32_t rows = (uint32_t)(uintptr_t)(lptr_t)&staged.kept[16 * (e >> 2) + 4 * j + (e & 3)][8 * (t & 1)];
+    // the token whose columns a transposing read of words gives to a lane: byte t & 7 of group 2 * (j / 2) + t / 8
+    const int we = (t & 3) * 2 + (t >> 2 & 1), wtoken = 16 * (we >> 2) + 4 * (2 * (j >> 1) + (t >> 3)) + (we & 3);
     for (int head = first_head; head < a.c.n_kv_heads; head += head_step) {
         uint8_t* const out = cache_tile<D>(a.c, page, head, tile & tile_mask);
-        u32x4 kc[kHalves], vx[8][kHalves];
+        u32x4 kc[kHalves], x[kHalves], y[kHalves];
         uint8_t ks[kHalves], vs[kBlocks / 2];
+        uint32_t left = all;
+        // the tokens of the first source tile that is left; its words
+        auto next = [&](u32x4 (&v)[kHalves]) -> uint32_t {
+            if (left == 0) return 0;
+            const int token = __builtin_amdgcn_readlane(from, __builtin_ctz(left));
+            const uint32_t mine = left & (uint32_t)__builtin_amdgcn_ballot_w64(from >> 5 == token >> 5);
+            left &= ~mine;
+            const uint8_t* in = source_of(token, head) + 16 * D + lane * 16;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) v[h] = *(const u32x4*)(in + h * 1024);
+            return mine;
+        };
+        uint32_t mine = next(x);
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
-            const uint8_t* in = source(kfrom[h], head);
-            const int half = kfrom[h] >> 4 & 1, old = kfrom[h] & 15, block = D == 128 ? j : j & 1;
+            const int token = __shfl(from, 16 * (D == 128 ? h : j >> 1) + t), half = token >> 4 & 1, old = token & 15, block = D == 128 ? j : j & 1;
+            const uint8_t* in = source_of(token, head);
             kc[h] = *(const u32x4*)(in + ((half * kBlocks + block) * 16 + old) * 16);
             ks[h] = in[32 * D + (block * 16 + old) * 2 + half];
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint8_t* in = source(vfrom[e], head);
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) vx[e][h] = *(const u32x4*)(in + 16 * D + h * 1024 + (16 * (vfrom[e] >> 2 & 3) + t) * 16);
-        }
-#pragma unroll
         for (int i = 0; i < kBlocks / 2; ++i)
-            vs[i] = source(sfrom, head)[33 * D + (((sfrom >> 2 & 3) * kBlocks + 2 * i + (t & 1)) * 2 + (sfrom >> 4 & 1)) * 4 + (sfrom & 3)];
+            vs[i] = source_of(sfrom, head)[33 * D + (((sfrom >> 2 & 3) * kBlocks + 2 * i + (t & 1)) * 2 + (sfrom >> 4 & 1)) * 4 + (sfrom & 3)];
+        // kept tokens that come from nowhere are zero (their scales are not: NaN)
+#pragma unroll
+        for (int i = 0; i < 32 * (D / 2) / 1024; ++i) *(u32x4*)&staged.kept[(i * 64 + lane) / (D / 32)][16 * (lane % (D / 32))] = u32x4{0, 0, 0, 0};
+        while (mine != 0) {
+            const uint32_t after = next(y);
+#pragma unroll
+            for (int p = 0; p < kBlocks; ++p) {
+                const uint32_t c0 = x[p >> 1][2 * (p & 1)], c1 = x[p >> 1][2 * (p & 1) + 1];
+                *(u32x2*)staged.words[p][j][t] = u32x2{(c0 & 0x0f0f0f0fu) | (c1 & 0x0f0f0f0fu) << 4, (c0 >> 4 & 0x0f0f0f0fu) | (c1 & 0xf0f0f0f0u)};
+            }
+            meet();
+#pragma unroll
+            for (int p = 0; p < kBlocks; ++p) {
+                const i32x2 w = lds_read_tr8(words + p * (4 * 16 * 8));
+                *(i32x2*)&staged.source[wtoken][16 * p + column] = w;
+            }
+            meet();
+#pragma unroll
+            for (int i = 0; i < 32 * (D / 2) / 1024; ++i) {
+                const int token = (i * 64 + lane) / (D / 32), piece = 16 * (lane % (D / 32));
+                const u32x4 row = *(const u32x4*)&staged.source[__shfl(from, token) & 31][piece];
+                if (mine >> token & 1) *(u32x4*)&staged.kept[token][piece] = row;
+            }
+            meet();
+            mine = after;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) x[h] = y[h];
+        }
+        meet();
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
-            const int half = D == 128 ? h : j >> 1, block = D == 128 ? j : j & 1;
-            *(u32x4*)(out + h * 1024 + lane * 16) = kfrom[h] >= 0 ? kc[h] : u32x4{0, 0, 0, 0};
-            out[32 * D + (block * 16 + t) * 2 + half] = kfrom[h] >= 0 ? ks[h] : 16 * half + t < count ? 255 : 0;
+            const int token = 16 * (D == 128 ? h : j >> 1) + t, block = D == 128 ? j : j & 1;
+            const bool there = all >> token & 1;
+            *(u32x4*)(out + h * 1024 + lane * 16) = there ? kc[h] : u32x4{0, 0, 0, 0};
+            out[32 * D + (block * 16 + t) * 2 + (token >> 4)] = there ? ks[h] : token < count ? 255 : 0;
+            u32x4 word;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const i32x2 w = lds_read_tr8(rows + 16 * (2 * h + p));
+                const uint32_t even = w[0], odd = w[1];
+                word[2 * p] = (even & 0x0f0f0f0fu) | (odd & 0x0f0f0f0fu) << 4;
+                word[2 * p + 1] = (even >> 4 & 0x0f0f0f0fu) | (odd & 0xf0f0f0f0u);
+            }
+            *(u32x4*)(out + 16 * D + h * 1024 + lane * 16) = word;
         }
-        u32x4 y[kHalves] = {};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int shift = 4 * ((vfrom[e] >> 4 & 1) * 4 + (vfrom[e] & 3));
-            const uint32_t mask = vfrom[e] >= 0 ? 15 : 0;
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[h][i] |= (vx[e][h][i] >> shift & mask) << (4 * e);
-        }
-#pragma unroll
-        for (int h = 0; h < kHalves; ++h) *(u32x4*)(out + 16 * D + h * 1024 + lane * 16) = y[h];
 #pragma unroll
         for (int i = 0; i < kBlocks / 2; ++i)
             out[33 * D + (j * kBlocks + 2 * i + (t & 1)) * 8 + se] = sfrom >= 0 ? vs[i] : stoken < count ? 255 : 0;
+        meet();
     }
 }
 
