@@ -20,7 +20,6 @@
 namespace pyr {
 namespace {
 
-constexpr int kWaves = 4;
 constexpr float kGrowth = 4096.f;                 // how far a lane's weights of a tile may outgrow the reference
 
 struct AttendArgs {
@@ -188,7 +187,7 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT, R>& w, const Tile<D, R>&
     }
 }
 
-template <int D, int NT, int R>
+template <int D, int NT, int R, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, NT == 1 && (D == 64 || R == 4) ? 3 : 2) void cache_attention_kernel(AttendArgs a) {
     constexpr int kRow = D + 4;                   // floats of a row in LDS
     __shared__ __align__(16) float results[kWaves][16][kRow];
@@ -387,12 +386,18 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs a) {
 template <int D>
 int launch(const CacheAttention& x, const CacheView& c, const AttendArgs& a, void* out, float* lse, hipStream_t stream) {
     const int64_t grid = (int64_t)a.n_seqs * a.splits * x.col_groups * c.n_kv_heads;
-    const dim3 blocks((unsigned)grid), threads(64 * kWaves);
+    const dim3 blocks((unsigned)grid), threads(64 * x.waves);
     constexpr int kMost = D / 32;      // columns of a product hold at most so many times the rows
-    if (x.col_tiles == 2) hipLaunchKernelGGL((cache_attention_kernel<D, 2, 1>), blocks, threads, 0, stream, a);
-    else if (x.repeats == 1) hipLaunchKernelGGL((cache_attention_kernel<D, 1, 1>), blocks, threads, 0, stream, a);
-    else if (x.repeats == 2) hipLaunchKernelGGL((cache_attention_kernel<D, 1, 2>), blocks, threads, 0, stream, a);
-    else hipLaunchKernelGGL((cache_attention_kernel<D, 1, kMost>), blocks, threads, 0, stream, a);
+    if (x.col_tiles == 2) hipLaunchKernelGGL((cache_attention_kernel<D, 2, 1, 4>), blocks, threads, 0, stream, a);
+    else if (x.waves == 4) {
+        if (x.repeats == 1) hipLaunchKernelGGL((cache_attention_kernel<D, 1, 1, 4>), blocks, threads, 0, stream, a);
+        else if (x.repeats == 2) hipLaunchKernelGGL((cache_attention_kernel<D, 1, 2, 4>), blocks, threads, 0, stream, a);
+        else hipLaunchKernelGGL((cache_attention_kernel<D, 1, kMost, 4>), blocks, threads, 0, stream, a);
+    } else {
+        if (x.repeats == 1) hipLaunchKernelGGL((cache_attention_kernel<D, 1, 1, 8>), blocks, threads, 0, stream, a);
+        else if (x.repeats == 2) hipLaunchKernelGGL((cache_attention_kernel<D, 1, 2, 8>), blocks, threads, 0, stream, a);
+        else hipLaunchKernelGGL((cache_attention_kernel<D, 1, kMost, 8>), blocks, threads, 0, stream, a);
+    }
     const int rc = check_launch();
     if (rc != PYR_OK || a.splits == 1) return rc;
     const int32_t rows_of_seq = a.n_tokens * a.n_q_heads, rows = a.n_seqs * rows_of_seq;
@@ -403,22 +408,39 @@ int launch(const CacheAttention& x, const CacheView& c, const AttendArgs& a, voi
 
 }  // namespace
 
+// What is waited for at the end is the wavefront with the most tiles (0.4 us each), so few heads are split along the cache, into at most
+// kWorkgroups parts of kShortest tiles and more - unless a launch that joins the parts (4 us, and 3 us of the host's) costs more than it saves.
+// Workgroups of eight wavefronts do with half as many parts; one fits a compute unit, so they are taken where they fill nearly all of them
+// in one go.  Measured, us (four wavefronts, eight): one token of 1 x 1000 on 32/8 heads 9.5 / 8.2 (unsplit), 1 x 1434 on 32 12.2 / 10.2, 32 x 4096 on
+// 32/8 29.7 / 26.6, 1 x 32768 on 32/8 13.6 / 12.9; 20 of 100 ... 8000 on 64/8 (160 heads) 31 / 38, 40 x 1500 on 32/8 (320 heads) 17 / 21.
+// Unsplit up to 1500 tokens: 1 x 1434 on 32 heads 10.3 against 9.8 and a launch; 1 x 2048 11.9 / 9.9.  More than 16 rows a head: 256 workgroups, as
+// the parts' results are larger (16 x 2048 on 64/8 heads, nine tokens: 36 us, with 512 43).
 CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_len) {
+    constexpr int64_t kUnsplit = 48, kShortest = 16, kUnits = 256, kFilled = 200;
     CacheAttention x{};
     const int cols = n_tokens * (n_q_heads / n_kv_heads);
     const int tiles = (cols + 15) / 16;
     x.col_tiles = tiles == 1 ? 1 : 2;
     x.col_groups = (tiles + x.col_tiles - 1) / x.col_tiles;
+    x.repeats = cols <= 4 && head_dim == 128 ? 4 : cols <= 8 ? 2 : 1;
     const int64_t units = (int64_t)n_seqs * n_kv_heads * x.col_groups, key_tiles = (max_len + 31) / 32;
-    const int64_t kWorkgroups = x.col_tiles == 1 ? 512 : 256, kShortest = 16;
-    int64_t splits = units > 0 ? (kWorkgroups + units - 1) / units : 1;
-    int64_t chunk = splits > 0 ? (key_tiles + splits - 1) / splits : key_tiles;
-    if (chunk < kShortest) chunk = kShortest;
-    chunk = (chunk + kWaves - 1) / kWaves * kWaves;
+    int64_t splits = 1;
+    x.waves = 4;
+    if (units > 0 && key_tiles <= kUnsplit) x.waves = x.col_tiles == 1 && units <= kUnits ? 8 : 4;
+    else if (units > 0 && x.col_tiles == 1 && units <= kUnits && kUnits / units * units >= kFilled) {
+        x.waves = 8;
+        splits = kUnits / units;
+    } else if (units > 0) {
+        const int64_t workgroups = x.col_tiles == 1 ? 2 * kUnits : kUnits;
+        splits = (workgroups + units - 1) / units;
+    }
+    int64_t chunk = (key_tiles + splits - 1) / splits;
+    if (splits > 1 && chunk < kShortest) chunk = kShortest;
+    chunk = (chunk + x.waves - 1) / x.waves * x.waves;
+    if (chunk == 0) chunk = x.waves;
     splits = (key_tiles + chunk - 1) / chunk;
     x.chunk = (int32_t)chunk;
     x.splits = splits < 1 ? 1 : (int32_t)splits;
-    x.repeats = cols <= 4 && head_dim == 128 ? 4 : cols <= 8 ? 2 : 1;
     const int64_t rows = (int64_t)n_seqs * n_tokens * n_q_heads;
     x.part_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * head_dim * sizeof(float);
     x.stat_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * 4 * sizeof(float);

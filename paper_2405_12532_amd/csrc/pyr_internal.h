@@ -156,10 +156,10 @@ int launch_gather_positions(const int32_t* pos, const int32_t* kept_idx, int64_t
 struct CacheView;
 constexpr int kMaxCacheRows = PYR_CACHE_MAX_ROWS, kMaxCacheSlots = PYR_CACHE_MAX_SLOTS;
 
-// How an attention over the cache is cut up: 16-row column tiles of a workgroup; times that one holds the rows; workgroups per head and split; 32-token
+// How an attention over the cache is cut up: 16-row column tiles of a workgroup; times that one holds the rows; wavefronts; workgroups per head and split; 32-token
 // tiles of a split; splits; what their partial results take.
 struct CacheAttention {
-    int32_t col_tiles, repeats, col_groups, chunk, splits;
+    int32_t col_tiles, repeats, waves, col_groups, chunk, splits;
     size_t part_bytes, stat_bytes;
 };
 CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_len);
