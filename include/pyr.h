@@ -434,7 +434,8 @@ PYR_API int pyr_cache_load(const pyr_cache* cache, const int32_t* slots, const i
  *   out                dev bf16 [n, n_tokens, Hq, d], written
  *   lse                dev fp32 [n, n_tokens, Hq], written, as pyr_attention's; may be NULL
  *   workspace          dev, >= pyr_cache_attention_workspace_bytes(), 256-byte aligned; not read where that is 0
- * A token that sees nothing (an empty slot, a skipped row, fewer tokens in the cache than n_tokens): zeros in out, -inf in lse.  A page outside the pool: NaN.
+ * A row that sees nothing (an empty slot, a skipped row, fewer tokens in the cache than n_tokens): zeros in out, -inf in lse.  A token of NaN makes
+ * the rows that see it NaN, unless its K is a number and its weight 0 in fp32; what a row does not see never reaches it.  A page outside the pool: NaN.
  * One launch, and one that adds up partial results where few long sequences are split.
  */
 PYR_API int pyr_cache_attention_workspace_bytes(const pyr_cache* cache, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len,
@@ -520,6 +521,21 @@ PYR_API int pyr_diag_layer(const pyr_shape* shape, const int32_t* seq_offsets_ho
  */
 PYR_API int pyr_diag_update(const pyr_shape* shape, const int32_t* seq_offsets_host, int32_t w, int32_t compute_units, int32_t xcds,
                             int32_t* order_out);
+
+/*
+ * Diagnostic, not part of the method: how pyr_cache_attention cuts up a call, so that a test can assert that it reaches the path it is written for.
+ * Host only; launches nothing.
+ *   route_out          host, written:
+ */
+typedef struct pyr_cache_route {
+    int32_t col_tiles;          /* 16-row tiles of query rows in a workgroup ...                                     */
+    int32_t repeats;            /* ... and how many times the rows stand in one                                      */
+    int32_t waves;              /* wavefronts of a workgroup                                                         */
+    int32_t col_groups;         /* workgroups per KV head and split                                                  */
+    int32_t chunk, splits;      /* 32-token tiles of a split; splits along the cache: more than one take a second launch */
+} pyr_cache_route;
+PYR_API int pyr_diag_cache_attention(const pyr_cache* cache, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len,
+                                     pyr_cache_route* route_out);
 
 #ifdef __cplusplus
 }

@@ -35,6 +35,10 @@ class PyrCache(ctypes.Structure):
         "n_pages", "page_tokens", "n_slots", "max_pages", "n_kv_heads", "head_dim")]
 
 
+class PyrCacheRoute(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("col_tiles", "repeats", "waves", "col_groups", "chunk", "splits")]
+
+
 class PyrError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -83,6 +87,7 @@ _SIGNATURES = {
     "pyr_cache_load": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _I32, _VP, _VP, _I32, _VP]),
     "pyr_cache_attention_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(PyrCache), _I32, _I32, _I32, _I32, ctypes.POINTER(_SZ)]),
     "pyr_cache_attention": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _I32, _I32, _I32, _F32, _VP, _VP, _VP, _SZ, _VP]),
+    "pyr_diag_cache_attention": (ctypes.c_int, [ctypes.POINTER(PyrCache), _I32, _I32, _I32, _I32, ctypes.POINTER(PyrCacheRoute)]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -373,6 +378,14 @@ def cache_attention(cache, q, slots, n, n_tokens, n_q_heads, max_len, softmax_sc
     _check(load().pyr_cache_attention(ctypes.byref(cache), _ptr(q), _ptr(slots), int(n), int(n_tokens), int(n_q_heads), int(max_len),
                                       float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace), int(workspace_bytes_), _stream(stream)),
            "pyr_cache_attention")
+
+
+def diag_cache_attention(cache, n, n_tokens, n_q_heads, max_len) -> PyrCacheRoute:
+    """How cache_attention cuts up a call (host only)."""
+    out = PyrCacheRoute()
+    _check(load().pyr_diag_cache_attention(ctypes.byref(cache), int(n), int(n_tokens), int(n_q_heads), int(max_len), ctypes.byref(out)),
+           "pyr_diag_cache_attention")
+    return out
 
 
 # ----------------------------------------------------------------------------- convenience for tests / smoke

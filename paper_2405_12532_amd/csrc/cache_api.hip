@@ -178,4 +178,15 @@ int pyr_cache_attention(const pyr_cache* cache, const void* q, const int32_t* sl
                                        (float*)((char*)workspace + align_up(plan.part_bytes)), (hipStream_t)stream);
 }
 
+int pyr_diag_cache_attention(const pyr_cache* cache, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len, pyr_cache_route* route_out) {
+    if (route_out == nullptr) return PYR_ERR_NULL;
+    int rc = check_sizes(cache);
+    if (rc != PYR_OK) return rc;
+    pyr::CacheAttention plan;
+    rc = check_attention(cache, n, n_tokens, n_q_heads, max_len, &plan);
+    if (rc != PYR_OK) return rc;
+    *route_out = pyr_cache_route{plan.col_tiles, plan.repeats, plan.waves, plan.col_groups, plan.chunk, plan.splits};
+    return PYR_OK;
+}
+
 }  // extern "C"

@@ -58,6 +58,11 @@ __device__ __forceinline__ void load_tile(Tile<D, R>& t, const uint8_t* tile, in
         t.vs[v] = *(const u32x2*)(tile + (uint32_t)(33 * D + (lane >> 4) * (D / 4) + 8 * ((lane & 15) / (16 / R)) + 8 * R * v));
 }
 
+__device__ __forceinline__ float times(float x, float y) {      // 0 where one of them is 0
+    float z;
+    asm("v_mul_legacy_f32 %0, %1, %2" : "=v"(z) : "v"(x), "v"(y));
+    return z;
+}
 __device__ __forceinline__ float max_of_groups(float x) {      // over the lanes with the same lane & 15
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
@@ -119,17 +124,13 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT, R>& w, const Tile<D, R>&
     bf16x8 ones;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
-    uint32_t hidden[NT];                          // bit e: the row does not see the lane's e-th token
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        hidden[n] = 0;
         if (masked) {
+            const int see = w.seen[n] - first_token - 4 * (lane >> 4);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (first_token + 16 * (e >> 2) + 4 * (lane >> 4) + (e & 3) >= w.seen[n]) {
-                    p[n][e] = -INFINITY;
-                    hidden[n] |= 1u << e;
-                }
+                if (16 * (e >> 2) + (e & 3) >= see) p[n][e] = -INFINITY;
         }
         // weights against the reference as it is; where their sum shows that a row has outgrown it (or has none yet), again against a new one
         float x[8], sum;
@@ -166,18 +167,12 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT, R>& w, const Tile<D, R>&
         float vs[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) vs[e] = scale_of((t.vs[v][e >> 2] >> (8 * (e & 3))) & 255);
+        // (0 times any scale is 0 here: a token that a row does not see may have any scale byte, NaN among them)
         bf16x8 ps[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ps[n][e] = (__bf16)(p[n][e] * vs[e]);
-            if (masked) {
-                // (a token that a row does not see may have any scale byte, NaN among them)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (hidden[n] >> e & 1) ps[n][e] = (__bf16)0.f;
-            }
-        }
+            for (int e = 0; e < 8; ++e) ps[n][e] = (__bf16)times(p[n][e], vs[e]);
 #pragma unroll
         for (int i = 2 * R * v; i < 2 * R * (v + 1); ++i) {
             const bf16x8 x = values_of(t.v[i >> 2][i & 3], 1.f);
@@ -189,20 +184,20 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT, R>& w, const Tile<D, R>&
 
 template <int D, int NT, int R, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, NT == 1 && (D == 64 || R == 4) ? 3 : 2) void cache_attention_kernel(AttendArgs a) {
-    constexpr int kRow = D + 4;                   // floats of a row in LDS
-    __shared__ __align__(16) float results[kWaves][16][kRow];
-    __shared__ float stats[kWaves][NT][16][4];    // reference, sum, sum of the rounded
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4;
+    constexpr int kRow = D + 4, kCols = 16 * NT / R;       // floats of a row in LDS; rows of a workgroup
+    __shared__ __align__(16) float results[kWaves][kCols][kRow];
+    __shared__ __align__(16) float stats[kWaves][kCols][4];      // reference, sum, sum of the rounded
+    __shared__ int32_t places[kCols];                      // rows of q and out; -1: none
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, c = lane & 15;
     const int hkv = a.c.n_kv_heads, g = a.n_q_heads / hkv, cols = a.n_tokens * g;
-    // workgroup -> (sequence, split, column group, head): neighbours read neighbouring heads of the same pages
-    const int col_groups = (cols + 16 * NT - 1) / (16 * NT);
-    int id = blockIdx.x;
-    const int head = id % hkv;
-    id /= hkv;
-    const int first_col = (id % col_groups) * (16 * NT);
-    id /= col_groups;
-    const int split = id % a.splits, b = id / a.splits;
-    const int begin = split * a.chunk;
+    // workgroup -> (sequence, column group, head), split: neighbours read neighbouring heads of the same pages
+    int b = blockIdx.x / hkv, first_col = 0;
+    const int head = blockIdx.x - b * hkv, split = blockIdx.y, begin = split * a.chunk;
+    if (cols > kCols) {
+        const int col_groups = (cols + kCols - 1) / kCols, all = b;
+        b = all / col_groups;
+        first_col = (all - b * col_groups) * kCols;
+    }
 
     // the wavefront's tiles: begin + wave, + kWaves, ...; lane l holds the page of the l-th of 64 (asked for together with the length)
     const int slot = cache_slot(a.c, a.slots, b);
@@ -213,22 +208,22 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && (D == 64 || R == 4) ? 3 : 2
     const int len = slot < 0 ? 0 : cache_len(a.c, slot);
     const int tiles = (len + 31) >> 5;
     const int end = split == a.splits - 1 ? tiles : min(tiles, begin + a.chunk);
-    if (a.splits > 1 && begin >= end && split > 0) return;           // (the join does not look at it)
+    if (split > 0 && begin >= end) return;                           // (the join does not look at it)
 
     Rows<D, NT, R> w;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int col = first_col + 16 * n + (lane & 15) % (16 / R);
-        const int token = col / g;
+        const int at = 16 * n + c % (16 / R), col = first_col + at, token = (int)((uint32_t)col / (uint32_t)g);
+        const int row = col < cols ? (b * a.n_tokens + token) * a.n_q_heads + head * g + (col - token * g) : -1;
+        if (wave == 0 && j == 0) places[at] = row;
         w.seen[n] = len - a.n_tokens + 1 + token;
         w.m[n] = -FLT_MAX;
         w.l[n] = 0.f;
         w.weight[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const uint16_t* row = a.q + (((int64_t)b * a.n_tokens + token) * a.n_q_heads + head * g + (col - token * g)) * D;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
             const int channel = D == 128 ? 32 * j + 8 * i : 32 * (j & 1) + 8 * (i + 2 * (j >> 1));
-            w.q[n][i] = col < cols ? *(const bf16x8*)(row + channel) : bf16x8{};
+            w.q[n][i] = row >= 0 ? *(const bf16x8*)(a.q + (int64_t)row * D + channel) : bf16x8{};
         }
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) w.o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -237,7 +232,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && (D == 64 || R == 4) ? 3 : 2
 
     bool bad = false;
     const int count = max(0, (end - begin - wave + kWaves - 1) / kWaves);
-    auto fetch = [&](Tile<D, R>& t, int i) {                            // (i goes up by one from call to call)
+    auto fetch = [&](Tile<D, R>& t, int i) {                         // (i goes up by one from call to call)
         if (i >= count) return;
         if ((i & 63) == 0) {
             if (i > 0) pages = page_of(i);
@@ -249,13 +244,13 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && (D == 64 || R == 4) ? 3 : 2
         const int tile = begin + wave + i * kWaves;
         load_tile<D, R, NT == 1>(t, cache_tile<D>(a.c, page, head, tile & ((1 << tile_shift) - 1)), lane);
     };
+    Tile<D, R> t0, t1;
+    fetch(t0, 0);
+    fetch(t1, 1);
     auto attend = [&](const Tile<D, R>& t, int i) {
         const int token = (begin + wave + i * kWaves) * 32;
         attend_tile<D, NT, R>(w, t, token, token + 32 > all_see, a.scale, lane);
     };
-    Tile<D, R> t0, t1;
-    fetch(t0, 0);
-    fetch(t1, 1);
     for (int i = 0; i < count; i += 2) {
         attend(t0, i);
         fetch(t0, i + 2);
@@ -265,60 +260,52 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && (D == 64 || R == 4) ? 3 : 2
         }
     }
 
-    // the wavefronts' results: references and sums first, then the rows, weighted by 2^(reference - largest)
+    // the wavefronts' results meet in LDS, weighted by 2^(reference - largest)
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
+        const int at = 16 * n + c % (16 / R);
         w.l[n] = bad ? NAN : sum_of_groups(w.l[n]);
-        if (j == 0) *(f32x4*)stats[wave][n][lane & 15] = f32x4{w.m[n], w.l[n], bad ? NAN : w.weight[n][0], 0.f};
-    }
-    const int64_t rows = (int64_t)a.n_seqs * a.n_tokens * a.n_q_heads;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
+        if (j == 0) *(f32x4*)stats[wave][at] = f32x4{w.m[n], w.l[n], bad ? NAN : w.weight[n][0], 0.f};
 #pragma unroll
         for (int p = 0; p < D / 32; ++p) {
             // rows 4 j + r of products 2 p and 2 p + 1 are channels 32 p + 2 (4 j + r) and the next
-            float* to = &results[wave][(lane & 15) % (16 / R)][32 * p + 8 * j];
+            float* to = &results[wave][at][32 * p + 8 * j];
             const f32x4 x = w.o[n][2 * p], y = w.o[n][2 * p + 1];
-            if ((lane & 15) / (16 / R) == p % R) {
+            if (c / (16 / R) == p % R) {
                 *(f32x4*)to = f32x4{x[0], y[0], x[1], y[1]};
                 *(f32x4*)(to + 4) = f32x4{x[2], y[2], x[3], y[3]};
             }
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < (16 / R) * (D / 4); i += 64 * kWaves) {
-            const int r = i / (D / 4), c4 = i % (D / 4);
-            const int col = first_col + 16 * n + r;
-            if (col >= cols) continue;
-            f32x4 st[kWaves];
+    }
+    __syncthreads();
+    const int64_t part = split * ((int64_t)a.n_seqs * a.n_tokens * a.n_q_heads);
+#pragma unroll 1
+    for (int i = threadIdx.x; i < kCols * (D / 4); i += 64 * kWaves) {
+        const int r = i / (D / 4), c4 = i % (D / 4), row = places[r];
+        if (row < 0) continue;
+        float top = stats[0][r][0], sum = 0.f, weight = 0.f;
 #pragma unroll
-            for (int v = 0; v < kWaves; ++v) st[v] = *(const f32x4*)stats[v][n][r];
-            float top = st[0][0], sum = 0.f, weight = 0.f;
+        for (int v = 1; v < kWaves; ++v) top = fmaxf(top, stats[v][r][0]);
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int v = 1; v < kWaves; ++v) top = fmaxf(top, st[v][0]);
-            f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int v = 0; v < kWaves; ++v) {
-                const float f = __builtin_amdgcn_exp2f(st[v][0] - top);
-                sum += f * st[v][1];
-                weight += f * st[v][2];
-                o += f * *(const f32x4*)&results[v][r][4 * c4];
-            }
-            const int token = col / g;
-            const int64_t at = ((int64_t)b * a.n_tokens + token) * a.n_q_heads + head * g + (col - token * g);
-            if (a.splits == 1) {
-                const float f = weight == 0.f ? 0.f : 1.f / weight;
-                bf16x4 y;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) y[x] = (__bf16)(o[x] * f);
-                *(bf16x4*)((uint16_t*)a.out + at * D + 4 * c4) = y;
-                if (a.lse != nullptr && c4 == 0) a.lse[at] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
-            } else {
-                const int64_t part = split * rows + at;
-                *(f32x4*)((float*)a.out + part * D + 4 * c4) = o;
-                if (c4 == 0) *(f32x4*)(a.lse + 4 * part) = f32x4{top, sum, weight, 0.f};
-            }
+        for (int v = 0; v < kWaves; ++v) {
+            const f32x4 st = *(const f32x4*)stats[v][r];
+            const float f = __builtin_amdgcn_exp2f(st[0] - top);
+            sum += f * st[1];
+            weight += f * st[2];
+            o += f * *(const f32x4*)&results[v][r][4 * c4];
         }
-        __syncthreads();
+        if (a.splits == 1) {
+            const float f = weight == 0.f ? 0.f : 1.f / weight;
+            bf16x4 y;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[x] = (__bf16)(o[x] * f);
+            *(bf16x4*)((uint16_t*)a.out + (int64_t)row * D + 4 * c4) = y;
+            if (a.lse != nullptr && c4 == 0) a.lse[row] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+        } else {
+            *(f32x4*)((float*)a.out + (part + row) * D + 4 * c4) = o;
+            if (c4 == 0) *(f32x4*)(a.lse + 4 * (part + row)) = f32x4{top, sum, weight, 0.f};
+        }
     }
 }
 
@@ -385,8 +372,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs a) {
 
 template <int D>
 int launch(const CacheAttention& x, const CacheView& c, const AttendArgs& a, void* out, float* lse, hipStream_t stream) {
-    const int64_t grid = (int64_t)a.n_seqs * a.splits * x.col_groups * c.n_kv_heads;
-    const dim3 blocks((unsigned)grid), threads(64 * x.waves);
+    const dim3 blocks((unsigned)((int64_t)a.n_seqs * x.col_groups * c.n_kv_heads), (unsigned)x.splits), threads(64 * x.waves);
     constexpr int kMost = D / 32;      // columns of a product hold at most so many times the rows
     if (x.col_tiles == 2) hipLaunchKernelGGL((cache_attention_kernel<D, 2, 1, 4>), blocks, threads, 0, stream, a);
     else if (x.waves == 4) {

@@ -106,6 +106,7 @@ ATTEND = [  # lens, hq, hkv, d, page, tokens
 @pytest.mark.parametrize("lens,hq,hkv,d,page,tokens", ATTEND)
 def test_attention(lib, lens, hq, hkv, d, page, tokens):
     pair = Pair(lib, lens, hkv, d, page, seed=hq)
+    assert lib.diag_cache_attention(pair.cache, len(lens) + 2, tokens, hq, max(lens)).col_tiles == (1 if tokens * hq // hkv <= 16 else 2)
     qt, q = bf16(pair.rng.normal(size=(len(lens) + 2, tokens, hq, d)) * 0.2)
     slots = [int(s) for s in pair.rng.permutation(len(lens))] + [-1, 0]
     out, lse = attend(pair, qt, slots, tokens, max(lens))
@@ -121,7 +122,8 @@ def test_attention(lib, lens, hq, hkv, d, page, tokens):
 @pytest.mark.parametrize("lens,hq,hkv,d,tokens", [([5000, 1, 700, 0], 4, 2, 128, 1), ([4097, 4096], 8, 1, 64, 3), ([9000], 2, 1, 64, 1)])
 def test_attention_split_along_the_cache(lib, lens, hq, hkv, d, tokens):
     pair = Pair(lib, lens, hkv, d, 64)
-    assert lib.cache_attention_workspace_bytes(pair.cache, len(lens), tokens, hq, max(lens)) > 0
+    r = lib.diag_cache_attention(pair.cache, len(lens), tokens, hq, max(lens))
+    assert r.splits > 1 and r.waves == (8 if r.col_tiles == 1 else 4) and lib.cache_attention_workspace_bytes(pair.cache, len(lens), tokens, hq, max(lens)) > 0
     qt, q = bf16(pair.rng.normal(size=(len(lens), tokens, hq, d)) * 0.2)
     slots = list(range(len(lens)))
     reads = {s: pair.o.read(s) for s in slots}
@@ -129,6 +131,28 @@ def test_attention_split_along_the_cache(lib, lens, hq, hkv, d, tokens):
     check_attention(pair, q, slots, out, lse, reads=reads)
     again, lse2 = attend(pair, qt, slots, tokens, max(lens))
     assert torch.equal(again.view(torch.int16), out.view(torch.int16)) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("d,hq,hkv,tokens,repeats,col_tiles", [(128, 4, 2, 1, 4, 1), (128, 16, 2, 1, 2, 1), (128, 12, 2, 2, 1, 1), (64, 6, 2, 2, 2, 1),
+                                                               (64, 18, 2, 1, 1, 1), (64, 16, 2, 4, 1, 2), (128, 16, 2, 3, 1, 2)])
+def test_attention_by_workgroups_of_four_wavefronts(lib, d, hq, hkv, tokens, repeats, col_tiles):
+    """Many heads, none of them split; and half of them among long ones, split."""
+    lens = [0, 1, 33, 64, 70, 15, 31, 32] * 17
+    pair = Pair(lib, lens[:12], hkv, d, 32)
+    n = len(lens)
+    slots = [int(s) for s in pair.rng.integers(-1, 12, n)]
+    qt, q = bf16(pair.rng.normal(size=(n, tokens, hq, d)) * 0.2)
+    r = lib.diag_cache_attention(pair.cache, n, tokens, hq, 70)
+    assert (r.waves, r.splits, r.repeats, r.col_tiles) == (4, 1, repeats, col_tiles)
+    out, lse = attend(pair, qt, slots, tokens, 70)
+    check_attention(pair, q, slots, out, lse)
+    pair = Pair(lib, [1700, 40, 600, 0], hkv, d, 64)
+    n = 66
+    slots = [int(s) for s in pair.rng.integers(-1, 4, n)]
+    r = lib.diag_cache_attention(pair.cache, n, tokens, hq, 1700)
+    assert (r.waves, r.repeats, r.col_tiles) == (4, repeats, col_tiles) and r.splits > 1
+    out, lse = attend(pair, qt[:n].contiguous(), slots, tokens, 1700)
+    check_attention(pair, q[:n], slots, out, lse, reads={s: pair.o.read(s) for s in range(4)})
 
 
 @pytest.mark.parametrize("d", [64, 128])
