@@ -305,7 +305,7 @@ PYR_API int pyr_decode_update(const void* q_win, const void* k, const void* v,
 /*
  * A cache held in 4 bits, for the generation phase of many sequences: pages in device memory that the slots of a table share.
  * K and V of a token are stored as 4-bit floating-point numbers (e2m1: a sign and 0, 0.5, 1, 1.5, 2, 3, 4 or 6) times a power of two per 32
- * channels of a head (one byte, 2^(byte - 127); 255: not a number) - 34 bytes for 32 channels of K and V, 4.25 bits a number against
+ * channels of a head (one byte from 1 to 252, 2^(byte - 127), or 255: not a number) - 34 bytes for 32 channels of K and V, 4.25 bits a number against
  * bf16's 16.  A block's power of two is the smallest that brings its largest magnitude to 7 or less (7 is rounded to 6), between 2^-126 and 2^125; numbers are
  * rounded to the nearest, ties to the even code; a block with an infinity or a NaN is stored as NaN as a whole.
  *
@@ -407,7 +407,7 @@ PYR_API int pyr_cache_compact(const pyr_cache* cache, const int32_t* slots, int3
  *   offsets            dev int32 [n+1];  slots, start  dev int32 [n]
  *   max_new            no offsets[i+1] - offsets[i] is larger (tokens beyond it are not stored, or some of them)
  * Tokens that have no page, a start of -1 (pyr_cache_reserve found no room) and rows outside k and v are not stored; nothing else in the pages
- * changes.  Two rows of a call must not store the same tokens.
+ * changes.  Of rows that name the same slot the first is stored.
  */
 PYR_API int pyr_cache_store(const pyr_cache* cache, const void* k, const void* v, int32_t n_rows, const int32_t* row_idx, int32_t n_list,
                     const int32_t* offsets, const int32_t* slots, const int32_t* start, int32_t n, int32_t max_new, void* stream);
@@ -425,7 +425,8 @@ PYR_API int pyr_cache_load(const pyr_cache* cache, const int32_t* slots, const i
  * Attention of each sequence's newest n_tokens tokens over its cache, theirs included (store them first): token i of slots[b] sees the tokens
  * 0 .. lens[slots[b]] - n_tokens + i.
  *   out[b,i,h,:] = sum_t softmax_t(scale * q[b,i,h,:].k[t,h/g,:]) v[t,h/g,:]
- * bf16 MFMA products on the cache's exact values (P times V's power of two is rounded to bf16), fp32 accumulation and softmax.
+ * bf16 MFMA products on the cache's exact values (P times V's power of two is rounded to bf16), fp32 accumulation and softmax; sums of P V leave
+ * fp32's range where V has numbers of 2^110 and more.
  *   q                  dev bf16 [n, n_tokens, Hq, d]
  *   slots              dev int32 [n]
  *   max_len            about the longest sequence (it decides how the work is cut up and how large the workspace is, not the result: longer

@@ -204,7 +204,7 @@ class Cache:
     def store(self, k, v, row_idx, offsets, slots, start):
         """k, v float64 [rows, hkv, d]"""
         for i, s in enumerate(slots):
-            if not 0 <= s < len(self.lens) or start[i] < 0:
+            if not 0 <= s < len(self.lens) or start[i] < 0 or s in list(slots)[:i]:
                 continue
             for j in range(int(offsets[i + 1] - offsets[i])):
                 row = offsets[i] + j if row_idx is None else row_idx[offsets[i] + j]

@@ -155,10 +155,11 @@ __device__ __forceinline__ int hand_out(Shared& s, const CacheView& c, int n, in
                 if (free[i] >> k & 1) s.free[before + rank[i]++] = (uint16_t)(place_of(i) + k);
         __syncthreads();
         const int taken = min(total, need - found);
-        int ends[2];
-        if (taken > 0) rows_of_ranks(s, n, found, taken - 1, ends);
-        const int rows = taken > 0 ? ends[1] - ends[0] + 1 : 0;
-        if (rows >= kWaves && taken >= 24 * rows) {
+        constexpr int kLong = 24;
+        int ends[2] = {0, -1};
+        if (taken >= kLong * kWaves) rows_of_ranks(s, n, found, taken - 1, ends);
+        const int rows = ends[1] - ends[0] + 1;
+        if (rows >= kWaves && taken >= kLong * rows) {
             for (int row = ends[0] + (threadIdx.x >> 6); row <= ends[1]; row += kWaves) {
                 const int first = s.first[row], entry = s.entry[row] - first, last = min(s.first[row + 1], found + taken);
                 for (int r = max(first, found) + lane; r < last; r += 64) {
@@ -246,9 +247,11 @@ __global__ __launch_bounds__(64 * kWaves) void cache_fork_kernel(CacheView c, co
     const Counts counts = look(c, 0), ahead = look(c, kThreads * kEach);
     clear<kWaves>(s, c);
     const int part = (1 << c.shift) - 1;
+    int mine = -1;                        // the parent of this thread's first row
     auto need = [&](int i, int* entry) -> int {
         const int parent = parents[i], child = children[i];
         s.slot[i] = -1;
+        if (i == threadIdx.x) mine = parent;
         if (parent == -1 && child == -1) return 0;
         if (parent < 0 || parent >= c.n_slots || child < 0 || child >= c.n_slots) {
             refuse(s, PYR_CACHE_BAD_SLOT);
@@ -265,8 +268,10 @@ __global__ __launch_bounds__(64 * kWaves) void cache_fork_kernel(CacheView c, co
         return (len & part) != 0 ? 1 : 0;
     };
     const int all = sum_needs<kWaves>(s, n, need);
-    for (int i = threadIdx.x; i < n; i += kThreads)
-        if (parents[i] >= 0 && parents[i] < c.n_slots && (s.seen[parents[i] >> 5] >> (parents[i] & 31) & 1) != 0) refuse(s, PYR_CACHE_BAD_SLOT);
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const int parent = i < kThreads ? mine : parents[i];
+        if (parent >= 0 && parent < c.n_slots && (s.seen[parent >> 5] >> (parent & 31) & 1) != 0) refuse(s, PYR_CACHE_BAD_SLOT);
+    }
     __syncthreads();
     int state = s.status;
     if (state == 0) state = hand_out<kWaves>(s, c, n, all, counts, ahead);

@@ -75,6 +75,8 @@ __global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a, i
     const int slot = cache_slot(a.c, a.slots, b);
     const int start = a.start[b];
     const int first = max(a.offsets[b], 0), last = min(a.offsets[b + 1], a.n_list);
+    bool again = false;                                           // an earlier row has the slot: its tile may be written by two wavefronts at once
+    for (int i = lane; i < b; i += 64) again |= a.slots[i] == slot;
     if (slot < 0 || start < 0 || first >= last || head >= a.c.n_kv_heads) return;
     const int64_t end = min((int64_t)start + (last - first), (int64_t)a.c.max_pages << a.c.shift);       // tokens start .. end - 1
     const int tile = (start >> 5) + (place - b * tiles_of_piece);
@@ -93,7 +95,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a, i
     }
     if (page < 0 || page >= a.c.n_pages) return;
     const uint32_t stored = (uint32_t)__builtin_amdgcn_ballot_w64(from >= 0);                            // bit t: token t
-    if (stored == 0) return;
+    if (stored == 0 || __builtin_amdgcn_ballot_w64(again) != 0) return;
     uint8_t* const out = cache_tile<D>(a.c, page, head, tile & ((1 << (a.c.shift - 5)) - 1));
 
     // what is read: rows (one that is not there: row 0, not stored) and, where the tile is not written as a whole, V's codes

@@ -53,6 +53,19 @@ def test_store_through_an_index_list(lib):
     assert np.array_equal(pair.pages.cpu().numpy(), pair.o.pages)
 
 
+def test_store_takes_the_first_row_of_a_slot(lib):
+    """A slot named again, next to or over what its first row stores, also far down the list."""
+    pair = Pair(lib, [64] * 4, 2, 64, 32)
+    n = 150
+    slots = [0, 1, 0, 1, 2] + [-1] * 140 + [2, 3, 0, 3, 9]
+    start = [0, 7, 10, 7, 40] + [0] * 140 + [50, 1, 0, 20, 0]
+    kt, k = bf16(pair.rng.normal(size=(10 * n, 2, 64)))
+    offsets = np.arange(n + 1) * 10
+    lib.cache_store(pair.cache, kt, kt, 10 * n, None, 10 * n, dev(offsets), dev(slots), dev(start), n, 10)
+    pair.o.store(k, k, None, offsets, slots, start)
+    assert np.array_equal(pair.pages.cpu().numpy(), pair.o.pages)
+
+
 def test_store_leaves_out_tokens_without_a_page(lib):
     pair = Pair(lib, [64, 64], 2, 64, 32)
     pair.o.table[0, 1], pair.o.table[1, 0] = -1, len(pair.o.refs)                        # a page that is not there, one outside the pool

@@ -70,6 +70,16 @@ def test_sizes():
     assert binding.cache_attention_workspace_bytes(long, 1, 1, 8, 1 << 30) == size          # (no more than a slot holds)
 
 
+def test_a_cache_of_tensors_that_do_not_belong_together():
+    import torch
+    pages, refs, table, lens = torch.zeros(4 * 2176 * 2, dtype=torch.uint8), torch.zeros(4, dtype=torch.int32), torch.zeros((3, 2), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    c = binding.make_cache(pages, refs, table, lens, 32, 2, 64)
+    assert (c.n_pages, c.page_tokens, c.n_slots, c.max_pages, c.n_kv_heads, c.head_dim) == (4, 32, 3, 2, 2, 64)
+    for bad in ((pages[1:], refs, table, lens), (pages, refs, table.t(), lens), (pages, refs, table, lens[1:]), (pages, torch.zeros(5, dtype=torch.int32), table, lens)):
+        with pytest.raises(ValueError):
+            binding.make_cache(*bad, 32, 2, 64)
+
+
 def test_how_an_attention_is_cut_up():
     c = cache(n_pages=1 << 15, max_pages=2048, n_slots=256, n_kv_heads=8)
     for n, tokens, hq, most, want in ((1, 1, 32, 1000, (1, 4, 8, 1, 1)), (1, 1, 32, 1537, (1, 4, 8, 1, 4)), (1, 1, 64, 1 << 16, (1, 2, 8, 1, 32)),
