@@ -41,10 +41,10 @@ int check_rows(const pyr_cache* c, int32_t n) {                  // of a call th
     return (int64_t)n * (1 + (int64_t)c->max_pages) >= kMost ? PYR_ERR_UNSUPPORTED : PYR_OK;
 }
 
-pyr::CacheView view(const pyr_cache* c) {
+pyr::PoolView view(const pyr_cache* c) {
     int shift = 5;
     while ((1 << shift) < c->page_tokens) ++shift;
-    return pyr::CacheView{(uint8_t*)c->pages, c->refs, c->table, c->lens, c->n_pages, c->n_slots, c->max_pages, shift, c->n_kv_heads};
+    return pyr::PoolView{{(uint8_t*)c->pages, c->table, c->lens, c->n_pages, c->n_slots, c->max_pages, shift, c->n_kv_heads}, c->refs};
 }
 
 int check_attention(const pyr_cache* c, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len, pyr::CacheAttention* plan) {
@@ -118,7 +118,7 @@ int pyr_cache_compact(const pyr_cache* cache, const int32_t* slots, int32_t n, c
     pyr_cache_compact_workspace_bytes(cache, n, &need);
     if (!workspace_ok(workspace, workspace_bytes, need)) return PYR_ERR_WORKSPACE;
     if ((int64_t)n * (((int64_t)max_keep + 31) / 32) * head_groups(cache) >= kMost) return PYR_ERR_UNSUPPORTED;
-    const pyr::CacheView c = view(cache);
+    const pyr::PoolView c = view(cache);
     rc = pyr::launch_cache_cut(c, slots, out_offsets, n, n_kept, max_keep, (int32_t*)workspace, status, (hipStream_t)stream);
     if (rc != PYR_OK) return rc;
     return pyr::launch_cache_move(c, cache->head_dim, slots, kept_idx, n_kept, seq_offsets, out_offsets, (const int32_t*)workspace, status, n, max_keep,

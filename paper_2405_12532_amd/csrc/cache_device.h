@@ -25,10 +25,12 @@ typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 // The parts of a pyr_cache that kernels use; token numbers in the pool (page * page_tokens + place) fit 31 bits.
 struct CacheView {
     uint8_t* pages;
-    int32_t* refs;
     int32_t* table;
     int32_t* lens;
     int32_t n_pages, n_slots, max_pages, shift /* log2(page_tokens) */, n_kv_heads;
+};
+struct PoolView : CacheView {
+    int32_t* refs;
 };
 
 __device__ __forceinline__ int cache_slot(const CacheView& c, const int32_t* slots, int b) {      // -1: a row that is skipped

@@ -60,7 +60,7 @@ __device__ __forceinline__ int scan(Shared& s, int x, int* total) {
 __device__ __forceinline__ bool claim(Shared& s, int slot) { return (atomicOr(&s.seen[slot >> 5], 1u << (slot & 31)) >> (slot & 31) & 1) == 0; }
 
 template <int kWaves>
-__device__ __forceinline__ void clear(Shared& s, const CacheView& c) {
+__device__ __forceinline__ void clear(Shared& s, const PoolView& c) {
     for (int i = threadIdx.x; i < (c.n_slots + 31) / 32; i += 64 * kWaves) s.seen[i] = 0;
     if (threadIdx.x == 0) s.status = 0;
     __syncthreads();
@@ -94,7 +94,7 @@ struct Counts {
     int4 x[kQuads];
 };
 __device__ __forceinline__ int place_of(int quad) { return (threadIdx.x >> 6) * (64 * kEach) + quad * 256 + (threadIdx.x & 63) * 4; }
-__device__ __forceinline__ Counts look(const CacheView& c, int base) {
+__device__ __forceinline__ Counts look(const PoolView& c, int base) {
     Counts y;
     const bool aligned = ((uintptr_t)c.refs & 15) == 0;
 #pragma unroll
@@ -129,7 +129,7 @@ __device__ __forceinline__ void rows_of_ranks(const Shared& s, int n, int first,
 // row at a time where there are many rows of many pages (25000 pages of 200 rows 30 -> 19 us), else every lane looks for the row of its page
 // (25000 of one row 11 us against 26).
 template <int kWaves>
-__device__ __forceinline__ int hand_out(Shared& s, const CacheView& c, int n, int need, Counts counts, Counts ahead) {
+__device__ __forceinline__ int hand_out(Shared& s, const PoolView& c, int n, int need, Counts counts, Counts ahead) {
     constexpr int kThreads = 64 * kWaves, kMany = 4;
     const int lane = threadIdx.x & 63;
     int found = 0;
@@ -198,10 +198,10 @@ __device__ __forceinline__ int hand_out(Shared& s, const CacheView& c, int n, in
     return need - found;
 }
 
-__device__ __forceinline__ int pages_of(const CacheView& c, int tokens) { return (int)(((int64_t)tokens + (1 << c.shift) - 1) >> c.shift); }
+__device__ __forceinline__ int pages_of(const PoolView& c, int tokens) { return (int)(((int64_t)tokens + (1 << c.shift) - 1) >> c.shift); }
 
 template <int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void cache_reserve_kernel(CacheView c, const int32_t* __restrict__ slots, const int32_t* __restrict__ n_new, int n,
+__global__ __launch_bounds__(64 * kWaves) void cache_reserve_kernel(PoolView c, const int32_t* __restrict__ slots, const int32_t* __restrict__ n_new, int n,
                                                                  int32_t* __restrict__ start, int32_t* __restrict__ status) {
     constexpr int kThreads = 64 * kWaves;
     __shared__ Shared s;
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_reserve_kernel(CacheView c,
 
 // A child's row: the last page of a parent that is not full gets a page of its own here; the rest is cache_fork_copy_kernel's.
 template <int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void cache_fork_kernel(CacheView c, const int32_t* __restrict__ parents, const int32_t* __restrict__ children, int n,
+__global__ __launch_bounds__(64 * kWaves) void cache_fork_kernel(PoolView c, const int32_t* __restrict__ parents, const int32_t* __restrict__ children, int n,
                                                               int32_t* __restrict__ status) {
     constexpr int kThreads = 64 * kWaves;
     __shared__ Shared s;
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_fork_kernel(CacheView c, co
 }
 
 // The full pages are shared, the tiles in use of the last one are copied.  grid: (n, heads); the first head's workgroup does the row too.
-__global__ __launch_bounds__(256) void cache_fork_copy_kernel(CacheView c, const int32_t* __restrict__ parents, const int32_t* __restrict__ children,
+__global__ __launch_bounds__(256) void cache_fork_copy_kernel(PoolView c, const int32_t* __restrict__ parents, const int32_t* __restrict__ children,
                                                               const int32_t* __restrict__ status, int tile_chunks) {
     const int state = *status, parent = parents[blockIdx.x], child = children[blockIdx.x];
     if (state != 0 || parent < 0) return;
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256) void cache_fork_copy_kernel(CacheView c, const
 }
 
 // A slot named twice is given back once, by the workgroup that takes its length.
-__global__ __launch_bounds__(256) void cache_release_kernel(CacheView c, const int32_t* __restrict__ slots) {
+__global__ __launch_bounds__(256) void cache_release_kernel(PoolView c, const int32_t* __restrict__ slots) {
     __shared__ int len;
     const int slot = cache_slot(c, slots, blockIdx.x);
     if (slot < 0) return;
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(256) void cache_release_kernel(CacheView c, const i
 // Rows cut to the lengths out_offsets[i + 1] - out_offsets[i], in fresh pages; what they were goes to old_rows [n, 1 + max_pages] (length, pages)
 // for cache_move_kernel, and the old pages are given back (after the new ones were handed out, so that the two have none in common).
 template <int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void cache_cut_kernel(CacheView c, const int32_t* __restrict__ slots, const int32_t* __restrict__ out_offsets, int n,
+__global__ __launch_bounds__(64 * kWaves) void cache_cut_kernel(PoolView c, const int32_t* __restrict__ slots, const int32_t* __restrict__ out_offsets, int n,
                                                              int n_list, int max_keep, int32_t* __restrict__ old_rows, int32_t* __restrict__ status) {
     constexpr int kThreads = 64 * kWaves;
     __shared__ Shared s;
@@ -402,15 +402,15 @@ __global__ __launch_bounds__(64 * kWaves) void cache_cut_kernel(CacheView c, con
 }  // namespace
 
 // A workgroup of four wavefronts where it looks at all the counts in two goes: its barriers are shorter.
-static bool few(const CacheView& c, int32_t n) { return n <= 256 && c.n_pages <= 8192; }
+static bool few(const PoolView& c, int32_t n) { return n <= 256 && c.n_pages <= 8192; }
 
-int launch_cache_reserve(const CacheView& c, const int32_t* slots, const int32_t* n_new, int32_t n, int32_t* start, int32_t* status, hipStream_t stream) {
+int launch_cache_reserve(const PoolView& c, const int32_t* slots, const int32_t* n_new, int32_t n, int32_t* start, int32_t* status, hipStream_t stream) {
     if (few(c, n)) hipLaunchKernelGGL(cache_reserve_kernel<4>, dim3(1), dim3(256), 0, stream, c, slots, n_new, n, start, status);
     else hipLaunchKernelGGL(cache_reserve_kernel<16>, dim3(1), dim3(1024), 0, stream, c, slots, n_new, n, start, status);
     return check_launch();
 }
 
-int launch_cache_fork(const CacheView& c, int32_t head_dim, const int32_t* parents, const int32_t* children, int32_t n, int32_t* status, hipStream_t stream) {
+int launch_cache_fork(const PoolView& c, int32_t head_dim, const int32_t* parents, const int32_t* children, int32_t n, int32_t* status, hipStream_t stream) {
     if (few(c, n)) hipLaunchKernelGGL(cache_fork_kernel<4>, dim3(1), dim3(256), 0, stream, c, parents, children, n, status);
     else hipLaunchKernelGGL(cache_fork_kernel<16>, dim3(1), dim3(1024), 0, stream, c, parents, children, n, status);
     const int rc = check_launch();
@@ -419,13 +419,13 @@ int launch_cache_fork(const CacheView& c, int32_t head_dim, const int32_t* paren
     return check_launch();
 }
 
-int launch_cache_release(const CacheView& c, const int32_t* slots, int32_t n, hipStream_t stream) {
+int launch_cache_release(const PoolView& c, const int32_t* slots, int32_t n, hipStream_t stream) {
     if (n == 0) return PYR_OK;
     hipLaunchKernelGGL(cache_release_kernel, dim3(n), dim3(256), 0, stream, c, slots);
     return check_launch();
 }
 
-int launch_cache_cut(const CacheView& c, const int32_t* slots, const int32_t* out_offsets, int32_t n, int32_t n_list, int32_t max_keep, int32_t* old_rows,
+int launch_cache_cut(const PoolView& c, const int32_t* slots, const int32_t* out_offsets, int32_t n, int32_t n_list, int32_t max_keep, int32_t* old_rows,
                      int32_t* status, hipStream_t stream) {
     if (few(c, n)) hipLaunchKernelGGL(cache_cut_kernel<4>, dim3(1), dim3(256), 0, stream, c, slots, out_offsets, n, n_list, max_keep, old_rows, status);
     else hipLaunchKernelGGL(cache_cut_kernel<16>, dim3(1), dim3(1024), 0, stream, c, slots, out_offsets, n, n_list, max_keep, old_rows, status);

@@ -56,22 +56,22 @@ struct StoreArgs {
     CacheView c;
     const uint16_t *k, *v;
     const int32_t *row_idx, *offsets, *slots, *start;
-    int32_t n_rows, n_list;
+    int32_t n_rows, n_list, tiles_of_piece, head_groups;
 };
 static_assert(sizeof(StoreArgs) <= 112, "short arguments");
 
 // Rows are read and quantised as they lie in memory, 16 bytes a lane; their codes and scales meet in LDS, from where the lanes take them in
 // the tile's order, V's through transposing reads that turn bytes of two channels of a token into words of eight tokens of a channel.
 template <int D>
-__global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a, int32_t tiles_of_piece, int32_t head_groups) {
+__global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a) {
     constexpr int kBlocks = D / 32, kHalves = D / 64, kRow = D / 2 + 16;      // bytes of a token's codes in LDS
     struct Staged {
         uint8_t k[32][kRow], v[32][kRow], scales[2 * D];
     };
     __shared__ __align__(16) Staged all_staged[kWaves];
     const int lane = threadIdx.x & 63, t = lane & 15, j = lane >> 4;
-    const int place = blockIdx.x / head_groups, b = place / tiles_of_piece;
-    const int head = (blockIdx.x - place * head_groups) * kWaves + (threadIdx.x >> 6);
+    const int place = blockIdx.x / a.head_groups, b = place / a.tiles_of_piece;
+    const int head = (blockIdx.x - place * a.head_groups) * kWaves + (threadIdx.x >> 6);
     const int slot = cache_slot(a.c, a.slots, b);
     const int start = a.start[b];
     const int first = max(a.offsets[b], 0), last = min(a.offsets[b + 1], a.n_list);
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a, i
     for (int i = lane; i < b; i += 64) again |= a.slots[i] == slot;
     if (slot < 0 || start < 0 || first >= last || head >= a.c.n_kv_heads) return;
     const int64_t end = min((int64_t)start + (last - first), (int64_t)a.c.max_pages << a.c.shift);       // tokens start .. end - 1
-    const int tile = (start >> 5) + (place - b * tiles_of_piece);
+    const int tile = (start >> 5) + (place - b * a.tiles_of_piece);
     const int64_t token0 = (int64_t)tile * 32;
     if (token0 >= end) return;
     const int page = a.c.table[(int64_t)slot * a.c.max_pages + (token0 >> a.c.shift)];
@@ -102,8 +102,10 @@ __global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a, i
     constexpr int kLanes = D / 8, kLoads = 32 * kLanes / 64;      // lanes of a row
     const int64_t row_words = (int64_t)a.c.n_kv_heads * D;
     u32x4 kx[kLoads], vx[kLoads];
+    auto some = [&](int i) { return (stored >> (i * (64 / kLanes)) & ((1u << (64 / kLanes)) - 1)) != 0; };      // (of a load's rows: one token is one load)
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
+        if (!some(i)) continue;
         const int64_t at = max(__shfl(from, i * (64 / kLanes) + lane / kLanes), 0) * row_words + head * D + 8 * (lane % kLanes);
         kx[i] = __builtin_nontemporal_load((const u32x4*)(a.k + at));
         vx[i] = __builtin_nontemporal_load((const u32x4*)(a.v + at));
@@ -122,6 +124,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a, i
     Staged& staged = all_staged[threadIdx.x >> 6];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
+        if (!some(i)) continue;
         const int token = i * (64 / kLanes) + lane / kLanes, piece = lane % kLanes, block = piece >> 2;
         uint32_t ks, vs;
         *(uint32_t*)&staged.k[token][4 * piece] = codes_of(kx[i], &ks);
@@ -249,7 +252,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_load_kernel(LoadArgs a) {
 struct MoveArgs {
     CacheView c;
     const int32_t *slots, *kept_idx, *seq_offsets, *out_offsets, *old_rows, *status;
-    int32_t n_list, tiles_of_seq;
+    int32_t n_list, tiles_of_seq, head_groups;
 };
 static_assert(sizeof(MoveArgs) <= 112, "short arguments");
 
@@ -259,15 +262,15 @@ static_assert(sizeof(MoveArgs) <= 112, "short arguments");
 // K's codes are gathered by 16 bytes.  V's are taken a source tile at a time (kept tokens come in order, so that there are two or three; any order
 // works): read as they lie, turned in LDS to a row of bytes per token, the kept rows copied, and turned back into words of eight tokens.
 template <int D>
-__global__ __launch_bounds__(64 * kWaves) void cache_move_kernel(MoveArgs a, int32_t head_groups) {
+__global__ __launch_bounds__(64 * kWaves) void cache_move_kernel(MoveArgs a) {
     constexpr int kBlocks = D / 32, kHalves = D / 64, kRow = D / 2 + 16;
     struct Staged {
         uint8_t words[kBlocks][4][16][8], source[32][kRow], kept[32][kRow];
     };
     __shared__ __align__(16) Staged all_staged[kWaves];
     const int lane = threadIdx.x & 63, t = lane & 15, j = lane >> 4;
-    const int place = blockIdx.x / head_groups, b = place / a.tiles_of_seq, tile = place - b * a.tiles_of_seq;
-    const int first_head = (blockIdx.x - place * head_groups) * kWaves + (threadIdx.x >> 6), head_step = head_groups * kWaves;
+    const int place = blockIdx.x / a.head_groups, b = place / a.tiles_of_seq, tile = place - b * a.tiles_of_seq;
+    const int first_head = (blockIdx.x - place * a.head_groups) * kWaves + (threadIdx.x >> 6), head_step = a.head_groups * kWaves;
     const int tile_shift = a.c.shift - 5, tile_mask = (1 << tile_shift) - 1;
     const int status = *a.status, slot = cache_slot(a.c, a.slots, b), first = a.out_offsets[b], base = a.seq_offsets[b];
     if (status != 0 || slot < 0) return;
@@ -382,11 +385,10 @@ int launch_cache_store(const CacheView& c, int32_t head_dim, const void* k, cons
                        const int32_t* offsets, const int32_t* slots, const int32_t* start, int32_t n_seqs, int32_t max_new, hipStream_t stream) {
     if (n_seqs == 0 || max_new == 0) return PYR_OK;
     const int32_t tiles = (max_new + 30) / 32 + 1;
-    const StoreArgs a{c, (const uint16_t*)k, (const uint16_t*)v, row_idx, offsets, slots, start, n_rows, n_list};
-    const int32_t head_groups = (c.n_kv_heads + kWaves - 1) / kWaves;
-    const dim3 grid((unsigned)((int64_t)n_seqs * tiles * head_groups));
-    if (head_dim == 128) hipLaunchKernelGGL(cache_store_kernel<128>, grid, dim3(64 * kWaves), 0, stream, a, tiles, head_groups);
-    else hipLaunchKernelGGL(cache_store_kernel<64>, grid, dim3(64 * kWaves), 0, stream, a, tiles, head_groups);
+    const StoreArgs a{c, (const uint16_t*)k, (const uint16_t*)v, row_idx, offsets, slots, start, n_rows, n_list, tiles, (c.n_kv_heads + kWaves - 1) / kWaves};
+    const dim3 grid((unsigned)((int64_t)n_seqs * tiles * a.head_groups));
+    if (head_dim == 128) hipLaunchKernelGGL(cache_store_kernel<128>, grid, dim3(64 * kWaves), 0, stream, a);
+    else hipLaunchKernelGGL(cache_store_kernel<64>, grid, dim3(64 * kWaves), 0, stream, a);
     return check_launch();
 }
 
@@ -403,13 +405,12 @@ int launch_cache_load(const CacheView& c, int32_t head_dim, const int32_t* slots
 int launch_cache_move(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* kept_idx, int32_t n_list, const int32_t* seq_offsets,
                       const int32_t* out_offsets, const int32_t* old_rows, const int32_t* status, int32_t n_seqs, int32_t max_keep, hipStream_t stream) {
     if (n_seqs == 0 || max_keep == 0) return PYR_OK;
-    const MoveArgs a{c, slots, kept_idx, seq_offsets, out_offsets, old_rows, status, n_list, (max_keep + 31) / 32};
+    MoveArgs a{c, slots, kept_idx, seq_offsets, out_offsets, old_rows, status, n_list, (max_keep + 31) / 32, (c.n_kv_heads + kWaves - 1) / kWaves};
     const int64_t places = (int64_t)n_seqs * a.tiles_of_seq;
-    int32_t head_groups = (c.n_kv_heads + kWaves - 1) / kWaves;
-    while (head_groups > 1 && places * ((head_groups + 1) / 2) >= 1024) head_groups = (head_groups + 1) / 2;
-    const dim3 grid((unsigned)(places * head_groups));
-    if (head_dim == 128) hipLaunchKernelGGL(cache_move_kernel<128>, grid, dim3(64 * kWaves), 0, stream, a, head_groups);
-    else hipLaunchKernelGGL(cache_move_kernel<64>, grid, dim3(64 * kWaves), 0, stream, a, head_groups);
+    while (a.head_groups > 1 && places * ((a.head_groups + 1) / 2) >= 1024) a.head_groups = (a.head_groups + 1) / 2;
+    const dim3 grid((unsigned)(places * a.head_groups));
+    if (head_dim == 128) hipLaunchKernelGGL(cache_move_kernel<128>, grid, dim3(64 * kWaves), 0, stream, a);
+    else hipLaunchKernelGGL(cache_move_kernel<64>, grid, dim3(64 * kWaves), 0, stream, a);
     return check_launch();
 }
 

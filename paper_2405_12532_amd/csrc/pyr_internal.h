@@ -154,6 +154,7 @@ int launch_gather_positions(const int32_t* pos, const int32_t* kept_idx, int64_t
 
 // The cache held in 4 bits (cache_device.h says how it lies in memory; cache_api.hip checks the arguments).
 struct CacheView;
+struct PoolView;
 constexpr int kMaxCacheRows = PYR_CACHE_MAX_ROWS, kMaxCacheSlots = PYR_CACHE_MAX_SLOTS;
 
 // How an attention over the cache is cut up: 16-row column tiles of a workgroup; times that one holds the rows; wavefronts; workgroups per head and split; 32-token
@@ -169,11 +170,11 @@ int launch_cache_store(const CacheView& c, int32_t head_dim, const void* k, cons
                        const int32_t* offsets, const int32_t* slots, const int32_t* start, int32_t n_seqs, int32_t max_new, hipStream_t stream);
 int launch_cache_load(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* offsets, int32_t n_seqs, int32_t max_len,
                       void* k, void* v, int32_t n_rows, hipStream_t stream);
-int launch_cache_reserve(const CacheView& c, const int32_t* slots, const int32_t* n_new, int32_t n, int32_t* start, int32_t* status, hipStream_t stream);
-int launch_cache_fork(const CacheView& c, int32_t head_dim, const int32_t* parents, const int32_t* children, int32_t n, int32_t* status, hipStream_t stream);
-int launch_cache_release(const CacheView& c, const int32_t* slots, int32_t n, hipStream_t stream);
+int launch_cache_reserve(const PoolView& c, const int32_t* slots, const int32_t* n_new, int32_t n, int32_t* start, int32_t* status, hipStream_t stream);
+int launch_cache_fork(const PoolView& c, int32_t head_dim, const int32_t* parents, const int32_t* children, int32_t n, int32_t* status, hipStream_t stream);
+int launch_cache_release(const PoolView& c, const int32_t* slots, int32_t n, hipStream_t stream);
 // A cut is two launches: the rows of the table, which leaves the old ones in old_rows [n, 1 + max_pages], and the tokens.
-int launch_cache_cut(const CacheView& c, const int32_t* slots, const int32_t* out_offsets, int32_t n, int32_t n_list, int32_t max_keep, int32_t* old_rows,
+int launch_cache_cut(const PoolView& c, const int32_t* slots, const int32_t* out_offsets, int32_t n, int32_t n_list, int32_t max_keep, int32_t* old_rows,
                      int32_t* status, hipStream_t stream);
 int launch_cache_move(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* kept_idx, int32_t n_list, const int32_t* seq_offsets,
                       const int32_t* out_offsets, const int32_t* old_rows, const int32_t* status, int32_t n_seqs, int32_t max_keep, hipStream_t stream);
