@@ -3,14 +3,15 @@
 //
 // A wavefront owns one tile (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte, and the halves of a byte are
 // tokens of the same tile.
-// Bound: reading and writing HBM.
+// Bound: reading and writing HBM.  70 % of 8 x 2048 rows on 32 heads, d = 128, K and V: stored 42 us, 239 MB, 5.7 TB/s, read back 36 us, 6.6 TB/s; cut
+// from 8 x 2048 tokens 28 us (122 MB with the whole lines that single tokens of a tile take, 4.3 TB/s), 4 x 32768 tokens on 8 heads cut to one half 47 us
+// (255 MB so, 5.4 TB/s).  V's rows of eight tokens gathered word by word instead took 29 us with 178 registers and 73 us with 128.
 #include "cache_device.h"
 
 namespace pyr {
 namespace {
 
-// bf16 rows are read and written past the caches (nontemporal), codes are not: 70 % of 8 x 2048 tokens on 32 heads stored and read back 103 -> 78 us,
-// cut and read back 97 -> 86 us.
+// bf16 rows are read and written past the caches (nontemporal), codes are not: stored and read back 103 -> 78 us, cut and read back 97 -> 86 us.
 constexpr int kWaves = 4;
 
 __device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b) {      // of both halves
