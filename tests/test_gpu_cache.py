@@ -309,6 +309,21 @@ def test_pages_of_a_large_pool_are_handed_out_from_the_lowest(lib):
     assert pair.refs.cpu().tolist() == used.astype(int).tolist() and not pair.lens.any() and (pair.table == -1).all()
 
 
+def test_counts_that_are_not_aligned(lib):
+    """The counts of a pool begin anywhere (several caches may share one tensor)."""
+    pair = Pair(lib, [40, 0], 1, 64, 32, n_slots=2, max_pages=200, spare=301)
+    pair.o.refs[5:200:3] = 1
+    pair.up()
+    all_refs = torch.zeros(len(pair.o.refs) + 1, dtype=torch.int32, device="cuda")
+    all_refs[1:] = pair.refs
+    pair.refs = all_refs[1:]
+    pair.cache = lib.make_cache(pair.pages, pair.refs, pair.table, pair.lens, 32, 1, 64)
+    assert pair.refs.data_ptr() % 16 != 0
+    assert both_reserve(pair, [1, 0], [199 * 32, 7]) == 0
+    assert both_reserve(pair, [0], [100 * 32]) > 0
+    assert int(all_refs[0]) == 0
+
+
 def test_rows_that_cannot_be_are_refused_on_the_device(lib):
     pair = Pair(lib, [40, 50, 0], 1, 64, 32, n_slots=3, max_pages=3, spare=6)
     for slots, n_new, status in (([0, 0], [1, 1], -1), ([3], [1], -1), ([-2], [1], -1), ([0], [-1], -2), ([0], [57], -2), ([1, 1], [1, 100], -2),
@@ -324,6 +339,48 @@ def test_rows_that_cannot_be_are_refused_on_the_device(lib):
     assert both_compact(pair, [0], kept, [0], [0, 5], 5) == 0
     k, v = pair.o.read(0)
     assert [bool(np.isnan(x).all()) for x in k] == [False, True, True, False, True]
+
+
+def test_offsets_past_32_bits(lib):
+    """A pool of 5 GB and rows of 2^31 numbers and more: the same calls on their last pages and rows as on a small pool and few rows, bit for bit."""
+    hkv, d, page, many, rows = 32, 128, 1024, 1100, 530000
+    big_pages = many * lib.cache_page_bytes(page, hkv, d)
+    assert big_pages > 1 << 32 and rows * hkv * d > 1 << 31
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    near = [torch.randn((1500, hkv, d), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    far = [torch.empty((rows, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for x, y in zip(near, far):
+        y[rows - 1500:] = x
+    q = torch.randn((1, 1, 32, d), generator=gen, device="cuda").to(torch.bfloat16)
+    results = []
+    for n_pages, k, v in ((6, *near), (many, *far)):
+        n_rows, lift, shift = k.shape[0], n_pages - 6, k.shape[0] - 1500
+        pages = torch.empty(n_pages * lib.cache_page_bytes(page, hkv, d), dtype=torch.uint8, device="cuda")
+        refs, table, lens = torch.ones(n_pages, dtype=torch.int32, device="cuda"), torch.full((2, 3), -1, dtype=torch.int32, device="cuda"), dev([0, 0])
+        refs[lift:] = 0
+        pages[-6 * lib.cache_page_bytes(page, hkv, d):] = 0
+        c = lib.make_cache(pages, refs, table, lens, page, hkv, d)
+        status, start, idx = dev([9]), dev([9]), torch.arange(shift, n_rows, dtype=torch.int32, device="cuda")
+        lib.cache_reserve(c, dev([0]), dev([1500]), 1, start, status)
+        lib.cache_store(c, k, v, n_rows, idx, 1500, dev([0, 1500]), dev([0]), start, 1, 1500)
+        lib.cache_fork(c, dev([0]), dev([1]), 1, status)
+        size = lib.cache_compact_workspace_bytes(c, 1)
+        ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+        kept = torch.arange(1, 1500, 2, dtype=torch.int32, device="cuda")
+        lib.cache_compact(c, dev([1]), 1, kept, 750, dev([0]), dev([0, 750]), 750, status, ws, size)
+        k_out, v_out = torch.empty_like(k), torch.empty_like(k)
+        lib.cache_load(c, dev([1]), dev([n_rows - 750, n_rows]), 1, 750, k_out, v_out, n_rows)
+        out = torch.empty_like(q)
+        size = lib.cache_attention_workspace_bytes(c, 1, 1, 32, 1500)
+        ws = torch.empty(max(size, 256), dtype=torch.uint8, device="cuda")
+        lib.cache_attention(c, q, dev([0]), 1, 1, 32, 1500, 0.0, out, None, ws, size)
+        torch.cuda.synchronize()
+        assert int(status) == 0 and int(start) == 0 and lens.cpu().tolist() == [1500, 750]
+        results.append((table.cpu() - lift * (table.cpu() >= 0), refs[lift:].cpu(), pages[-6 * lib.cache_page_bytes(page, hkv, d):].clone(),
+                        k_out[n_rows - 750:].view(torch.int16).clone(), v_out[n_rows - 750:].view(torch.int16).clone(), out.view(torch.int16)))
+        del pages, k_out, v_out
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
 
 
 # ------------------------------------------------------------------------------------------------ streams, graphs, together
@@ -386,6 +443,80 @@ def test_captured_steps_grow_the_sequences_on_every_replay(lib):
             assert torch.equal(getattr(pairs[0], name), getattr(pairs[1], name)), (i, name)
         check_attention(pairs[0], qs[i][1], [2, 0, 1, 3, -1], bufs[0]["out"], bufs[0]["lse"])
     pairs[0].check()
+
+
+def test_captured_steps_run_out_of_pages(lib):
+    """Every replay asks for 20 tokens a row; the pool holds two replays' worth.  From the third on nothing changes but the status."""
+    pair = Pair(lib, [10, 30], 2, 64, 32, n_slots=2, max_pages=20, spare=4)
+    kt, k = bf16(pair.rng.normal(size=(40, 2, 64)))
+    slots, n_new, offsets, start = dev([0, 1]), dev([20, 20]), dev([0, 20, 40]), dev([7, 7])
+    qt, q = bf16(pair.rng.normal(size=(2, 20, 2, 64)) * 0.3)
+    out, lse = torch.empty_like(qt), torch.empty(2, 20, 2, dtype=torch.float32, device="cuda")
+    assert lib.cache_attention_workspace_bytes(pair.cache, 2, 20, 2, 200) == 0
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        lib.cache_reserve(pair.cache, slots, n_new, 2, start, pair.status)
+        lib.cache_store(pair.cache, kt, kt, 40, None, 40, offsets, slots, start, 2, 20)
+        lib.cache_attention(pair.cache, qt, slots, 2, 20, 2, 200, 0.0, out, lse, None, 0)
+    said = []
+    for _ in range(6):
+        g.replay()
+        want, status = pair.o.reserve([0, 1], [20, 20])
+        pair.o.store(k, k, None, [0, 20, 40], [0, 1], want)
+        said.append(status)
+        assert int(pair.status) == status and start.cpu().tolist() == want.tolist()
+        pair.check()
+        check_attention(pair, q, [0, 1], out, lse)
+    assert said[0] == 0 and said[-1] > 0 and said[-1] == said[-2]
+
+
+def test_captured_branches(lib):
+    """release, fork, compact and load in a graph, while the parents change between replays."""
+    pair = Pair(lib, [100, 70], 2, 128, 32, n_slots=4, max_pages=8, spare=20)
+    parents, children, status = dev([0, 1]), dev([2, 3]), pair.status
+    kept, off, koff = np.array([5, 99, 40, 100, 130, 169]), [0, 100], [0, 3, 6]
+    kept_d, off_d, koff_d = dev(kept), dev(off), dev(koff)
+    size = lib.cache_compact_workspace_bytes(pair.cache, 2)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    k_out, v_out = (torch.empty((6, 2, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        lib.cache_release(pair.cache, children, 2)
+        lib.cache_fork(pair.cache, parents, children, 2, status)
+        lib.cache_compact(pair.cache, children, 2, kept_d, 6, off_d, koff_d, 3, status, ws, size)
+        lib.cache_load(pair.cache, children, koff_d, 2, 3, k_out, v_out, 6)
+    for i in range(4):
+        g.replay()
+        pair.o.release([2, 3])
+        assert pair.o.fork([0, 1], [2, 3]) == 0 and pair.o.compact([2, 3], kept, off, koff, 3) == 0
+        pair.check()
+        assert int(status) == 0
+        assert np.array_equal(k_out.double().cpu().numpy(), np.concatenate([pair.o.read(2)[0], pair.o.read(3)[0]]))
+        assert np.array_equal(v_out.double().cpu().numpy(), np.concatenate([pair.o.read(2)[1], pair.o.read(3)[1]]))
+        kt, k = bf16(pair.rng.normal(size=(i + 1, 2, 128)))
+        start = dev([0])
+        lib.cache_reserve(pair.cache, dev([1]), dev([i + 1]), 1, start, status)
+        lib.cache_store(pair.cache, kt, kt, i + 1, None, i + 1, dev([0, i + 1]), dev([1]), start, 1, i + 1)
+        pair.o.store(k, k, None, [0, i + 1], [1], pair.o.reserve([1], [i + 1])[0])
+
+
+def test_two_attentions_at_once(lib):
+    """Two streams read one cache, each with its own workspace."""
+    pair = Pair(lib, [3000, 500], 2, 128, 64)
+    qs = [bf16(pair.rng.normal(size=(2, 1, 8, 128)) * 0.2) for _ in range(2)]
+    reads = {s: pair.o.read(s) for s in range(2)}
+    size = lib.cache_attention_workspace_bytes(pair.cache, 2, 1, 8, 3000)
+    assert size > 0
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], []
+    bufs = [(torch.empty(size, dtype=torch.uint8, device="cuda"), torch.empty_like(q[0]), torch.empty(2, 1, 8, dtype=torch.float32, device="cuda")) for q in qs]
+    slots = dev([0, 1])
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for st, q, (ws, out, lse) in zip(streams, qs, bufs):
+            lib.cache_attention(pair.cache, q[0], slots, 2, 1, 8, 3000, 0.0, out, lse, ws, size, stream=st)
+    torch.cuda.synchronize()
+    for q, (ws, out, lse) in zip(qs, bufs):
+        check_attention(pair, q[1], [0, 1], out, lse, reads=reads)
 
 
 def test_from_a_prompt_to_the_cache_and_through_its_updates(lib):
