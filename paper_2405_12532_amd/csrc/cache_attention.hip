@@ -11,11 +11,11 @@
 // the end.  One more product, of ones and the rounded P, sums what O is divided by: rounding P by itself (2^-9) would show in rows that one token
 // dominates; lse comes from the sum before rounding.  P, both sums and O are fp32.
 // A row's reference is its largest logit when it was last moved, and it is moved when the weights of a tile add up to more than 2^12 in a lane; so most
-// tiles neither look for a maximum nor rescale (12 of 160 instructions).  Two tiles are in flight per wavefront.
+// tiles neither look for a maximum nor rescale.  Two tiles are in flight per wavefront.
 //
 // Bound: reading the cache.  64 x 2048 tokens on 32 heads, d = 128: 87 us for 571 MB, 6.6 TB/s (counters: read = the cache's bytes; vector instructions
-// 51 % of the time, 169 a tile, matrix pipe 20 %); loads that go through the caches 94 us, P' made for every block instead of once for four 102 us, four
-// wavefronts a SIMD with two registers spilled 94 us, the loop's two copies made one that moves registers 90 us.
+// 51 % of the time, 169 a tile, matrix pipe 20 %).  On the way there: through the caches, with P' made for every block 102, past them 94, P' made once for
+// four blocks 87; four wavefronts a SIMD with two registers spilled 95, one copy of the loop with moves of registers instead of two 90.
 #include <float.h>
 #include <math.h>
 

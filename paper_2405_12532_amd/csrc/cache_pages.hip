@@ -2,7 +2,7 @@
 // counts are all the state there is.  Pages are handed out from the lowest, in the order of the rows that ask, so that what a call
 // does follows from the state alone; a call that finds too few changes nothing.  Everything a call decides is decided by one workgroup
 // (limits: kMaxRows rows a call, kMaxSlots slots), which looks through the counts 16 per lane at a time and stops at the last page it needs.
-// Bound: the latency of the launch and of that workgroup's dependent loads: room for a token each of 64 sequences 3 us, for 2048 pages 7 us, for 25000 of
+// Bound: the latency of the launch and of that workgroup's dependent loads: room for a token each of 64 sequences 3 us, for 2048 pages 6 us, for 25000 of
 // 54000 pages 22 us; a fork 4 to 6 us and its copy 3 to 5 us, a release 2 to 5 us, the table's part of a cut 8 us.
 #include "cache_device.h"
 
@@ -141,8 +141,10 @@ __device__ __forceinline__ int hand_out(Shared& s, const PoolView& c, int n, int
         for (int i = 0; i < kQuads; ++i) {
             const int4 x = counts.x[i];
             free[i] = (x.x == 0) | (x.y == 0) << 1 | (x.z == 0) << 2 | (x.w == 0) << 3;
+            rank[i] = of_wave;
+            if (__builtin_amdgcn_ballot_w64(free[i] != 0) == 0) continue;      // (most of a pool is in use)
             const int mine = __popc(free[i]), sum = scan_wave(mine);
-            rank[i] = of_wave + sum - mine;
+            rank[i] += sum - mine;
             of_wave += __builtin_amdgcn_readlane(sum, 63);
         }
         counts = ahead;
@@ -150,10 +152,13 @@ __device__ __forceinline__ int hand_out(Shared& s, const PoolView& c, int n, int
         int total;
         const int before = scan_waves<kWaves>(s, of_wave, &total);
 #pragma unroll
-        for (int i = 0; i < kQuads; ++i)
+        for (int i = 0; i < kQuads; ++i) {
+            if (__builtin_amdgcn_ballot_w64(free[i] != 0) == 0) continue;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (free[i] >> k & 1) s.free[before + rank[i]++] = (uint16_t)(place_of(i) + k);
+        }
+        if (total == 0) continue;
         __syncthreads();
         const int taken = min(total, need - found);
         constexpr int kLong = 24;
@@ -402,8 +407,9 @@ __global__ __launch_bounds__(64 * kWaves) void cache_cut_kernel(PoolView c, cons
 
 }  // namespace
 
-// A workgroup of four wavefronts where it looks at all the counts in two goes: its barriers are shorter.
-static bool few(const PoolView& c, int32_t n) { return n <= 256 && c.n_pages <= 8192; }
+// A workgroup of four wavefronts where one look of it takes all counts: its barriers are shorter (a page of 1500 for one of 8 rows 4.3 us, sixteen wavefronts
+// 5.3), though it takes longer over many pages (2048 of 4000 7.1 us, 5.9).
+static bool few(const PoolView& c, int32_t n) { return n <= 256 && c.n_pages <= 4 * 64 * kEach; }
 
 int launch_cache_reserve(const PoolView& c, const int32_t* slots, const int32_t* n_new, int32_t n, int32_t* start, int32_t* status, hipStream_t stream) {
     if (few(c, n)) hipLaunchKernelGGL(cache_reserve_kernel<4>, dim3(1), dim3(256), 0, stream, c, slots, n_new, n, start, status);
