@@ -313,7 +313,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && (D == 64 || R == 4) ? 3 : 2
     }
 }
 
-// The splits of a row, weighted by 2^(reference - largest) and added up: one workgroup a row, D / 4 threads a split.
+// The splits of a row, weighted by 2^(reference - largest) and added up: D / 4 threads a split, kSets splits of a row at a time.
 struct JoinArgs {
     CacheView c;
     const int32_t* slots;
@@ -325,23 +325,22 @@ struct JoinArgs {
 };
 static_assert(sizeof(JoinArgs) <= 112, "short arguments");
 
-template <int D>
+template <int D, int kSets>
 __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs a) {
-    constexpr int kQuads = D / 4, kSets = 256 / kQuads;
-    __shared__ float tops[4];
-    __shared__ f32x4 sums[kSets][kQuads];
-    __shared__ float weights[kSets][2];
-    const int row = blockIdx.x, set = threadIdx.x / kQuads, quad = threadIdx.x % kQuads;
+    constexpr int kQuads = D / 4, kThreads = kQuads * kSets, kRows = 256 / kThreads;
+    __shared__ f32x4 sums[kRows][kSets][kQuads];
+    __shared__ float weights[kRows][kSets][2], tops[kRows][kSets];
+    const int r = threadIdx.x / kThreads, set = threadIdx.x % kThreads / kQuads, quad = threadIdx.x % kQuads;
+    const int row = min((int)blockIdx.x * kRows + r, a.rows - 1);          // (the last workgroup's spare threads: the last row again)
     const int slot = cache_slot(a.c, a.slots, row / a.rows_of_seq);
     const int tiles = slot < 0 ? 0 : (cache_len(a.c, slot) + 31) >> 5;
     const int live = min(a.splits, max(1, (tiles + a.chunk - 1) / a.chunk));
     float top = -FLT_MAX;
-    for (int s = threadIdx.x; s < live; s += 256) top = fmaxf(top, a.stats[(int64_t)s * a.rows + row][0]);
-#pragma unroll
-    for (int x = 1; x < 64; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    for (int s = set; s < live; s += kSets) top = fmaxf(top, a.stats[(int64_t)s * a.rows + row][0]);
+    tops[r][set] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+#pragma unroll
+    for (int x = 0; x < kSets; ++x) top = fmaxf(top, tops[r][x]);
     float sum = 0.f, weight = 0.f;
     f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -353,18 +352,18 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs a) {
         weight += f * st[2];
         o += f * *(const f32x4*)(a.parts + at * D + 4 * quad);
     }
-    sums[set][quad] = o;
+    sums[r][set][quad] = o;
     if (quad == 0) {
-        weights[set][0] = sum;
-        weights[set][1] = weight;
+        weights[r][set][0] = sum;
+        weights[r][set][1] = weight;
     }
     __syncthreads();
     if (set != 0) return;
 #pragma unroll
     for (int x = 1; x < kSets; ++x) {
-        o += sums[x][quad];
-        sum += weights[x][0];
-        weight += weights[x][1];
+        o += sums[r][x][quad];
+        sum += weights[r][x][0];
+        weight += weights[r][x][1];
     }
     const float f = weight == 0.f ? 0.f : 1.f / weight;
     bf16x4 y;
@@ -392,19 +391,25 @@ int launch(const CacheAttention& x, const CacheView& c, const AttendArgs& a, voi
     if (rc != PYR_OK || a.splits == 1) return rc;
     const int32_t rows_of_seq = a.n_tokens * a.n_q_heads, rows = a.n_seqs * rows_of_seq;
     const JoinArgs j{c, a.slots, (const float*)a.out, (const f32x4*)a.lse, (uint16_t*)out, lse, rows, rows_of_seq, a.chunk, a.splits};
-    hipLaunchKernelGGL(cache_join_kernel<D>, dim3((unsigned)rows), dim3(256), 0, stream, j);
+    constexpr int kFew = 2, kMany = 1024 / D;
+    if (a.splits <= 2 * kFew) {
+        constexpr int kRows = 256 / (D / 4 * kFew);
+        hipLaunchKernelGGL((cache_join_kernel<D, kFew>), dim3((unsigned)((rows + kRows - 1) / kRows)), dim3(256), 0, stream, j);
+    } else {
+        hipLaunchKernelGGL((cache_join_kernel<D, kMany>), dim3((unsigned)rows), dim3(256), 0, stream, j);
+    }
     return check_launch();
 }
 
 }  // namespace
 
-// What is waited for at the end is the wavefront with the most tiles (0.4 us each), so few heads are split along the cache, into at most
-// kWorkgroups parts of kShortest tiles and more - unless a launch that joins the parts (4 us, and 3 us of the host's) costs more than it saves.
+// What is waited for at the end is the wavefront with the most tiles (0.4 us each), so few heads are split along the cache, until there are 2 * kUnits
+// workgroups of kShortest tiles and more - unless a launch that joins the parts (4 us, and 3 us of the host's) costs more than it saves.
 // Workgroups of eight wavefronts do with half as many parts; one fits a compute unit, so they are taken where they fill nearly all of them
 // in one go.  Measured, us (four wavefronts, eight): one token of 1 x 1000 on 32/8 heads 9.5 / 8.2 (unsplit), 1 x 1434 on 32 12.2 / 10.2, 32 x 4096 on
 // 32/8 29.7 / 26.6, 1 x 32768 on 32/8 13.6 / 12.9; 20 of 100 ... 8000 on 64/8 (160 heads) 31 / 38, 40 x 1500 on 32/8 (320 heads) 17 / 21.
-// Unsplit up to 1500 tokens: 1 x 1434 on 32 heads 10.3 against 9.8 and a launch; 1 x 2048 11.9 / 9.9.  More than 16 rows a head: 256 workgroups, as
-// the parts' results are larger (16 x 2048 on 64/8 heads, nine tokens: 36 us, with 512 43).
+// Unsplit up to 1500 tokens: 1 x 1434 on 32 heads 10.3 against 9.8 and a launch; 1 x 2048 11.9 / 9.9.  More than 16 rows a head: parts twice as long, as
+// their results are twice as large (us for parts of 16, 32 and 64 tiles: 8 x 4096 on 64/8 heads, four tokens 21.4 / 19.7 / 26; 16 x 2048, nine 36 / 35 / 32.5).
 CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_len) {
     constexpr int64_t kUnsplit = 48, kShortest = 16, kUnits = 256, kFilled = 200;
     CacheAttention x{};
@@ -421,11 +426,11 @@ CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_
         x.waves = 8;
         splits = kUnits / units;
     } else if (units > 0) {
-        const int64_t workgroups = x.col_tiles == 1 ? 2 * kUnits : kUnits;
-        splits = (workgroups + units - 1) / units;
+        splits = (2 * kUnits + units - 1) / units;
     }
     int64_t chunk = (key_tiles + splits - 1) / splits;
-    if (splits > 1 && chunk < kShortest) chunk = kShortest;
+    const int64_t shortest = x.col_tiles * kShortest;
+    if (splits > 1 && chunk < shortest) chunk = shortest;
     chunk = (chunk + x.waves - 1) / x.waves * x.waves;
     if (chunk == 0) chunk = x.waves;
     splits = (key_tiles + chunk - 1) / chunk;

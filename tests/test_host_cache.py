@@ -84,7 +84,7 @@ def test_how_an_attention_is_cut_up():
     c = cache(n_pages=1 << 15, max_pages=2048, n_slots=256, n_kv_heads=8)
     for n, tokens, hq, most, want in ((1, 1, 32, 1000, (1, 4, 8, 1, 1)), (1, 1, 32, 1537, (1, 4, 8, 1, 4)), (1, 1, 64, 1 << 16, (1, 2, 8, 1, 32)),
                                       (20, 1, 64, 8000, (1, 2, 4, 1, 4)), (64, 1, 32, 1 << 17, (1, 4, 4, 1, 1)), (33, 2, 64, 100, (1, 1, 4, 1, 1)),
-                                      (1, 5, 64, 100, (2, 1, 4, 2, 1)), (4, 4, 64, 4096, (2, 1, 4, 1, 8)), (0, 1, 8, 100, (1, 4, 4, 1, 1)), (1, 1, 8, 0, (1, 4, 8, 1, 1))):
+                                      (1, 5, 64, 100, (2, 1, 4, 2, 1)), (4, 4, 64, 4096, (2, 1, 4, 1, 4)), (0, 1, 8, 100, (1, 4, 4, 1, 1)), (1, 1, 8, 0, (1, 4, 8, 1, 1))):
         r = binding.diag_cache_attention(c, n, tokens, hq, most)
         assert (r.col_tiles, r.repeats, r.waves, r.col_groups, r.splits) == want, (n, tokens, hq, most)
         assert r.chunk > 0 and r.chunk % r.waves == 0
