@@ -128,23 +128,32 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT, R>& w, const Tile<D, R>&
     bf16x8 ones;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
+    if (masked) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        if (masked) {
+        for (int n = 0; n < NT; ++n) {
             const int see = w.seen[n] - first_token - 4 * (lane >> 4);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (16 * (e >> 2) + (e & 3) >= see) p[n][e] = -INFINITY;
         }
-        // weights against the reference as it is; where their sum shows that a row has outgrown it (or has none yet), again against a new one
-        float x[8], sum;
-        auto weigh = [&] {
+    }
+    // weights against the references as they are; where their sums show that a row has outgrown its own (or has none yet), again against new ones
+    float x[NT][8], sum[NT];
+    auto weigh = [&] {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][e], scale, -w.m[n]));
-            sum = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-        };
-        weigh();
-        if (__builtin_amdgcn_ballot_w64(!(sum <= kGrowth)) != 0) {
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[n][e], scale, -w.m[n]));
+            sum[n] = ((x[n][0] + x[n][1]) + (x[n][2] + x[n][3])) + ((x[n][4] + x[n][5]) + (x[n][6] + x[n][7]));
+        }
+    };
+    weigh();
+    bool outgrown = false;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) outgrown |= !(sum[n] <= kGrowth);
+    if (__builtin_amdgcn_ballot_w64(outgrown) != 0) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
             float top = p[n][0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) top = fmaxf(top, p[n][e]);
@@ -155,15 +164,15 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT, R>& w, const Tile<D, R>&
             w.weight[n] *= f;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) w.o[n][i] *= f;
-            weigh();
         }
-        w.l[n] += sum;
+        weigh();
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        w.l[n] += sum[n];
         bf16x8 rounded;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            p[n][e] = x[e];
-            rounded[e] = (__bf16)x[e];
-        }
+        for (int e = 0; e < 8; ++e) rounded[e] = (__bf16)x[n][e];
         w.weight[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, rounded, w.weight[n], 0, 0, 0);
     }
 #pragma unroll
@@ -176,12 +185,12 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT, R>& w, const Tile<D, R>&
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ps[n][e] = (__bf16)times(p[n][e], vs[e]);
+            for (int e = 0; e < 8; ++e) ps[n][e] = (__bf16)times(x[n][e], vs[e]);
 #pragma unroll
         for (int i = 2 * R * v; i < 2 * R * (v + 1); ++i) {
-            const bf16x8 x = values_of(t.v[i >> 2][i & 3], 1.f);
+            const bf16x8 y = values_of(t.v[i >> 2][i & 3], 1.f);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) w.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, ps[n], w.o[n][i], 0, 0, 0);
+            for (int n = 0; n < NT; ++n) w.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, ps[n], w.o[n][i], 0, 0, 0);
         }
     }
 }
