@@ -333,7 +333,9 @@ PYR_API int pyr_decode_update(const void* q_win, const void* k, const void* v,
  *
  * Host checks of every call: PYR_ERR_NULL; PYR_ERR_SHAPE (negative sizes; n_slots > PYR_CACHE_MAX_SLOTS; n > PYR_CACHE_MAX_ROWS where pages are handed out or shared);
  * PYR_ERR_UNSUPPORTED (head_dim not 64 or 128, page_tokens not a power of two from 32 to 1024, pages not 256-byte aligned, rows not 16-byte aligned,
- * 2^31 or more tokens in the pool, a row of the table or a batch, or entries of the table); PYR_ERR_WORKSPACE; PYR_ERR_LAUNCH.
+ * 2^31 or more tokens in the pool, a row of the table or a batch, or entries of the table; 2^24 or more workgroups, which take a KV head of a sequence in
+ * the attention, a sequence's 32 tokens of up to four heads where rows go in or out, and 32 kept tokens where slots are cut); PYR_ERR_WORKSPACE;
+ * PYR_ERR_LAUNCH.  Limits that only cut up the work (max_keep, max_new, max_len) may be as large as an int32.
  */
 #define PYR_CACHE_MAX_ROWS 4096
 #define PYR_CACHE_MAX_SLOTS 262144

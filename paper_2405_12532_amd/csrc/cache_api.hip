@@ -9,6 +9,7 @@ constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 constexpr int64_t kMost = (int64_t)1 << 31;
+constexpr int64_t kMostGroups = (int64_t)1 << 24;                // workgroups of 256 threads: a launch has fewer than 2^32 threads
 int64_t head_groups(const pyr_cache* c) { return (c->n_kv_heads + 3) / 4; }      // (workgroups of a tile, at most)
 
 int check_layout(const pyr_cache* c) {
@@ -36,6 +37,11 @@ int check_cache(const pyr_cache* c) {
     return PYR_OK;
 }
 
+int32_t within_row(const pyr_cache* c, int32_t tokens) {         // a limit on tokens of a slot, no larger than a row of the table needs (it may be INT32_MAX)
+    const int64_t capacity = (int64_t)c->max_pages * c->page_tokens;
+    return tokens < capacity ? tokens : (int32_t)capacity;
+}
+
 int check_rows(const pyr_cache* c, int32_t n) {                  // of a call that hands out or shares pages
     if (n < 0 || n > PYR_CACHE_MAX_ROWS) return PYR_ERR_SHAPE;
     return (int64_t)n * (1 + (int64_t)c->max_pages) >= kMost ? PYR_ERR_UNSUPPORTED : PYR_OK;
@@ -51,9 +57,8 @@ int check_attention(const pyr_cache* c, int32_t n, int32_t n_tokens, int32_t n_q
     if (n < 0 || n_tokens < 1 || n_q_heads < 1 || max_len < 0) return PYR_ERR_SHAPE;
     if (n_q_heads % c->n_kv_heads != 0 || n_q_heads > 32767) return PYR_ERR_UNSUPPORTED;
     if ((int64_t)n * n_tokens >= kMost || (int64_t)n * n_tokens * n_q_heads >= kMost) return PYR_ERR_UNSUPPORTED;
-    const int64_t capacity = (int64_t)c->max_pages * c->page_tokens;
-    *plan = pyr::plan_cache_attention(n, n_tokens, n_q_heads, c->n_kv_heads, c->head_dim, max_len < capacity ? max_len : capacity);
-    if ((int64_t)n * plan->splits * plan->col_groups * c->n_kv_heads >= kMost) return PYR_ERR_UNSUPPORTED;
+    *plan = pyr::plan_cache_attention(n, n_tokens, n_q_heads, c->n_kv_heads, c->head_dim, within_row(c, max_len));
+    if ((int64_t)n * plan->col_groups * c->n_kv_heads * plan->waves >= 4 * kMostGroups) return PYR_ERR_UNSUPPORTED;
     return PYR_OK;
 }
 
@@ -95,6 +100,7 @@ int pyr_cache_release(const pyr_cache* cache, const int32_t* slots, int32_t n, v
     if (n < 0) return PYR_ERR_SHAPE;
     if (n == 0) return PYR_OK;
     if (!slots) return PYR_ERR_NULL;
+    if (n >= kMostGroups) return PYR_ERR_UNSUPPORTED;
     return pyr::launch_cache_release(view(cache), slots, n, (hipStream_t)stream);
 }
 
@@ -117,7 +123,8 @@ int pyr_cache_compact(const pyr_cache* cache, const int32_t* slots, int32_t n, c
     size_t need = 0;
     pyr_cache_compact_workspace_bytes(cache, n, &need);
     if (!workspace_ok(workspace, workspace_bytes, need)) return PYR_ERR_WORKSPACE;
-    if ((int64_t)n * (((int64_t)max_keep + 31) / 32) * head_groups(cache) >= kMost) return PYR_ERR_UNSUPPORTED;
+    max_keep = within_row(cache, max_keep < n_kept ? max_keep : n_kept);      // (more are refused on the device)
+    if ((int64_t)n * (((int64_t)max_keep + 31) / 32) >= kMostGroups) return PYR_ERR_UNSUPPORTED;
     const pyr::PoolView c = view(cache);
     rc = pyr::launch_cache_cut(c, slots, out_offsets, n, n_kept, max_keep, (int32_t*)workspace, status, (hipStream_t)stream);
     if (rc != PYR_OK) return rc;
@@ -133,7 +140,8 @@ int pyr_cache_store(const pyr_cache* cache, const void* k, const void* v, int32_
     if (n == 0 || n_rows == 0 || n_list == 0 || max_new == 0) return PYR_OK;
     if (!k || !v || !offsets || !slots || !start) return PYR_ERR_NULL;
     if (!aligned16(k) || !aligned16(v)) return PYR_ERR_UNSUPPORTED;
-    if ((int64_t)n * (((int64_t)max_new + 30) / 32 + 1) * head_groups(cache) >= kMost) return PYR_ERR_UNSUPPORTED;
+    max_new = within_row(cache, max_new < n_list ? max_new : n_list);
+    if ((int64_t)n * (((int64_t)max_new + 30) / 32 + 1) * head_groups(cache) >= kMostGroups) return PYR_ERR_UNSUPPORTED;
     return pyr::launch_cache_store(view(cache), cache->head_dim, k, v, n_rows, row_idx, n_list, offsets, slots, start, n, max_new, (hipStream_t)stream);
 }
 
@@ -145,9 +153,8 @@ int pyr_cache_load(const pyr_cache* cache, const int32_t* slots, const int32_t* 
     if (n == 0 || n_rows == 0 || max_len == 0) return PYR_OK;
     if ((!k_out && !v_out) || !slots || !offsets) return PYR_ERR_NULL;
     if (!aligned16(k_out) || !aligned16(v_out)) return PYR_ERR_UNSUPPORTED;
-    const int64_t capacity = (int64_t)cache->max_pages * cache->page_tokens;
-    if (max_len > capacity) max_len = (int32_t)capacity;
-    if ((int64_t)n * (((int64_t)max_len + 31) / 32) * head_groups(cache) >= kMost) return PYR_ERR_UNSUPPORTED;
+    max_len = within_row(cache, max_len < n_rows ? max_len : n_rows);
+    if ((int64_t)n * (((int64_t)max_len + 31) / 32) * head_groups(cache) >= kMostGroups) return PYR_ERR_UNSUPPORTED;
     return pyr::launch_cache_load(view(cache), cache->head_dim, slots, offsets, n, max_len, k_out, v_out, n_rows, (hipStream_t)stream);
 }
 

@@ -385,7 +385,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_move_kernel(MoveArgs a) {
 int launch_cache_store(const CacheView& c, int32_t head_dim, const void* k, const void* v, int32_t n_rows, const int32_t* row_idx, int32_t n_list,
                        const int32_t* offsets, const int32_t* slots, const int32_t* start, int32_t n_seqs, int32_t max_new, hipStream_t stream) {
     if (n_seqs == 0 || max_new == 0) return PYR_OK;
-    const int32_t tiles = (max_new + 30) / 32 + 1;
+    const int32_t tiles = (int32_t)(((int64_t)max_new + 30) / 32) + 1;
     const StoreArgs a{c, (const uint16_t*)k, (const uint16_t*)v, row_idx, offsets, slots, start, n_rows, n_list, tiles, (c.n_kv_heads + kWaves - 1) / kWaves};
     const dim3 grid((unsigned)((int64_t)n_seqs * tiles * a.head_groups));
     if (head_dim == 128) hipLaunchKernelGGL(cache_store_kernel<128>, grid, dim3(64 * kWaves), 0, stream, a);
@@ -396,7 +396,7 @@ int launch_cache_store(const CacheView& c, int32_t head_dim, const void* k, cons
 int launch_cache_load(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* offsets, int32_t n_seqs, int32_t max_len,
                       void* k, void* v, int32_t n_rows, hipStream_t stream) {
     if (n_seqs == 0 || max_len == 0) return PYR_OK;
-    const LoadArgs a{c, slots, offsets, (uint16_t*)k, (uint16_t*)v, n_rows, (max_len + 31) / 32, (c.n_kv_heads + kWaves - 1) / kWaves};
+    const LoadArgs a{c, slots, offsets, (uint16_t*)k, (uint16_t*)v, n_rows, (int32_t)(((int64_t)max_len + 31) / 32), (c.n_kv_heads + kWaves - 1) / kWaves};
     const dim3 grid((unsigned)((int64_t)n_seqs * a.tiles_of_seq * a.head_groups));
     if (head_dim == 128) hipLaunchKernelGGL(cache_load_kernel<128>, grid, dim3(64 * kWaves), 0, stream, a);
     else hipLaunchKernelGGL(cache_load_kernel<64>, grid, dim3(64 * kWaves), 0, stream, a);
@@ -406,7 +406,7 @@ int launch_cache_load(const CacheView& c, int32_t head_dim, const int32_t* slots
 int launch_cache_move(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* kept_idx, int32_t n_list, const int32_t* seq_offsets,
                       const int32_t* out_offsets, const int32_t* old_rows, const int32_t* status, int32_t n_seqs, int32_t max_keep, hipStream_t stream) {
     if (n_seqs == 0 || max_keep == 0) return PYR_OK;
-    MoveArgs a{c, slots, kept_idx, seq_offsets, out_offsets, old_rows, status, n_list, (max_keep + 31) / 32, (c.n_kv_heads + kWaves - 1) / kWaves};
+    MoveArgs a{c, slots, kept_idx, seq_offsets, out_offsets, old_rows, status, n_list, (int32_t)(((int64_t)max_keep + 31) / 32), (c.n_kv_heads + kWaves - 1) / kWaves};
     const int64_t places = (int64_t)n_seqs * a.tiles_of_seq;
     while (a.head_groups > 1 && places * ((a.head_groups + 1) / 2) >= 1024) a.head_groups = (a.head_groups + 1) / 2;
     const dim3 grid((unsigned)(places * a.head_groups));

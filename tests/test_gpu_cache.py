@@ -76,6 +76,24 @@ def test_store_leaves_out_tokens_without_a_page(lib):
     assert np.array_equal(pair.pages.cpu().numpy(), pair.o.pages)
 
 
+@pytest.mark.parametrize("hkv,d", [(5, 128), (2, 64)])
+def test_limits_that_limit_nothing(lib, hkv, d):
+    """max_new, max_keep and max_len as large as they can be given."""
+    most = 2 ** 31 - 1
+    pair = Pair(lib, [100, 70], hkv, d, 32, spare=8)
+    kt, k = bf16(pair.rng.normal(size=(90, hkv, d)))
+    lib.cache_store(pair.cache, kt, kt, 90, None, 90, dev([0, 60, 90]), dev([0, 1]), dev([37, 40]), 2, most)
+    pair.o.store(k, k, None, [0, 60, 90], [0, 1], [37, 40])
+    kept = list(range(0, 100, 2)) + list(range(100, 170, 3))
+    assert both_compact(pair, [0, 1], kept, [0, 100], [0, 50, 74], most) == 0
+    pair.check()
+    out = torch.empty((74, hkv, d), dtype=torch.bfloat16, device="cuda")
+    lib.cache_load(pair.cache, dev([0, 1]), dev([0, 50, 74]), 2, most, out, None, 74)
+    assert np.array_equal(out.double().cpu().numpy(), np.concatenate([pair.o.read(0)[0], pair.o.read(1)[0]]))
+    qt, q = bf16(pair.rng.normal(size=(2, 1, hkv, d)))
+    check_attention(pair, q, [0, 1], *attend(pair, qt, [0, 1], 1, most))
+
+
 @pytest.mark.parametrize("hkv,d,page", [(1, 128, 32), (6, 64, 128), (5, 128, 64), (8, 64, 32)])
 def test_load_gives_the_exact_values(lib, hkv, d, page):
     lens = [0, 1, 33, 64, 200, 31, 9]

@@ -135,3 +135,16 @@ def test_attention_arguments_that_cannot_be():
     assert attend(heads=6) == UNSUPPORTED and attend(heads=40000) == UNSUPPORTED and attend(n=1 << 30) == UNSUPPORTED
     assert attend(ws=None) == WORKSPACE and attend(ws=0x180) == WORKSPACE and attend(size=1000) == WORKSPACE
     assert attend(n=0) == OK
+
+
+def test_calls_of_more_workgroups_than_a_launch_has():
+    """2^24 of 256 threads; limits as large as an int32 are brought down to what a slot holds first."""
+    most = 2 ** 31 - 1
+    c = cache(n_slots=262144, page_tokens=1024, max_pages=256, n_pages=4096)                # 8192 tiles a slot
+    ref = ctypes.byref(c)
+    assert call("pyr_cache_release", ref, 0x1000, 1 << 24, None) == UNSUPPORTED
+    assert call("pyr_cache_compact", ref, 0x1000, 2048, 0x2000, most, 0x3000, 0x4000, most, 0x5000, 0x100, 1 << 30, None) == UNSUPPORTED
+    assert call("pyr_cache_store", ref, 0x1000, 0x2000, most, None, most, 0x3000, 0x4000, 0x5000, 2048, most, None) == UNSUPPORTED
+    assert call("pyr_cache_load", ref, 0x1000, 0x2000, 2048, most, 0x3000, 0x4000, most, None) == UNSUPPORTED
+    assert call("pyr_cache_attention", ref, 0x1000, 0x2000, 1 << 22, 1, 4, most, 0.0, 0x3000, None, 0x100, 1 << 30, None) == UNSUPPORTED
+    binding.cache_attention_workspace_bytes(c, (1 << 22) - 1, 1, 4, most)
