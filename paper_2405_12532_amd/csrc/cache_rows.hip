@@ -194,7 +194,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_load_kernel(LoadArgs a) {
     const int head = (blockIdx.x - place * a.head_groups) * kWaves + (threadIdx.x >> 6);
     const int slot = cache_slot(a.c, a.slots, b);
     const int first = a.offsets[b], last = min(a.offsets[b + 1], a.n_rows);
-    if (slot < 0 || first < 0 || head >= a.c.n_kv_heads) return;
+    if (slot < 0 || first < 0 || last <= first || head >= a.c.n_kv_heads) return;
     const int page = a.c.table[(int64_t)slot * a.c.max_pages + (tile >> (a.c.shift - 5))];
     const int count = min(last - first, cache_len(a.c, slot)) - 32 * tile;      // tokens of this tile and behind it
     if (count <= 0 || page < 0 || page >= a.c.n_pages) return;

@@ -121,6 +121,13 @@ def test_load_gives_the_exact_values(lib, hkv, d, page):
     assert torch.equal(only.view(torch.int16), out[1].view(torch.int16))
 
 
+def test_load_takes_offsets_that_go_down_for_no_rows(lib):
+    pair = Pair(lib, [40, 40, 40], 2, 64, 32)
+    out = torch.full((50, 2, 64), 77.0, dtype=torch.bfloat16, device="cuda")
+    lib.cache_load(pair.cache, dev([0, 1, 2]), dev([30, -2 ** 31, 9, 3]), 3, 64, out, out, 40)
+    assert bool((out == 77.0).all())
+
+
 # ------------------------------------------------------------------------------------------------ attention
 ATTEND = [  # lens, hq, hkv, d, page, tokens
     ([0, 1, 2, 31, 32, 33, 64, 65, 127, 300], 4, 4, 128, 64, 1),
