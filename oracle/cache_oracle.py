@@ -209,7 +209,7 @@ class Cache:
             for j in range(int(offsets[i + 1] - offsets[i])):
                 row = offsets[i] + j if row_idx is None else row_idx[offsets[i] + j]
                 token = start[i] + j
-                if token >= self.table.shape[1] * self.page or not 0 <= row < len(k) or not 0 <= self.table[s, token // self.page] < len(self.refs):
+                if token >= self.lens[s] or not 0 <= row < len(k) or not 0 <= self.table[s, token // self.page] < len(self.refs):
                     continue
                 self._put(self.table[s, token // self.page], token, *quantise(k[row]), *quantise(v[row]))
 

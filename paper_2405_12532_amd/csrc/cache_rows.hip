@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a) {
     bool again = false;                                           // an earlier row has the slot: its tile may be written by two wavefronts at once
     for (int i = lane; i < b; i += 64) again |= a.slots[i] == slot;
     if (slot < 0 || start < 0 || first >= last || head >= a.c.n_kv_heads) return;
-    const int64_t end = min((int64_t)start + (last - first), (int64_t)a.c.max_pages << a.c.shift);       // tokens start .. end - 1
+    const int64_t end = min((int64_t)start + (last - first), (int64_t)cache_len(a.c, slot));      // tokens start .. end - 1 (the table holds anything behind the length)
     const int tile = (start >> 5) + (place - b * a.tiles_of_piece);
     const int64_t token0 = (int64_t)tile * 32;
     if (token0 >= end) return;

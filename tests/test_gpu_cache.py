@@ -76,6 +76,19 @@ def test_store_leaves_out_tokens_without_a_page(lib):
     assert np.array_equal(pair.pages.cpu().numpy(), pair.o.pages)
 
 
+def test_store_stops_at_the_length(lib):
+    """Entries of the table behind it may hold anything, another slot's pages among them."""
+    pair = Pair(lib, [32, 20, 64], 2, 64, 32, max_pages=4)
+    for s, n in ((0, 1), (1, 1), (2, 2)):
+        pair.o.table[s, n:] = pair.o.table[(s + 1) % 3, 0]
+    pair.up()
+    kt, k = bf16(pair.rng.normal(size=(210, 2, 64)))
+    lib.cache_store(pair.cache, kt, kt, 210, None, 210, dev([0, 70, 140, 210]), dev([0, 1, 2]), dev([32, 10, 33]), 3, 70)
+    pair.o.store(k, k, None, [0, 70, 140, 210], [0, 1, 2], [32, 10, 33])
+    pair.check()
+    assert np.array_equal(pair.pages.cpu().numpy(), pair.o.pages)
+
+
 @pytest.mark.parametrize("hkv,d", [(5, 128), (2, 64)])
 def test_limits_that_limit_nothing(lib, hkv, d):
     """max_new, max_keep and max_len as large as they can be given."""
