@@ -370,7 +370,8 @@ PYR_API int pyr_cache_reserve(const pyr_cache* cache, const int32_t* slots, cons
 
 /*
  * children[i] becomes a copy of parents[i]: full pages are shared, of a page filled in part the tokens are copied into a fresh one.  Several children
- * may have one parent.  A row is skipped if both are -1.
+ * may have one parent.  A row is skipped if both are -1.  A parent's page outside the pool is passed on as it is; where that is the page filled in
+ * part, the child's fresh one keeps what lay in it.
  *   parents, children  dev int32 [n]; children are empty slots
  *   status             dev int32 [1], written
  */
