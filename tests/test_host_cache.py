@@ -148,3 +148,14 @@ def test_calls_of_more_workgroups_than_a_launch_has():
     assert call("pyr_cache_load", ref, 0x1000, 0x2000, 2048, most, 0x3000, 0x4000, most, None) == UNSUPPORTED
     assert call("pyr_cache_attention", ref, 0x1000, 0x2000, 1 << 22, 1, 4, most, 0.0, 0x3000, None, 0x100, 1 << 30, None) == UNSUPPORTED
     binding.cache_attention_workspace_bytes(c, (1 << 22) - 1, 1, 4, most)
+
+
+@pytest.mark.parametrize("which,change", [(1, lambda t: t.long()), (2, lambda t: t.long()), (3, lambda t: t.short()), (1, lambda t: t.view(2, 2)), (2, lambda t: t.view(-1)),
+                                          (3, lambda t: t.view(3, 1))])
+def test_a_cache_of_tensors_of_another_type_or_shape(which, change):
+    import torch
+    tensors = [torch.zeros(4 * 2176 * 2, dtype=torch.uint8), torch.zeros(4, dtype=torch.int32), torch.zeros((3, 2), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)]
+    binding.make_cache(*tensors, 32, 2, 64)
+    tensors[which] = change(tensors[which])
+    with pytest.raises(ValueError):
+        binding.make_cache(*tensors, 32, 2, 64)
