@@ -159,3 +159,21 @@ def test_a_cache_of_tensors_of_another_type_or_shape(which, change):
     tensors[which] = change(tensors[which])
     with pytest.raises(ValueError):
         binding.make_cache(*tensors, 32, 2, 64)
+
+
+def test_an_attention_of_any_number_of_heads_is_cut_up():
+    """Splits cover the cache, and their workgroups are no more than what a launch and its join are worth."""
+    c = cache(n_pages=1 << 15, max_pages=2048, n_slots=4096, n_kv_heads=1)
+    for d, g, tokens in ((128, 4, 1), (64, 8, 1), (128, 16, 1), (128, 8, 4)):
+        c.head_dim = d
+        for n in list(range(1, 1100, 7)) + [64, 65, 128, 129, 200, 256, 257, 384, 385, 512, 513, 768, 769]:
+            for most in (0, 1, 1200, 1300, 1537, 2048, 2049, 100000):
+                r = binding.diag_cache_attention(c, n, tokens, g, most)
+                tiles = -(-most // 32)
+                assert r.splits >= 1 and (r.splits - 1) * r.chunk < max(tiles, 1) <= r.splits * r.chunk
+                assert r.splits == 1 or (n * r.splits < 1024 and r.chunk >= 16)
+    c.head_dim = 128
+    assert [binding.diag_cache_attention(c, n, 1, 4, 8000).splits for n in (160, 384, 385, 480, 769)] == [4, 2, 1, 1, 1]
+    assert [binding.diag_cache_attention(c, n, 1, 4, 1280).splits for n in (64, 65, 160)] == [1, 1, 1]
+    assert [binding.diag_cache_attention(c, n, 1, 4, 1500).splits > 1 for n in (64, 65, 160)] == [True, False, False]
+    assert [binding.diag_cache_attention(c, n, 1, 4, 2048).splits > 1 for n in (65, 128, 129, 256)] == [True, True, False, False]
