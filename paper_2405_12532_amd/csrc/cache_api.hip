@@ -56,7 +56,7 @@ pyr::PoolView view(const pyr_cache* c) {
 int check_attention(const pyr_cache* c, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len, pyr::CacheAttention* plan) {
     if (n < 0 || n_tokens < 1 || n_q_heads < 1 || max_len < 0) return PYR_ERR_SHAPE;
     if (n_q_heads % c->n_kv_heads != 0 || n_q_heads > 32767) return PYR_ERR_UNSUPPORTED;
-    if ((int64_t)n * n_tokens >= kMost || (int64_t)n * n_tokens * n_q_heads >= kMost) return PYR_ERR_UNSUPPORTED;
+    if ((int64_t)n * n_tokens >= kMost || (int64_t)(n > 1 ? n : 1) * n_tokens * n_q_heads >= kMost) return PYR_ERR_UNSUPPORTED;
     *plan = pyr::plan_cache_attention(n, n_tokens, n_q_heads, c->n_kv_heads, c->head_dim, within_row(c, max_len));
     if ((int64_t)n * plan->col_groups * c->n_kv_heads * plan->waves >= 4 * kMostGroups) return PYR_ERR_UNSUPPORTED;
     return PYR_OK;

@@ -148,6 +148,7 @@ def test_calls_of_more_workgroups_than_a_launch_has():
     assert call("pyr_cache_load", ref, 0x1000, 0x2000, 2048, most, 0x3000, 0x4000, most, None) == UNSUPPORTED
     assert call("pyr_cache_attention", ref, 0x1000, 0x2000, 1 << 22, 1, 4, most, 0.0, 0x3000, None, 0x100, 1 << 30, None) == UNSUPPORTED
     binding.cache_attention_workspace_bytes(c, (1 << 22) - 1, 1, 4, most)
+    assert call("pyr_cache_attention", ref, 0x1000, 0x2000, 0, 1 << 29, 8, most, 0.0, 0x3000, None, 0x100, 1 << 30, None) == UNSUPPORTED
 
 
 @pytest.mark.parametrize("which,change", [(1, lambda t: t.long()), (2, lambda t: t.long()), (3, lambda t: t.short()), (1, lambda t: t.view(2, 2)), (2, lambda t: t.view(-1)),
