@@ -175,5 +175,6 @@ def test_an_attention_of_any_number_of_heads_is_cut_up():
                 assert r.splits == 1 or (n * r.splits < 1024 and r.chunk >= 16)
     c.head_dim = 128
     assert [binding.diag_cache_attention(c, n, 1, 4, 8000).splits for n in (160, 384, 385, 480, 769)] == [4, 2, 1, 1, 1]
+    assert [binding.diag_cache_attention(c, n, 4, 8, 8000).splits for n in (160, 384, 385, 480, 769)] == [4, 2, 1, 1, 1]
     assert [binding.diag_cache_attention(c, n, 1, 4, 1536).splits for n in (1, 64, 160, 300)] == [1, 1, 1, 1]
     assert [binding.diag_cache_attention(c, n, 1, 4, 2048).splits > 1 for n in (1, 144, 145, 256)] == [True, True, False, False]
