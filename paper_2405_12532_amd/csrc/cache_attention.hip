@@ -443,8 +443,8 @@ int launch(const CacheAttention& x, const CacheView& c, const AttendArgs& a, voi
 // 20 x 1800 on 64/8 12.4 / 15.1, 20 x 2100 13.8 / 15.0, lengths of 100 ... 2000 12.8 / 12.9 (160).  Heads of 128 channels that all have a place at once
 // (three workgroups of four wavefronts a compute unit) are not split into more than have: 60 x 1800 on 64/8 heads (480) 24 / 30, 60 x 8000
 // 85 / 93, though lengths of 300 ... 5000 take 44 / 41; with four tokens 60 x 1800 37.5 / 48, lengths of 100 ... 2000 32 / 40, of 300 ... 5000 70 / 71.
-// More than 16 rows a head: parts twice as long, as their results are twice as large (us for
-// parts of 16, 32 and 64 tiles: 8 x 4096 on 64/8 heads, four tokens 21.4 / 19.7 / 26; 16 x 2048, nine 36 / 35 / 32.5).
+// More than 16 rows a head: parts twice as long, as their results are twice as large (us for parts of 16, 32 and 64 tiles:
+// 8 x 4096 on 64/8 heads, four tokens 21.4 / 19.7 / 26; 16 x 2048, nine 36 / 35 / 32.5).
 CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_len) {
     constexpr int64_t kShortest = 16, kUnits = 256, kFilled = 200;
     CacheAttention x{};
