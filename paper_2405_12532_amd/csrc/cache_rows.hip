@@ -180,7 +180,7 @@ struct LoadArgs {
     CacheView c;
     const int32_t *slots, *offsets;
     uint16_t *k, *v;
-    int32_t n_rows, tiles_of_seq, head_groups;
+    int32_t n_rows, max_len, tiles_of_seq, head_groups;
 };
 static_assert(sizeof(LoadArgs) <= 112, "short arguments");
 
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache_load_kernel(LoadArgs a) {
     const int first = a.offsets[b], last = min(a.offsets[b + 1], a.n_rows);
     if (slot < 0 || first < 0 || last <= first || head >= a.c.n_kv_heads) return;
     const int page = a.c.table[(int64_t)slot * a.c.max_pages + (tile >> (a.c.shift - 5))];
-    const int count = min(last - first, cache_len(a.c, slot)) - 32 * tile;      // tokens of this tile and behind it
+    const int count = min(min(last - first, cache_len(a.c, slot)), a.max_len) - 32 * tile;      // tokens of this tile and behind it
     if (count <= 0 || page < 0 || page >= a.c.n_pages) return;
     const uint8_t* const in = cache_tile<D>(a.c, page, head, tile & ((1 << (a.c.shift - 5)) - 1));
     uint16_t(*const rows)[kRow] = staged[threadIdx.x >> 6];
@@ -396,7 +396,7 @@ int launch_cache_store(const CacheView& c, int32_t head_dim, const void* k, cons
 int launch_cache_load(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* offsets, int32_t n_seqs, int32_t max_len,
                       void* k, void* v, int32_t n_rows, hipStream_t stream) {
     if (n_seqs == 0 || max_len == 0) return PYR_OK;
-    const LoadArgs a{c, slots, offsets, (uint16_t*)k, (uint16_t*)v, n_rows, (int32_t)(((int64_t)max_len + 31) / 32), (c.n_kv_heads + kWaves - 1) / kWaves};
+    const LoadArgs a{c, slots, offsets, (uint16_t*)k, (uint16_t*)v, n_rows, max_len, (int32_t)(((int64_t)max_len + 31) / 32), (c.n_kv_heads + kWaves - 1) / kWaves};
     const dim3 grid((unsigned)((int64_t)n_seqs * a.tiles_of_seq * a.head_groups));
     if (head_dim == 128) hipLaunchKernelGGL(cache_load_kernel<128>, grid, dim3(64 * kWaves), 0, stream, a);
     else hipLaunchKernelGGL(cache_load_kernel<64>, grid, dim3(64 * kWaves), 0, stream, a);

@@ -134,6 +134,24 @@ def test_load_gives_the_exact_values(lib, hkv, d, page):
     assert torch.equal(only.view(torch.int16), out[1].view(torch.int16))
 
 
+@pytest.mark.parametrize("hkv,d,page", [(3, 128, 64), (5, 64, 32)])
+@pytest.mark.parametrize("max_len", [0, 1, 31, 32, 33, 40, 65, 99])
+def test_load_stops_at_its_limit(lib, hkv, d, page, max_len):
+    """A max_len below the lengths and the rows there are for them, inside a tile and at its ends."""
+    lens, room = [100, 64, 7], [100, 80, 7]
+    pair = Pair(lib, lens, hkv, d, page)
+    offsets = np.concatenate([[0], np.cumsum(room)])
+    out = [torch.full((int(offsets[-1]), hkv, d), 77.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    lib.cache_load(pair.cache, dev([0, 1, 2]), dev(offsets), 3, max_len, out[0], out[1], int(offsets[-1]))
+    want = [np.full((int(offsets[-1]), hkv, d), 77.0) for _ in range(2)]
+    for b in range(3):
+        n = min(lens[b], room[b], max_len)
+        for o, x in zip(want, pair.o.read(b)):
+            o[offsets[b]:offsets[b] + n] = x[:n]
+    for o, x in zip(out, want):
+        assert np.array_equal(o.double().cpu().numpy(), x)
+
+
 def test_load_takes_offsets_that_go_down_for_no_rows(lib):
     pair = Pair(lib, [40, 40, 40], 2, 64, 32)
     out = torch.full((50, 2, 64), 77.0, dtype=torch.bfloat16, device="cuda")
