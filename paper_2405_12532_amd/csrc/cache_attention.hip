@@ -80,6 +80,10 @@ __device__ __forceinline__ float sum_of_groups(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// An element of the output.  O is finite as long as V is, so that an infinite one comes from a block of V that is no number (its scale is +inf in P', and a
+// code that is not 0 leaves it at that) or has left fp32's range: NaN either way.
+__device__ __forceinline__ __bf16 quotient(float o, float f) { return (__bf16)(__builtin_isinf(o) ? NAN : o * f); }
+
 // Up to 16 / R rows fill the columns of a product R times over: column c is row c % (16 / R), and of V's blocks v R .. v R + R - 1 it has the scales of
 // block v R + c / (16 / R).  So P' is made once per R blocks, and of a block's products those of its columns count.
 template <int D, int NT, int R>
@@ -312,7 +316,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && (D == 64 || R == 4) ? 3 : 2
             const float f = weight == 0.f ? 0.f : 1.f / weight;
             bf16x4 y;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) y[x] = (__bf16)(o[x] * f);
+            for (int x = 0; x < 4; ++x) y[x] = quotient(o[x], f);
             *(bf16x4*)((uint16_t*)a.out + (int64_t)row * D + 4 * c4) = y;
             if (a.lse != nullptr && c4 == 0) a.lse[row] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
         } else {
@@ -398,7 +402,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs a) {
     const float f = weight == 0.f ? 0.f : 1.f / weight;
     bf16x4 y;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) y[x] = (__bf16)(o[x] * f);
+    for (int x = 0; x < 4; ++x) y[x] = quotient(o[x], f);
     *(bf16x4*)(a.out + (int64_t)row * D + 4 * quad) = y;
     if (a.lse != nullptr && quad == 0) a.lse[row] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
 }

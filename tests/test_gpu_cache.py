@@ -262,6 +262,34 @@ def test_blocks_that_are_no_number_reach_the_rows_that_see_them_alone(lib, d):
     assert not np.isnan(o[:, :, :2]).any() and np.isnan(o[0, 2, 2:]).all() and not np.isnan(o[0, :2]).any() and np.isnan(o[2, :, 2:]).all()
 
 
+@pytest.mark.parametrize("d,hq,hkv,tokens,n,most,waves,repeats,col_tiles,splits", [
+    (128, 8, 2, 1, 3, 90, 8, 4, 1, 1), (128, 16, 2, 1, 3, 90, 8, 2, 1, 1), (128, 24, 2, 1, 3, 90, 8, 1, 1, 1), (64, 8, 2, 2, 3, 90, 8, 2, 1, 1),
+    (64, 24, 2, 1, 3, 90, 8, 1, 1, 1), (128, 24, 2, 2, 3, 90, 4, 1, 2, 1), (64, 24, 2, 2, 3, 90, 4, 1, 2, 1), (128, 8, 2, 1, 150, 90, 4, 4, 1, 1),
+    (128, 8, 2, 2, 150, 1700, 4, 2, 1, 2), (64, 24, 2, 1, 150, 90, 4, 1, 1, 1), (128, 8, 2, 1, 3, 1700, 8, 4, 1, 4), (64, 24, 2, 2, 3, 1700, 4, 1, 2, 2),
+    (128, 8, 2, 2, 3, 4096, 8, 2, 1, 8), (64, 8, 2, 1, 3, 4096, 8, 2, 1, 8)])
+def test_blocks_of_v_that_are_no_number_whatever_their_codes(lib, d, hq, hkv, tokens, n, most, waves, repeats, col_tiles, splits):
+    """A scale byte of 255 makes NaN of every code, for the rows that see the token alone; in every kernel and both joins."""
+    pair = Pair(lib, [70, 45, 1400, 60], hkv, d, 32, max_pages=128)
+    _, codes, _, scale = orc.tile_places(d)
+    for slot, token, head, block in ((0, 69, 1, 0), (1, 3, 0, d // 32 - 1), (2, 1100, 1, 1), (2, 1399, 0, 0)):
+        tile = pair.o.pages[pair.o.table[slot, token // 32], head, 0]
+        tile[scale[token % 32, block]] = 255
+        for c in range(32):                                                              # all sixteen codes, twice
+            byte, high = codes[token % 32, 32 * block + c]
+            tile[byte] = (tile[byte] & (0x0F if high else 0xF0)) | (c % 16) << (4 * high)
+    pair.up()
+    r = lib.diag_cache_attention(pair.cache, n, tokens, hq, most)
+    assert (r.waves, r.repeats, r.col_tiles, r.splits) == (waves, repeats, col_tiles, splits)
+    qt, q = bf16(pair.rng.normal(size=(n, tokens, hq, d)) * 0.2)
+    slots = ([0, 1, 2, 3] * n)[:n]
+    reads = {s: pair.o.read(s) for s in range(4)}
+    out, lse = attend(pair, qt, slots, tokens, most)
+    check_attention(pair, q, slots, out, lse, reads=reads)
+    nan = torch.isnan(out).cpu().numpy().reshape(n, tokens, hq, d // 32, 32)
+    assert (nan.all(axis=4) == nan.any(axis=4)).all() and nan[1, :, :hq // 2, -1].all() and nan[2, :, hq // 2:, 1].all()
+    assert nan[0, -1, hq // 2:, 0].all() and not nan[0, :-1].any() and not nan[:, :, :, 2:d // 32 - 1].any() and not torch.isnan(lse).any()
+
+
 def test_a_page_outside_the_pool_gives_nan(lib):
     pair = Pair(lib, [100, 100], 2, 128, 32)
     pair.o.table[0, 2] = len(pair.o.refs)
