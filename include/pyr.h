@@ -410,7 +410,7 @@ PYR_API int pyr_cache_compact(const pyr_cache* cache, const int32_t* slots, int3
  *   offsets            dev int32 [n+1];  slots, start  dev int32 [n]
  *   max_new            no offsets[i+1] - offsets[i] is larger (tokens beyond it are not stored, or some of them)
  * Tokens from lens[slots[i]] on (they were not reserved), tokens that have no page, a start of -1 (pyr_cache_reserve found no room) and rows outside
- * k and v are not stored; nothing else in the pages changes.  Of rows that name the same slot the first is stored.
+ * k and v or the list (an offset may be below 0) are not stored; nothing else in the pages changes.  Of rows that name the same slot the first is stored.
  */
 PYR_API int pyr_cache_store(const pyr_cache* cache, const void* k, const void* v, int32_t n_rows, const int32_t* row_idx, int32_t n_list,
                     const int32_t* offsets, const int32_t* slots, const int32_t* start, int32_t n, int32_t max_new, void* stream);

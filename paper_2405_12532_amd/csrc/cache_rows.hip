@@ -74,15 +74,16 @@ __global__ __launch_bounds__(64 * kWaves) void cache_store_kernel(StoreArgs a) {
     const int place = blockIdx.x / a.head_groups, b = place / a.tiles_of_piece;
     const int head = (blockIdx.x - place * a.head_groups) * kWaves + (threadIdx.x >> 6);
     const int slot = cache_slot(a.c, a.slots, b);
-    const int start = a.start[b];
-    const int first = max(a.offsets[b], 0), last = min(a.offsets[b + 1], a.n_list);
+    const int place_of_piece = a.start[b], offset = a.offsets[b];
+    const int first = max(offset, 0), last = min(a.offsets[b + 1], a.n_list);
     bool again = false;                                           // an earlier row has the slot: its tile may be written by two wavefronts at once
     for (int i = lane; i < b; i += 64) again |= a.slots[i] == slot;
-    if (slot < 0 || start < 0 || first >= last || head >= a.c.n_kv_heads) return;
-    const int64_t end = min((int64_t)start + (last - first), (int64_t)cache_len(a.c, slot));      // tokens start .. end - 1 (the table holds anything behind the length)
-    const int tile = (start >> 5) + (place - b * a.tiles_of_piece);
-    const int64_t token0 = (int64_t)tile * 32;
+    if (slot < 0 || place_of_piece < 0 || first >= last || head >= a.c.n_kv_heads) return;
+    const int64_t start = place_of_piece + ((int64_t)first - offset);      // (rows below 0 are not there: their tokens stay)
+    const int64_t end = min(start + (last - first), (int64_t)cache_len(a.c, slot));      // tokens start .. end - 1 (the table holds anything behind the length)
+    const int64_t token0 = (start & ~31) + 32 * (int64_t)(place - b * a.tiles_of_piece);
     if (token0 >= end) return;
+    const int tile = (int)(token0 >> 5);
     const int page = a.c.table[(int64_t)slot * a.c.max_pages + (token0 >> a.c.shift)];
     // lane l: the row that token l & 31 of the tile gets; -1: none
     int from = -1;

@@ -53,6 +53,24 @@ def test_store_through_an_index_list(lib):
     assert np.array_equal(pair.pages.cpu().numpy(), pair.o.pages)
 
 
+@pytest.mark.parametrize("hkv,d", [(3, 128), (2, 64)])
+def test_store_of_rows_in_front_of_the_first(lib, hkv, d):
+    """Offsets below 0: row offsets[i] + j is not there for the first j, the token that would get it stays, and the others keep their places."""
+    least = -2 ** 31
+    kt, k = bf16(np.random.default_rng(1).normal(size=(40, hkv, d)))
+    idx = np.random.default_rng(2).integers(0, 40, 40).astype(np.int32)
+    for rows in (None, idx):
+        pair = Pair(lib, [64, 50, 40, 130], hkv, d, 32)
+        listed = None if rows is None else dev(rows)
+        for offsets, slots, start, most in (([-5, 20, least, 30], [0, 1, 2], [3, 0, 0], 25), ([-40, 10, 40], [3, 1], [0, 1], 50), ([-90, 40], [3], [5], 130), ([least, least + 7], [0], [2], 7)):
+            lib.cache_store(pair.cache, kt, kt, 40, listed, 40, dev(offsets), dev(slots), dev(start), len(slots), most)
+            for i, s in enumerate(slots):
+                skipped = max(-offsets[i], 0)
+                if offsets[i] + skipped < offsets[i + 1]:
+                    pair.o.store(k, k, rows, [offsets[i] + skipped, offsets[i + 1]], [s], [start[i] + skipped])
+            assert np.array_equal(pair.pages.cpu().numpy(), pair.o.pages), (offsets, rows is None)
+
+
 def test_store_takes_the_first_row_of_a_slot(lib):
     """A slot named again, next to or over what its first row stores, also far down the list."""
     pair = Pair(lib, [64] * 4, 2, 64, 32)
