@@ -321,7 +321,8 @@ def decode_update(q_win, k, v, seq_offsets_dev, seq_offsets_host, shape, w, soft
 def make_cache(pages, refs, table, lens, page_tokens: int, n_kv_heads: int, head_dim: int) -> PyrCache:
     """The description of a cache that the calls below take.  pages: uint8, whole pages (cache_page_bytes); refs int32 [n_pages], table int32
     [n_slots, max_pages], lens int32 [n_slots].  It keeps the tensors alive."""
-    if not all(t.is_contiguous() for t in (pages, refs, table, lens)) or any(t.element_size() != 4 for t in (refs, table, lens)) or \
+    import torch
+    if not all(t.is_contiguous() for t in (pages, refs, table, lens)) or any(t.dtype != torch.int32 for t in (refs, table, lens)) or \
             (refs.dim(), table.dim(), lens.dim()) != (1, 2, 1) or lens.shape[0] != table.shape[0] or \
             pages.numel() * pages.element_size() < refs.shape[0] * cache_page_bytes(page_tokens, n_kv_heads, head_dim):
         raise ValueError("contiguous pages and int32 refs, table and lens of one cache")

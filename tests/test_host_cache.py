@@ -178,3 +178,13 @@ def test_an_attention_of_any_number_of_heads_is_cut_up():
     assert [binding.diag_cache_attention(c, n, 4, 8, 8000).splits for n in (160, 384, 385, 480, 769)] == [4, 2, 1, 1, 1]
     assert [binding.diag_cache_attention(c, n, 1, 4, 1536).splits for n in (1, 64, 160, 300)] == [1, 1, 1, 1]
     assert [binding.diag_cache_attention(c, n, 1, 4, 2048).splits > 1 for n in (1, 144, 145, 256)] == [True, True, False, False]
+
+
+@pytest.mark.parametrize("which", [1, 2, 3])
+def test_a_cache_of_other_tensors_of_four_bytes(which):
+    import torch
+    for other in (torch.float32, torch.uint32):
+        tensors = [torch.zeros(4 * 2176 * 2, dtype=torch.uint8), torch.zeros(4, dtype=torch.int32), torch.zeros((3, 2), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)]
+        tensors[which] = tensors[which].to(other)
+        with pytest.raises(ValueError):
+            binding.make_cache(*tensors, 32, 2, 64)
