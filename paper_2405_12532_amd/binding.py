@@ -323,9 +323,10 @@ def make_cache(pages, refs, table, lens, page_tokens: int, n_kv_heads: int, head
     [n_slots, max_pages], lens int32 [n_slots].  It keeps the tensors alive."""
     import torch
     if not all(t.is_contiguous() for t in (pages, refs, table, lens)) or any(t.dtype != torch.int32 for t in (refs, table, lens)) or \
+            any(t.device != pages.device for t in (refs, table, lens)) or \
             (refs.dim(), table.dim(), lens.dim()) != (1, 2, 1) or lens.shape[0] != table.shape[0] or \
             pages.numel() * pages.element_size() < refs.shape[0] * cache_page_bytes(page_tokens, n_kv_heads, head_dim):
-        raise ValueError("contiguous pages and int32 refs, table and lens of one cache")
+        raise ValueError("contiguous pages and int32 refs, table and lens of one cache, on one device")
     cache = PyrCache(_ptr(pages), _ptr(refs), _ptr(table), _ptr(lens), refs.shape[0], int(page_tokens), table.shape[0], table.shape[1],
                      int(n_kv_heads), int(head_dim))
     cache.tensors = (pages, refs, table, lens)

@@ -188,3 +188,12 @@ def test_a_cache_of_other_tensors_of_four_bytes(which):
         tensors[which] = tensors[which].to(other)
         with pytest.raises(ValueError):
             binding.make_cache(*tensors, 32, 2, 64)
+
+
+@pytest.mark.parametrize("which", [0, 1, 2, 3])
+def test_a_cache_of_tensors_on_two_devices(which):
+    import torch
+    tensors = [torch.zeros(4 * 2176 * 2, dtype=torch.uint8), torch.zeros(4, dtype=torch.int32), torch.zeros((3, 2), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)]
+    tensors[which] = tensors[which].to("meta")
+    with pytest.raises(ValueError):
+        binding.make_cache(*tensors, 32, 2, 64)
