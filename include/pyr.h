@@ -428,8 +428,9 @@ PYR_API int pyr_cache_load(const pyr_cache* cache, const int32_t* slots, const i
  * Attention of each sequence's newest n_tokens tokens over its cache, theirs included (store them first): token i of slots[b] sees the tokens
  * 0 .. lens[slots[b]] - n_tokens + i.
  *   out[b,i,h,:] = sum_t softmax_t(scale * q[b,i,h,:].k[t,h/g,:]) v[t,h/g,:]
- * bf16 MFMA products on the cache's exact values (P times V's power of two is rounded to bf16), fp32 accumulation and softmax; sums of P V leave
- * fp32's range where V has numbers of 2^110 and more.
+ * bf16 MFMA products on the cache's exact values (P times V's power of two is rounded to bf16), fp32 accumulation and softmax.  Sums of P V stay in fp32's
+ * range as long as V's largest power of two times the sequence's tokens is below 2^114 (a number whose sum leaves it is NaN).  What of P times a power of two
+ * lies below 2^-126 may lose its bits: an output is off by another 2^-123 for every token and one, at most.
  *   q                  dev bf16 [n, n_tokens, Hq, d]
  *   slots              dev int32 [n]
  *   max_len            about the longest sequence (it decides how the work is cut up and how large the workspace is, not the result: longer

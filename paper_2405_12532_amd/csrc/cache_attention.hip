@@ -11,7 +11,8 @@
 // the end.  One more product, of ones and the rounded P, sums what O is divided by: rounding P by itself (2^-9) would show in rows that one token
 // dominates; lse comes from the sum before rounding.  P, both sums and O are fp32.
 // A row's reference is its largest logit when it was last moved, and it is moved when the weights of a tile add up to more than 2^12 in a lane; so most
-// tiles neither look for a maximum nor rescale.  Two tiles are in flight per wavefront.
+// tiles neither look for a maximum nor rescale.  A tile adds at most 2^14 max|V| to an element of O, a wavefront's
+// first one at most max|V| a token: less than 2^10 max|V| a token in all.  Two tiles are in flight per wavefront.
 //
 // Bound: reading the cache.  64 x 2048 tokens on 32 heads, d = 128: 87 us for 571 MB, 6.6 TB/s (counters: read = the cache's bytes; vector instructions
 // 51 % of the time, 169 a tile, matrix pipe 20 %).  On the way there: through the caches, with P' made for every block 102, past them 94, P' made once for

@@ -262,6 +262,62 @@ def test_attention_with_large_and_growing_logits(lib, d):
     check_attention(pair, q, [0, 1], out, lse, scale=1.0)
 
 
+def with_scales_of_v(pair, lo, hi):
+    """Every held token's V gets scale bytes lo .. hi - 1."""
+    c = pair.o
+    for s in range(len(c.lens)):
+        for t in range(int(c.lens[s])):
+            kc, ks, vc, vs = c._get(c.table[s, t // c.page], t)
+            c._put(c.table[s, t // c.page], t, kc, ks, vc, pair.rng.integers(lo, hi, vs.shape).astype(np.uint8))
+    pair.up()
+
+
+@pytest.mark.parametrize("d,hq,tokens", [(128, 8, 1), (64, 8, 3), (128, 24, 2)])
+@pytest.mark.parametrize("lo,hi", [(1, 9), (10, 20), (16, 30)])
+def test_attention_over_the_smallest_numbers(lib, d, hq, tokens, lo, hi):
+    """V down to the smallest power of two.  What of P times it lies below 2^-126 may lose its bits: 6 * 2^-126 of a token's number, and 2^-126 of every product,
+    sum and change of the reference, together less than 2^-123 a token, against weights that add up to one and more, and 2^-123 for the output's own."""
+    pair = Pair(lib, [100, 1, 33], 2, d, 32)
+    with_scales_of_v(pair, lo, hi)
+    qt, q = bf16(pair.rng.normal(size=(3, tokens, hq, d)) * 0.2)
+    out, lse = attend(pair, qt, [0, 1, 2], tokens, 100)
+    out = out.double().cpu().numpy()
+    for b in range(3):
+        k, v = pair.o.read(b)
+        ref, _ = orc.attention(q[b], k, v)
+        size, _ = orc.attention(q[b], k, np.abs(v))
+        top = (np.abs(k).reshape(-1, d) @ np.abs(q[b]).reshape(-1, d).T).max() / np.sqrt(d)
+        dx = (d + 4) * 2.0 ** -24 * top + 2.0 ** -20 + 2.0 ** -23 * top
+        bound = (2.0 ** -8 + 2 * dx) * size * 1.01 + 2.0 ** -8 * np.abs(ref) + (len(k) + 1) * 2.0 ** -123
+        assert (np.abs(out[b] - ref) <= bound).all(), (b, (np.abs(out[b] - ref) / bound).max())
+
+
+@pytest.mark.parametrize("d,hq,tokens", [(128, 8, 1), (64, 8, 3), (128, 24, 2)])
+@pytest.mark.parametrize("lens", [[500, 1, 33], [2000, 64, 7]])
+def test_attention_over_the_largest_numbers(lib, d, hq, tokens, lens):
+    """V's power of two times the tokens just below 2^114, with logits that grow along the cache."""
+    pair = Pair(lib, [0] * 3, 2, d, 64, n_slots=3, max_pages=40, spare=45)
+    k, v = (pair.rng.normal(size=(sum(lens), 2, d)) for _ in range(2))
+    offsets = np.concatenate([[0], np.cumsum(lens)])
+    for b in range(3):
+        k[offsets[b]:offsets[b + 1]] += (np.arange(lens[b]) // 32 * 0.035)[:, None, None]
+        v[offsets[b]:offsets[b + 1]] = np.clip(np.abs(v[offsets[b]:offsets[b + 1]]), 0, 3) / 3 * 0.8 * 2.0 ** 116 / lens[b]
+    kt, k = bf16(k)
+    vt, v = bf16(v)
+    start = torch.empty(3, dtype=torch.int32, device="cuda")
+    lib.cache_reserve(pair.cache, dev([0, 1, 2]), dev(lens), 3, start, pair.status)
+    lib.cache_store(pair.cache, kt, vt, sum(lens), None, sum(lens), dev(offsets), dev([0, 1, 2]), start, 3, max(lens))
+    pair.o.reserve([0, 1, 2], lens)
+    pair.o.store(k, v, None, offsets, [0, 1, 2], [0, 0, 0])
+    for s in range(3):
+        powers = np.concatenate([pair.o._get(pair.o.table[s, t // 64], t)[3].ravel() for t in range(lens[s])])
+        assert 112.5 < int(powers.max()) - 127 + np.log2(lens[s]) < 114
+    qt, q = bf16(np.abs(pair.rng.normal(size=(3, tokens, hq, d))) * 30 / d ** 0.5)
+    out, lse = attend(pair, qt, [0, 1, 2], tokens, max(lens))
+    assert torch.isfinite(out).all()
+    check_attention(pair, q, [0, 1, 2], out, lse)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_blocks_that_are_no_number_reach_the_rows_that_see_them_alone(lib, d):
     pair = Pair(lib, [80, 80, 80], 2, d, 32)
