@@ -380,7 +380,7 @@ PYR_API int pyr_cache_fork(const pyr_cache* cache, const int32_t* parents, const
 
 /*
  * Slots are emptied: their pages' counts go down (0: free), their entries of the table become -1, lens 0.  A slot named twice is
- * emptied once; slots outside the table are skipped.
+ * emptied once; slots outside the table are skipped, pages outside the pool have no count that goes down.
  *   slots              dev int32 [n]
  */
 PYR_API int pyr_cache_release(const pyr_cache* cache, const int32_t* slots, int32_t n, void* stream);
@@ -391,7 +391,7 @@ PYR_API int pyr_cache_release(const pyr_cache* cache, const int32_t* slots, int3
  * them, seq_offsets as the batch they ran on (lens[slots[i]] rows each); any order and repetitions are fine.
  * The tokens go into fresh pages, then the old ones are given back: the pool needs room for both.  A slot that shares pages leaves the others as they are.
  *   slots              dev int32 [n]
- *   kept_idx           dev int32 [n_kept]; an index outside the slot's tokens gives a token of NaN
+ *   kept_idx           dev int32 [n_kept]; an index outside the slot's tokens, or a token on a page outside the pool, gives a token of NaN
  *   seq_offsets        dev int32 [n] or more;  out_offsets  dev int32 [n+1], within 0 .. n_kept
  *   max_keep           no out_offsets[i+1] - out_offsets[i] is larger
  *   status             dev int32 [1], written
@@ -417,7 +417,8 @@ PYR_API int pyr_cache_store(const pyr_cache* cache, const void* k, const void* v
 
 /*
  * The cache as bf16 rows (exactly: every number of the cache is one of bf16's), packed as pyr_decode_update and pyr_score read them: row
- * offsets[i] + j is token j of slots[i], j < min(lens[slots[i]], offsets[i+1] - offsets[i], max_len).  Rows that no token goes to stay as they were.
+ * offsets[i] + j is token j of slots[i], j < min(lens[slots[i]], offsets[i+1] - offsets[i], max_len).  Rows that no token goes to stay as they were,
+ * those of tokens on a page outside the pool among them.
  *   offsets            dev int32 [n+1];  slots  dev int32 [n]
  *   k_out, v_out       dev bf16 [n_rows, Hkv, d]; one of them may be NULL; rows from n_rows on are not written
  */
@@ -440,7 +441,8 @@ PYR_API int pyr_cache_load(const pyr_cache* cache, const int32_t* slots, const i
  *   lse                dev fp32 [n, n_tokens, Hq], written, as pyr_attention's; may be NULL
  *   workspace          dev, >= pyr_cache_attention_workspace_bytes(), 256-byte aligned; not read where that is 0
  * A row that sees nothing (an empty slot, a skipped row, fewer tokens in the cache than n_tokens): zeros in out, -inf in lse.  A token of NaN makes
- * the rows that see it NaN, unless its K is a number and its weight 0 in fp32; what a row does not see never reaches it.  A page outside the pool: NaN.
+ * the rows that see it NaN, unless its K is a number and its weight 0 in fp32 already when its tile was taken; what a row does not see never reaches it.  A page outside the pool
+ * among those of a sequence: NaN in all of its rows, in out and lse.
  * One launch, and one that adds up partial results where few long sequences are split.
  */
 PYR_API int pyr_cache_attention_workspace_bytes(const pyr_cache* cache, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len,

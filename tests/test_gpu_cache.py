@@ -416,6 +416,40 @@ def both_compact(pair, slots, kept, seq_offsets, out_offsets, max_keep):
     return status
 
 
+@pytest.mark.parametrize("hkv,d", [(5, 128), (2, 64)])
+@pytest.mark.parametrize("page", ["behind the pool", "below it"])
+def test_pages_outside_the_pool_are_not_followed(lib, hkv, d, page):
+    """Attended to: all rows of the sequence are NaN.  Loaded: their tokens' rows stay.  Cut: their tokens are NaN.  Given back: nobody's count goes down."""
+    pair = Pair(lib, [90, 70], hkv, d, 32, spare=6)
+    k, v = pair.o.read(0)
+    qt, q = bf16(pair.rng.normal(size=(2, 3, hkv, d)) * 0.2)
+    lost = int(pair.o.table[0, 1])                                                       # tokens 32 .. 63
+    pair.o.table[0, 1] = len(pair.o.refs) if page == "behind the pool" else -2 ** 31
+    pair.up()
+    out, lse = attend(pair, qt, [0, 1], 3, 90)
+    assert torch.isnan(out[0]).all() and torch.isnan(lse[0]).all()
+    check_attention(pair, q[1:], [1], out[1:], lse[1:])
+    out = [torch.full((90, hkv, d), 77.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    lib.cache_load(pair.cache, dev([0]), dev([0, 90]), 1, 90, out[0], out[1], 90)
+    for o, x in zip(out, (k, v)):
+        o = o.double().cpu().numpy()
+        assert np.array_equal(o[:32], x[:32]) and np.array_equal(o[64:], x[64:]) and (o[32:64] == 77).all()
+    kept = [0, 40, 31, 32, 89, 63, 64]
+    assert compact(pair, [0], kept, [0], [0, 7], 7) == 0
+    out = [torch.empty((7, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    lib.cache_load(pair.cache, dev([0]), dev([0, 7]), 1, 7, out[0], out[1], 7)
+    inside = np.array([True, False, True, False, True, False, True])
+    for o, x in zip(out, (k, v)):
+        o = o.double().cpu().numpy()
+        assert np.array_equal(o[inside], x[kept][inside]) and np.isnan(o[~inside]).all()
+    refs = pair.refs.cpu().numpy()
+    assert refs[lost] == 1 and refs.sum() == 1 + 1 + 3                                   # (it, the cut's page, slot 1's)
+    pair.table[1, 2] = len(refs) if page == "behind the pool" else -1
+    lib.cache_release(pair.cache, dev([0, 1]), 2)
+    refs = pair.refs.cpu().numpy()
+    assert refs[lost] == 1 and refs.sum() == 2 and (refs >= 0).all() and not pair.lens.any() and (pair.table[1] == -1).all()
+
+
 @pytest.mark.parametrize("hkv,d,page", [(1, 64, 32), (3, 128, 64), (9, 64, 256)])
 def test_pages_through_a_life(lib, hkv, d, page):
     pair = Pair(lib, [100, 0, page, 2 * page + 1, 31], hkv, d, page, n_slots=12, max_pages=12, spare=20)
