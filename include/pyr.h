@@ -418,7 +418,7 @@ PYR_API int pyr_cache_store(const pyr_cache* cache, const void* k, const void* v
 /*
  * The cache as bf16 rows (exactly: every number of the cache is one of bf16's), packed as pyr_decode_update and pyr_score read them: row
  * offsets[i] + j is token j of slots[i], j < min(lens[slots[i]], offsets[i+1] - offsets[i], max_len).  Rows that no token goes to stay as they were,
- * those of tokens on a page outside the pool among them.
+ * those of tokens on a page outside the pool among them; a sequence whose offset is below 0 is skipped.
  *   offsets            dev int32 [n+1];  slots  dev int32 [n]
  *   k_out, v_out       dev bf16 [n_rows, Hkv, d]; one of them may be NULL; rows from n_rows on are not written
  */

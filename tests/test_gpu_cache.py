@@ -177,6 +177,15 @@ def test_load_takes_offsets_that_go_down_for_no_rows(lib):
     assert bool((out == 77.0).all())
 
 
+def test_load_skips_sequences_in_front_of_the_first_row(lib):
+    pair = Pair(lib, [40, 40], 2, 64, 32)
+    out = [torch.full((50, 2, 64), 77.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    lib.cache_load(pair.cache, dev([0, 1]), dev([-5, 20, 50]), 2, 64, out[0], out[1], 50)
+    for o, x in zip(out, pair.o.read(1)):
+        o = o.double().cpu().numpy()
+        assert (o[:20] == 77).all() and np.array_equal(o[20:], x[:30])
+
+
 # ------------------------------------------------------------------------------------------------ attention
 ATTEND = [  # lens, hq, hkv, d, page, tokens
     ([0, 1, 2, 31, 32, 33, 64, 65, 127, 300], 4, 4, 128, 64, 1),
