@@ -510,6 +510,59 @@ def test_pages_of_a_large_pool_are_handed_out_from_the_lowest(lib):
     assert pair.refs.cpu().tolist() == used.astype(int).tolist() and not pair.lens.any() and (pair.table == -1).all()
 
 
+@pytest.mark.parametrize("pool,rows", [(3500, 40), (20000, 360)])
+def test_many_pages_a_row(lib, pool, rows):
+    """Rows of dozens of pages and one of 300, handed out a row per wavefront, by both workgroups; given back; and asked for in vain."""
+    pair = Pair(lib, [], 1, 64, 32, n_slots=rows, max_pages=320, spare=pool)
+    used = pair.rng.random(pool) < 0.25
+    pair.o.refs[used] = 1
+    pair.up()
+    slots = [int(s) for s in pair.rng.permutation(rows)]
+    n_new = [int(x) for x in pair.rng.integers(25 * 32, 50 * 32, rows)]
+    n_new[3], n_new[5], n_new[-1] = 300 * 32, 0, 40 * 32 + 1
+    start, status = pair.o.reserve(slots, n_new)
+    assert status == 0 and reserve(pair, slots, n_new) == (start.tolist(), 0)
+    assert np.array_equal(pair.table.cpu().numpy(), pair.o.table) and pair.refs.cpu().tolist() == pair.o.refs.tolist()
+    more = [min(60 * 32, 320 * 32 - int(pair.o.lens[s])) for s in slots]
+    start, status = pair.o.reserve(slots, more)
+    assert status > 0 and reserve(pair, slots, more) == (start.tolist(), status)
+    assert np.array_equal(pair.table.cpu().numpy(), pair.o.table) and pair.refs.cpu().tolist() == pair.o.refs.tolist()
+    assert pair.lens.cpu().tolist() == pair.o.lens.tolist()
+    lib.cache_release(pair.cache, dev(slots), rows)
+    assert pair.refs.cpu().tolist() == used.astype(int).tolist() and not pair.lens.any() and (pair.table == -1).all()
+
+
+@pytest.mark.parametrize("n,spare", [(260, 700), (3, 4300), (3, 20000)])
+def test_forks_and_cuts_of_many_rows_or_in_a_large_pool(lib, n, spare):
+    rng = np.random.default_rng(n)
+    lens = [int(x) for x in rng.integers(0, 37, n)]
+    lens[:3] = [64, 33, 32]
+    pair = Pair(lib, lens, 1, 64, 32, n_slots=2 * n, max_pages=2, spare=spare)
+    parents, children = list(range(n)), [n + int(x) for x in rng.permutation(n)]
+    parents[n // 2], children[n // 2] = -1, -1
+    assert both_fork(pair, parents, children) == 0
+    mine = [0 if c < 0 else int(pair.o.lens[c]) for c in children]
+    off = np.concatenate([[0], np.cumsum(mine)])
+    kept = [np.sort(rng.permutation(x)[:(2 * x + 2) // 3]) + o for x, o in zip(mine, off)]
+    koff = np.concatenate([[0], np.cumsum([len(x) for x in kept])])
+    assert both_compact(pair, children, np.concatenate(kept).astype(np.int32), off, koff, 44) == 0
+    both_release(pair, list(range(2 * n)))
+    assert not pair.refs.any()
+
+
+@pytest.mark.parametrize("n,waves,length", [(1, 8, 17000), (300, 4, 9000)])
+def test_attention_of_more_tiles_than_a_wavefront_has_lanes(lib, n, waves, length):
+    """A wavefront holds the pages of 64 of its tiles at a time; a call that is cut up for short sequences meets a long one."""
+    pair = Pair(lib, [length], 1, 64, 32)
+    r = lib.diag_cache_attention(pair.cache, n, 1, 4, 100)
+    assert (r.waves, r.splits) == (waves, 1) and length > 65 * 32 * waves
+    slots = [0] + [-1] * (n - 1)
+    slots.reverse()
+    qt, q = bf16(pair.rng.normal(size=(n, 1, 4, 64)) * 0.2)
+    out, lse = attend(pair, qt, slots, 1, 100)
+    check_attention(pair, q, slots, out, lse, reads={0: pair.o.read(0)})
+
+
 def test_counts_that_are_not_aligned(lib):
     """The counts of a pool begin anywhere (several caches may share one tensor)."""
     pair = Pair(lib, [40, 0], 1, 64, 32, n_slots=2, max_pages=200, spare=301)
