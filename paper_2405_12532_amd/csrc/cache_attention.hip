@@ -8,7 +8,7 @@
 //   O^T = V^T P^T    16 channels x 16 rows, contracted over the 32 tokens.  V's codes are converted without their scale, which depends on the
 //                    token and the block of 32 channels: it is a factor of P instead, P' = P * 2^e per block, rounded to bf16 (as P is in pyr_attention)
 // and the layout of the tile makes every operand what a lane loads or has computed: nothing passes through LDS but the wavefronts' results at
-// the end.  One more product, of ones and the rounded P, sums what O is divided by: rounding P by itself (2^-9) would show in rows that one token
+// the end.  One more product, of ones and the rounded P, sums what O is divided by: rounding P by itself (up to 2^-8) would show in rows that one token
 // dominates; lse comes from the sum before rounding.  P, both sums and O are fp32.
 // A row's reference is its largest logit when it was last moved, and it is moved when the weights of a tile add up to more than 2^12 in a lane; so most
 // tiles neither look for a maximum nor rescale.  A tile adds at most 2^14 max|V| to an element of O, a wavefront's
@@ -439,7 +439,7 @@ int launch(const CacheAttention& x, const CacheView& c, const AttendArgs& a, voi
 }  // namespace
 
 // What is waited for at the end is the wavefront with the most tiles (0.4 us each), so few heads are split along the cache, until there are 2 * kUnits
-// workgroups of kShortest tiles and more - unless a launch that joins the parts (4 us, and 3 us of the host's) costs more than it saves.
+// workgroups of kShortest tiles and more - unless a launch that joins the parts (2 to 3 us, and 3 us of the host's) costs more than it saves.
 // Workgroups of eight wavefronts do with half as many parts; one fits a compute unit, so they are taken where they fill nearly all of them
 // in one go.  Measured, us (four wavefronts, eight): one token of 1 x 1000 on 32/8 heads 9.5 / 8.2 (unsplit), 1 x 1434 on 32 12.2 / 10.2, 32 x 4096 on
 // 32/8 29.7 / 26.6, 1 x 32768 on 32/8 13.6 / 12.9; 20 of 100 ... 8000 on 64/8 (160 heads) 31 / 38, 40 x 1500 on 32/8 (320 heads) 17 / 21.

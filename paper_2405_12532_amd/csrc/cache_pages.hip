@@ -3,7 +3,7 @@
 // does follows from the state alone; a call that finds too few changes nothing.  Everything a call decides is decided by one workgroup
 // (limits: kMaxRows rows a call, kMaxSlots slots), which looks through the counts 16 per lane at a time and stops at the last page it needs.
 // Bound: the latency of the launch and of that workgroup's dependent loads: room for a token each of 64 sequences 3 us, for 2048 pages 6 us, for 25000 of
-// 54000 pages 22 us; a fork 4 to 6 us and its copy 3 to 5 us, a release 2 to 5 us, the table's part of a cut 8 us.
+// 54000 pages 23 us; a fork 4 to 6 us and its copy 3 to 5 us, a release 2 to 5 us, the table's part of a cut 8 us.
 #include "cache_device.h"
 
 namespace pyr {
@@ -127,7 +127,7 @@ __device__ __forceinline__ void rows_of_ranks(const Shared& s, int n, int first,
 
 // The lowest `need` free pages go to the rows, with a count of one; counts, ahead: the first two looks, asked for beforehand.  Returns how many are
 // lacking; then none is taken.  What a look finds is listed in LDS first, so that neighbouring lanes write neighbouring entries: a wavefront takes a
-// row at a time where there are many rows of many pages (25000 pages of 200 rows 30 -> 19 us), else every lane looks for the row of its page
+// row at a time where there are many rows of many pages (25000 pages of 200 rows 41 -> 23 us), else every lane looks for the row of its page
 // (25000 of one row 11 us against 26).
 template <int kWaves>
 __device__ __forceinline__ int hand_out(Shared& s, const PoolView& c, int n, int need, Counts counts, Counts ahead) {

@@ -3,9 +3,9 @@
 //
 // A wavefront owns one tile (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte, and the halves of a byte are
 // tokens of the same tile.
-// Bound: reading and writing HBM.  70 % of 8 x 2048 rows on 32 heads, d = 128, K and V: stored 42 us, 239 MB, 5.7 TB/s, read back 36 us, 6.6 TB/s; cut
-// from 8 x 2048 tokens 28 us (122 MB with the whole lines that single tokens of a tile take, 4.3 TB/s), 4 x 32768 tokens on 8 heads cut to one half 47 us
-// (255 MB so, 5.4 TB/s).  V's eight tokens gathered word by word took as long with 178 registers, and twice as long with 128 and spills.
+// Bound: reading and writing HBM.  70 % of 8 x 2048 rows on 32 heads, d = 128, K and V: stored 43 us, 239 MB, 5.6 TB/s, read back 36 us, 6.5 TB/s; cut
+// from 8 x 2048 tokens 29 us (122 MB with the whole lines that single tokens of a tile take, 4.2 TB/s), 4 x 32768 tokens on 8 heads cut to one half 48 us
+// (255 MB so, 5.3 TB/s).  V's eight tokens gathered word by word took as long with 178 registers, and twice as long with 128 and spills.
 #include "cache_device.h"
 
 namespace pyr {
