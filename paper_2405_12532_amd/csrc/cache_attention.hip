@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs a) {
     auto stats_of = [&](int s) { return *(const f32x3*)(a.stats + (int64_t)s * a.rows + row); };
     auto part_of = [&](int s) { return *(const f32x4*)(a.parts + ((int64_t)s * a.rows + row) * D + 4 * quad); };
     // the first kAhead of a set are asked for together with the slot, whose length says afterwards whether they are there (1 x 16384 on 64/8 heads 11.6 ->
-    // 10.4 us with the attention, 8 x 1800 11.2 -> 10.2)
+    // 10.1 us with the attention, 8 x 1800 11.2 -> 10.2)
     constexpr int kAhead = kSets == 2 ? 2 : 4;
     f32x3 st[kAhead];                    // (three: a register of a fourth is taken for something else, and its load waited for first)
     f32x4 part[kAhead];

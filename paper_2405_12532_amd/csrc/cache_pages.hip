@@ -3,7 +3,7 @@
 // does follows from the state alone; a call that finds too few changes nothing.  Everything a call decides is decided by one workgroup
 // (limits: kMaxRows rows a call, kMaxSlots slots), which looks through the counts 16 per lane at a time and stops at the last page it needs.
 // Bound: the latency of the launch and of that workgroup's dependent loads: room for a token each of 64 sequences 3 us, for 2048 pages 6 us, for 25000 of
-// 54000 pages 23 us; a fork 4 to 6 us and its copy 3 to 5 us, a release 2 to 5 us, the table's part of a cut 8 us.
+// 54000 pages 23 us; a fork 4 to 6 us and its copy 3 to 5 us, a release 2 to 5 us, the table's part of a cut 9 us.
 #include "cache_device.h"
 
 namespace pyr {
