@@ -1,0 +1,641 @@
+"""The operators on a cache held in 8 bits, as cases that can be timed and compared.
+
+A cache is a pool of pages that the slots of a table share.  32 tokens of a KV head are a block: K and V are 8-bit floating-point numbers
+(e4m3: sign, four exponent bits, three mantissa bits, up to 448, no infinities, 0x7f and 0xff: not a number) times a power of two, one for
+K and one for V of a block.  A block also keeps the largest and the smallest number that each channel of its K has held, as whole
+multiples of 4 * 2^power, rounded outward.  A case is what a serving program does with it:
+
+  append   new rows of Q, K and V, as the projections leave them: Q and K are turned by their positions, K and V go into the cache; or rows of K
+           and V that a selection kept, as they are.  The tokens of the blocks that changed are read back as bf16.
+  attend   attention of the newest token of every sequence, or of its newest few, over the sequence's cache
+  sparse   the same over some blocks alone: the first ones, the last ones and those in between whose bounds promise the largest logits
+
+A block that gets tokens behind others keeps its power of two or takes a larger one, which its older numbers are rounded to.
+Lengths come from the case itself ("lens": a seed), so every input seed has the same shapes.  What is held in 8 bits is returned as the
+values it stands for.
+
+A page, of hkv heads and T = page_tokens / 32 blocks a head, one part behind the other, up to a multiple of 256 bytes:
+  [hkv][T] 64 * d bytes   codes: K [half 2][s d/64][j 4][t 16][byte 16], token 16 half + t, channel 64 s + 16 j + byte;
+                          V [g d/32][j 4][r 16][p 2][e 8], token 16 (e / 4) + 4 j + e % 4, channel 32 g + 16 p + r
+  [hkv][T] 2 * d bytes    bounds of K: the largest, then the smallest of every channel, int8
+  [hkv][T] 2 bytes        powers of K and of V: 2^(byte - 127)
+"""
+import math
+import random
+
+import torch
+
+own = False                                         # False: plain torch operations; True: the library's entry points
+
+
+def listed():
+    return [
+        # the smallest step: one token of one short conversation on a small model, launches and latency are all there is
+        dict(name="append-1x1-d64", kind="append", n=1, lo=1, hi=1, base=256, hq=8, hkv=8, d=64, page=64, rot=64, far=256),
+        # a serving batch's new tokens on a 7B-shaped layer, from the fused projection's rows, far into their texts
+        dict(name="append-64x1", kind="append", n=64, lo=1, hi=1, base=1337, hq=32, hkv=32, d=128, page=64, rot=128, far=100000),
+        # the prompt's pivotal tokens go into the cache right after their selection: 70 % of 8 prompts of 2k tokens, turned already
+        dict(name="append-8x2048-kept", kind="append", n=8, lo=2048, hi=2048, base=0, hq=32, hkv=32, d=128, page=64, keep=70, rot=0, far=0),
+        # pieces of ragged prompts behind what the cache holds already, beginning and ending inside a block; half of the channels turn, in pairs
+        dict(name="append-ragged7-d64", kind="append", n=7, lo=100, hi=3000, lens=7, base=77, hq=32, hkv=8, d=64, page=32, rot=32, pairs=1, far=77),
+        # the smallest decode
+        dict(name="attend-1x256-d64", kind="attend", n=1, lo=256, hi=256, hq=8, hkv=8, d=64, page=64, tokens=1),
+        # one long document, many query heads on few key/value heads: the work has to be split along the cache
+        dict(name="attend-1x16384-gqa", kind="attend", n=1, lo=16384, hi=16384, hq=64, hkv=8, d=128, page=64, tokens=1),
+        # a serving batch of 2k tokens on a 7B-shaped layer: bound by the cache's bytes
+        dict(name="attend-64x2048", kind="attend", n=64, lo=2048, hi=2048, hq=32, hkv=32, d=128, page=64, tokens=1),
+        # a ragged batch on a 13B-shaped layer, 60 % of the tokens kept, four drafted tokens to verify
+        dict(name="attend-ragged32-4tokens", kind="attend", n=32, lo=307, hi=4915, lens=4, hq=40, hkv=40, d=128, page=128, tokens=4),
+        # a short conversation's newest token over an eighth of its blocks
+        dict(name="sparse-1x2048-d64", kind="sparse", n=1, lo=2048, hi=2048, hq=8, hkv=8, d=64, page=64, tokens=1, first=1, recent=2, best=5),
+        # a serving batch over a quarter of its blocks: bound by the cache's bytes
+        dict(name="sparse-64x2048", kind="sparse", n=64, lo=2048, hi=2048, hq=32, hkv=32, d=128, page=64, tokens=1, first=1, recent=3, best=12),
+        # one very long document, 2k of 131072 tokens: finding the blocks costs as much as reading them
+        dict(name="sparse-1x131072-gqa", kind="sparse", n=1, lo=131072, hi=131072, hq=64, hkv=8, d=128, page=128, tokens=1, first=2, recent=8, best=54),
+        # a ragged batch with grouped heads, three drafted tokens to verify, each with blocks of its own
+        dict(name="sparse-ragged16-3tokens", kind="sparse", n=16, lo=500, hi=16000, lens=16, hq=32, hkv=8, d=128, page=64, tokens=3, first=1, recent=4, best=27),
+    ]
+
+
+_HEADS = [(8, 8, 64), (32, 8, 64), (12, 12, 64), (32, 32, 128), (40, 40, 128), (32, 8, 128), (64, 8, 128), (24, 24, 128)]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["append", "append", "attend", "attend", "sparse", "sparse"])
+    hq, hkv, d = rng.choice(_HEADS)
+    n = _log_int(rng, 1, 128)
+    tokens = 1 if rng.random() < 0.6 else rng.randint(2, 9)
+    # values of K, so that a drawn case costs no more than the largest listed one: rows in bf16 are twice the cache's and come with the
+    # queries', more than 16 query rows on a head of K cost products, blocks that are chosen are read once for every token
+    most = (64 * 2048 * 32 * 128) // (6 * max(1, hq // hkv) if kind == "append" else -(-tokens * (hq // hkv) // 16) if kind == "attend" else 1)
+    top = max(1, min(_log_int(rng, 1, 131072 if kind == "sparse" else 65536), most // (hkv * d * n)))
+    low = top if rng.random() < 0.5 else max(1, int(top * rng.uniform(0.1, 0.9)))
+    case = dict(kind=kind, n=n, lo=low, hi=top, hq=hq, hkv=hkv, d=d, page=rng.choice([32, 64, 128, 256]))
+    if low < top:
+        case["lens"] = rng.randrange(1000)
+    if kind == "append":
+        if rng.random() < 0.3:
+            case["lo"] = case["hi"] = min(top, rng.randint(1, 9))            # a step of generation
+            case.pop("lens", None)
+        case["base"] = rng.choice([0, 32, rng.randint(1, 400)])
+        case["rot"] = rng.choice([0, 16, d // 2, d, d])
+        if case["rot"]:
+            case["far"] = rng.choice([0, rng.randint(1, 2000000)])
+            case["pairs"] = rng.randint(0, 1)
+        else:
+            case["far"] = 0
+            case["keep"] = rng.randint(30, 100)
+    else:
+        case["tokens"] = tokens
+        case["pad"] = 0 if rng.random() < 0.7 else rng.randint(1, n)         # rows of a padded batch at its end
+    if kind == "sparse":
+        case["first"], case["recent"] = rng.randint(0, 4), rng.randint(1, 8)
+        room = max(1, (64 * 2048 * 32 * 128) // (64 * hkv * d * n * tokens))   # half of what the largest attention reads
+        case["best"] = max(0, min(_log_int(rng, 1, 256), room))
+    return case
+
+
+def _lengths(case):
+    if case["lo"] == case["hi"]:
+        return [case["lo"]] * case["n"]
+    rng = random.Random(case["lens"])
+    return [rng.randint(case["lo"], case["hi"]) for _ in range(case["n"])]
+
+
+def _keeps(case, lens):
+    return [max(1, (case["keep"] * S + 50) // 100) for S in lens] if "keep" in case else lens
+
+
+def _offsets(lens):
+    off = [0]
+    for S in lens:
+        off.append(off[-1] + S)
+    return off
+
+
+# ------------------------------------------------------------------------------------------------ inputs
+def _ints(values):
+    return torch.tensor(values, dtype=torch.int32).cuda()
+
+
+class _Pool:
+    """The cache of a case: pages in an order that a long-running server leaves, free ones among them, all bytes of what is not
+    held at random.  held: tokens in the slots; spare: pages that stay free."""
+
+    def __init__(self, case, held, spare, gen):
+        self.hkv, self.d, self.page, self.tiles = case["hkv"], case["d"], case["page"], case["page"] // 32
+        pages = [-(-S // self.page) for S in held]
+        self.max_pages = max(1, max(pages))
+        self.n_pages = sum(pages) + spare
+        order = torch.randperm(self.n_pages, generator=gen, device="cuda").to(torch.int32)
+        self.table = torch.full((len(held), self.max_pages), -1, dtype=torch.int32, device="cuda")
+        self.refs = torch.zeros(self.n_pages, dtype=torch.int32, device="cuda")
+        first = _offsets(pages)
+        at = torch.arange(self.max_pages, device="cuda")
+        there = at[None, :] < torch.tensor(pages, device="cuda")[:, None]
+        rank = torch.tensor(first[:-1], device="cuda")[:, None] + at[None, :]
+        rows = order[rank.clamp(max=self.n_pages - 1)]
+        self.table.copy_(torch.where(there, rows, torch.full_like(rows, -1)))
+        self.refs[order[:first[-1]].long()] = 1
+        self.lens = _ints(held)
+        blocks = self.hkv * self.tiles
+        self.page_bytes = -(-blocks * (66 * self.d + 2) // 256) * 256
+        self.pages = torch.randint(0, 256, (self.n_pages, self.page_bytes), generator=gen, device="cuda", dtype=torch.uint8)
+        cut = blocks * 64 * self.d, blocks * 66 * self.d
+        self.codes = self.pages[:, :cut[0]].unflatten(1, (self.hkv, self.tiles, 64 * self.d))
+        self.bounds = self.pages[:, cut[0]:cut[1]].view(torch.int8).unflatten(1, (self.hkv, self.tiles, 2, self.d))
+        self.powers = self.pages[:, cut[1]:cut[1] + 2 * blocks].unflatten(1, (self.hkv, self.tiles, 2))
+
+
+def _rows(gen, count, heads, d, u, spread):
+    """bf16 rows [count, heads, d]: normal numbers along a direction u per head that tokens have to a degree of their own (so that they
+    differ in importance by orders of magnitude, as in a trained model; neighbours are alike); spread == 0: plain ones."""
+    x = torch.randn((count, heads, d), generator=gen, device="cuda")
+    if spread:
+        each = torch.randn(count, generator=gen, device="cuda")
+        near = torch.randn(-(-count // 24), generator=gen, device="cuda").repeat_interleave(24)[:count]
+        x += (spread * (0.6 * each + 0.8 * near))[:, None, None] * u[None]
+    return x.to(torch.bfloat16)
+
+
+def _fill(pool, held, gen, u):
+    """Every held token's K and V, a piece of the batch at a time."""
+    step = max(1, (1 << 26) // (pool.hkv * pool.d * max(max(held), 1)))
+    for b in range(0, len(held), step):
+        part = held[b:b + step]
+        off = _offsets(part)
+        k, v = _rows(gen, off[-1], pool.hkv, pool.d, u, 3.0), _rows(gen, off[-1], pool.hkv, pool.d, u, 0.0)
+        _plain_append(pool, k, v, None, _ints(off), _ints(list(range(b, b + len(part)))), _ints([0] * len(part)), max(part), None)
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    kind, lens, n = case["kind"], _lengths(case), case["n"]
+    hq, hkv, d = case["hq"], case["hkv"], case["d"]
+    u = torch.randn((hkv, d), generator=gen, device="cuda")
+    u /= u.norm(dim=1, keepdim=True)
+    s = dict(kind=kind, n=n, hq=hq, slots=_ints(list(range(n))))
+    if kind == "append":
+        # what the cache holds already has been put there; the new rows' pages are reserved
+        base, keeps = case["base"], _keeps(case, lens)
+        held = [base + k for k in keeps]
+        s["pool"] = _Pool(case, held, 1 + n // 8, gen)
+        if base:
+            _fill(s["pool"], [base] * n, gen, u)
+        total, off, koff = sum(lens), _offsets(lens), _offsets(keeps)
+        if case["rot"]:
+            # rows of a fused projection
+            s["qkv"] = torch.empty((total, (hq + 2 * hkv) * d), dtype=torch.bfloat16, device="cuda")
+            s["q"], s["k"], s["v"] = (x.unflatten(1, (-1, d)) for x in s["qkv"].split([hq * d, hkv * d, hkv * d], dim=1))
+            s["q"].copy_(_rows(gen, total, hq, d, u.repeat_interleave(hq // hkv, 0), 1.0))
+            s["k"].copy_(_rows(gen, total, hkv, d, u, 3.0))
+            s["v"].copy_(_rows(gen, total, hkv, d, u, 0.0))
+            s["q_out"] = torch.empty((total, hq, d), dtype=torch.bfloat16, device="cuda")
+            s["positions"] = torch.cat([torch.arange(S, dtype=torch.int32) + case["far"] + 13 * b for b, S in enumerate(lens)]).cuda()
+            s["freqs"] = (10000.0 ** (-torch.arange(case["rot"] // 2, dtype=torch.float64) * 2 / case["rot"])).float().cuda()
+        else:
+            s["k"], s["v"] = _rows(gen, total, hkv, d, u, 3.0), _rows(gen, total, hkv, d, u, 0.0)
+        s["rot"], s["pairs"] = case["rot"], case.get("pairs", 0)
+        s["row_idx"] = _choose(gen, lens, keeps) if case.get("keep", 100) < 100 else None
+        s["offsets"], s["start"], s["max_new"] = _ints(koff), _ints([base] * n), max(keeps)
+        from_ = base // 32 * 32
+        s["from"], s["read_off"], s["max_read"] = _ints([from_] * n), _ints(_offsets([S - from_ for S in held])), max(held) - from_
+        s["k_out"] = torch.empty((sum(held) - n * from_, hkv, d), dtype=torch.bfloat16, device="cuda")
+        s["v_out"] = torch.empty_like(s["k_out"])
+        return s
+    s["pool"] = _Pool(case, lens, 1 + n // 8, gen)
+    _fill(s["pool"], lens, gen, u)
+    pad, t = min(case.get("pad", 0), n), case["tokens"]
+    s["slots"], s["max_len"], s["tokens"] = _ints(list(range(n - pad)) + [-1] * pad), max(lens), t
+    q = torch.randn((n * t, hkv, hq // hkv, d), generator=gen, device="cuda")
+    q += (0.35 * math.sqrt(d)) * u[None, :, None, :]
+    s["q"] = q.reshape(n, t, hq, d).to(torch.bfloat16)
+    s["out"] = torch.empty_like(s["q"])
+    s["lse"] = torch.empty((n, t, hq), dtype=torch.float32, device="cuda")
+    if kind == "sparse":
+        s["first"], s["recent"], s["best"] = case["first"], case["recent"], case["best"]
+        s["blocks"] = torch.empty((n, t, hkv, case["first"] + case["recent"] + case["best"]), dtype=torch.int32, device="cuda")
+    return s
+
+
+def _choose(gen, lens, keeps):
+    """keeps[b] rows of every sequence, ascending, as row numbers of the packed batch."""
+    chosen, at = [], 0
+    for S, k in zip(lens, keeps):
+        chosen.append(torch.randperm(S, generator=gen, device="cuda")[:k].sort().values.to(torch.int32) + at)
+        at += S
+    return torch.cat(chosen)
+
+
+# ------------------------------------------------------------------------------------------------ the plain form
+def _unpack(tiles, d):
+    """[..., 64 * d] bytes -> codes of K and V [..., 32, d]"""
+    lead, m = tiles.shape[:-1], len(tiles.shape) - 1
+    dims = tuple(range(m))
+    k = tiles[..., :32 * d].reshape(*lead, 2, d // 64, 4, 16, 16)                              # half s j t byte
+    k = k.permute(*dims, m, m + 3, m + 1, m + 2, m + 4).reshape(*lead, 32, d)
+    v = tiles[..., 32 * d:].reshape(*lead, d // 32, 4, 16, 2, 2, 4)                            # g j r p e/4 e%4
+    v = v.permute(*dims, m + 4, m + 1, m + 5, m, m + 3, m + 2).reshape(*lead, 32, d)
+    return k, v
+
+
+def _pack(k, v):
+    lead, d, m = k.shape[:-2], k.shape[-1], len(k.shape) - 2
+    dims = tuple(range(m))
+    k = k.reshape(*lead, 2, 16, d // 64, 4, 16).permute(*dims, m, m + 2, m + 3, m + 1, m + 4).reshape(*lead, 32 * d)
+    v = v.reshape(*lead, 2, 4, 4, d // 32, 2, 16).permute(*dims, m + 3, m + 1, m + 5, m + 4, m, m + 2).reshape(*lead, 32 * d)
+    return torch.cat([k, v], dim=-1)
+
+
+def _two_to(e):
+    """2^e in fp32 for e in -126 .. 127, by its bits"""
+    return ((e.int() + 127) << 23).view(torch.float32)
+
+
+def _numbers(codes):
+    return codes.view(torch.float8_e4m3fn).float()
+
+
+def _codes(x):
+    return x.to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+def _power(top):
+    """The smallest e with top <= 448 * 2^e, -100 at least; top: fp32, finite"""
+    bits = top.view(torch.int32)
+    return ((bits >> 23) - 127 - 8 + ((bits & 0x7FFFFF) > 0x600000).int()).clamp(-100, 120)
+
+
+def _turn(x, positions, freqs, rot, pairs):
+    """x fp32 [..., heads, d], positions [...]"""
+    angle = positions.double().unsqueeze(-1) * freqs.double()
+    c, s = angle.cos().float().unsqueeze(-2), angle.sin().float().unsqueeze(-2)
+    if pairs:
+        a, b = x[..., 0:rot:2], x[..., 1:rot:2]
+        turned = torch.stack((a * c - b * s, b * c + a * s), dim=-1).flatten(-2)
+    else:
+        a, b = x[..., :rot // 2], x[..., rot // 2:rot]
+        turned = torch.cat((a * c - b * s, b * c + a * s), dim=-1)
+    return torch.cat((turned, x[..., rot:]), dim=-1)
+
+
+def _plain_append(pool, k, v, row_idx, offsets, slots, start, max_new, turn):
+    """Tokens start[b] .. of slots[b] become rows offsets[b] .. offsets[b + 1] - 1 (of row_idx)."""
+    off, slot, start = offsets.long(), slots.long(), start.long()
+    count = off[1:] - off[:-1]
+    tile = start[:, None] // 32 + torch.arange((max_new + 31) // 32 + 1, device="cuda")        # [n, tiles] of a slot
+    token = tile[:, :, None] * 32 + torch.arange(32, device="cuda")                            # [n, tiles, 32]
+    mine = (token >= start[:, None, None]) & (token < (start + count)[:, None, None])
+    b, c = torch.nonzero(mine.any(dim=2), as_tuple=True)
+    tile, token, mine = tile[b, c], token[b, c], mine[b, c]
+    page, at = pool.table[slot[b], tile // pool.tiles].long(), tile % pool.tiles
+    row = torch.where(mine, (off[b] - start[b])[:, None] + token, torch.zeros_like(token))
+    row = row if row_idx is None else row_idx[row].long()
+    x = k[row].float()
+    if turn is not None:
+        x = _turn(x, turn[0][row], *turn[1:])
+    x = torch.stack((x, v[row].float()), dim=1).permute(0, 1, 3, 2, 4)                         # [tiles, K V, hkv, 32, d]
+    fine = torch.isfinite(x) & mine[:, None, None, :, None]
+    need = _power(torch.where(fine, x, torch.zeros_like(x)).abs().amax(dim=(3, 4)))            # [tiles, K V, hkv]
+    old_power = pool.powers[page, :, at].int().permute(0, 2, 1) - 127
+    behind = (tile * 32 < start[b])[:, None, None]                                             # there are older tokens in the block
+    e = torch.where(behind, torch.maximum(need, old_power), need)
+    shift = torch.where(behind, e - old_power, torch.zeros_like(e))
+    old = torch.stack(_unpack(pool.codes[page, :, at], pool.d), dim=1)                          # [tiles, K V, hkv, 32, d]
+    kept = torch.where((shift > 0)[..., None, None], _codes(_numbers(old) * _two_to(-shift.clamp(max=100))[..., None, None]), old)
+    new = _codes(x * _two_to(-e)[..., None, None])
+    codes = torch.where(mine[:, None, None, :, None], new, kept)
+    pool.codes[page, :, at] = _pack(codes[:, 0], codes[:, 1])
+    pool.powers[page, :, at] = (e + 127).to(torch.uint8).permute(0, 2, 1)
+    # bounds: of the older tokens, rounded outward again where the power grew, and of the new ones
+    y = _numbers(new[:, 0])
+    mask = mine[:, None, :, None]
+    none = torch.isnan(y)
+    up = torch.where(mask, torch.where(none, torch.full_like(y, 508.0), y), torch.full_like(y, -508.0)).amax(dim=2)
+    down = torch.where(mask, torch.where(none, torch.full_like(y, -508.0), y), torch.full_like(y, 508.0)).amin(dim=2)
+    old_bounds, f = pool.bounds[page, :, at].float(), _two_to(-shift[:, 0].clamp(max=100))[..., None]
+    before = behind[:, 0, :, None]
+    up = torch.where(before, torch.maximum(torch.ceil(up / 4), torch.ceil(old_bounds[:, :, 0] * f)), torch.ceil(up / 4))
+    down = torch.where(before, torch.minimum(torch.floor(down / 4), torch.floor(old_bounds[:, :, 1] * f)), torch.floor(down / 4))
+    pool.bounds[page, :, at] = torch.stack((up, down), dim=2).to(torch.int8)
+
+
+def _plain_values(pool, page, tile, head=slice(None)):
+    """K and V in fp32 [..., 32, d] of blocks"""
+    k, v = _unpack(pool.codes[page, head, tile], pool.d)
+    p = _two_to(pool.powers[page, head, tile].int() - 127)
+    return _numbers(k) * p[..., 0, None, None], _numbers(v) * p[..., 1, None, None]
+
+
+def _plain_load(s):
+    pool, slot, off, from_ = s["pool"], s["slots"].long(), s["read_off"].long(), s["from"].long()
+    count = torch.minimum(pool.lens[slot].long() - from_, off[1:] - off[:-1])
+    tile = from_[:, None] // 32 + torch.arange(-(-s["max_read"] // 32), device="cuda")          # (from is a multiple of 32)
+    b, c = torch.nonzero(32 * torch.arange(tile.shape[1], device="cuda") < count[:, None], as_tuple=True)
+    k, v = _plain_values(pool, pool.table[slot[b], tile[b, c] // pool.tiles].long(), tile[b, c] % pool.tiles)
+    place = 32 * c[:, None] + torch.arange(32, device="cuda")
+    m, t = torch.nonzero(place < count[b][:, None], as_tuple=True)
+    row = (off[b][:, None] + place)[m, t]
+    s["k_out"][row] = k[m, :, t].to(torch.bfloat16)
+    s["v_out"][row] = v[m, :, t].to(torch.bfloat16)
+
+
+def _held(s):
+    slot = s["slots"].long()
+    return torch.where(slot >= 0, s["pool"].lens[slot.clamp(min=0)].long(), torch.zeros_like(slot))
+
+
+def _softmax(x, v):
+    """x [rows, columns, keys] masked logits, v [rows, keys, d]"""
+    top = x.amax(dim=2, keepdim=True)
+    p = torch.exp(x - torch.where(top > -math.inf, top, torch.zeros_like(top)))
+    total = p.sum(dim=2, keepdim=True)
+    out = torch.bmm(p, v) / torch.where(total > 0, total, torch.ones_like(total))
+    return out, ((top + torch.log(total)) / math.log(2.0))[..., 0]
+
+
+def _plain_attend(s):
+    pool, q, (n, tokens, hq, d) = s["pool"], s["q"].float(), s["q"].shape
+    held, hkv = _held(s), pool.hkv
+    table = pool.table[s["slots"].long().clamp(min=0)].long().clamp(min=0)                     # [n, pages]
+    tiles = pool.codes[table].permute(0, 2, 1, 3, 4)                                            # [n, hkv, pages, T, 64 d]
+    k, v = (_numbers(x) for x in _unpack(tiles, d))
+    p = _two_to((pool.powers[table].int() - 127).clamp(-126, 127)).permute(0, 2, 1, 3, 4)
+    k, v = (k * p[..., 0, None, None]).flatten(2, 4), (v * p[..., 1, None, None]).flatten(2, 4)
+    there = (torch.arange(k.shape[2], device="cuda") < held[:, None])[:, None, :, None]
+    zero = torch.zeros((), device="cuda")
+    k, v = torch.where(there, k, zero).flatten(0, 1), torch.where(there, v, zero).flatten(0, 1)
+    q = q.reshape(n, tokens, hkv, hq // hkv, d).permute(0, 2, 1, 3, 4).reshape(n * hkv, -1, d)
+    x = torch.bmm(q, k.transpose(1, 2).contiguous()) / math.sqrt(d)
+    x = x.reshape(n, hkv, tokens, hq // hkv, -1)
+    seen = held[:, None] - tokens + 1 + torch.arange(tokens, device="cuda")                     # [n, tokens] keys that a token sees
+    x = x.masked_fill(torch.arange(x.shape[4], device="cuda") >= seen[:, None, :, None, None], -math.inf)
+    out, lse = _softmax(x.reshape(n * hkv, -1, x.shape[4]), v)
+    s["out"].copy_(out.reshape(n, hkv, tokens, -1, d).permute(0, 2, 1, 3, 4).reshape(n, tokens, hq, d).to(torch.bfloat16))
+    s["lse"].copy_(lse.reshape(n, hkv, tokens, -1).permute(0, 2, 1, 3).reshape(n, tokens, hq))
+
+
+def _whole_queries(q):
+    """q fp32 [..., d] -> whole numbers from -127 to 127 and the power of two they are multiples of"""
+    top = torch.where(torch.isfinite(q), q, torch.zeros_like(q)).abs().amax(dim=-1)
+    bits = top.view(torch.int32)
+    e = ((bits >> 23) - 127 - 6 + ((bits & 0x7FFFFF) > 0x7E0000).int()).clamp(-100, 122)
+    return torch.nan_to_num(torch.round(q * _two_to(-e).unsqueeze(-1)).clamp(-127, 127), nan=0.0), e
+
+
+def _plain_select(s):
+    """The blocks [n, tokens, hkv, first + recent + best] that every token of every KV head attends to, ascending, -1 behind them."""
+    pool, (n, tokens, hq, d) = s["pool"], s["q"].shape
+    held, hkv = _held(s), pool.hkv
+    table = pool.table[s["slots"].long().clamp(min=0)].long().clamp(min=0)
+    bounds = pool.bounds[table].permute(0, 2, 1, 3, 4, 5).reshape(n * hkv, -1, 2 * d).float()     # [n hkv, blocks, 2 d]
+    power = pool.powers[table][..., 0].int().permute(0, 2, 1, 3).reshape(n, hkv, 1, 1, -1) - 127
+    whole, e = _whole_queries(s["q"].float().reshape(n, tokens, hkv, hq // hkv, d).permute(0, 2, 1, 3, 4))
+    parts = torch.cat((whole.clamp(min=0), whole.clamp(max=0)), dim=-1).reshape(n * hkv, -1, 2 * d)
+    dots = torch.bmm(parts, bounds.transpose(1, 2).contiguous()).reshape(n, hkv, tokens, hq // hkv, -1)   # whole numbers below 2^24: exact
+    score = (dots * _two_to((e.unsqueeze(-1) + power + 2).clamp(-120, 100))).amax(dim=3)          # [n, hkv, tokens, blocks]
+    seen = (held[:, None] - tokens + 1 + torch.arange(tokens, device="cuda")).clamp(min=0)
+    count = ((seen + 31) // 32)[:, None, :, None]
+    at = torch.arange(score.shape[3], device="cuda")
+    sure = (at < s["first"]) | (at >= count - s["recent"])
+    score = torch.where(at < count, torch.where(sure, torch.full_like(score, math.inf), score), torch.full_like(score, -math.inf))
+    width = s["blocks"].shape[3]
+    rank = torch.sort(score, dim=3, descending=True, stable=True).indices[..., :width]
+    rank = torch.nn.functional.pad(rank, (0, width - rank.shape[3]), value=1 << 30)
+    chosen = torch.where((rank < count) & (torch.arange(width, device="cuda") < count), rank, torch.full_like(rank, 1 << 30)).sort(dim=3).values
+    s["blocks"].copy_(torch.where(chosen < 1 << 30, chosen, torch.full_like(chosen, -1)).permute(0, 2, 1, 3))
+
+
+def _plain_attend_blocks(s):
+    pool, q, (n, tokens, hq, d) = s["pool"], s["q"].float(), s["q"].shape
+    held, hkv, blocks = _held(s), pool.hkv, s["blocks"].long()
+    at = blocks.clamp(min=0)
+    page = pool.table[s["slots"].long().clamp(min=0)[:, None, None, None], at // pool.tiles].long().clamp(min=0)
+    head = torch.arange(hkv, device="cuda")[:, None]
+    k, v = _plain_values(pool, page, at % pool.tiles, head)                                    # [n, tokens, hkv, width, 32, d]
+    seen = (held[:, None] - tokens + 1 + torch.arange(tokens, device="cuda"))[:, :, None, None, None]
+    there = (blocks[..., None] >= 0) & (32 * at[..., None] + torch.arange(32, device="cuda") < seen)
+    zero = torch.zeros((), device="cuda")
+    rows = n * tokens * hkv
+    k = torch.where(there[..., None], k, zero).reshape(rows, -1, d)
+    v = torch.where(there[..., None], v, zero).reshape(rows, -1, d)
+    x = torch.bmm(q.reshape(rows, hq // hkv, d), k.transpose(1, 2).contiguous()) / math.sqrt(d)
+    out, lse = _softmax(x.masked_fill(~there.reshape(rows, 1, -1), -math.inf), v)
+    s["out"].copy_(out.reshape(n, tokens, hq, d).to(torch.bfloat16))
+    s["lse"].copy_(lse.reshape(n, tokens, hq))
+
+
+# ------------------------------------------------------------------------------------------------ a pass
+def _handle(s, lib):
+    """What a program makes once for its cache and keeps: the description of the cache, a workspace."""
+    if "cache" not in s:
+        p, size = s["pool"], 0
+        s["cache"] = lib.make_cache8(p.pages, p.refs, p.table, p.lens, p.page, p.hkv, p.d)
+        if "q_out" in s:
+            s["rotation"] = lib.make_rotation(s["freqs"], s["positions"], s["rot"], s["pairs"])
+        if s["kind"] == "attend":
+            size = lib.cache8_attention_workspace_bytes(s["cache"], s["n"], s["tokens"], s["hq"], s["max_len"], 0)
+        elif s["kind"] == "sparse":
+            s["select_bytes"] = lib.cache8_select_workspace_bytes(s["cache"], s["n"], s["tokens"], s["hq"], s["max_len"])
+            s["select_ws"] = torch.empty(max(s["select_bytes"], 1), dtype=torch.uint8, device="cuda")
+            size = lib.cache8_attention_workspace_bytes(s["cache"], s["n"], s["tokens"], s["hq"], s["max_len"], s["blocks"].shape[3])
+        s["ws_bytes"], s["ws"] = size, torch.empty(max(size, 1), dtype=torch.uint8, device="cuda")
+    return s["cache"]
+
+
+def _run_own(s):
+    from paper_2405_12532_amd import binding as lib
+    cache, n, kind = _handle(s, lib), s["n"], s["kind"]
+    if kind == "append":
+        idx, rows = s["row_idx"], s["k"].shape[0]
+        q, q_out, turned = (s["q"], s["q_out"], s["rotation"]) if "q_out" in s else (None, None, None)
+        lib.cache8_append(cache, s["k"], s["v"], s["k"].stride(0), s["v"].stride(0), rows, idx, rows if idx is None else idx.shape[0], s["offsets"], s["slots"],
+                          s["start"], n, s["max_new"], turned, q, 0 if q is None else q.stride(0), 0 if q is None else s["hq"], q_out)
+        lib.cache8_load(cache, s["slots"], s["from"], s["read_off"], n, s["max_read"], s["k_out"], s["v_out"], s["k_out"].shape[0])
+        return
+    blocks = None
+    if kind == "sparse":
+        blocks = s["blocks"]
+        lib.cache8_select(cache, s["q"], s["slots"], n, s["tokens"], s["hq"], s["max_len"], s["first"], s["recent"], s["best"], blocks,
+                          s["select_ws"], s["select_bytes"])
+    lib.cache8_attention(cache, s["q"], s["slots"], n, s["tokens"], s["hq"], s["max_len"], 0.0, blocks, 0 if blocks is None else blocks.shape[3],
+                         s["out"], s["lse"], s["ws"], s["ws_bytes"])
+
+
+def _run_plain(s):
+    pool, kind = s["pool"], s["kind"]
+    if kind == "append":
+        turn = (s["positions"], s["freqs"], s["rot"], s["pairs"]) if "q_out" in s else None
+        _plain_append(pool, s["k"], s["v"], s["row_idx"], s["offsets"], s["slots"], s["start"], s["max_new"], turn)
+        if turn is not None:
+            s["q_out"].copy_(_turn(s["q"].float(), *turn).to(torch.bfloat16))
+        _plain_load(s)
+    elif kind == "attend":
+        _plain_attend(s)
+    else:
+        _plain_select(s)
+        _plain_attend_blocks(s)
+
+
+def run(s):
+    if own:
+        _run_own(s)
+    else:
+        _run_plain(s)
+    if s["kind"] == "append":
+        r = dict(k=s["k_out"], v=s["v_out"])
+        # (turned numbers next to a border may be rounded either way: their bounds with them)
+        return dict(r, q=s["q_out"]) if "q_out" in s else dict(r, bounds=s["pool"].bounds)
+    r = dict(out=s["out"], lse=s["lse"])
+    return dict(r, blocks=s["blocks"]) if s["kind"] == "sparse" else r
+
+
+def work(case):
+    lens, kind = _lengths(case), case["kind"]
+    hq, hkv, d, n = case["hq"], case["hkv"], case["d"], case["n"]
+    token8, token16 = 2 * hkv * d, 4 * hkv * d                                                 # bytes of a token, K and V
+    if kind == "append":
+        new = sum(_keeps(case, lens))
+        back = new + n * (case["base"] % 32)
+        queries = 4 * hq * d + 4 if case["rot"] else 0
+        return dict(bytes=new * (token16 + token8 + queries + (4 if case.get("keep", 100) < 100 else 0)) + back * (token8 + token16), flops=6.0 * new * (hq + hkv) * case["rot"] // 2)
+    t = case["tokens"]
+    live = lens[:n - min(case.get("pad", 0), n)]
+    rows = 4 * n * t * hq * (d + 1)
+    if kind == "attend":
+        return dict(bytes=sum(live) * token8 + rows, flops=4.0 * d * hq * t * sum(live))
+    width = case["first"] + case["recent"] + case["best"]
+    blocks = sum(-(-S // 32) for S in live)
+    read = sum(min(S, 32 * width) for S in live)
+    # the bounds of every block once, the chosen blocks of every token (they may all differ), the lists
+    return dict(bytes=blocks * hkv * (2 * d + 1) + read * t * token8 + rows + 8 * n * t * hkv * width, flops=4.0 * d * hq * t * (read + blocks))
+
+
+# ------------------------------------------------------------------------------------------------ 64 bits
+def _exact_two_to(e):
+    return (e.long() + 1023 << 52).view(torch.float64)
+
+
+def _exact_number(code):
+    """e4m3 by its definition"""
+    code = code.long()
+    e, m = code >> 3 & 15, (code & 7).double()
+    x = torch.where(e == 0, m * 2.0 ** -9, (8 + m) * _exact_two_to(e - 10))
+    return torch.where(code % 128 == 127, math.nan, torch.where(code >= 128, -x, x))
+
+
+def _exact_nearest(x):
+    """The nearest e4m3 number, ties to the even one; |x| <= 448"""
+    part, e = torch.frexp(x)
+    step = _exact_two_to(torch.clamp(e - 4, min=-9))
+    return torch.round(x / step) * step
+
+
+def _exact_held(pool, b, first, count):
+    """K and V [tokens, hkv, d] in 64 bits of a slot's tokens first .., byte by byte from the pages' description."""
+    d, dev, hkv = pool.d, "cuda", pool.hkv
+    t = torch.arange(first, first + count, device=dev)
+    page = pool.table[b].long()[t // pool.page] * pool.page_bytes
+    block = torch.arange(hkv, device=dev) * pool.tiles + (t % pool.page // 32)[:, None]                     # [tokens, hkv]
+    i, c, flat = (t % 32)[:, None, None], torch.arange(d, device=dev), pool.pages.flatten()
+    base = (page[:, None] + block * (64 * d))[:, :, None]
+    kbyte = base + (((i // 16) * (d // 64) + c // 64) * 4 + c % 64 // 16) * 256 + (i % 16) * 16 + c % 16
+    vbyte = base + 32 * d + ((c // 32 * 4 + i % 16 // 4) * 16 + c % 16) * 16 + c % 32 // 16 * 8 + i // 16 * 4 + i % 4
+    power = page[:, None] + hkv * pool.tiles * 66 * d + 2 * block
+    return (_exact_number(flat[kbyte]) * _exact_two_to(flat[power].long() - 127)[..., None],
+            _exact_number(flat[vbyte]) * _exact_two_to(flat[power + 1].long() - 127)[..., None])
+
+
+def _exact_attend(q, k, v, hidden):
+    """q [tokens, hq, d], k and v [S, hkv, d], hidden [tokens, hkv or 1, S]: keys that a token does not see"""
+    tokens, hq, d = q.shape
+    hkv, g = k.shape[1], q.shape[1] // k.shape[1]
+    qh = q.reshape(tokens, hkv, g, d).permute(1, 0, 2, 3).reshape(hkv, tokens * g, d)
+    x = torch.bmm(qh, k.permute(1, 2, 0).contiguous()).reshape(hkv, tokens, g, -1) / math.sqrt(d)
+    x.masked_fill_(hidden.permute(1, 0, 2)[:, :, None], -math.inf)
+    norm = torch.logsumexp(x, dim=3, keepdim=True)
+    p = torch.where(norm > -math.inf, torch.exp(x - norm), torch.zeros_like(x)).reshape(hkv, tokens * g, -1)
+    out = torch.bmm(p, v.permute(1, 0, 2).contiguous()).reshape(hkv, tokens, g, d)
+    return out.permute(1, 0, 2, 3).reshape(tokens, hq, d), norm[..., 0].permute(1, 0, 2).reshape(tokens, hq) / math.log(2.0)
+
+
+def _exact_blocks(s, b, S):
+    """Whether a token of a KV head attends to a block: [tokens, hkv, blocks]"""
+    pool, q = s["pool"], s["q"][b].double()
+    tokens, hq, d = q.shape
+    hkv, n_blocks = pool.hkv, -(-S // 32)
+    block = torch.arange(n_blocks, device="cuda")
+    page, at = pool.table[b].long()[block // pool.tiles], block % pool.tiles
+    flat, part = pool.pages.flatten(), hkv * pool.tiles * 64 * d
+    entry = page[:, None] * pool.page_bytes + part + (torch.arange(hkv, device="cuda") * pool.tiles + at[:, None]) * (2 * d)     # [blocks, hkv]
+    bound = flat[entry[..., None] + torch.arange(2 * d, device="cuda")].long()
+    bound = torch.where(bound >= 128, bound - 256, bound).double()
+    power = flat[page[:, None] * pool.page_bytes + hkv * pool.tiles * 66 * d + (torch.arange(hkv, device="cuda") * pool.tiles + at[:, None]) * 2].long() - 127
+    top = torch.where(torch.isfinite(q), q, 0.0).abs().amax(dim=-1)
+    part, e = torch.frexp(top)
+    e = torch.where(top > 0, e - 7 + (part > 127 / 128).long(), -1000).clamp(-100, 122)                       # top <= 127 * 2^e
+    whole = torch.nan_to_num(torch.round(q / _exact_two_to(e)[..., None]).clamp(-127, 127), nan=0.0).reshape(tokens, hkv, -1, d)
+    up, down = bound[..., :d], bound[..., d:]
+    dots = torch.bmm(whole.clamp(min=0).permute(1, 0, 2, 3).reshape(hkv, -1, d), up.permute(1, 2, 0).contiguous()) + \
+        torch.bmm(whole.clamp(max=0).permute(1, 0, 2, 3).reshape(hkv, -1, d), down.permute(1, 2, 0).contiguous())
+    scale = _exact_two_to((e.reshape(tokens, hkv, -1).permute(1, 0, 2)[..., None] + power.t()[:, None, None] + 2).clamp(-120, 100))
+    score = (dots.reshape(hkv, tokens, -1, n_blocks) * scale).amax(dim=2).permute(1, 0, 2)                    # [tokens, hkv, blocks]
+    chosen = torch.zeros(score.shape, dtype=torch.bool, device="cuda")
+    for i in range(tokens):
+        count = (max(0, S - tokens + 1 + i) + 31) // 32
+        lo, hi = min(s["first"], count), max(min(s["first"], count), count - s["recent"])
+        chosen[i, :, :lo] = True
+        chosen[i, :, hi:count] = True
+        best = torch.argsort(score[i, :, lo:hi], dim=1, descending=True, stable=True)[:, :s["best"]] + lo
+        chosen[i].scatter_(1, best, True)
+    return chosen
+
+
+def exact(case, seed):
+    kind, lens, n = case["kind"], _lengths(case), case["n"]
+    s = prepare(case, seed)
+    pool = s["pool"]
+    if kind != "append":
+        t = case["tokens"]
+        out, lse = torch.zeros(s["out"].shape, dtype=torch.float64, device="cuda"), torch.full(s["lse"].shape, -math.inf, dtype=torch.float64, device="cuda")
+        for b in range(n - min(case.get("pad", 0), n)):
+            k, v = _exact_held(pool, b, 0, lens[b])
+            hidden = (torch.arange(lens[b], device="cuda") > torch.arange(lens[b] - t, lens[b], device="cuda")[:, None])[:, None]
+            if kind == "sparse":
+                hidden = hidden | ~_exact_blocks(s, b, lens[b]).repeat_interleave(32, 2)[..., :lens[b]]
+            out[b], lse[b] = _exact_attend(s["q"][b].double(), k, v, hidden)
+        return dict(out=out, lse=lse, blocks=None) if kind == "sparse" else dict(out=out, lse=lse)
+    rot, base, keeps, hkv = case["rot"], case["base"], _keeps(case, lens), case["hkv"]
+
+    def turned(x):
+        x, angle = x.double(), s["positions"].double()[:, None] * s["freqs"].double()
+        z = torch.polar(torch.ones_like(angle), angle)[:, None]
+        a, b = (slice(0, rot, 2), slice(1, rot, 2)) if s["pairs"] else (slice(0, rot // 2), slice(rot // 2, rot))
+        z, y = torch.complex(x[..., a].contiguous(), x[..., b].contiguous()) * z, x.clone()
+        y[..., a], y[..., b] = z.real, z.imag
+        return y
+    k_rows, v_rows = turned(s["k"]) if rot else s["k"].double(), s["v"].double()
+    koff, ks, vs = _offsets(keeps), [], []
+    from_ = base // 32 * 32
+    for b in range(n):
+        rows = torch.arange(koff[b], koff[b + 1], device="cuda")
+        rows = rows if s["row_idx"] is None else s["row_idx"][rows].long()
+        old = _exact_held(pool, b, from_, base - from_)
+        block = torch.arange(base - from_ + keeps[b], device="cuda") // 32
+        page = pool.table[b].long()[from_ // pool.page]
+        for x, before, which, to in ((k_rows[rows], old[0], 0, ks), (v_rows[rows], old[1], 1, vs)):
+            top = torch.zeros((int(block[-1]) + 1, hkv), dtype=torch.float64, device="cuda")
+            top.scatter_reduce_(0, block[base - from_:, None].expand(-1, hkv), x.abs().amax(dim=2), "amax")
+            part, e = torch.frexp(top)
+            e = torch.where(top > 0, e - 9 + (part > 0.875).long(), -100).clamp(-100, 120)                  # top <= 448 * 2^e
+            if base > from_:
+                e[0] = torch.maximum(e[0], pool.powers[page, :, from_ % pool.page // 32, which].long() - 127)
+            power = _exact_two_to(e)[block][..., None]
+            to.append(_exact_nearest(torch.cat([before, x]) / power) * power)
+    r = dict(k=torch.cat(ks), v=torch.cat(vs))
+    return dict(r, q=turned(s["q"])) if rot else dict(r, bounds=None)
