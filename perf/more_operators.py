@@ -69,9 +69,11 @@ def draw(rng):
     hq, hkv, d = rng.choice(_HEADS)
     n = _log_int(rng, 1, 128)
     tokens = 1 if rng.random() < 0.6 else rng.randint(2, 9)
-    # values of K, so that a drawn case costs no more than the largest listed one: rows in bf16 are twice the cache's and come with the
-    # queries', more than 16 query rows on a head of K cost products, blocks that are chosen are read once for every token
-    most = (64 * 2048 * 32 * 128) // (6 * max(1, hq // hkv) if kind == "append" else -(-tokens * (hq // hkv) // 16) if kind == "attend" else 1)
+    if kind == "sparse":                                                     # (every token reads blocks of its own)
+        n = max(1, min(n, 640000 // (hkv * d * tokens)))
+    # values of K, so that a drawn case costs no more than the largest listed one: rows in bf16 are twice the cache's, go in and come back,
+    # with the queries', more than 16 query rows on a head of K cost products
+    most = (60 * 2048 * 32 * 128) // (6 + 2 * (hq // hkv) if kind == "append" else -(-tokens * (hq // hkv) // 16) if kind == "attend" else 1)
     top = max(1, min(_log_int(rng, 1, 131072 if kind == "sparse" else 65536), most // (hkv * d * n)))
     low = top if rng.random() < 0.5 else max(1, int(top * rng.uniform(0.1, 0.9)))
     case = dict(kind=kind, n=n, lo=low, hi=top, hq=hq, hkv=hkv, d=d, page=rng.choice([32, 64, 128, 256]))
