@@ -270,7 +270,7 @@ def _codes(x):
 def _power(top):
     """The smallest e with top <= 448 * 2^e, -100 at least; top: fp32, finite"""
     bits = top.view(torch.int32)
-    return ((bits >> 23) - 127 - 8 + ((bits & 0x7FFFFF) > 0x600000).int()).clamp(-100, 120)
+    return ((bits >> 23) - 127 - 8 + ((bits & 0x7FFFFF) > 0x600000).int()).clamp(-100, 119)
 
 
 def _turn(x, positions, freqs, rot, pairs):
@@ -634,7 +634,7 @@ def exact(case, seed):
             top = torch.zeros((int(block[-1]) + 1, hkv), dtype=torch.float64, device="cuda")
             top.scatter_reduce_(0, block[base - from_:, None].expand(-1, hkv), x.abs().amax(dim=2), "amax")
             part, e = torch.frexp(top)
-            e = torch.where(top > 0, e - 9 + (part > 0.875).long(), -100).clamp(-100, 120)                  # top <= 448 * 2^e
+            e = torch.where(top > 0, e - 9 + (part > 0.875).long(), -100).clamp(-100, 119)                  # top <= 448 * 2^e
             if base > from_:
                 e[0] = torch.maximum(e[0], pool.powers[page, :, from_ % pool.page // 32, which].long() - 127)
             power = _exact_two_to(e)[block][..., None]
