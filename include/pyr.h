@@ -452,6 +452,114 @@ PYR_API int pyr_cache_attention(const pyr_cache* cache, const void* q, const int
                         void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * A cache held in 8 bits, in pages that the slots of a table share as those of the cache in 4 bits are: twice the bytes, two more bits of every number.  Pages
+ * are handed out and given back by pyr_cache_reserve and pyr_cache_release on `pool`, whose pages have pyr_cache8_page_bytes() bytes; all other calls on
+ * it are the pyr_cache8_* below.  What is said above of slots, pages, counts, statuses, graphs and host checks holds here as well.
+ *
+ * 32 tokens of a KV head are a block.  K and V of a block are 8-bit floating-point numbers (e4m3: a sign, four exponent bits and three mantissa bits, up to
+ * 448, no infinities) times a power of two, one for K and one for V: the smallest that brings the largest magnitude of what has been stored to 448 or
+ * less, from 2^-100 to 2^119.  Numbers are rounded to the nearest, ties to the even code; an infinity, a NaN, and what would be rounded to more than
+ * 448 * 2^119 is stored as NaN, by itself.  A block that gets tokens behind others keeps its power or takes a larger one, which its older numbers are
+ * rounded to (exact, but for those that leave four significant bits: below 2^-6 of a unit).  Storing a block's first token starts it
+ * anew: what lay behind the new tokens in it holds nothing then.
+ * A block keeps bounds of its K, for pyr_cache8_select: the largest and the smallest number that a channel has held since then, rounded outward to whole
+ * multiples of 4 times the power, from -112 to 112; +-127 where one of them was NaN.  When the power grows they are divided and rounded outward.
+ *
+ * Layout, for programs that read or write pages themselves: for H = n_kv_heads and T = page_tokens / 32, one behind the other, up to a multiple of 256 bytes
+ *   [H][T] 64 d bytes   K's codes [half 2][s d/64][j 4][t 16][byte 16]: token 16 * half + t, channel 64 s + 16 j + byte;
+ *                       V's codes [g d/32][j 4][r 16][p 2][e 8]: token 16 * (e / 4) + 4 j + e % 4, channel 32 g + 16 p + r
+ *   [H][T]  2 d bytes   bounds: the largest [d], the smallest [d], int8
+ *   [H][T]  2 bytes     powers of K and of V: 2^(byte - 127)
+ *
+ * Host checks as above, and PYR_ERR_UNSUPPORTED for pages of 2^31 bytes or more.
+ */
+typedef struct pyr_cache8 {
+    pyr_cache pool;       /* pages of pyr_cache8_page_bytes() bytes                                  */
+} pyr_cache8;
+
+/* Host only.  Bytes of a page; reads page_tokens, n_kv_heads and head_dim of the pool. */
+PYR_API int pyr_cache8_page_bytes(const pyr_cache8* cache, size_t* bytes_out);
+
+/* As pyr_cache_fork; of a page filled in part all bytes are copied. */
+PYR_API int pyr_cache8_fork(const pyr_cache8* cache, const int32_t* parents, const int32_t* children, int32_t n, int32_t* status, void* stream);
+
+/* Position encodings by rotation: channels a and b of pair i become a cos(p f_i) - b sin(p f_i) and b cos(p f_i) + a sin(p f_i) at position p. */
+typedef struct pyr_rotation {
+    const float* freqs;        /* dev fp32 [dims / 2]: f_i, radians a position; finite                                 */
+    const int32_t* positions;  /* dev int32 [n_rows]: p of every row, also of rows that a list leaves out             */
+    int32_t dims;              /* channels that turn, the first ones of a head: a multiple of 16, at most head_dim    */
+    int32_t interleaved;       /* pair i is channels i and i + dims / 2 (0) or 2 i and 2 i + 1 (else)                  */
+} pyr_rotation;
+
+/*
+ * Rows of K and V into the cache, turned by their positions on the way: token start[i] + j of slots[i] becomes row offsets[i] + j, or row
+ * row_idx[offsets[i] + j], j < min(offsets[i+1] - offsets[i], max_new).  The rows of a prompt's selection go in as they are (rotation NULL): row_idx = kept_idx.
+ * A new token's go in as the projections leave them; its position is an argument, as a cache that was cut holds fewer tokens than the text has.
+ *   k, v               dev bf16 [n_rows, Hkv, d], rows k_stride and v_stride elements apart (a multiple of 8; 0: Hkv * d)
+ *   row_idx            dev int32 [n_list] or NULL (then n_list = n_rows)
+ *   offsets            dev int32 [n+1];  slots, start  dev int32 [n]
+ *   rotation           host, its pointers dev; NULL or dims 0: nothing turns.  p f_i is reduced to a part of a turn in 64 bits, the turn itself is fp32, and K is
+ *                      rounded once, to its code
+ *   q                  dev bf16 [n_rows, Hq, d], rows q_stride elements apart, or NULL
+ *   q_out              dev bf16 [n_rows, Hq, d], written: the rows of q whose tokens are stored, turned; the others stay as they were
+ * Tokens from lens[slots[i]] on (they were not reserved), tokens that have no page and a start of -1 are not stored; a row outside k and v or the list is
+ * stored as NaN; nothing else in the pages changes, but for what a larger power does to its block.  Of rows that name the same slot the first is stored.
+ * q_out must not overlap k, v or q - but it may be q itself, packed.
+ */
+PYR_API int pyr_cache8_append(const pyr_cache8* cache, const void* k, const void* v, int64_t k_stride, int64_t v_stride, int32_t n_rows,
+                      const int32_t* row_idx, int32_t n_list, const int32_t* offsets, const int32_t* slots, const int32_t* start, int32_t n, int32_t max_new,
+                      const pyr_rotation* rotation, const void* q, int64_t q_stride, int32_t n_q_heads, void* q_out, void* stream);
+
+/*
+ * The cache as bf16 rows (exactly), packed as pyr_decode_update and pyr_score read them: row offsets[i] + j is token first[i] + j of slots[i],
+ * j < min(lens[slots[i]] - first[i], offsets[i+1] - offsets[i], max_len).  Rows that no token goes to stay as they were, those of tokens on a
+ * page outside the pool among them; a sequence whose offset or first token is below 0 is skipped.
+ *   first              dev int32 [n] or NULL: 0
+ *   offsets            dev int32 [n+1];  slots  dev int32 [n]
+ *   k_out, v_out       dev bf16 [n_rows, Hkv, d]; one of them may be NULL; rows from n_rows on are not written
+ */
+PYR_API int pyr_cache8_load(const pyr_cache8* cache, const int32_t* slots, const int32_t* first, const int32_t* offsets, int32_t n, int32_t max_len,
+                    void* k_out, void* v_out, int32_t n_rows, void* stream);
+
+/*
+ * The blocks that each of a sequence's newest n_tokens tokens attends to, for every KV head.  Token i of slots[b] sees the tokens 0 .. s - 1,
+ * s = lens[slots[b]] - n_tokens + i + 1, and so the blocks 0 .. c - 1, c = ceil(s / 32).  It takes the first n_first of them, the last n_recent and, of
+ * those in between, the n_best with the highest scores (ties: the lower number):
+ *   score = max over the group's query heads h of 2^x sum_c max(u_c hi_c, u_c lo_c)
+ * with the block's bounds hi and lo, u_c = q_c / 2^e rounded to the nearest whole number (ties to even, from -127 to 127, 0 for NaN), 2^e the smallest power of two
+ * that brings the head's largest finite |q_c| to 127 or less (2^-100 at least), x = min(max(e + 2 + the power of the block's K, -120), 100).  Sums of whole numbers
+ * below 2^22: a score is exact in fp32, and the choice the same wherever it is made.
+ *   q                  dev bf16 [n, n_tokens, Hq, d];  slots  dev int32 [n]
+ *   max_len            at least the longest sequence; of a longer one the blocks from ceil(max_len / 32) on are not among those that are scored
+ *   n_first, n_best    0 or more;  n_recent  1 or more
+ *   blocks             dev int32 [n, n_tokens, Hkv, n_first + n_recent + n_best], written: ascending, -1 behind the last
+ *   workspace          dev, >= pyr_cache8_select_workspace_bytes(), 256-byte aligned; not read where that is 0
+ * One launch, or two where few long sequences are scored.
+ */
+PYR_API int pyr_cache8_select_workspace_bytes(const pyr_cache8* cache, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len, size_t* bytes_out);
+PYR_API int pyr_cache8_select(const pyr_cache8* cache, const void* q, const int32_t* slots, int32_t n, int32_t n_tokens, int32_t n_q_heads,
+                      int32_t max_len, int32_t n_first, int32_t n_recent, int32_t n_best, int32_t* blocks, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/*
+ * Attention of each sequence's newest n_tokens tokens over its cache, theirs included, as pyr_cache_attention; or over the blocks of a list for every token and
+ * KV head, of which a token sees what it sees without one.
+ *   blocks             dev int32 [n, n_tokens, Hkv, n_blocks], as pyr_cache8_select writes it or any other; NULL with n_blocks 0: all blocks.
+ *                      An entry that is no block which the token sees is left out, one that is there twice counts twice.
+ *   max_len            as in pyr_cache_attention; not looked at where there are lists
+ *   q, slots, softmax_scale, out, lse, workspace  as in pyr_cache_attention
+ * bf16 MFMA products on the cache's exact values (P is rounded to bf16), fp32 accumulation and softmax.  Sums of P V stay in fp32's range as long as V's
+ * largest power of two times the sequence's tokens is below 2^105 (a number whose sum leaves it is NaN).
+ * A row that sees nothing (an empty slot, a skipped row, a list without blocks): zeros in out, -inf in lse.  A K that is NaN makes the rows that see it NaN, a V
+ * the channel of those rows; what a row does not see never reaches it.  A page outside the pool among those that it takes: NaN in the sequence's rows, or the list's.
+ */
+PYR_API int pyr_cache8_attention_workspace_bytes(const pyr_cache8* cache, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len,
+                                         int32_t n_blocks, size_t* bytes_out);
+PYR_API int pyr_cache8_attention(const pyr_cache8* cache, const void* q, const int32_t* slots, int32_t n, int32_t n_tokens, int32_t n_q_heads,
+                         int32_t max_len, float softmax_scale, const int32_t* blocks, int32_t n_blocks, void* out, float* lse,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Diagnostic for the benchmark report, not part of the method: a launch of nothing but bf16 MFMAs
  * (v_mfma_f32_32x32x16_bf16 back to back, two wavefronts per SIMD, every compute unit), so that the
  * rate this very GPU sustains can be printed beside the published peak.
@@ -543,6 +651,10 @@ typedef struct pyr_cache_route {
 } pyr_cache_route;
 PYR_API int pyr_diag_cache_attention(const pyr_cache* cache, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len,
                                      pyr_cache_route* route_out);
+
+/* The same of pyr_cache8_attention (repeats: always 1). */
+PYR_API int pyr_diag_cache8_attention(const pyr_cache8* cache, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len, int32_t n_blocks,
+                                      pyr_cache_route* route_out);
 
 #ifdef __cplusplus
 }

@@ -35,6 +35,14 @@ class PyrCache(ctypes.Structure):
         "n_pages", "page_tokens", "n_slots", "max_pages", "n_kv_heads", "head_dim")]
 
 
+class PyrCache8(ctypes.Structure):
+    _fields_ = [("pool", PyrCache)]
+
+
+class PyrRotation(ctypes.Structure):
+    _fields_ = [("freqs", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
 class PyrCacheRoute(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("col_tiles", "repeats", "waves", "col_groups", "chunk", "splits")]
 
@@ -88,6 +96,16 @@ _SIGNATURES = {
     "pyr_cache_attention_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(PyrCache), _I32, _I32, _I32, _I32, ctypes.POINTER(_SZ)]),
     "pyr_cache_attention": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _I32, _I32, _I32, _F32, _VP, _VP, _VP, _SZ, _VP]),
     "pyr_diag_cache_attention": (ctypes.c_int, [ctypes.POINTER(PyrCache), _I32, _I32, _I32, _I32, ctypes.POINTER(PyrCacheRoute)]),
+    "pyr_cache8_page_bytes": (ctypes.c_int, [ctypes.POINTER(PyrCache8), ctypes.POINTER(_SZ)]),
+    "pyr_cache8_fork": (ctypes.c_int, [ctypes.POINTER(PyrCache8), _VP, _VP, _I32, _VP, _VP]),
+    "pyr_cache8_append": (ctypes.c_int, [ctypes.POINTER(PyrCache8), _VP, _VP, _I64, _I64, _I32, _VP, _I32, _VP, _VP, _VP, _I32, _I32,
+                                         ctypes.POINTER(PyrRotation), _VP, _I64, _I32, _VP, _VP]),
+    "pyr_cache8_load": (ctypes.c_int, [ctypes.POINTER(PyrCache8), _VP, _VP, _VP, _I32, _I32, _VP, _VP, _I32, _VP]),
+    "pyr_cache8_select_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(PyrCache8), _I32, _I32, _I32, _I32, ctypes.POINTER(_SZ)]),
+    "pyr_cache8_select": (ctypes.c_int, [ctypes.POINTER(PyrCache8), _VP, _VP, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _VP, _VP, _SZ, _VP]),
+    "pyr_cache8_attention_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(PyrCache8), _I32, _I32, _I32, _I32, _I32, ctypes.POINTER(_SZ)]),
+    "pyr_cache8_attention": (ctypes.c_int, [ctypes.POINTER(PyrCache8), _VP, _VP, _I32, _I32, _I32, _I32, _F32, _VP, _I32, _VP, _VP, _VP, _SZ, _VP]),
+    "pyr_diag_cache8_attention": (ctypes.c_int, [ctypes.POINTER(PyrCache8), _I32, _I32, _I32, _I32, _I32, ctypes.POINTER(PyrCacheRoute)]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -391,6 +409,89 @@ def diag_cache_attention(cache, n, n_tokens, n_q_heads, max_len) -> PyrCacheRout
     out = PyrCacheRoute()
     _check(load().pyr_diag_cache_attention(ctypes.byref(cache), int(n), int(n_tokens), int(n_q_heads), int(max_len), ctypes.byref(out)),
            "pyr_diag_cache_attention")
+    return out
+
+
+# ----------------------------------------------------------------------------- the cache held in 8 bits
+def make_cache8(pages, refs, table, lens, page_tokens: int, n_kv_heads: int, head_dim: int) -> PyrCache8:
+    """The description of a cache held in 8 bits that the calls below take; cache_reserve and cache_release take its `pool`.  pages: uint8, whole
+    pages (cache8_page_bytes); refs int32 [n_pages], table int32 [n_slots, max_pages], lens int32 [n_slots].  It keeps the tensors alive."""
+    import torch
+    if not all(t.is_contiguous() for t in (pages, refs, table, lens)) or any(t.dtype != torch.int32 for t in (refs, table, lens)) or \
+            any(t.device != pages.device for t in (refs, table, lens)) or \
+            (refs.dim(), table.dim(), lens.dim()) != (1, 2, 1) or lens.shape[0] != table.shape[0] or \
+            pages.numel() * pages.element_size() < refs.shape[0] * cache8_page_bytes(page_tokens, n_kv_heads, head_dim):
+        raise ValueError("contiguous pages and int32 refs, table and lens of one cache, on one device")
+    cache = PyrCache8(PyrCache(_ptr(pages), _ptr(refs), _ptr(table), _ptr(lens), refs.shape[0], int(page_tokens), table.shape[0], table.shape[1],
+                               int(n_kv_heads), int(head_dim)))
+    cache.tensors = (pages, refs, table, lens)
+    return cache
+
+
+def make_rotation(freqs, positions, dims: int, interleaved: bool = False) -> PyrRotation:
+    """freqs fp32 [dims / 2], positions int32, one for every row.  It keeps the tensors alive."""
+    import torch
+    if not (freqs.is_contiguous() and positions.is_contiguous()) or freqs.dtype != torch.float32 or positions.dtype != torch.int32 or \
+            freqs.numel() < int(dims) // 2 or freqs.device != positions.device:
+        raise ValueError("contiguous fp32 frequencies, one for two channels, and int32 positions, on one device")
+    rotation = PyrRotation(_ptr(freqs), _ptr(positions), int(dims), int(bool(interleaved)))
+    rotation.tensors = (freqs, positions)
+    return rotation
+
+
+def cache8_page_bytes(page_tokens: int, n_kv_heads: int, head_dim: int) -> int:
+    out, cache = _SZ(0), PyrCache8(PyrCache(page_tokens=int(page_tokens), n_kv_heads=int(n_kv_heads), head_dim=int(head_dim)))
+    _check(load().pyr_cache8_page_bytes(ctypes.byref(cache), ctypes.byref(out)), "pyr_cache8_page_bytes")
+    return int(out.value)
+
+
+def cache8_fork(cache, parents, children, n, status, stream=None):
+    _check(load().pyr_cache8_fork(ctypes.byref(cache), _ptr(parents), _ptr(children), int(n), _ptr(status), _stream(stream)), "pyr_cache8_fork")
+
+
+def cache8_append(cache, k, v, k_stride, v_stride, n_rows, row_idx, n_list, offsets, slots, start, n, max_new, rotation=None, q=None, q_stride=0,
+                  n_q_heads=0, q_out=None, stream=None):
+    _check(load().pyr_cache8_append(ctypes.byref(cache), _ptr(k), _ptr(v), int(k_stride), int(v_stride), int(n_rows), _ptr(row_idx), int(n_list),
+                                    _ptr(offsets), _ptr(slots), _ptr(start), int(n), int(max_new), None if rotation is None else ctypes.byref(rotation),
+                                    _ptr(q), int(q_stride), int(n_q_heads), _ptr(q_out), _stream(stream)), "pyr_cache8_append")
+
+
+def cache8_load(cache, slots, first, offsets, n, max_len, k_out, v_out, n_rows, stream=None):
+    _check(load().pyr_cache8_load(ctypes.byref(cache), _ptr(slots), _ptr(first), _ptr(offsets), int(n), int(max_len), _ptr(k_out), _ptr(v_out),
+                                  int(n_rows), _stream(stream)), "pyr_cache8_load")
+
+
+def cache8_select_workspace_bytes(cache, n, n_tokens, n_q_heads, max_len) -> int:
+    out = _SZ(0)
+    _check(load().pyr_cache8_select_workspace_bytes(ctypes.byref(cache), int(n), int(n_tokens), int(n_q_heads), int(max_len), ctypes.byref(out)),
+           "pyr_cache8_select_workspace_bytes")
+    return int(out.value)
+
+
+def cache8_select(cache, q, slots, n, n_tokens, n_q_heads, max_len, n_first, n_recent, n_best, blocks, workspace, workspace_bytes_, stream=None):
+    _check(load().pyr_cache8_select(ctypes.byref(cache), _ptr(q), _ptr(slots), int(n), int(n_tokens), int(n_q_heads), int(max_len), int(n_first),
+                                    int(n_recent), int(n_best), _ptr(blocks), _ptr(workspace), int(workspace_bytes_), _stream(stream)), "pyr_cache8_select")
+
+
+def cache8_attention_workspace_bytes(cache, n, n_tokens, n_q_heads, max_len, n_blocks) -> int:
+    out = _SZ(0)
+    _check(load().pyr_cache8_attention_workspace_bytes(ctypes.byref(cache), int(n), int(n_tokens), int(n_q_heads), int(max_len), int(n_blocks),
+                                                       ctypes.byref(out)), "pyr_cache8_attention_workspace_bytes")
+    return int(out.value)
+
+
+def cache8_attention(cache, q, slots, n, n_tokens, n_q_heads, max_len, softmax_scale, blocks, n_blocks, out, lse, workspace, workspace_bytes_,
+                     stream=None):
+    _check(load().pyr_cache8_attention(ctypes.byref(cache), _ptr(q), _ptr(slots), int(n), int(n_tokens), int(n_q_heads), int(max_len), float(softmax_scale),
+                                       _ptr(blocks), int(n_blocks), _ptr(out), _ptr(lse), _ptr(workspace), int(workspace_bytes_), _stream(stream)),
+           "pyr_cache8_attention")
+
+
+def diag_cache8_attention(cache, n, n_tokens, n_q_heads, max_len, n_blocks) -> PyrCacheRoute:
+    """How cache8_attention cuts up a call (host only)."""
+    out = PyrCacheRoute()
+    _check(load().pyr_diag_cache8_attention(ctypes.byref(cache), int(n), int(n_tokens), int(n_q_heads), int(max_len), int(n_blocks), ctypes.byref(out)),
+           "pyr_diag_cache8_attention")
     return out
 
 

@@ -1,0 +1,522 @@
+// New rows into the cache held in 8 bits, turned by their positions on the way (Algorithm 1, the new rows of KV = cat(PvC_past, KV); what
+// Gather(KV, index) keeps of a prompt goes the same way, through its index), tokens of it back to bf16, and pages copied for a fork.
+//
+// A turn by position p takes channels a and b of a pair i to a cos(p f_i) - b sin(p f_i) and b cos(p f_i) + a sin(p f_i).  p f_i is reduced to a
+// quarter of a turn in 64 bits, so that far positions lose nothing; sine and cosine are then Taylor's sums on [-pi/4, pi/4], below 2^-24 off.  A
+// workgroup takes 32 tokens and some heads: the pairs are worked out once, meet in LDS and turn K and Q of all its heads.
+// A wavefront owns one block (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte.
+// Bound: reading and writing HBM.
+#include "cache8_device.h"
+
+namespace pyr {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr uint32_t kAllTokens = 0xffffffffu;
+
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float x) { return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), kCtrl, 0xf, 0xf, false)); }
+
+// op over the lanes whose number differs from a lane's in bits of `mask` alone (mask: bits from the lowest of D / 8 lanes on, or from 1 on)
+template <int kFrom, class Op>
+__device__ __forceinline__ float across(float x, Op op) {
+    if (kFrom <= 1) x = op(x, dpp<0xb1>(x));
+    if (kFrom <= 2) x = op(x, dpp<0x4e>(x));
+    if (kFrom <= 4) x = op(x, dpp<0x124>(x));       // (what the lane four further holds, inside 16 lanes; then eight)
+    if (kFrom <= 8) x = op(x, dpp<0x128>(x));
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
+
+typedef __attribute__((address_space(3))) char* lptr_t;
+typedef __attribute__((ext_vector_type(2))) int i32x2;
+
+// Transposing LDS read (ds_read_b64_tr_b8).  Inside every group of 16 lanes, lane j receives byte (j & 7) of the 8-byte words addressed by lanes
+// (j >> 3), 2 + (j >> 3), 4 + (j >> 3) ... 14 + (j >> 3), in this order.
+__device__ __forceinline__ i32x2 lds_read_tr8(uint32_t lds_addr) {
+    return __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3)))*)(uintptr_t)lds_addr);
+}
+__device__ __forceinline__ void meet() {            // (a wavefront's own part of LDS)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+__device__ __forceinline__ float low_of(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float high_of(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
+
+// cos and sin of position * freq
+__device__ __forceinline__ f32x2 turn_of(int position, float freq) {
+    const double quarters = (double)position * ((double)freq * 0.63661977236758134308);      // of a turn: times 2 / pi
+    const double nearest = __builtin_rint(quarters);
+    const float x = (float)(quarters - nearest) * 1.57079632679489661923f, y = x * x;
+    const float s = x * (1.f + y * (-1.f / 6 + y * (1.f / 120 + y * (-1.f / 5040 + y * (1.f / 362880)))));
+    const float c = 1.f + y * (-0.5f + y * (1.f / 24 + y * (-1.f / 720 + y * (1.f / 40320))));
+    const int quadrant = (int)(nearest - 4.0 * __builtin_floor(nearest * 0.25));
+    const float a = quadrant & 1 ? s : c, b = quadrant & 1 ? c : s;
+    return f32x2{quadrant == 1 || quadrant == 2 ? -a : a, quadrant >= 2 ? -b : b};
+}
+
+// Workgroups count through the head groups first: the heads of a row lie side by side in memory.
+struct AppendArgs {
+    CacheView c;
+    const uint16_t *k, *v, *q;
+    uint16_t* q_out;
+    const int32_t *row_idx, *offsets, *slots, *start, *positions;
+    const float* freqs;
+    int32_t k_stride, v_stride, q_stride;                         // of rows, in 16 bytes
+    int32_t n_rows, n_list, max_new, tiles_of_piece, head_groups, n_q_heads, dims;
+};
+
+enum { kAsIs, kHalves, kPairs };                                  // channel c turns with c + dims / 2, or 2 c with 2 c + 1
+
+template <int D, int kTurn>
+__global__ __launch_bounds__(64 * kWaves) void cache8_append_kernel(AppendArgs a) {
+    constexpr int kLanes = D / 8, kTokens = 64 / kLanes, kLoads = 32 / kTokens;      // lanes of a row, rows of a load, loads of a tile
+    constexpr int kRow = D + 16;                                  // bytes of a token's codes in LDS
+    __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : 32][kTurn == kAsIs ? 1 : D / 2];
+    __shared__ __align__(16) uint8_t all_staged[kWaves][32][kRow];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = lane % kLanes;
+    const int place = blockIdx.x / a.head_groups, b = place / a.tiles_of_piece;
+    const int slot = cache_slot(a.c, a.slots, b);
+    const int start = a.start[b], offset = a.offsets[b];
+    const int64_t wanted = (int64_t)a.offsets[b + 1] - offset;
+    bool again = false;                                           // an earlier row has the slot: its block may be written by two wavefronts at once
+    for (int i = lane; i < b; i += 64) again |= a.slots[i] == slot;
+    if (slot < 0 || start < 0 || wanted <= 0) return;
+    const int64_t end = min((int64_t)start + min(wanted, (int64_t)a.max_new), (int64_t)cache_len(a.c, slot));      // (the table holds anything behind the length)
+    const int64_t token0 = (start & ~31) + 32 * (int64_t)(place - b * a.tiles_of_piece);
+    if (token0 >= end) return;
+    const int block = (int)(token0 >> 5);
+    const int page = a.c.table[(int64_t)slot * a.c.max_pages + (token0 >> a.c.shift)];
+    // lane l: the row that token l & 31 of the block gets; -1: one that is not there, a token of NaN
+    const int64_t token = token0 + (lane & 31);
+    const bool mine = token >= start && token < end;
+    int from = -1;
+    if (mine) {
+        const int64_t row = offset + (token - start);
+        if (row >= 0 && row < a.n_list) from = a.row_idx != nullptr ? a.row_idx[row] : (int)row;
+        if (from < 0 || from >= a.n_rows) from = -1;
+    }
+    if (page < 0 || page >= a.c.n_pages) return;
+    const uint32_t stored = (uint32_t)__builtin_amdgcn_ballot_w64(mine), there = (uint32_t)__builtin_amdgcn_ballot_w64(from >= 0);
+    if (stored == 0 || __builtin_amdgcn_ballot_w64(again) != 0) return;
+    const bool gone = stored != there;
+
+    if constexpr (kTurn != kAsIs) {
+        constexpr int kPairs = D / 2, kAtOnce = 64 / kPairs;
+        const int pair = lane % kPairs;
+        const int position = from >= 0 ? a.positions[from] : 0;
+        const float freq = pair < a.dims / 2 ? a.freqs[pair] : 0.f;
+        for (int t = wave * kAtOnce; t < 32; t += kWaves * kAtOnce) {
+            if ((stored >> t & ((1u << kAtOnce) - 1)) == 0) continue;
+            const int mine_t = t + lane / kPairs;
+            const f32x2 turn = turn_of(__shfl(position, mine_t), freq);
+            if (pair < a.dims / 2) turns[mine_t][pair] = turn;
+        }
+        __syncthreads();
+    }
+    // the token whose row a lane reads in load i: a token that is not stored reads the first one's (what it computes changes no largest and no
+    // smallest, and is not written)
+    const int first = __builtin_ctz(stored);
+    auto token_of = [&](int i) { return i * kTokens + lane / kLanes; };
+    auto source_of = [&](int i) { return stored >> token_of(i) & 1 ? token_of(i) : first; };
+    auto some = [&](int i) { return (stored >> (i * kTokens) & ((1u << kTokens) - 1)) != 0; };      // (of a load's tokens: one token is one load)
+
+    // eight channels of a row, turned
+    auto turned = [&](u32x4 words, int t, float (&x)[8]) {
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = low_of(words[i]);
+            x[2 * i + 1] = high_of(words[i]);
+        }
+        if constexpr (kTurn == kHalves) {
+            const int half = a.dims / 16;                         // (lanes)
+            const int with = piece < half ? half : piece < 2 * half ? -half : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t other = (uint32_t)__shfl((int)words[i], lane + with);
+                y[2 * i] = low_of(other);
+                y[2 * i + 1] = high_of(other);
+            }
+            if (with != 0) {
+                const f32x2* turn = &turns[t][8 * (piece < half ? piece : piece - half)];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i], turn[i][0], (with > 0 ? -y[i] : y[i]) * turn[i][1]);
+            }
+        } else if constexpr (kTurn == kPairs) {
+            if (piece < a.dims / 8) {
+                const f32x2* turn = &turns[t][4 * piece];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = x[2 * i], r = x[2 * i + 1];
+                    x[2 * i] = __builtin_fmaf(p, turn[i][0], -(r * turn[i][1]));
+                    x[2 * i + 1] = __builtin_fmaf(r, turn[i][0], p * turn[i][1]);
+                }
+            }
+        }
+    };
+
+    const Page8<D> at(a.c, page);
+    uint8_t(*const staged)[kRow] = all_staged[wave];
+    const int heads = a.c.n_kv_heads + a.n_q_heads, step = a.head_groups * kWaves;
+    const bool behind = token0 < start;                           // there are older tokens in the block, whose powers and bounds count
+    for (int head = (blockIdx.x - place * a.head_groups) * kWaves + wave; head < heads; head += step) {
+        if (head >= a.c.n_kv_heads) {                             // a head of Q: rows turned, where there are rows
+            const int h = head - a.c.n_kv_heads;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                if (!some(i)) continue;
+                const int t = token_of(i), row = __shfl(from, t);
+                const u32x4 words = __builtin_nontemporal_load((const u32x4*)a.q + (int64_t)max(row, 0) * a.q_stride + h * kLanes + piece);
+                float x[8];
+                turned(words, t, x);
+                bf16x8 y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = (__bf16)x[e];
+                if (row >= 0) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, y), (u32x4*)a.q_out + ((int64_t)row * a.n_q_heads + h) * kLanes + piece);
+            }
+            continue;
+        }
+        u32x4 kx[kLoads], vx[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if (!some(i)) continue;
+            const int64_t row = max(__shfl(from, source_of(i)), 0);
+            kx[i] = __builtin_nontemporal_load((const u32x4*)a.k + row * a.k_stride + head * kLanes + piece);
+            vx[i] = __builtin_nontemporal_load((const u32x4*)a.v + row * a.v_stride + head * kLanes + piece);
+        }
+        uint8_t* const codes = at.codes(head, block);
+        uint16_t* const powers = at.powers(head, block);
+        u32x2* const bounds = (u32x2*)at.bounds(head, block) + piece;      // largest; kLanes further the smallest
+        const uint32_t old_powers = behind ? *powers : 0;
+        const u32x2 old_up = behind ? bounds[0] : u32x2{}, old_down = behind ? bounds[kLanes] : u32x2{};
+
+        // K turned; the largest magnitudes (as bits: what is no number is above all others)
+        float x[kLoads][8];
+        uint32_t ktop = 0, vtop = 0;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if (!some(i)) continue;
+            turned(kx[i], source_of(i), x[i]);
+            if (gone && (there >> source_of(i) & 1) == 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[i][e] = NAN;
+                vx[i] = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ktop = max(ktop, __float_as_uint(x[i][e]) & 0x7fffffffu);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vtop = max(vtop, max(vx[i][e] << 16 & 0x7fff0000u, vx[i][e] & 0x7fff0000u));
+        }
+        constexpr uint32_t kNoNumber = 0x7f680000u;               // 464 * 2^119: what lies above has no code
+        bool special = __builtin_amdgcn_ballot_w64(ktop > kNoNumber || vtop > kNoNumber) != 0;
+        if (special) {
+            ktop = vtop = 0;
+            auto count = [](uint32_t& top, float y) {
+                const uint32_t bits = __float_as_uint(y) & 0x7fffffffu;
+                if (bits < 0x7f800000u) top = max(top, bits);
+            };
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                if (!some(i)) continue;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    count(ktop, x[i][e]);
+                    count(vtop, e & 1 ? high_of(vx[i][e >> 1]) : low_of(vx[i][e >> 1]));
+                }
+            }
+        }
+        int kp = power8_of(across<1>(__uint_as_float(ktop), larger)), vp = power8_of(across<1>(__uint_as_float(vtop), larger));
+        int kgrow = 0, vgrow = 0;
+        if (behind) {
+            const int old_kp = old_powers & 255, old_vp = old_powers >> 8;
+            kp = max(kp, old_kp);
+            vp = max(vp, old_vp);
+            kgrow = min(kp - old_kp, 100);
+            vgrow = min(vp - old_vp, 100);
+        }
+        const float kscale = scale_of(kp), vscale = scale_of(vp);
+
+        // bounds
+        {
+            float up[8], down[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                up[e] = -INFINITY;
+                down[e] = INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                if (!some(i)) continue;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    up[e] = fmaxf(up[e], x[i][e]);
+                    down[e] = fminf(down[e], x[i][e]);
+                }
+            }
+            bool none[8];                                         // a number of the channel has no code
+#pragma unroll
+            for (int e = 0; e < 8; ++e) none[e] = false;
+            if (special) {
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    if (!some(i)) continue;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) none[e] |= !(fabsf(x[i][e]) <= __uint_as_float(kNoNumber));
+                }
+            }
+            u32x2 out_up = {}, out_down = {};
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                float y[4];                                       // largest, smallest of two channels
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    y[2 * f] = across<kLanes>(up[e + f], larger);
+                    y[2 * f + 1] = across<kLanes>(down[e + f], smaller);
+                }
+                const uint32_t c = codes8_of(y[0], y[1], y[2], y[3], kscale);
+                const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, false), r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, true);
+                const float z[4] = {p[0], p[1], r[0], r[1]};
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    const int n = e + f;
+                    float largest = __builtin_ceilf(z[2 * f] * 0.25f), smallest = __builtin_floorf(z[2 * f + 1] * 0.25f);
+                    if (special && __builtin_amdgcn_ballot_w64(none[n]) != 0) {
+                        const float flag = across<kLanes>(none[n] ? 1.f : 0.f, larger);
+                        if (flag != 0.f) largest = 127.f, smallest = -127.f;
+                    }
+                    if (behind) {
+                        const float f1 = __uint_as_float((uint32_t)(127 - kgrow) << 23);
+                        const int o = (int8_t)(old_up[n >> 2] >> (8 * (n & 3))), u = (int8_t)(old_down[n >> 2] >> (8 * (n & 3)));
+                        largest = fmaxf(largest, __builtin_ceilf((float)o * f1));
+                        smallest = fminf(smallest, __builtin_floorf((float)u * f1));
+                    }
+                    out_up[n >> 2] |= ((uint32_t)(int)largest & 255) << (8 * (n & 3));
+                    out_down[n >> 2] |= ((uint32_t)(int)smallest & 255) << (8 * (n & 3));
+                }
+            }
+            if (lane < kLanes) {
+                bounds[0] = out_up;
+                bounds[kLanes] = out_down;
+            }
+            if (lane == 0) *powers = (uint16_t)(kp | vp << 8);
+        }
+
+        // older numbers to the larger power
+        u32x4* const vcodes = (u32x4*)(codes + 32 * D) + lane;
+        const bool grows = kgrow > 0 || vgrow > 0;
+        if (grows) {
+            const float kby = __uint_as_float((uint32_t)(127 + kgrow) << 23), vby = __uint_as_float((uint32_t)(127 + vgrow) << 23);
+            u32x4* const kcodes = (u32x4*)codes + lane;
+#pragma unroll 1
+            for (int g = 0; g < D / 32; ++g) {
+                u32x4 y = kcodes[64 * g], z = vcodes[64 * g];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    y[i] = regrown(y[i], kby);
+                    z[i] = regrown(z[i], vby);
+                }
+                kcodes[64 * g] = y;
+                vcodes[64 * g] = z;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");      // (the bytes are read and written again below, by other lanes)
+            __builtin_amdgcn_s_waitcnt(0);
+        }
+
+        // K: eight channels of a token a lane.  V: in LDS as rows, from where transposing reads give eight tokens of a channel; a few tokens byte by byte
+        const bool few = __builtin_popcount(stored) <= 4;
+        const uint32_t kplace = ((piece >> 3) * 4 + (piece >> 1 & 3)) * 256 + (piece & 1) * 8;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if (!some(i)) continue;
+            const int t = token_of(i);
+            const u32x2 k8 = {codes8_of(x[i][0], x[i][1], x[i][2], x[i][3], kscale), codes8_of(x[i][4], x[i][5], x[i][6], x[i][7], kscale)};
+            i16x2 lo = {0, 0}, hi = {0, 0};
+            lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, (uint32_t)vx[i][0]), vscale, false);
+            lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, (uint32_t)vx[i][1]), vscale, true);
+            hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, (uint32_t)vx[i][2]), vscale, false);
+            hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, (uint32_t)vx[i][3]), vscale, true);
+            const u32x2 v8 = {__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+            const bool write = stored >> t & 1;
+            if (write) *(u32x2*)(codes + (t >> 4) * (16 * D) + kplace + (t & 15) * 16) = k8;
+            if (few) {
+                uint8_t* to = codes + 32 * D + ((piece >> 2) * 4 + (t >> 2 & 3)) * 256 + (piece & 1) * 128 + (piece >> 1 & 1) * 8 + (t >> 4) * 4 + (t & 3);
+                if (write) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) to[16 * e] = (uint8_t)(v8[e >> 2] >> (8 * (e & 3)));
+                }
+            } else {
+                *(u32x2*)&staged[t][8 * piece] = v8;
+            }
+        }
+        if (few) continue;
+        meet();
+        const int r = lane & 15, j = lane >> 4, e = r >> 1;
+        // the bytes of a word that stay as they are: tokens 16 h + 4 j + i, i = 0 .. 3
+        uint32_t keep[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((stored >> (16 * (i >> 2) + 4 * j + (i & 3)) & 1) == 0) keep[i >> 2] |= 0xffu << (8 * (i & 3));
+        const uint32_t rows = (uint32_t)(uintptr_t)(lptr_t)&staged[16 * (e >> 2) + 4 * j + (e & 3)][8 * (r & 1)];
+#pragma unroll
+        for (int g = 0; g < D / 32; ++g) {
+            const i32x2 p = lds_read_tr8(rows + 32 * g), s = lds_read_tr8(rows + 32 * g + 16);
+            u32x4 word = {(uint32_t)p[0], (uint32_t)p[1], (uint32_t)s[0], (uint32_t)s[1]};
+            if (stored != kAllTokens) {
+                const u32x4 old = vcodes[64 * g];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) word[i] = (word[i] & ~keep[i & 1]) | (old[i] & keep[i & 1]);
+            }
+            vcodes[64 * g] = word;
+        }
+        meet();                                                   // (the next head's rows go to the same place)
+    }
+}
+
+struct LoadArgs {
+    CacheView c;
+    const int32_t *slots, *first, *offsets;
+    uint16_t *k, *v;
+    int32_t n_rows, max_len, tiles_of_seq, head_groups;
+};
+static_assert(sizeof(LoadArgs) <= 112, "short arguments");
+
+// A block's codes meet in LDS as rows, V's through transposing reads, from where a wavefront writes whole rows of the head, 16 bytes a lane.
+template <int D>
+__global__ __launch_bounds__(64 * kWaves) void cache8_load_kernel(LoadArgs a) {
+    constexpr int kGroups = D / 32, kRow = D + 16;
+    __shared__ __align__(16) uint8_t all_rows[kWaves][32][kRow];
+    __shared__ __align__(16) uint8_t all_words[kWaves][kGroups][64][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t = lane & 15, j = lane >> 4;
+    const int place = blockIdx.x / a.head_groups, b = place / a.tiles_of_seq;
+    const int head = (blockIdx.x - place * a.head_groups) * kWaves + wave;
+    const int slot = cache_slot(a.c, a.slots, b);
+    const int offset = a.offsets[b], end_row = min(a.offsets[b + 1], a.n_rows), begin = a.first != nullptr ? a.first[b] : 0;
+    if (slot < 0 || offset < 0 || end_row <= offset || begin < 0 || head >= a.c.n_kv_heads) return;
+    const int64_t token0 = (begin & ~31) + 32 * (int64_t)(place - b * a.tiles_of_seq);
+    const int64_t end = min((int64_t)begin + min(end_row - offset, a.max_len), (int64_t)cache_len(a.c, slot));      // tokens begin .. end - 1
+    if (token0 >= end) return;
+    const int block = (int)(token0 >> 5);
+    const int page = a.c.table[(int64_t)slot * a.c.max_pages + (token0 >> a.c.shift)];
+    if (page < 0 || page >= a.c.n_pages) return;
+    const Page8<D> at(a.c, page);
+    const u32x4* in = (const u32x4*)at.codes(head, block) + lane;
+    uint8_t(*const rows)[kRow] = all_rows[wave];
+    uint8_t(*const words)[64][16] = all_words[wave];
+    u32x4 kc[kGroups], vc[kGroups];
+    const uint32_t powers = *at.powers(head, block);
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) kc[g] = in[64 * g];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) vc[g] = in[64 * (kGroups + g)];
+    const int64_t row_words = (int64_t)a.c.n_kv_heads * D;
+    auto write_rows = [&](uint16_t* out, float scale) {
+        constexpr int kLanes = D / 8;
+        meet();
+#pragma unroll
+        for (int i = 0; i < 32 * kLanes / 64; ++i) {
+            const int token = i * (64 / kLanes) + lane / kLanes, channel = 8 * (lane % kLanes);
+            const u32x2 x = *(const u32x2*)&rows[token][channel];
+            const int64_t row = offset + (token0 + token - begin);
+            if (token0 + token >= begin && token0 + token < end)
+                __builtin_nontemporal_store(__builtin_bit_cast(u32x4, values8_of(x[0], x[1], scale)), (u32x4*)(out + row * row_words + head * D + channel));
+        }
+        meet();
+    };
+    if (a.k != nullptr) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) *(u32x4*)&rows[16 * (g / (D / 64)) + t][64 * (g % (D / 64)) + 16 * j] = kc[g];
+        write_rows(a.k, scale_of(powers & 255));
+    }
+    if (a.v != nullptr) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) *(u32x4*)words[g][lane] = vc[g];
+        meet();
+        // a lane's word of a transposing read: channel r = t / 2 of eight, of both halves of 16 in turn; what it gets: those of token e of the group's eight
+        const uint32_t from = (uint32_t)(uintptr_t)(lptr_t)&words[0][16 * j + (t >> 1) + 8 * (t & 1)][0];
+        const int e = t & 7, token = 16 * (e >> 2) + 4 * j + (e & 3);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+                *(i32x2*)&rows[token][32 * g + 16 * p + 8 * (t >> 3)] = lds_read_tr8(from + 1024 * g + 8 * p);
+        }
+        write_rows(a.v, scale_of(powers >> 8));
+    }
+}
+
+// The page of a parent that is filled in part, as it is.  grid: (n, pieces of a page)
+__global__ __launch_bounds__(256) void cache8_fork_copy_kernel(CacheView c, const int32_t* __restrict__ parents, const int32_t* __restrict__ children,
+                                                               const int32_t* __restrict__ status, uint32_t page_chunks) {
+    const int state = *status, parent = parents[blockIdx.x], child = children[blockIdx.x];
+    if (state != 0 || parent < 0) return;
+    const int len = cache_len(c, parent), full = len >> c.shift;
+    if ((len & ((1 << c.shift) - 1)) == 0) return;
+    const int src = c.table[(int64_t)parent * c.max_pages + full], dst = c.table[(int64_t)child * c.max_pages + full];
+    if (src < 0 || src >= c.n_pages || dst < 0 || dst >= c.n_pages) return;
+    const u32x4* from = (const u32x4*)c.pages + (int64_t)src * page_chunks;
+    u32x4* to = (u32x4*)c.pages + (int64_t)dst * page_chunks;
+    constexpr int kMany = 4;
+    const uint32_t first = blockIdx.y * (256 * kMany) + threadIdx.x;
+    u32x4 x[kMany];
+#pragma unroll
+    for (int k = 0; k < kMany; ++k)
+        if (first + 256 * k < page_chunks) x[k] = from[first + 256 * k];
+#pragma unroll
+    for (int k = 0; k < kMany; ++k)
+        if (first + 256 * k < page_chunks) to[first + 256 * k] = x[k];
+}
+
+int groups_of(int heads, int most) { return heads < kWaves * most ? (heads + kWaves - 1) / kWaves : most; }
+
+}  // namespace
+
+int launch_cache8_append(const CacheView& c, int32_t head_dim, const Cache8Rows& rows, const int32_t* offsets, const int32_t* slots, const int32_t* start,
+                         int32_t n_seqs, int32_t max_new, hipStream_t stream) {
+    const int64_t tiles = ((int64_t)max_new + 30) / 32 + 1;
+    const int heads = c.n_kv_heads + rows.n_q_heads;
+    // workgroups of all heads share one reckoning of the turns, but few tokens need all the workgroups they can get
+    int64_t groups = 2048 / (n_seqs * tiles);
+    groups = groups_of(heads, (int)(groups < 1 ? 1 : groups > 8192 ? 8192 : groups));
+    const AppendArgs a{c, (const uint16_t*)rows.k, (const uint16_t*)rows.v, (const uint16_t*)rows.q, (uint16_t*)rows.q_out, rows.row_idx, offsets, slots, start,
+                       rows.positions, rows.freqs, rows.k_stride, rows.v_stride, rows.q_stride, rows.n_rows, rows.n_list, max_new, (int32_t)tiles, (int32_t)groups,
+                       rows.n_q_heads, rows.dims};
+    const dim3 blocks((unsigned)(n_seqs * tiles * groups)), threads(64 * kWaves);
+    const int turn = rows.dims == 0 ? kAsIs : rows.interleaved ? kPairs : kHalves;
+    if (head_dim == 128) {
+        if (turn == kAsIs) hipLaunchKernelGGL((cache8_append_kernel<128, kAsIs>), blocks, threads, 0, stream, a);
+        else if (turn == kHalves) hipLaunchKernelGGL((cache8_append_kernel<128, kHalves>), blocks, threads, 0, stream, a);
+        else hipLaunchKernelGGL((cache8_append_kernel<128, kPairs>), blocks, threads, 0, stream, a);
+    } else {
+        if (turn == kAsIs) hipLaunchKernelGGL((cache8_append_kernel<64, kAsIs>), blocks, threads, 0, stream, a);
+        else if (turn == kHalves) hipLaunchKernelGGL((cache8_append_kernel<64, kHalves>), blocks, threads, 0, stream, a);
+        else hipLaunchKernelGGL((cache8_append_kernel<64, kPairs>), blocks, threads, 0, stream, a);
+    }
+    return check_launch();
+}
+
+int launch_cache8_load(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* first, const int32_t* offsets, int32_t n_seqs,
+                       int32_t max_len, void* k, void* v, int32_t n_rows, hipStream_t stream) {
+    const int64_t tiles = ((int64_t)max_len + (first != nullptr ? 62 : 31)) / 32;
+    const int groups = (c.n_kv_heads + kWaves - 1) / kWaves;
+    const LoadArgs a{c, slots, first, offsets, (uint16_t*)k, (uint16_t*)v, n_rows, max_len, (int32_t)tiles, groups};
+    const dim3 blocks((unsigned)(n_seqs * tiles * groups)), threads(64 * kWaves);
+    if (head_dim == 128) hipLaunchKernelGGL((cache8_load_kernel<128>), blocks, threads, 0, stream, a);
+    else hipLaunchKernelGGL((cache8_load_kernel<64>), blocks, threads, 0, stream, a);
+    return check_launch();
+}
+
+int launch_cache8_fork_copy(const CacheView& c, int32_t head_dim, const int32_t* parents, const int32_t* children, int32_t n, const int32_t* status,
+                            hipStream_t stream) {
+    if (n == 0) return PYR_OK;
+    const uint32_t chunks = (uint32_t)(cache8_page_bytes(head_dim, c.n_kv_heads, 1 << (c.shift - 5)) / 16);
+    hipLaunchKernelGGL(cache8_fork_copy_kernel, dim3((unsigned)n, (chunks + 1023) / 1024), dim3(256), 0, stream, c, parents, children, status, chunks);
+    return check_launch();
+}
+
+}  // namespace pyr

@@ -91,7 +91,7 @@ int pyr_cache_fork(const pyr_cache* cache, const int32_t* parents, const int32_t
     if (rc == PYR_OK) rc = check_rows(cache, n);
     if (rc != PYR_OK) return rc;
     if (!status || (n > 0 && (!parents || !children))) return PYR_ERR_NULL;
-    return pyr::launch_cache_fork(view(cache), cache->head_dim, parents, children, n, status, (hipStream_t)stream);
+    return pyr::launch_cache_fork(view(cache), 34 * cache->head_dim, parents, children, n, status, (hipStream_t)stream);
 }
 
 int pyr_cache_release(const pyr_cache* cache, const int32_t* slots, int32_t n, void* stream) {

@@ -363,7 +363,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(JoinArgs a) {
     }
     const int slot = cache_slot(a.c, a.slots, row / a.rows_of_seq);
     const int tiles = slot < 0 ? 0 : (cache_len(a.c, slot) + 31) >> 5;
-    const int live = min(a.splits, max(1, (tiles + a.chunk - 1) / a.chunk));
+    const int live = a.chunk == 0 ? a.splits : min(a.splits, max(1, (tiles + a.chunk - 1) / a.chunk));      // (0: all parts are there)
     float top = -FLT_MAX;
 #pragma unroll
     for (int x = 0; x < kAhead; ++x)
@@ -424,16 +424,18 @@ int launch(const CacheAttention& x, const CacheView& c, const AttendArgs& a, voi
     }
     const int rc = check_launch();
     if (rc != PYR_OK || a.splits == 1) return rc;
-    const int32_t rows_of_seq = a.n_tokens * a.n_q_heads, rows = a.n_seqs * rows_of_seq;
-    const JoinArgs j{c, a.slots, (const float*)a.out, (const f32x4*)a.lse, (uint16_t*)out, lse, rows, rows_of_seq, a.chunk, a.splits};
+    return launch_cache_join(c, D, a.slots, (const float*)a.out, a.lse, a.n_seqs, a.n_tokens * a.n_q_heads, a.chunk, a.splits, out, lse, stream);
+}
+
+template <int D>
+void launch_join(const JoinArgs& j, hipStream_t stream) {
     constexpr int kFew = 2, kMany = 1024 / D;
-    if (a.splits <= 2 * kFew) {
+    if (j.splits <= 2 * kFew) {
         constexpr int kRows = 256 / (D / 4 * kFew);
-        hipLaunchKernelGGL((cache_join_kernel<D, kFew>), dim3((unsigned)((rows + kRows - 1) / kRows)), dim3(256), 0, stream, j);
+        hipLaunchKernelGGL((cache_join_kernel<D, kFew>), dim3((unsigned)((j.rows + kRows - 1) / kRows)), dim3(256), 0, stream, j);
     } else {
-        hipLaunchKernelGGL((cache_join_kernel<D, kMany>), dim3((unsigned)rows), dim3(256), 0, stream, j);
+        hipLaunchKernelGGL((cache_join_kernel<D, kMany>), dim3((unsigned)j.rows), dim3(256), 0, stream, j);
     }
-    return check_launch();
 }
 
 }  // namespace
@@ -482,6 +484,14 @@ CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_
     x.part_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * head_dim * sizeof(float);
     x.stat_bytes = x.splits == 1 ? 0 : (size_t)x.splits * rows * 4 * sizeof(float);
     return x;
+}
+
+int launch_cache_join(const CacheView& c, int32_t head_dim, const int32_t* slots, const float* parts, const float* stats, int32_t n_seqs, int32_t rows_of_seq,
+                      int32_t chunk, int32_t splits, void* out, float* lse, hipStream_t stream) {
+    const JoinArgs j{c, slots, parts, (const f32x4*)stats, (uint16_t*)out, lse, n_seqs * rows_of_seq, rows_of_seq, chunk, splits};
+    if (head_dim == 128) launch_join<128>(j, stream);
+    else launch_join<64>(j, stream);
+    return check_launch();
 }
 
 int launch_cache_attention(const CacheAttention& x, const CacheView& c, int32_t head_dim, const void* q, const int32_t* slots, int32_t n_seqs,

@@ -417,12 +417,14 @@ int launch_cache_reserve(const PoolView& c, const int32_t* slots, const int32_t*
     return check_launch();
 }
 
-int launch_cache_fork(const PoolView& c, int32_t head_dim, const int32_t* parents, const int32_t* children, int32_t n, int32_t* status, hipStream_t stream) {
+int launch_cache_fork(const PoolView& c, int32_t tile_bytes, const int32_t* parents, const int32_t* children, int32_t n, int32_t* status, hipStream_t stream) {
     if (few(c, n)) hipLaunchKernelGGL(cache_fork_kernel<4>, dim3(1), dim3(256), 0, stream, c, parents, children, n, status);
     else hipLaunchKernelGGL(cache_fork_kernel<16>, dim3(1), dim3(1024), 0, stream, c, parents, children, n, status);
     const int rc = check_launch();
     if (rc != PYR_OK || n == 0) return rc;
-    hipLaunchKernelGGL(cache_fork_copy_kernel, dim3(n, c.n_kv_heads), dim3(256), 0, stream, c, parents, children, (const int32_t*)status, 34 * head_dim / 16);
+    // (tile_bytes 0: the first head's workgroup shares the full pages, and the last one is copied by the caller)
+    hipLaunchKernelGGL(cache_fork_copy_kernel, dim3(n, tile_bytes > 0 ? c.n_kv_heads : 1), dim3(256), 0, stream, c, parents, children, (const int32_t*)status,
+                       tile_bytes / 16);
     return check_launch();
 }
 

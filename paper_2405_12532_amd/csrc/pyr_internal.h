@@ -166,18 +166,52 @@ struct CacheAttention {
 CacheAttention plan_cache_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_len);
 int launch_cache_attention(const CacheAttention& plan, const CacheView& c, int32_t head_dim, const void* q, const int32_t* slots, int32_t n_seqs,
                            int32_t n_tokens, int32_t n_q_heads, float scale_log2, void* out, float* lse, void* parts, float* stats, hipStream_t stream);
+// The parts of a split attention added up: parts [splits, rows, head_dim], stats [splits, rows, 4] (reference, sum, sum of the rounded).  chunk: tiles of a part, so
+// that those behind a sequence's end are left out; 0: all parts are there.
+int launch_cache_join(const CacheView& c, int32_t head_dim, const int32_t* slots, const float* parts, const float* stats, int32_t n_seqs, int32_t rows_of_seq,
+                      int32_t chunk, int32_t splits, void* out, float* lse, hipStream_t stream);
 int launch_cache_store(const CacheView& c, int32_t head_dim, const void* k, const void* v, int32_t n_rows, const int32_t* row_idx, int32_t n_list,
                        const int32_t* offsets, const int32_t* slots, const int32_t* start, int32_t n_seqs, int32_t max_new, hipStream_t stream);
 int launch_cache_load(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* offsets, int32_t n_seqs, int32_t max_len,
                       void* k, void* v, int32_t n_rows, hipStream_t stream);
 int launch_cache_reserve(const PoolView& c, const int32_t* slots, const int32_t* n_new, int32_t n, int32_t* start, int32_t* status, hipStream_t stream);
-int launch_cache_fork(const PoolView& c, int32_t head_dim, const int32_t* parents, const int32_t* children, int32_t n, int32_t* status, hipStream_t stream);
+// tile_bytes: of a tile of a page; 0: the rows of the table alone, the pages filled in part are copied by the caller.
+int launch_cache_fork(const PoolView& c, int32_t tile_bytes, const int32_t* parents, const int32_t* children, int32_t n, int32_t* status, hipStream_t stream);
 int launch_cache_release(const PoolView& c, const int32_t* slots, int32_t n, hipStream_t stream);
 // A cut is two launches: the rows of the table, which leaves the old ones in old_rows [n, 1 + max_pages], and the tokens.
 int launch_cache_cut(const PoolView& c, const int32_t* slots, const int32_t* out_offsets, int32_t n, int32_t n_list, int32_t max_keep, int32_t* old_rows,
                      int32_t* status, hipStream_t stream);
 int launch_cache_move(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* kept_idx, int32_t n_list, const int32_t* seq_offsets,
                       const int32_t* out_offsets, const int32_t* old_rows, const int32_t* status, int32_t n_seqs, int32_t max_keep, hipStream_t stream);
+
+// The cache held in 8 bits (cache8_device.h says how it lies in memory; cache8_api.hip checks the arguments).
+// New rows: strides in 16 bytes; q NULL: none; dims 0: nothing turns.
+struct Cache8Rows {
+    const void *k, *v, *q;
+    void* q_out;
+    const int32_t *row_idx, *positions;
+    const float* freqs;
+    int32_t k_stride, v_stride, q_stride, n_rows, n_list, n_q_heads, dims, interleaved;
+};
+int launch_cache8_append(const CacheView& c, int32_t head_dim, const Cache8Rows& rows, const int32_t* offsets, const int32_t* slots, const int32_t* start,
+                         int32_t n_seqs, int32_t max_new, hipStream_t stream);
+int launch_cache8_load(const CacheView& c, int32_t head_dim, const int32_t* slots, const int32_t* first, const int32_t* offsets, int32_t n_seqs,
+                       int32_t max_len, void* k, void* v, int32_t n_rows, hipStream_t stream);
+int launch_cache8_fork_copy(const CacheView& c, int32_t head_dim, const int32_t* parents, const int32_t* children, int32_t n, const int32_t* status,
+                            hipStream_t stream);
+// n_blocks > 0: attention over lists of so many blocks.
+CacheAttention plan_cache8_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_len, int32_t n_blocks);
+int launch_cache8_attention(const CacheAttention& plan, const CacheView& c, int32_t head_dim, const void* q, const int32_t* slots, int32_t n_seqs,
+                            int32_t n_tokens, int32_t n_q_heads, const int32_t* blocks, int32_t n_blocks, float scale_log2, void* out, float* lse, void* parts,
+                            float* stats, hipStream_t stream);
+// How a choice of blocks is cut up: blocks within max_len; chunks of candidates that a launch of its own scores (0: none), and what their keys take.
+struct CacheSelect {
+    int32_t max_blocks, chunk, chunks;
+    size_t key_bytes;
+};
+CacheSelect plan_cache8_select(int32_t n_seqs, int32_t n_tokens, int32_t n_kv_heads, int64_t max_len);
+int launch_cache8_select(const CacheSelect& plan, const CacheView& c, int32_t head_dim, const void* q, const int32_t* slots, int32_t n_seqs, int32_t n_tokens,
+                         int32_t n_q_heads, int32_t n_first, int32_t n_recent, int32_t n_best, int32_t* blocks, void* keys, hipStream_t stream);
 
 // Raise a kernel's dynamic LDS limit to `bytes`, once per device (done_mask: one bit per device id).
 int ensure_dynamic_lds(const void* kernel, int bytes, std::atomic<uint64_t>* done_mask);
