@@ -6,6 +6,8 @@
 // workgroup takes 32 tokens and some heads: the pairs are worked out once, meet in LDS and turn K and Q of all its heads.
 // A wavefront owns one block (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte.
 // Bound: reading and writing HBM.
+#include <type_traits>
+
 #include "cache8_device.h"
 
 namespace pyr {
@@ -73,6 +75,135 @@ struct AppendArgs {
 
 enum { kAsIs, kHalves, kPairs };                                  // channel c turns with c + dims / 2, or 2 c with 2 c + 1
 
+constexpr uint32_t kNoNumber = 0x7f680000u;                       // 464 * 2^119: what lies above has no code
+
+// Eight channels of a row, turned.  turns: of the row's token; lanes of a row are neighbours.
+template <int kTurn>
+__device__ __forceinline__ void turned(u32x4 words, const f32x2* turns, int dims, int piece, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = low_of(words[i]);
+        x[2 * i + 1] = high_of(words[i]);
+    }
+    if constexpr (kTurn == kHalves) {
+        const int half = dims / 16;                               // (lanes)
+        const int with = piece < half ? half : piece < 2 * half ? -half : 0;
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t other = (uint32_t)__shfl((int)words[i], (int)(threadIdx.x & 63) + with);
+            y[2 * i] = low_of(other);
+            y[2 * i + 1] = high_of(other);
+        }
+        if (with != 0) {
+            const f32x2* turn = turns + 8 * (piece < half ? piece : piece - half);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i], turn[i][0], (with > 0 ? -y[i] : y[i]) * turn[i][1]);
+        }
+    } else if constexpr (kTurn == kPairs) {
+        if (piece < dims / 8) {
+            const f32x2* turn = turns + 4 * piece;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = x[2 * i], r = x[2 * i + 1];
+                x[2 * i] = __builtin_fmaf(p, turn[i][0], -(r * turn[i][1]));
+                x[2 * i + 1] = __builtin_fmaf(r, turn[i][0], p * turn[i][1]);
+            }
+        }
+    }
+}
+__device__ __forceinline__ u32x4 rounded(const float (&x)[8]) {
+    bf16x8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (__bf16)x[e];
+    return __builtin_bit_cast(u32x4, y);
+}
+
+// The largest magnitudes, as bits: what is no number is above all others.
+__device__ __forceinline__ void raise(uint32_t& top, const float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+}
+__device__ __forceinline__ void raise(uint32_t& top, u32x4 words) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max(top, max(words[e] << 16 & 0x7fff0000u, words[e] & 0x7fff0000u));
+}
+// The same without what is no number.
+__device__ __forceinline__ void raise_finite(uint32_t& top, float x) {
+    const uint32_t bits = __float_as_uint(x) & 0x7fffffffu;
+    if (bits < 0x7f800000u) top = max(top, bits);
+}
+
+__device__ __forceinline__ u32x2 codes_of(const float (&x)[8], float scale) {
+    return u32x2{codes8_of(x[0], x[1], x[2], x[3], scale), codes8_of(x[4], x[5], x[6], x[7], scale)};
+}
+__device__ __forceinline__ u32x2 codes_of(u32x4 words, float scale) {
+    i16x2 lo = {0, 0}, hi = {0, 0};
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, (uint32_t)words[0]), scale, false);
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, (uint32_t)words[1]), scale, true);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, (uint32_t)words[2]), scale, false);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, (uint32_t)words[3]), scale, true);
+    return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+
+// Bounds of eight channels: of the largest and smallest new numbers, of channels that hold a number without a code, and of what the block held (grown by 2^grow).
+__device__ __forceinline__ void bounds_of(const float (&up)[8], const float (&down)[8], const bool (&none)[8], float scale, bool behind, u32x2 old_up, u32x2 old_down, int grow,
+                                          u32x2& out_up, u32x2& out_down) {
+    const float shrink = __uint_as_float((uint32_t)(127 - grow) << 23);
+    out_up = out_down = u32x2{};
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const uint32_t c = codes8_of(up[e], up[e + 1], down[e], down[e + 1], scale);
+        const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, false), r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, true);
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            const int n = e + f;
+            float largest = none[n] ? 127.f : __builtin_ceilf(p[f] * 0.25f), smallest = none[n] ? -127.f : __builtin_floorf(r[f] * 0.25f);
+            if (behind) {
+                const int o = (int8_t)(old_up[n >> 2] >> (8 * (n & 3))), u = (int8_t)(old_down[n >> 2] >> (8 * (n & 3)));
+                largest = fmaxf(largest, __builtin_ceilf((float)o * shrink));
+                smallest = fminf(smallest, __builtin_floorf((float)u * shrink));
+            }
+            out_up[n >> 2] |= ((uint32_t)(int)largest & 255) << (8 * (n & 3));
+            out_down[n >> 2] |= ((uint32_t)(int)smallest & 255) << (8 * (n & 3));
+        }
+    }
+}
+
+// What a workgroup of an append is about: a block of a sequence, its tokens that are stored (bit t: token t), where the others' count as older ones.
+struct Piece {
+    int block, page, from;        // lane l: the row that token l & 31 of the block gets; -1: one that is not there, a token of NaN
+    uint32_t stored;              // 0: nothing to do
+    bool behind;                  // there are older tokens in the block, whose powers and bounds count
+};
+__device__ __forceinline__ Piece piece_of(const AppendArgs& a, int place) {
+    Piece p{};
+    const int lane = threadIdx.x & 63, b = place / a.tiles_of_piece;
+    const int slot = cache_slot(a.c, a.slots, b);
+    const int start = a.start[b], offset = a.offsets[b];
+    const int64_t wanted = (int64_t)a.offsets[b + 1] - offset;
+    bool again = false;                                           // an earlier row has the slot: its block may be written by two wavefronts at once
+    for (int i = lane; i < b; i += 64) again |= a.slots[i] == slot;
+    if (slot < 0 || start < 0 || wanted <= 0) return p;
+    const int64_t token0 = (start & ~31) + 32 * (int64_t)(place - b * a.tiles_of_piece);
+    p.block = (int)(token0 >> 5);
+    // (asked for together with the length, which may say that it is not there)
+    p.page = a.c.table[(int64_t)slot * a.c.max_pages + min(token0 >> a.c.shift, (int64_t)a.c.max_pages - 1)];
+    const int64_t end = min((int64_t)start + min(wanted, (int64_t)a.max_new), (int64_t)cache_len(a.c, slot));      // (the table holds anything behind the length)
+    p.behind = token0 < start;
+    const int64_t token = token0 + (lane & 31);
+    const bool mine = token >= start && token < end;
+    p.from = -1;
+    if (mine) {
+        const int64_t row = offset + (token - start);
+        if (row >= 0 && row < a.n_list) p.from = a.row_idx != nullptr ? a.row_idx[row] : (int)row;
+        if (p.from < 0 || p.from >= a.n_rows) p.from = -1;
+    }
+    p.stored = (uint32_t)__builtin_amdgcn_ballot_w64(mine);
+    if (p.page < 0 || p.page >= a.c.n_pages || __builtin_amdgcn_ballot_w64(again) != 0) p.stored = 0;
+    return p;
+}
+
 template <int D, int kTurn>
 __global__ __launch_bounds__(64 * kWaves) void cache8_append_kernel(AppendArgs a) {
     constexpr int kLanes = D / 8, kTokens = 64 / kLanes, kLoads = 32 / kTokens;      // lanes of a row, rows of a load, loads of a tile
@@ -80,31 +211,12 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_kernel(AppendArgs a
     __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : 32][kTurn == kAsIs ? 1 : D / 2];
     __shared__ __align__(16) uint8_t all_staged[kWaves][32][kRow];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = lane % kLanes;
-    const int place = blockIdx.x / a.head_groups, b = place / a.tiles_of_piece;
-    const int slot = cache_slot(a.c, a.slots, b);
-    const int start = a.start[b], offset = a.offsets[b];
-    const int64_t wanted = (int64_t)a.offsets[b + 1] - offset;
-    bool again = false;                                           // an earlier row has the slot: its block may be written by two wavefronts at once
-    for (int i = lane; i < b; i += 64) again |= a.slots[i] == slot;
-    if (slot < 0 || start < 0 || wanted <= 0) return;
-    const int64_t end = min((int64_t)start + min(wanted, (int64_t)a.max_new), (int64_t)cache_len(a.c, slot));      // (the table holds anything behind the length)
-    const int64_t token0 = (start & ~31) + 32 * (int64_t)(place - b * a.tiles_of_piece);
-    if (token0 >= end) return;
-    const int block = (int)(token0 >> 5);
-    const int page = a.c.table[(int64_t)slot * a.c.max_pages + (token0 >> a.c.shift)];
-    // lane l: the row that token l & 31 of the block gets; -1: one that is not there, a token of NaN
-    const int64_t token = token0 + (lane & 31);
-    const bool mine = token >= start && token < end;
-    int from = -1;
-    if (mine) {
-        const int64_t row = offset + (token - start);
-        if (row >= 0 && row < a.n_list) from = a.row_idx != nullptr ? a.row_idx[row] : (int)row;
-        if (from < 0 || from >= a.n_rows) from = -1;
-    }
-    if (page < 0 || page >= a.c.n_pages) return;
-    const uint32_t stored = (uint32_t)__builtin_amdgcn_ballot_w64(mine), there = (uint32_t)__builtin_amdgcn_ballot_w64(from >= 0);
-    if (stored == 0 || __builtin_amdgcn_ballot_w64(again) != 0) return;
-    const bool gone = stored != there;
+    const int place = blockIdx.x / a.head_groups;
+    const Piece p = piece_of(a, place);
+    const uint32_t stored = p.stored, there = (uint32_t)__builtin_amdgcn_ballot_w64(p.from >= 0);
+    const int block = p.block, from = p.from;
+    const bool gone = stored != there, behind = p.behind;
+    if (stored == 0) return;
 
     if constexpr (kTurn != kAsIs) {
         constexpr int kPairs = D / 2, kAtOnce = 64 / kPairs;
@@ -126,45 +238,10 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_kernel(AppendArgs a
     auto source_of = [&](int i) { return stored >> token_of(i) & 1 ? token_of(i) : first; };
     auto some = [&](int i) { return (stored >> (i * kTokens) & ((1u << kTokens) - 1)) != 0; };      // (of a load's tokens: one token is one load)
 
-    // eight channels of a row, turned
-    auto turned = [&](u32x4 words, int t, float (&x)[8]) {
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = low_of(words[i]);
-            x[2 * i + 1] = high_of(words[i]);
-        }
-        if constexpr (kTurn == kHalves) {
-            const int half = a.dims / 16;                         // (lanes)
-            const int with = piece < half ? half : piece < 2 * half ? -half : 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t other = (uint32_t)__shfl((int)words[i], lane + with);
-                y[2 * i] = low_of(other);
-                y[2 * i + 1] = high_of(other);
-            }
-            if (with != 0) {
-                const f32x2* turn = &turns[t][8 * (piece < half ? piece : piece - half)];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i], turn[i][0], (with > 0 ? -y[i] : y[i]) * turn[i][1]);
-            }
-        } else if constexpr (kTurn == kPairs) {
-            if (piece < a.dims / 8) {
-                const f32x2* turn = &turns[t][4 * piece];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = x[2 * i], r = x[2 * i + 1];
-                    x[2 * i] = __builtin_fmaf(p, turn[i][0], -(r * turn[i][1]));
-                    x[2 * i + 1] = __builtin_fmaf(r, turn[i][0], p * turn[i][1]);
-                }
-            }
-        }
-    };
-
-    const Page8<D> at(a.c, page);
+    auto turns_of = [&](int t) -> const f32x2* { return kTurn == kAsIs ? nullptr : turns[kTurn == kAsIs ? 0 : t]; };
+    const Page8<D> at(a.c, p.page);
     uint8_t(*const staged)[kRow] = all_staged[wave];
     const int heads = a.c.n_kv_heads + a.n_q_heads, step = a.head_groups * kWaves;
-    const bool behind = token0 < start;                           // there are older tokens in the block, whose powers and bounds count
     for (int head = (blockIdx.x - place * a.head_groups) * kWaves + wave; head < heads; head += step) {
         if (head >= a.c.n_kv_heads) {                             // a head of Q: rows turned, where there are rows
             const int h = head - a.c.n_kv_heads;
@@ -174,11 +251,8 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_kernel(AppendArgs a
                 const int t = token_of(i), row = __shfl(from, t);
                 const u32x4 words = __builtin_nontemporal_load((const u32x4*)a.q + (int64_t)max(row, 0) * a.q_stride + h * kLanes + piece);
                 float x[8];
-                turned(words, t, x);
-                bf16x8 y;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = (__bf16)x[e];
-                if (row >= 0) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, y), (u32x4*)a.q_out + ((int64_t)row * a.n_q_heads + h) * kLanes + piece);
+                turned<kTurn>(words, turns_of(t), a.dims, piece, x);
+                if (row >= 0) __builtin_nontemporal_store(rounded(x), (u32x4*)a.q_out + ((int64_t)row * a.n_q_heads + h) * kLanes + piece);
             }
             continue;
         }
@@ -196,38 +270,31 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_kernel(AppendArgs a
         const uint32_t old_powers = behind ? *powers : 0;
         const u32x2 old_up = behind ? bounds[0] : u32x2{}, old_down = behind ? bounds[kLanes] : u32x2{};
 
-        // K turned; the largest magnitudes (as bits: what is no number is above all others)
+        // K turned; the largest magnitudes
         float x[kLoads][8];
         uint32_t ktop = 0, vtop = 0;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             if (!some(i)) continue;
-            turned(kx[i], source_of(i), x[i]);
+            turned<kTurn>(kx[i], turns_of(source_of(i)), a.dims, piece, x[i]);
             if (gone && (there >> source_of(i) & 1) == 0) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[i][e] = NAN;
                 vx[i] = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) ktop = max(ktop, __float_as_uint(x[i][e]) & 0x7fffffffu);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) vtop = max(vtop, max(vx[i][e] << 16 & 0x7fff0000u, vx[i][e] & 0x7fff0000u));
+            raise(ktop, x[i]);
+            raise(vtop, vx[i]);
         }
-        constexpr uint32_t kNoNumber = 0x7f680000u;               // 464 * 2^119: what lies above has no code
-        bool special = __builtin_amdgcn_ballot_w64(ktop > kNoNumber || vtop > kNoNumber) != 0;
+        const bool special = __builtin_amdgcn_ballot_w64(ktop > kNoNumber || vtop > kNoNumber) != 0;
         if (special) {
             ktop = vtop = 0;
-            auto count = [](uint32_t& top, float y) {
-                const uint32_t bits = __float_as_uint(y) & 0x7fffffffu;
-                if (bits < 0x7f800000u) top = max(top, bits);
-            };
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 if (!some(i)) continue;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    count(ktop, x[i][e]);
-                    count(vtop, e & 1 ? high_of(vx[i][e >> 1]) : low_of(vx[i][e >> 1]));
+                    raise_finite(ktop, x[i][e]);
+                    raise_finite(vtop, e & 1 ? high_of(vx[i][e >> 1]) : low_of(vx[i][e >> 1]));
                 }
             }
         }
@@ -270,36 +337,14 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_kernel(AppendArgs a
                     for (int e = 0; e < 8; ++e) none[e] |= !(fabsf(x[i][e]) <= __uint_as_float(kNoNumber));
                 }
             }
-            u32x2 out_up = {}, out_down = {};
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                float y[4];                                       // largest, smallest of two channels
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    y[2 * f] = across<kLanes>(up[e + f], larger);
-                    y[2 * f + 1] = across<kLanes>(down[e + f], smaller);
-                }
-                const uint32_t c = codes8_of(y[0], y[1], y[2], y[3], kscale);
-                const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, false), r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, true);
-                const float z[4] = {p[0], p[1], r[0], r[1]};
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    const int n = e + f;
-                    float largest = __builtin_ceilf(z[2 * f] * 0.25f), smallest = __builtin_floorf(z[2 * f + 1] * 0.25f);
-                    if (special && __builtin_amdgcn_ballot_w64(none[n]) != 0) {
-                        const float flag = across<kLanes>(none[n] ? 1.f : 0.f, larger);
-                        if (flag != 0.f) largest = 127.f, smallest = -127.f;
-                    }
-                    if (behind) {
-                        const float f1 = __uint_as_float((uint32_t)(127 - kgrow) << 23);
-                        const int o = (int8_t)(old_up[n >> 2] >> (8 * (n & 3))), u = (int8_t)(old_down[n >> 2] >> (8 * (n & 3)));
-                        largest = fmaxf(largest, __builtin_ceilf((float)o * f1));
-                        smallest = fminf(smallest, __builtin_floorf((float)u * f1));
-                    }
-                    out_up[n >> 2] |= ((uint32_t)(int)largest & 255) << (8 * (n & 3));
-                    out_down[n >> 2] |= ((uint32_t)(int)smallest & 255) << (8 * (n & 3));
-                }
+            for (int e = 0; e < 8; ++e) {
+                up[e] = across<kLanes>(up[e], larger);
+                down[e] = across<kLanes>(down[e], smaller);
+                if (special) none[e] = across<kLanes>(none[e] ? 1.f : 0.f, larger) != 0.f;
             }
+            u32x2 out_up, out_down;
+            bounds_of(up, down, none, kscale, behind, old_up, old_down, kgrow, out_up, out_down);
             if (lane < kLanes) {
                 bounds[0] = out_up;
                 bounds[kLanes] = out_down;
@@ -335,13 +380,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_kernel(AppendArgs a
         for (int i = 0; i < kLoads; ++i) {
             if (!some(i)) continue;
             const int t = token_of(i);
-            const u32x2 k8 = {codes8_of(x[i][0], x[i][1], x[i][2], x[i][3], kscale), codes8_of(x[i][4], x[i][5], x[i][6], x[i][7], kscale)};
-            i16x2 lo = {0, 0}, hi = {0, 0};
-            lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, (uint32_t)vx[i][0]), vscale, false);
-            lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, (uint32_t)vx[i][1]), vscale, true);
-            hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, (uint32_t)vx[i][2]), vscale, false);
-            hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2, (uint32_t)vx[i][3]), vscale, true);
-            const u32x2 v8 = {__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+            const u32x2 k8 = codes_of(x[i], kscale), v8 = codes_of(vx[i], vscale);
             const bool write = stored >> t & 1;
             if (write) *(u32x2*)(codes + (t >> 4) * (16 * D) + kplace + (t & 15) * 16) = k8;
             if (few) {
@@ -375,6 +414,173 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_kernel(AppendArgs a
             vcodes[64 * g] = word;
         }
         meet();                                                   // (the next head's rows go to the same place)
+    }
+}
+
+// op over the kLanes lanes that hold a row, in all of them
+template <int kLanes, class Op>
+__device__ __forceinline__ uint32_t within_row(uint32_t x, Op op) {
+    auto other = [&](auto ctrl) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xf, 0xf, false); };
+    x = op(x, other(std::integral_constant<int, 0xb1>{}));
+    x = op(x, other(std::integral_constant<int, 0x4e>{}));
+    x = op(x, other(std::integral_constant<int, 0x141>{}));      // (eight lanes mirrored, then sixteen)
+    if (kLanes == 16) x = op(x, other(std::integral_constant<int, 0x140>{}));
+    return x;
+}
+
+// The new tokens of a step, kMost of a sequence at most: D / 8 lanes take a head, so that several heads share a wavefront and nothing has to cross from token to token
+// but a power, and byte after byte of V goes to its place.  A wavefront has one group of heads.
+template <int D, int kTurn, int kMost>
+__global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendArgs a) {
+    constexpr int kLanes = D / 8, kHeads = 64 / kLanes;           // lanes of a head, heads of a wavefront
+    __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : kMost][kTurn == kAsIs ? 1 : D / 2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = lane % kLanes;
+    const int place = blockIdx.x / a.head_groups, group = (blockIdx.x - place * a.head_groups) * kWaves + wave;
+    const int kv_groups = (a.c.n_kv_heads + kHeads - 1) / kHeads;
+    const Piece p = piece_of(a, place);
+    if (p.stored == 0) return;
+    const int first = __builtin_ctz(p.stored), count = min(__builtin_popcount(p.stored), kMost);
+    const bool of_q = group >= kv_groups;
+    const int heads = of_q ? a.n_q_heads : a.c.n_kv_heads, wanted_head = (of_q ? group - kv_groups : group) * kHeads + lane / kLanes;
+    const bool real = wanted_head < heads;
+    const int head = min(wanted_head, max(heads - 1, 0));
+    u32x4 kx[kMost], vx[kMost];
+    int rows[kMost];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        rows[i] = __builtin_amdgcn_readlane(p.from, first + min(i, count - 1));
+        const int64_t row = max(rows[i], 0);
+        if (of_q) {
+            if (heads > 0) kx[i] = __builtin_nontemporal_load((const u32x4*)a.q + row * a.q_stride + head * kLanes + piece);
+        } else {
+            kx[i] = __builtin_nontemporal_load((const u32x4*)a.k + row * a.k_stride + head * kLanes + piece);
+            vx[i] = __builtin_nontemporal_load((const u32x4*)a.v + row * a.v_stride + head * kLanes + piece);
+        }
+    }
+    const Page8<D> at(a.c, p.page);
+    uint8_t* const codes = at.codes(head, p.block);
+    uint16_t* const powers = at.powers(head, p.block);
+    u32x2* const bounds = (u32x2*)at.bounds(head, p.block) + piece;
+    uint32_t old_powers = 0;
+    u32x2 old_up = {}, old_down = {};
+    if (p.behind && !of_q) {
+        old_powers = *powers;
+        old_up = bounds[0];
+        old_down = bounds[kLanes];
+    }
+    if constexpr (kTurn != kAsIs) {
+        constexpr int kPairsOf = D / 2;
+        const int pair = lane % kPairsOf;
+        const float freq = pair < a.dims / 2 ? a.freqs[pair] : 0.f;
+        const int position = p.from >= 0 ? a.positions[p.from] : 0;
+        for (int i = wave; i < count; i += kWaves) {
+            const f32x2 turn = turn_of(__builtin_amdgcn_readlane(position, first + i), freq);
+            if (lane < a.dims / 2) turns[i][pair] = turn;
+        }
+        __syncthreads();
+    }
+    if (of_q) {
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            if (i >= count) break;
+            float x[8];
+            turned<kTurn>(kx[i], turns[kTurn == kAsIs ? 0 : i], a.dims, piece, x);
+            if (real && rows[i] >= 0) __builtin_nontemporal_store(rounded(x), (u32x4*)a.q_out + ((int64_t)rows[i] * a.n_q_heads + head) * kLanes + piece);
+        }
+        return;
+    }
+    float x[kMost][8];
+    uint32_t ktop = 0, vtop = 0;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        if (i >= count) break;
+        turned<kTurn>(kx[i], turns[kTurn == kAsIs ? 0 : i], a.dims, piece, x[i]);
+        if (rows[i] < 0) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] = NAN;
+            vx[i] = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+        }
+        raise(ktop, x[i]);
+        raise(vtop, vx[i]);
+    }
+    const bool special = __builtin_amdgcn_ballot_w64(ktop > kNoNumber || vtop > kNoNumber) != 0;
+    if (special) {
+        ktop = vtop = 0;
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            if (i >= count) break;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                raise_finite(ktop, x[i][e]);
+                raise_finite(vtop, e & 1 ? high_of(vx[i][e >> 1]) : low_of(vx[i][e >> 1]));
+            }
+        }
+    }
+    auto larger_bits = [](uint32_t y, uint32_t z) { return max(y, z); };
+    int kp = power8_of(__uint_as_float(within_row<kLanes>(ktop, larger_bits))), vp = power8_of(__uint_as_float(within_row<kLanes>(vtop, larger_bits)));
+    int kgrow = 0, vgrow = 0;
+    if (p.behind) {
+        const int old_kp = old_powers & 255, old_vp = old_powers >> 8;
+        kp = max(kp, old_kp);
+        vp = max(vp, old_vp);
+        kgrow = min(kp - old_kp, 100);
+        vgrow = min(vp - old_vp, 100);
+    }
+    const float kscale = scale_of(kp), vscale = scale_of(vp);
+    {
+        float up[8], down[8];
+        bool none[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            up[e] = -INFINITY;
+            down[e] = INFINITY;
+            none[e] = false;
+#pragma unroll
+            for (int i = 0; i < kMost; ++i) {
+                if (i >= count) break;
+                up[e] = fmaxf(up[e], x[i][e]);
+                down[e] = fminf(down[e], x[i][e]);
+                if (special) none[e] |= !(fabsf(x[i][e]) <= __uint_as_float(kNoNumber));
+            }
+        }
+        u32x2 out_up, out_down;
+        bounds_of(up, down, none, kscale, p.behind, old_up, old_down, kgrow, out_up, out_down);
+        if (real) {
+            bounds[0] = out_up;
+            bounds[kLanes] = out_down;
+            if (piece == 0) *powers = (uint16_t)(kp | vp << 8);
+        }
+    }
+    if (__builtin_amdgcn_ballot_w64(real && (kgrow > 0 || vgrow > 0)) != 0) {
+        const float kby = __uint_as_float((uint32_t)(127 + kgrow) << 23), vby = __uint_as_float((uint32_t)(127 + vgrow) << 23);
+#pragma unroll 1
+        for (int g = 0; g < 16; ++g) {                            // (2 D words of 16 bytes each)
+            u32x4* const kw = (u32x4*)codes + kLanes * g + piece;
+            u32x4* const vw = (u32x4*)(codes + 32 * D) + kLanes * g + piece;
+            u32x4 y = *kw, z = *vw;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[i] = regrown(y[i], kby);
+                z[i] = regrown(z[i], vby);
+            }
+            if (real && kgrow > 0) *kw = y;
+            if (real && vgrow > 0) *vw = z;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");    // (the bytes are written again below, by other lanes)
+        __builtin_amdgcn_s_waitcnt(0);
+    }
+    const uint32_t kplace = ((piece >> 3) * 4 + (piece >> 1 & 3)) * 256 + (piece & 1) * 8;
+    const uint32_t vplace = 32 * D + (piece >> 2) * 1024 + (piece & 1) * 128 + (piece >> 1 & 1) * 8;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        if (i >= count) break;
+        const int t = first + i;
+        const u32x2 k8 = codes_of(x[i], kscale), v8 = codes_of(vx[i], vscale);
+        if (!real) continue;
+        *(u32x2*)(codes + (t >> 4) * (16 * D) + kplace + (t & 15) * 16) = k8;
+        uint8_t* to = codes + vplace + (t >> 2 & 3) * 256 + (t >> 4) * 4 + (t & 3);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[16 * e] = (uint8_t)(v8[e >> 2] >> (8 * (e & 3)));
     }
 }
 
@@ -472,30 +678,42 @@ __global__ __launch_bounds__(256) void cache8_fork_copy_kernel(CacheView c, cons
         if (first + 256 * k < page_chunks) to[first + 256 * k] = x[k];
 }
 
-int groups_of(int heads, int most) { return heads < kWaves * most ? (heads + kWaves - 1) / kWaves : most; }
+template <int D, int kTurn>
+void launch_append(const AppendArgs& a, int64_t pieces, hipStream_t stream) {
+    AppendArgs x = a;
+    constexpr int kHeads = 512 / D;                               // (of a wavefront)
+    const int groups = (a.c.n_kv_heads + kHeads - 1) / kHeads + (a.n_q_heads + kHeads - 1) / kHeads;
+    if (a.max_new <= 8) {
+        x.head_groups = (groups + kWaves - 1) / kWaves;
+        const dim3 blocks((unsigned)(pieces * x.head_groups)), threads(64 * kWaves);
+        if (a.max_new == 1) hipLaunchKernelGGL((cache8_append_few_kernel<D, kTurn, 1>), blocks, threads, 0, stream, x);
+        else hipLaunchKernelGGL((cache8_append_few_kernel<D, kTurn, 8>), blocks, threads, 0, stream, x);
+        return;
+    }
+    // workgroups of many heads share one reckoning of the turns, but few pieces need all the workgroups they can get
+    const int heads = a.c.n_kv_heads + a.n_q_heads;
+    const int64_t most = (heads + kWaves - 1) / kWaves, want = (2048 + pieces - 1) / pieces;
+    x.head_groups = (int32_t)(want < most ? want : most);
+    hipLaunchKernelGGL((cache8_append_kernel<D, kTurn>), dim3((unsigned)(pieces * x.head_groups)), dim3(64 * kWaves), 0, stream, x);
+}
 
 }  // namespace
 
 int launch_cache8_append(const CacheView& c, int32_t head_dim, const Cache8Rows& rows, const int32_t* offsets, const int32_t* slots, const int32_t* start,
                          int32_t n_seqs, int32_t max_new, hipStream_t stream) {
     const int64_t tiles = ((int64_t)max_new + 30) / 32 + 1;
-    const int heads = c.n_kv_heads + rows.n_q_heads;
-    // workgroups of all heads share one reckoning of the turns, but few tokens need all the workgroups they can get
-    int64_t groups = 2048 / (n_seqs * tiles);
-    groups = groups_of(heads, (int)(groups < 1 ? 1 : groups > 8192 ? 8192 : groups));
     const AppendArgs a{c, (const uint16_t*)rows.k, (const uint16_t*)rows.v, (const uint16_t*)rows.q, (uint16_t*)rows.q_out, rows.row_idx, offsets, slots, start,
-                       rows.positions, rows.freqs, rows.k_stride, rows.v_stride, rows.q_stride, rows.n_rows, rows.n_list, max_new, (int32_t)tiles, (int32_t)groups,
+                       rows.positions, rows.freqs, rows.k_stride, rows.v_stride, rows.q_stride, rows.n_rows, rows.n_list, max_new, (int32_t)tiles, 0,
                        rows.n_q_heads, rows.dims};
-    const dim3 blocks((unsigned)(n_seqs * tiles * groups)), threads(64 * kWaves);
     const int turn = rows.dims == 0 ? kAsIs : rows.interleaved ? kPairs : kHalves;
     if (head_dim == 128) {
-        if (turn == kAsIs) hipLaunchKernelGGL((cache8_append_kernel<128, kAsIs>), blocks, threads, 0, stream, a);
-        else if (turn == kHalves) hipLaunchKernelGGL((cache8_append_kernel<128, kHalves>), blocks, threads, 0, stream, a);
-        else hipLaunchKernelGGL((cache8_append_kernel<128, kPairs>), blocks, threads, 0, stream, a);
+        if (turn == kAsIs) launch_append<128, kAsIs>(a, n_seqs * tiles, stream);
+        else if (turn == kHalves) launch_append<128, kHalves>(a, n_seqs * tiles, stream);
+        else launch_append<128, kPairs>(a, n_seqs * tiles, stream);
     } else {
-        if (turn == kAsIs) hipLaunchKernelGGL((cache8_append_kernel<64, kAsIs>), blocks, threads, 0, stream, a);
-        else if (turn == kHalves) hipLaunchKernelGGL((cache8_append_kernel<64, kHalves>), blocks, threads, 0, stream, a);
-        else hipLaunchKernelGGL((cache8_append_kernel<64, kPairs>), blocks, threads, 0, stream, a);
+        if (turn == kAsIs) launch_append<64, kAsIs>(a, n_seqs * tiles, stream);
+        else if (turn == kHalves) launch_append<64, kHalves>(a, n_seqs * tiles, stream);
+        else launch_append<64, kPairs>(a, n_seqs * tiles, stream);
     }
     return check_launch();
 }

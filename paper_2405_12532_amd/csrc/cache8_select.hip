@@ -22,6 +22,13 @@ struct SelectArgs {
     int32_t n_tokens, n_q_heads, max_blocks, n_first, n_recent, n_best, chunk;
 };
 
+__device__ __forceinline__ float max_of_groups(float x) {      // over the lanes with the same lane & 15
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // Scores as numbers that compare like them.
 __device__ __forceinline__ uint32_t key_of(float score) {
     const uint32_t bits = __float_as_uint(score);
@@ -46,36 +53,33 @@ __device__ __forceinline__ Unit unit_of(const SelectArgs& a, int unit) {
     return u;
 }
 
-// The keys of candidates begin .. end - 1, by the wavefronts of a workgroup; put(i, key)
-template <int D, int kWaves, class Put>
-__device__ __forceinline__ void score_blocks(const SelectArgs& a, const Unit& u, int begin, int end, Put put) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, t = lane & 15;
-    const int g = a.n_q_heads / a.c.n_kv_heads, tile_shift = a.c.shift - 5;
-    const int32_t* row_pages = a.c.table + (int64_t)max(u.slot, 0) * a.c.max_pages;
-    const uint16_t* q = a.q + ((int64_t)u.row * a.n_q_heads + u.head * g) * D;
-    constexpr int kHalf = D / 64, kNone = -1000;
-    // 16 query heads at a time (the first 16 stay in registers)
-    i32x4 whole[2 * kHalf];
-    int power[4];                                 // of rows 4 j + x; kNone: no query head
-    auto take = [&](int first) {
-        u32x4 words[kHalf][2];
-        float top = 0.f;
-        const bool mine = first + t < g;
+// 16 query heads of the group as operands of the products, lane 16 j + t: bytes 16 j .. of head t's.
+template <int D>
+struct Queries {
+    static constexpr int kHalf = D / 64, kNone = -1000;
+    u32x4 words[kHalf][2];
+    i32x4 whole[2 * kHalf];                       // max(u, 0), then min(u, 0)
+    int power[4];                                 // of heads 4 j + x; kNone: no query head
+
+    __device__ __forceinline__ void load(const uint16_t* q, int head, int g, int lane) {
 #pragma unroll
         for (int s = 0; s < kHalf; ++s)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                words[s][h] = mine ? *(const u32x4*)(q + (int64_t)(first + t) * D + 64 * s + 16 * j + 8 * h) : u32x4{};
+            for (int h = 0; h < 2; ++h)
+                words[s][h] = head + (lane & 15) < g ? *(const u32x4*)(q + (int64_t)(head + (lane & 15)) * D + 64 * s + 16 * (lane >> 4) + 8 * h) : u32x4{};
+    }
+    __device__ __forceinline__ void round(int head, int g, int lane) {
+        float top = 0.f;
+#pragma unroll
+        for (int s = 0; s < kHalf; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float x = fabsf(__uint_as_float(words[s][h][e] << 16)), y = fabsf(__uint_as_float(words[s][h][e] & 0xffff0000u));
                     top = fmaxf(top, fmaxf(x < INFINITY ? x : 0.f, y < INFINITY ? y : 0.f));
                 }
-            }
-        auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-        top = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
-        p = __builtin_amdgcn_permlane16_swap(__float_as_uint(top), __float_as_uint(top), false, false);
-        top = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+        top = max_of_groups(top);
         const uint32_t bits = __float_as_uint(top);
         const int e = min(max((int)(bits >> 23) - 127 - 6 + ((bits & 0x7fffff) > 0x7e0000 ? 1 : 0), -100), 122);
         const float by = __uint_as_float((uint32_t)(127 - e) << 23);
@@ -97,143 +101,313 @@ __device__ __forceinline__ void score_blocks(const SelectArgs& a, const Unit& u,
                 whole[kHalf + s][w] = (int)down;
             }
 #pragma unroll
-        for (int x = 0; x < 4; ++x) power[x] = __shfl(mine ? e : kNone, 4 * j + x);
-    };
-    if (g <= 16) take(0);
-    // 64 blocks at a time: lane l holds page and power of the l-th
-    for (int base = begin + 64 * wave; base < end; base += 64 * kWaves) {
-        const int block = min(base + lane, end - 1);
-        int page = row_pages[block >> tile_shift];
-        if (page < 0 || page >= a.c.n_pages) page = 0;      // (the attention makes NaN of it)
-        const int block_power = (int)(*Page8<D>(a.c, page).powers(u.head, block) & 255) - 127;
-        i32x4 bounds[4][2 * kHalf];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {                       // (all loads of 64 blocks in flight)
-            const int n = __shfl(block, 16 * s + t), p = __shfl(page, 16 * s + t);
-            const i32x4* from = (const i32x4*)Page8<D>(a.c, p).bounds(u.head, n) + j;
-#pragma unroll
-            for (int i = 0; i < 2 * kHalf; ++i) bounds[s][i] = from[4 * i];
-        }
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int of_block = __shfl(block_power, 16 * s + t);
-            float best = -INFINITY;
-            for (int first = 0; first < g; first += 16) {
-                if (g > 16) take(first);
-                i32x4 d = {0, 0, 0, 0};
-#pragma unroll
-                for (int i = 0; i < 2 * kHalf; ++i) d = __builtin_amdgcn_mfma_i32_16x16x64_i8(whole[i], bounds[s][i], d, 0, 0, 0);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int e = min(max(power[x] + of_block + 2, -120), 100);
-                    const float score = (float)d[x] * __uint_as_float((uint32_t)(127 + e) << 23);
-                    best = fmaxf(best, power[x] == kNone ? -INFINITY : score);
-                }
-            }
-            auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(best), __float_as_uint(best), false, false);
-            best = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
-            p = __builtin_amdgcn_permlane16_swap(__float_as_uint(best), __float_as_uint(best), false, false);
-            best = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
-            const int n = base + 16 * s + t;
-            if (j == 0 && n < end) put(n, key_of(best));
-        }
+        for (int x = 0; x < 4; ++x) power[x] = __shfl(head + (lane & 15) < g ? e : kNone, 4 * (lane >> 4) + x);
     }
+};
+
+// The page of a block (0 where the table names none of the pool: the attention makes NaN of it).
+__device__ __forceinline__ int page_of(const SelectArgs& a, const int32_t* row_pages, int block) {
+    const int page = row_pages[block >> (a.c.shift - 5)];
+    return page < 0 || page >= a.c.n_pages ? 0 : page;
 }
 
-// grid: (units, chunks of candidates)
+// The keys of 64 blocks, lane l: that of block base + l (of end - 1 from there on); page: of its block.
+template <int D>
+__device__ __forceinline__ uint32_t keys_of(const SelectArgs& a, const Unit& u, Queries<D>& w, const uint16_t* q, int g, int base, int end, int page) {
+    constexpr int kHalf = D / 64;
+    const int lane = threadIdx.x & 63, j = lane >> 4, t = lane & 15;
+    const int block = min(base + lane, end - 1);
+    i32x4 bounds[4][2 * kHalf];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {                           // (all loads in flight)
+        const int n = __shfl(block, 16 * s + t), p = __shfl(page, 16 * s + t);
+        const i32x4* from = (const i32x4*)Page8<D>(a.c, p).bounds(u.head, n) + j;
+#pragma unroll
+        for (int i = 0; i < 2 * kHalf; ++i) bounds[s][i] = from[4 * i];
+    }
+    const int block_power = (int)(*Page8<D>(a.c, page).powers(u.head, block) & 255) - 127;
+    uint32_t key = 0;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const int of_block = __shfl(block_power, 16 * s + t);
+        float best = -INFINITY;
+        for (int first = 0; first < g; first += 16) {
+            if (g > 16) {
+                w.load(q, first, g, lane);
+                w.round(first, g, lane);
+            }
+            i32x4 d = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 2 * kHalf; ++i) d = __builtin_amdgcn_mfma_i32_16x16x64_i8(w.whole[i], bounds[s][i], d, 0, 0, 0);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int e = min(max(w.power[x] + of_block + 2, -120), 100);
+                const float score = (float)d[x] * __uint_as_float((uint32_t)(127 + e) << 23);
+                best = fmaxf(best, w.power[x] == Queries<D>::kNone ? -INFINITY : score);
+            }
+        }
+        best = max_of_groups(best);
+        if (j == s) key = key_of(best);
+    }
+    return key;
+}
+
+// grid: (units, chunks of candidates): keys to memory
 template <int D>
 __global__ __launch_bounds__(256) void cache8_score_kernel(SelectArgs a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = a.n_q_heads / a.c.n_kv_heads;
     const Unit u = unit_of(a, blockIdx.x);
     if (u.high - u.low <= a.n_best) return;
-    const int begin = u.low + (int)blockIdx.y * a.chunk, end = min(u.high, begin + a.chunk);
+    const int begin = u.low + (int)blockIdx.y * a.chunk + 64 * wave, end = min(u.high, u.low + ((int)blockIdx.y + 1) * a.chunk);
     if (begin >= end) return;
+    const int32_t* row_pages = a.c.table + (int64_t)u.slot * a.c.max_pages;
+    const uint16_t* q = a.q + ((int64_t)u.row * a.n_q_heads + u.head * g) * D;
     uint32_t* keys = a.keys + (int64_t)blockIdx.x * a.max_blocks;
-    score_blocks<D, 4>(a, u, begin, end, [&](int n, uint32_t key) { keys[n] = key; });
+    Queries<D> w;
+    int page = page_of(a, row_pages, min(begin + lane, end - 1));
+    w.load(q, 0, g, lane);
+    w.round(0, g, lane);
+    for (int base = begin; base < end; base += 256) {
+        const uint32_t key = keys_of<D>(a, u, w, q, g, base, end, page);
+        if (base + 256 < end) page = page_of(a, row_pages, min(base + 256 + lane, end - 1));
+        if (base + lane < end) keys[base + lane] = key;
+    }
 }
 
-// One workgroup a unit.  kKeys: keys in LDS, worked out here; 0: they are in memory.
-// The n-th largest key is found byte by byte, from counts of the bytes among the keys that share the higher ones; of those equal to it the
-// first are taken.
-template <int D, int kKeys>
-__global__ __launch_bounds__(256) void cache8_select_kernel(SelectArgs a) {
-    constexpr int kWaves = 4, kThreads = 64 * kWaves;
-    __shared__ uint32_t held[kKeys == 0 ? 1 : kKeys];
-    __shared__ int counts[256], sums[kWaves], found[2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Unit u = unit_of(a, blockIdx.x);
-    const int width = a.n_first + a.n_recent + a.n_best, candidates = u.high - u.low;
-    int32_t* out = a.blocks + (int64_t)blockIdx.x * width;
-    const int chosen = min(candidates, a.n_best), tail = max(u.low, u.count - a.n_recent), all = u.low + chosen + (u.count - tail);
-    for (int i = threadIdx.x; i < u.low; i += kThreads) out[i] = i;
-    for (int i = threadIdx.x; i < u.count - tail; i += kThreads) out[u.low + chosen + i] = tail + i;
-    for (int i = all + threadIdx.x; i < width; i += kThreads) out[i] = -1;
-    if (candidates <= a.n_best) {
-        for (int i = threadIdx.x; i < candidates; i += kThreads) out[u.low + i] = u.low + i;
-        return;
+// What every list has: the first blocks, the last ones, -1 behind them, and all in between where n_best takes them.  true: that is all.
+template <int kThreads>
+__device__ __forceinline__ bool sure_blocks(const SelectArgs& a, const Unit& u, int32_t* out) {
+    const int width = a.n_first + a.n_recent + a.n_best, candidates = u.high - u.low, chosen = min(candidates, a.n_best);
+    const int tail = max(u.low, u.count - a.n_recent), all = u.low + chosen + (u.count - tail);
+    const bool done = candidates <= a.n_best || a.n_best == 0;
+    for (int i = threadIdx.x; i < width; i += kThreads) {
+        const int in_between = i - u.low;
+        if (in_between < 0) out[i] = i;
+        else if (i >= all) out[i] = -1;
+        else if (in_between >= chosen) out[i] = tail + in_between - chosen;
+        else if (done) out[i] = i;
     }
-    if (a.n_best == 0) return;
-    const uint32_t* keys = kKeys == 0 ? a.keys + (int64_t)blockIdx.x * a.max_blocks : held;
-    if constexpr (kKeys != 0) {
-        score_blocks<D, kWaves>(a, u, u.low, u.high, [&](int n, uint32_t key) { held[n - u.low] = key; });
-        __syncthreads();
-        keys -= u.low;
-    }
+    return done;
+}
+
+__device__ __forceinline__ uint64_t lanes_below() { return (1ull << (threadIdx.x & 63)) - 1; }
+
+// The candidates of a unit that a list takes, by one wavefront that holds all keys: candidate low + 64 i + lane is key i of a lane; 0: none (no score's key is 0).
+// The n-th largest key is found bit by bit, from counts of the keys that are at least the prefix with the bit set.
+template <int kPer>
+__device__ __forceinline__ void take_alone(const SelectArgs& a, const Unit& u, const uint32_t (&keys)[kPer], int32_t* out) {
+    auto count = [&](auto test) {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(test(keys[i])));
+        return n;
+    };
     uint32_t prefix = 0;
-    int wanted = a.n_best;                                    // so many of the keys that share the prefix, and all above
-#pragma unroll 1
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        counts[threadIdx.x] = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t tried = prefix | 1u << bit;
+        const int n = count([&](uint32_t key) { return key >= tried; });
+        if (n >= a.n_best) prefix = tried;
+        if (n == a.n_best) break;                             // (the others are below)
+    }
+    // in order: all above the n-th largest, and of those equal to it the first
+    int equal_left = a.n_best - count([&](uint32_t key) { return key > prefix; }), at = u.low;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const uint64_t equals = __builtin_amdgcn_ballot_w64(keys[i] == prefix), aboves = __builtin_amdgcn_ballot_w64(keys[i] > prefix);
+        const int rank = __builtin_popcountll(equals & lanes_below());
+        if (keys[i] > prefix || (keys[i] == prefix && rank < equal_left))
+            out[at + __builtin_popcountll(aboves & lanes_below()) + min(rank, equal_left)] = u.low + 64 * i + (threadIdx.x & 63);
+        const int taken = min(__builtin_popcountll(equals), equal_left);
+        at += __builtin_popcountll(aboves) + taken;
+        equal_left -= taken;
+    }
+}
+
+// One workgroup a unit, a wavefront for 64 candidates; their keys meet in LDS, and the first wavefront takes.
+template <int D, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 4) void cache8_select_kernel(SelectArgs a) {
+    __shared__ uint32_t held[kWaves == 1 ? 1 : kWaves][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = a.n_q_heads / a.c.n_kv_heads;
+    const Unit u = unit_of(a, blockIdx.x);
+    int32_t* out = a.blocks + (int64_t)blockIdx.x * (a.n_first + a.n_recent + a.n_best);
+    const int32_t* row_pages = a.c.table + (int64_t)max(u.slot, 0) * a.c.max_pages;
+    const uint16_t* q = a.q + ((int64_t)u.row * a.n_q_heads + u.head * g) * D;
+    const int first = u.low + 64 * wave;
+    Queries<D> w;
+    const int page = first < u.high ? page_of(a, row_pages, min(first + lane, u.high - 1)) : 0;
+    w.load(q, 0, g, lane);
+    if (sure_blocks<64 * kWaves>(a, u, out)) return;
+    uint32_t keys[kWaves] = {};
+    if (first < u.high) {
+        w.round(0, g, lane);
+        keys[0] = keys_of<D>(a, u, w, q, g, first, u.high, page);
+        if (first + lane >= u.high) keys[0] = 0;
+    }
+    if constexpr (kWaves > 1) {
+        held[wave][lane] = keys[0];
         __syncthreads();
-        for (int i = u.low + threadIdx.x; i < u.high; i += kThreads) {
-            const uint32_t key = keys[i];
-            if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&counts[key >> shift & 255], 1);
+        if (wave > 0) return;
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) keys[i] = held[i][lane];
+    }
+    take_alone<kWaves>(a, u, keys, out);
+}
+
+// For many candidates, 4096 at a time: candidate low + 64 (wave + kWaves i) + lane is key i of a lane.  kScored: their keys are in memory, else they are worked out
+// here, and there are no more than 4096.
+// The n-th largest key is found from counts of the keys in as many equal parts of the range that it lies in as there are threads: scores are spread widely
+// enough that two rounds mostly do, and few keys ask for the same counter.
+template <int D, int kWaves, bool kScored>
+__global__ __launch_bounds__(64 * kWaves) void cache8_select_many_kernel(SelectArgs a) {
+    constexpr int kThreads = 64 * kWaves, kPer = 4096 / kThreads, kBits = kWaves == 16 ? 10 : 9;
+    static_assert(kThreads == 1 << kBits && kPer * kWaves == 64, "");
+    __shared__ uint32_t counts[kThreads], ends[2][kWaves], sums[kWaves], found[3], parts[2][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = a.n_q_heads / a.c.n_kv_heads;
+    const Unit u = unit_of(a, blockIdx.x);
+    int32_t* out = a.blocks + (int64_t)blockIdx.x * (a.n_first + a.n_recent + a.n_best);
+    const int first = u.low + 64 * wave;
+    uint32_t keys[kPer];                                      // of a pass over the candidates; 0: none
+    const uint32_t* from = kScored ? a.keys + (int64_t)blockIdx.x * a.max_blocks : nullptr;
+    auto fetch = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int n = base + first + kThreads * i + lane;
+            keys[i] = n < u.high ? from[n] : 0;
         }
+    };
+    if constexpr (kScored) {
+        fetch(0);
+        if (sure_blocks<kThreads>(a, u, out)) return;
+    } else {
+        const int32_t* row_pages = a.c.table + (int64_t)max(u.slot, 0) * a.c.max_pages;
+        const uint16_t* q = a.q + ((int64_t)u.row * a.n_q_heads + u.head * g) * D;
+        Queries<D> w;
+        int page = first < u.high ? page_of(a, row_pages, min(first + lane, u.high - 1)) : 0;
+        w.load(q, 0, g, lane);
+        if (sure_blocks<kThreads>(a, u, out)) return;
+        w.round(0, g, lane);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int base = first + kThreads * i, next = base + kThreads;
+            keys[i] = 0;
+            if (base < u.high) {
+                keys[i] = keys_of<D>(a, u, w, q, g, base, u.high, page);
+                if (base + lane >= u.high) keys[i] = 0;
+                if (i + 1 < kPer && next < u.high) page = page_of(a, row_pages, min(next + lane, u.high - 1));
+            }
+        }
+    }
+    const int passes = kScored ? (u.high - u.low + 4095) / 4096 : 1;
+    auto each = [&](auto f) {                                 // over all keys that there are
+        for (int pass = 0; pass < passes; ++pass) {
+            if (passes > 1) fetch(4096 * pass);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (keys[i] != 0) f(keys[i]);
+        }
+    };
+    uint32_t low = 0xffffffffu, high = 0;
+    each([&](uint32_t key) {
+        low = min(low, key);
+        high = max(high, key);
+    });
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        low = min(low, (uint32_t)__shfl_xor((int)low, d));
+        high = max(high, (uint32_t)__shfl_xor((int)high, d));
+    }
+    if (lane == 0) {
+        ends[0][wave] = low;
+        ends[1][wave] = high;
+    }
+    counts[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+        low = min(low, ends[0][v]);
+        high = max(high, ends[1][v]);
+    }
+    uint32_t wanted = a.n_best, limit;                        // so many of the keys from low to high, and all above; all above limit are taken
+    int equal_left;                                           // of those equal to it, so many
+    for (int round = 0;; ++round) {
+        const uint32_t range = high - low;
+        const int shift = max(0, 32 - __clz((int)range) - kBits);      // (range 0: 32 leading zeros)
+        each([&](uint32_t key) {
+            if (key >= low && key <= high) atomicAdd(&counts[(key - low) >> shift], 1u);
+        });
         __syncthreads();
-        // thread i: keys whose byte is at least 255 - i
-        int sum = counts[255 - threadIdx.x];
-        const int own = sum;
+        // thread i: keys in its part, the i-th from the top, and above
+        const uint32_t own = counts[kThreads - 1 - threadIdx.x];
+        uint32_t sum = own;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-            const int other = __shfl_up(sum, d);
+            const uint32_t other = __shfl_up(sum, d);
             if (lane >= d) sum += other;
         }
         if (lane == 63) sums[wave] = sum;
         __syncthreads();
-        for (int w = 0; w < wave; ++w) sum += sums[w];
+        for (int v = 0; v < wave; ++v) sum += sums[v];
         if (sum >= wanted && sum - own < wanted) {
-            found[0] = 255 - threadIdx.x;
-            found[1] = wanted - (sum - own);
+            found[0] = kThreads - 1 - threadIdx.x;
+            found[1] = sum - own;
+            found[2] = own;
+        }
+        counts[threadIdx.x] = 0;
+        __syncthreads();
+        low += found[0] << shift;
+        wanted -= found[1];
+        // (found is not written again before two more barriers; 32 bits are four rounds at most)
+        if (shift == 0 || found[2] == wanted || round == 3) {
+            limit = shift == 0 ? low : low - 1;
+            equal_left = shift == 0 ? (int)wanted : 0;
+            break;
+        }
+        high = min(high, low + ((1u << shift) - 1));
+    }
+    // in order: all above the limit, and of those equal to it the first
+    int at = u.low;
+    for (int pass = 0; pass < passes; ++pass) {
+        if (passes > 1) fetch(4096 * pass);
+        uint32_t* const s = parts[pass & 1];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const uint32_t n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(keys[i] == limit)) | __builtin_popcountll(__builtin_amdgcn_ballot_w64(keys[i] > limit)) << 16;
+            if (lane == 0) s[kWaves * i + wave] = n;
         }
         __syncthreads();
-        prefix |= (uint32_t)found[0] << shift;
-        wanted = found[1];
-    }
-    // in order: above the n-th largest, and the first `wanted` that are equal to it
-    int before = 0, equal_before = 0;
-    for (int base = u.low; base < u.high; base += kThreads) {
-        const int i = base + threadIdx.x;
-        const uint32_t key = i < u.high ? keys[i] : 0;
-        const bool above = i < u.high && key > prefix, equal = i < u.high && key == prefix;
-        const uint64_t equals = __builtin_amdgcn_ballot_w64(equal);
-        __syncthreads();
-        if (lane == 0) sums[wave] = __builtin_popcountll(equals);
-        __syncthreads();
-        int rank = equal_before + __builtin_popcountll(equals & ((1ull << lane) - 1));
-        for (int w = 0; w < wave; ++w) rank += sums[w];
-        for (int w = 0; w < kWaves; ++w) equal_before += sums[w];
-        const bool taken = above || (equal && rank < wanted);
-        const uint64_t takens = __builtin_amdgcn_ballot_w64(taken);
-        __syncthreads();
-        if (lane == 0) sums[wave] = __builtin_popcountll(takens);
-        __syncthreads();
-        int at = before + __builtin_popcountll(takens & ((1ull << lane) - 1));
-        for (int w = 0; w < wave; ++w) at += sums[w];
-        for (int w = 0; w < kWaves; ++w) before += sums[w];
-        if (taken) out[u.low + at] = i;
+        const uint32_t mine = s[lane];
+        uint32_t sum = mine;                                  // (4096 at most in either half)
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t other = __shfl_up(sum, d);
+            if (lane >= d) sum += other;
+        }
+        const uint32_t all = (uint32_t)__shfl((int)sum, 63);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const uint32_t before = (uint32_t)__shfl((int)(sum - mine), kWaves * i + wave);
+            const uint64_t equals = __builtin_amdgcn_ballot_w64(keys[i] == limit), aboves = __builtin_amdgcn_ballot_w64(keys[i] > limit);
+            const int rank = (int)(before & 0xffff) + __builtin_popcountll(equals & lanes_below());
+            const int place = at + (int)(before >> 16) + __builtin_popcountll(aboves & lanes_below()) + min(rank, equal_left);
+            if ((keys[i] > limit || (keys[i] == limit && rank < equal_left)) && place < u.low + a.n_best) out[place] = 4096 * pass + first + kThreads * i + lane;
+        }
+        const int taken = min((int)(all & 0xffff), equal_left);
+        at += (int)(all >> 16) + taken;
+        equal_left -= taken;
     }
 }
 
-constexpr int kInLds = 4096;
+constexpr int kAtOnce = 4096, kAlone = 512;      // candidates whose keys a workgroup holds; that one scores by itself where units are few
+
+template <int D>
+void launch(const CacheSelect& x, const SelectArgs& a, unsigned units, hipStream_t stream) {
+    const int n = x.max_blocks;
+    if (x.chunks > 0) hipLaunchKernelGGL((cache8_select_many_kernel<D, 16, true>), dim3(units), dim3(1024), 0, stream, a);
+    else if (n <= 64) hipLaunchKernelGGL((cache8_select_kernel<D, 1>), dim3(units), dim3(64), 0, stream, a);
+    else if (n <= 256) hipLaunchKernelGGL((cache8_select_kernel<D, 4>), dim3(units), dim3(256), 0, stream, a);
+    else if (n <= 512) hipLaunchKernelGGL((cache8_select_kernel<D, 8>), dim3(units), dim3(512), 0, stream, a);
+    else hipLaunchKernelGGL((cache8_select_many_kernel<D, 8, false>), dim3(units), dim3(512), 0, stream, a);
+}
 
 }  // namespace
 
@@ -242,7 +416,7 @@ CacheSelect plan_cache8_select(int32_t n_seqs, int32_t n_tokens, int32_t n_kv_he
     const int64_t units = (int64_t)n_seqs * n_tokens * n_kv_heads, blocks = (max_len + 31) / 32;
     x.max_blocks = (int32_t)blocks;
     x.chunks = 0;
-    if (blocks > kInLds || (units < 128 && blocks > 512)) {
+    if (blocks > kAtOnce || (units < 128 && blocks > kAlone)) {
         x.chunk = (int32_t)((blocks / 4096 + 256) / 256 * 256);
         x.chunks = (int32_t)((blocks + x.chunk - 1) / x.chunk);
         x.key_bytes = (size_t)units * blocks * sizeof(uint32_t);
@@ -261,13 +435,8 @@ int launch_cache8_select(const CacheSelect& x, const CacheView& c, int32_t head_
         const int rc = check_launch();
         if (rc != PYR_OK) return rc;
     }
-    if (x.chunks > 0) {
-        if (head_dim == 128) hipLaunchKernelGGL((cache8_select_kernel<128, 0>), dim3(units), dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((cache8_select_kernel<64, 0>), dim3(units), dim3(256), 0, stream, a);
-    } else {
-        if (head_dim == 128) hipLaunchKernelGGL((cache8_select_kernel<128, kInLds>), dim3(units), dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((cache8_select_kernel<64, kInLds>), dim3(units), dim3(256), 0, stream, a);
-    }
+    if (head_dim == 128) launch<128>(x, a, units, stream);
+    else launch<64>(x, a, units, stream);
     return check_launch();
 }
 
