@@ -137,7 +137,7 @@ int pyr_cache8_append(const pyr_cache8* cache, const void* k, const void* v, int
     if (rows.dims > 0 && (!rows.positions || !rows.freqs)) return PYR_ERR_NULL;
     if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out)) return PYR_ERR_UNSUPPORTED;
     max_new = within_row(cache, max_new);
-    if ((int64_t)n * (((int64_t)max_new + 30) / 32 + 1) * ((c->n_kv_heads + (int64_t)n_q_heads + 3) / 4) >= kMostGroups) return PYR_ERR_UNSUPPORTED;
+    if ((int64_t)n * (((int64_t)max_new + 30) / 32 + 1) * ((2 * c->n_kv_heads + (int64_t)n_q_heads + 3) / 4) >= kMostGroups) return PYR_ERR_UNSUPPORTED;
     return pyr::launch_cache8_append(view(cache), d, rows, offsets, slots, start, n, max_new, (hipStream_t)stream);
 }
 

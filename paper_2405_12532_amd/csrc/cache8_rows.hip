@@ -32,7 +32,6 @@ __device__ __forceinline__ float across(float x, Op op) {
     return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
 
 typedef __attribute__((address_space(3))) char* lptr_t;
 typedef __attribute__((ext_vector_type(2))) int i32x2;
@@ -74,6 +73,10 @@ struct AppendArgs {
 };
 
 enum { kAsIs, kHalves, kPairs };                                  // channel c turns with c + dims / 2, or 2 c with 2 c + 1
+
+__device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b) {      // of both halves
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
 
 constexpr uint32_t kNoNumber = 0x7f680000u;                       // 464 * 2^119: what lies above has no code
 
@@ -204,216 +207,225 @@ __device__ __forceinline__ Piece piece_of(const AppendArgs& a, int place) {
     return p;
 }
 
+// Pieces of any length.  A wavefront goes through items: K, V or Q of the piece's block and a head.
 template <int D, int kTurn>
-__global__ __launch_bounds__(64 * kWaves) void cache8_append_kernel(AppendArgs a) {
-    constexpr int kLanes = D / 8, kTokens = 64 / kLanes, kLoads = 32 / kTokens;      // lanes of a row, rows of a load, loads of a tile
+constexpr int append_waves = D == 64 ? 4 : kTurn == kAsIs ? 3 : 2;      // of a SIMD, as registers allow
+template <int D, int kTurn>
+__global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn>)) void cache8_append_kernel(AppendArgs a) {
+    constexpr int kLanes = D / 8, kTokens = 64 / kLanes, kLoads = 32 / kTokens;      // lanes of a row, rows of a load, loads of a block
     constexpr int kRow = D + 16;                                  // bytes of a token's codes in LDS
     __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : 32][kTurn == kAsIs ? 1 : D / 2];
     __shared__ __align__(16) uint8_t all_staged[kWaves][32][kRow];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = lane % kLanes;
-    const int place = blockIdx.x / a.head_groups;
+    const int place = blockIdx.x / a.head_groups, hkv = a.c.n_kv_heads;
     const Piece p = piece_of(a, place);
     const uint32_t stored = p.stored, there = (uint32_t)__builtin_amdgcn_ballot_w64(p.from >= 0);
-    const int block = p.block, from = p.from;
+    const int block = p.block;
     const bool gone = stored != there, behind = p.behind;
     if (stored == 0) return;
 
+    // the row that a lane reads in load i: of a token that is not stored the first one's (what it computes changes no largest and no smallest, and is not
+    // written)
+    const int first = __builtin_ctz(stored);
+    auto token_of = [&](int i) { return i * kTokens + lane / kLanes; };
+    auto source_of = [&](int i) { return stored >> token_of(i) & 1 ? token_of(i) : first; };
+    auto there_of = [&](int i) { return (there >> source_of(i) & 1) != 0; };
+    int rows[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) rows[i] = max(__shfl(p.from, source_of(i)), 0);
+    auto load = [&](int item, u32x4 (&words)[kLoads]) {
+        const uint16_t* from = item < hkv ? a.k : item < 2 * hkv ? a.v : a.q;
+        const int64_t stride = item < hkv ? a.k_stride : item < 2 * hkv ? a.v_stride : a.q_stride;
+        const u32x4* at = (const u32x4*)from + (item < hkv ? item : item < 2 * hkv ? item - hkv : item - 2 * hkv) * kLanes + piece;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) words[i] = __builtin_nontemporal_load(at + rows[i] * stride);
+    };
+    const int items = 2 * hkv + a.n_q_heads, step = a.head_groups * kWaves;
+    int item = (blockIdx.x - place * a.head_groups) * kWaves + wave;
+    u32x4 words[kLoads];
+    if (item < items) load(item, words);
+
     if constexpr (kTurn != kAsIs) {
-        constexpr int kPairs = D / 2, kAtOnce = 64 / kPairs;
-        const int pair = lane % kPairs;
-        const int position = from >= 0 ? a.positions[from] : 0;
+        constexpr int kPairsOf = D / 2, kAtOnce = 64 / kPairsOf;
+        const int pair = lane % kPairsOf;
+        const int position = p.from >= 0 ? a.positions[p.from] : 0;
         const float freq = pair < a.dims / 2 ? a.freqs[pair] : 0.f;
         for (int t = wave * kAtOnce; t < 32; t += kWaves * kAtOnce) {
             if ((stored >> t & ((1u << kAtOnce) - 1)) == 0) continue;
-            const int mine_t = t + lane / kPairs;
+            const int mine_t = t + lane / kPairsOf;
             const f32x2 turn = turn_of(__shfl(position, mine_t), freq);
             if (pair < a.dims / 2) turns[mine_t][pair] = turn;
         }
         __syncthreads();
     }
-    // the token whose row a lane reads in load i: a token that is not stored reads the first one's (what it computes changes no largest and no
-    // smallest, and is not written)
-    const int first = __builtin_ctz(stored);
-    auto token_of = [&](int i) { return i * kTokens + lane / kLanes; };
-    auto source_of = [&](int i) { return stored >> token_of(i) & 1 ? token_of(i) : first; };
-    auto some = [&](int i) { return (stored >> (i * kTokens) & ((1u << kTokens) - 1)) != 0; };      // (of a load's tokens: one token is one load)
-
     auto turns_of = [&](int t) -> const f32x2* { return kTurn == kAsIs ? nullptr : turns[kTurn == kAsIs ? 0 : t]; };
+
     const Page8<D> at(a.c, p.page);
     uint8_t(*const staged)[kRow] = all_staged[wave];
-    const int heads = a.c.n_kv_heads + a.n_q_heads, step = a.head_groups * kWaves;
-    for (int head = (blockIdx.x - place * a.head_groups) * kWaves + wave; head < heads; head += step) {
-        if (head >= a.c.n_kv_heads) {                             // a head of Q: rows turned, where there are rows
-            const int h = head - a.c.n_kv_heads;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                if (!some(i)) continue;
-                const int t = token_of(i), row = __shfl(from, t);
-                const u32x4 words = __builtin_nontemporal_load((const u32x4*)a.q + (int64_t)max(row, 0) * a.q_stride + h * kLanes + piece);
-                float x[8];
-                turned<kTurn>(words, turns_of(t), a.dims, piece, x);
-                if (row >= 0) __builtin_nontemporal_store(rounded(x), (u32x4*)a.q_out + ((int64_t)row * a.n_q_heads + h) * kLanes + piece);
-            }
-            continue;
-        }
-        u32x4 kx[kLoads], vx[kLoads];
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            if (!some(i)) continue;
-            const int64_t row = max(__shfl(from, source_of(i)), 0);
-            kx[i] = __builtin_nontemporal_load((const u32x4*)a.k + row * a.k_stride + head * kLanes + piece);
-            vx[i] = __builtin_nontemporal_load((const u32x4*)a.v + row * a.v_stride + head * kLanes + piece);
-        }
-        uint8_t* const codes = at.codes(head, block);
-        uint16_t* const powers = at.powers(head, block);
-        u32x2* const bounds = (u32x2*)at.bounds(head, block) + piece;      // largest; kLanes further the smallest
-        const uint32_t old_powers = behind ? *powers : 0;
-        const u32x2 old_up = behind ? bounds[0] : u32x2{}, old_down = behind ? bounds[kLanes] : u32x2{};
-
-        // K turned; the largest magnitudes
-        float x[kLoads][8];
-        uint32_t ktop = 0, vtop = 0;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            if (!some(i)) continue;
-            turned<kTurn>(kx[i], turns_of(source_of(i)), a.dims, piece, x[i]);
-            if (gone && (there >> source_of(i) & 1) == 0) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[i][e] = NAN;
-                vx[i] = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-            }
-            raise(ktop, x[i]);
-            raise(vtop, vx[i]);
-        }
-        const bool special = __builtin_amdgcn_ballot_w64(ktop > kNoNumber || vtop > kNoNumber) != 0;
-        if (special) {
-            ktop = vtop = 0;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                if (!some(i)) continue;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    raise_finite(ktop, x[i][e]);
-                    raise_finite(vtop, e & 1 ? high_of(vx[i][e >> 1]) : low_of(vx[i][e >> 1]));
-                }
-            }
-        }
-        int kp = power8_of(across<1>(__uint_as_float(ktop), larger)), vp = power8_of(across<1>(__uint_as_float(vtop), larger));
-        int kgrow = 0, vgrow = 0;
+    const float most = __uint_as_float(kNoNumber);
+    const u32x4 kNoRow = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+    // the power of a block's K or V, whose codes the block held are rounded to it
+    auto settle = [&](float top, int old_power, uint8_t* power_at, uint8_t* codes, int* grow) {
+        int power = power8_of(across<1>(top, larger));
+        *grow = 0;
         if (behind) {
-            const int old_kp = old_powers & 255, old_vp = old_powers >> 8;
-            kp = max(kp, old_kp);
-            vp = max(vp, old_vp);
-            kgrow = min(kp - old_kp, 100);
-            vgrow = min(vp - old_vp, 100);
+            power = max(power, old_power);
+            *grow = min(power - old_power, 100);
         }
-        const float kscale = scale_of(kp), vscale = scale_of(vp);
-
-        // bounds
-        {
-            float up[8], down[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                up[e] = -INFINITY;
-                down[e] = INFINITY;
-            }
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                if (!some(i)) continue;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    up[e] = fmaxf(up[e], x[i][e]);
-                    down[e] = fminf(down[e], x[i][e]);
-                }
-            }
-            bool none[8];                                         // a number of the channel has no code
-#pragma unroll
-            for (int e = 0; e < 8; ++e) none[e] = false;
-            if (special) {
-#pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
-                    if (!some(i)) continue;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) none[e] |= !(fabsf(x[i][e]) <= __uint_as_float(kNoNumber));
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                up[e] = across<kLanes>(up[e], larger);
-                down[e] = across<kLanes>(down[e], smaller);
-                if (special) none[e] = across<kLanes>(none[e] ? 1.f : 0.f, larger) != 0.f;
-            }
-            u32x2 out_up, out_down;
-            bounds_of(up, down, none, kscale, behind, old_up, old_down, kgrow, out_up, out_down);
-            if (lane < kLanes) {
-                bounds[0] = out_up;
-                bounds[kLanes] = out_down;
-            }
-            if (lane == 0) *powers = (uint16_t)(kp | vp << 8);
-        }
-
-        // older numbers to the larger power
-        u32x4* const vcodes = (u32x4*)(codes + 32 * D) + lane;
-        const bool grows = kgrow > 0 || vgrow > 0;
-        if (grows) {
-            const float kby = __uint_as_float((uint32_t)(127 + kgrow) << 23), vby = __uint_as_float((uint32_t)(127 + vgrow) << 23);
-            u32x4* const kcodes = (u32x4*)codes + lane;
+        if (lane == 0) *power_at = (uint8_t)power;
+        if (*grow > 0) {
+            const float by = __uint_as_float((uint32_t)(127 + *grow) << 23);
+            u32x4* const lane_words = (u32x4*)codes + lane;
 #pragma unroll 1
             for (int g = 0; g < D / 32; ++g) {
-                u32x4 y = kcodes[64 * g], z = vcodes[64 * g];
+                u32x4 y = lane_words[64 * g];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    y[i] = regrown(y[i], kby);
-                    z[i] = regrown(z[i], vby);
-                }
-                kcodes[64 * g] = y;
-                vcodes[64 * g] = z;
+                for (int i = 0; i < 4; ++i) y[i] = regrown(y[i], by);
+                lane_words[64 * g] = y;
             }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");      // (the bytes are read and written again below, by other lanes)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");      // (the bytes are read and written again, by other lanes)
             __builtin_amdgcn_s_waitcnt(0);
         }
-
-        // K: eight channels of a token a lane.  V: in LDS as rows, from where transposing reads give eight tokens of a channel; a few tokens byte by byte
-        const bool few = __builtin_popcount(stored) <= 4;
-        const uint32_t kplace = ((piece >> 3) * 4 + (piece >> 1 & 3)) * 256 + (piece & 1) * 8;
+        return scale_of(power);
+    };
+    for (; item < items; item += step) {
+        if (item >= 2 * hkv) {                                    // a head of Q: rows turned, where there are rows
+            u32x4* const to = (u32x4*)a.q_out + (item - 2 * hkv) * kLanes + piece;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            if (!some(i)) continue;
-            const int t = token_of(i);
-            const u32x2 k8 = codes_of(x[i], kscale), v8 = codes_of(vx[i], vscale);
-            const bool write = stored >> t & 1;
-            if (write) *(u32x2*)(codes + (t >> 4) * (16 * D) + kplace + (t & 15) * 16) = k8;
-            if (few) {
-                uint8_t* to = codes + 32 * D + ((piece >> 2) * 4 + (t >> 2 & 3)) * 256 + (piece & 1) * 128 + (piece >> 1 & 1) * 8 + (t >> 4) * 4 + (t & 3);
-                if (write) {
+            for (int i = 0; i < kLoads; ++i) {
+                float x[8];
+                turned<kTurn>(words[i], turns_of(source_of(i)), a.dims, piece, x);
+                if ((stored & there) >> token_of(i) & 1) __builtin_nontemporal_store(rounded(x), to + (int64_t)rows[i] * (a.n_q_heads * kLanes));
+            }
+        } else if (item < hkv) {                                  // a head of K
+            uint8_t* const codes = at.codes(item, block);
+            uint8_t* const power_at = (uint8_t*)at.powers(item, block);
+            const int old_power = behind ? *power_at : 0;
+            constexpr bool kExpanded = kTurn != kAsIs;            // in fp32
+            float x[kExpanded ? kLoads : 1][8];
+            auto number = [&](int i, int e) { return kExpanded ? x[kExpanded ? i : 0][e] : e & 1 ? high_of(words[i][e >> 1]) : low_of(words[i][e >> 1]); };
+            float up[8], down[8];                                 // the largest, and the smallest the other way round: NaN prevails
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) to[16 * e] = (uint8_t)(v8[e >> 2] >> (8 * (e & 3)));
+            for (int e = 0; e < 8; ++e) up[e] = down[e] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kLoads; i += 2) {
+#pragma unroll
+                for (int n = i; n < i + 2; ++n) {
+                    if (gone && !there_of(n)) words[n] = kNoRow;
+                    if (kExpanded) turned<kTurn>(words[n], turns_of(source_of(n)), a.dims, piece, x[kExpanded ? n : 0]);
                 }
-            } else {
-                *(u32x2*)&staged[t][8 * piece] = v8;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float y = number(i, e), z = number(i + 1, e);
+                    up[e] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(up[e], y), z);
+                    down[e] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(down[e], -y), -z);
+                }
+                __builtin_amdgcn_sched_barrier(0);                // (else all rows are taken apart first, and registers run out)
             }
-        }
-        if (few) continue;
-        meet();
-        const int r = lane & 15, j = lane >> 4, e = r >> 1;
-        // the bytes of a word that stay as they are: tokens 16 h + 4 j + i, i = 0 .. 3
-        uint32_t keep[2] = {0, 0};
+            float top = __builtin_elementwise_maximum(up[0], down[0]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if ((stored >> (16 * (i >> 2) + 4 * j + (i & 3)) & 1) == 0) keep[i >> 2] |= 0xffu << (8 * (i & 3));
-        const uint32_t rows = (uint32_t)(uintptr_t)(lptr_t)&staged[16 * (e >> 2) + 4 * j + (e & 3)][8 * (r & 1)];
+            for (int e = 1; e < 8; ++e) top = __builtin_elementwise_maximum(top, __builtin_elementwise_maximum(up[e], down[e]));
+            if (__builtin_amdgcn_ballot_w64(!(top <= most)) != 0) {      // some have no code: the largest of those that are numbers, and no bounds where they are
+                uint32_t bits = 0;
 #pragma unroll
-        for (int g = 0; g < D / 32; ++g) {
-            const i32x2 p = lds_read_tr8(rows + 32 * g), s = lds_read_tr8(rows + 32 * g + 16);
-            u32x4 word = {(uint32_t)p[0], (uint32_t)p[1], (uint32_t)s[0], (uint32_t)s[1]};
-            if (stored != kAllTokens) {
-                const u32x4 old = vcodes[64 * g];
+                for (int i = 0; i < kLoads; ++i) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) word[i] = (word[i] & ~keep[i & 1]) | (old[i] & keep[i & 1]);
+                    for (int e = 0; e < 8; ++e) raise_finite(bits, number(i, e));
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                top = __uint_as_float(bits);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!(up[e] <= most && down[e] <= most)) up[e] = down[e] = NAN;
             }
-            vcodes[64 * g] = word;
+            int grow;
+            const float scale = settle(top, old_power, power_at, codes, &grow);
+            // over the tokens: lanes 16 r .. 16 r + 15 end up with the largest of even channels (r = 0), of odd ones, the smallest of even ones, of odd ones
+            float four[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float y[2];
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    const auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(up[2 * e + f]), __float_as_uint(down[2 * e + f]), false, false);
+                    y[f] = __builtin_elementwise_maximum(__uint_as_float(z[0]), __uint_as_float(z[1]));
+                }
+                const auto z = __builtin_amdgcn_permlane16_swap(__float_as_uint(y[0]), __float_as_uint(y[1]), false, false);
+                four[e] = __builtin_elementwise_maximum(__uint_as_float(z[0]), __uint_as_float(z[1]));
+                if (kLanes == 8) four[e] = __builtin_elementwise_maximum(four[e], dpp<0x128>(four[e]));
+            }
+            const uint32_t c = codes8_of(four[0], four[1], four[2], four[3], scale);
+            const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, false), z = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, true);
+            int8_t* const bounds = (int8_t*)at.bounds(item, block) + (lane >> 5) * D + 8 * piece + (lane >> 4 & 1);
+            const float shrink = __uint_as_float((uint32_t)(127 - grow) << 23);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float code = e < 2 ? y[e & 1] : z[e & 1];
+                float bound = code != code ? 127.f : __builtin_ceilf(code * 0.25f);
+                if (behind) {
+                    const float old = (float)bounds[2 * e];
+                    bound = fmaxf(bound, __builtin_ceilf((lane < 32 ? old : -old) * shrink));
+                }
+                if (kLanes == 16 || (lane & 8) == 0) bounds[2 * e] = (int8_t)(int)(lane < 32 ? bound : -bound);
+            }
+            // eight channels of a token a lane
+            const uint32_t to = ((piece >> 3) * 4 + (piece >> 1 & 3)) * 256 + (piece & 1) * 8;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int t = token_of(i);
+                const u32x2 y = kExpanded ? codes_of(x[kExpanded ? i : 0], scale) : codes_of(words[i], scale);
+                if (stored >> t & 1) *(u32x2*)(codes + (t >> 4) * (16 * D) + to + (t & 15) * 16) = y;
+            }
+        } else {                                                  // a head of V
+            uint8_t* const codes = at.codes(item - hkv, block) + 32 * D;
+            uint8_t* const power_at = (uint8_t*)at.powers(item - hkv, block) + 1;
+            const int old_power = behind ? *power_at : 0;
+            uint32_t pair = 0;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                if (gone && !there_of(i)) words[i] = kNoRow;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) pair = max_u16(pair, words[i][e] & 0x7fff7fffu);
+            }
+            float top = __uint_as_float(max(pair & 0xffff0000u, pair << 16));
+            if (__builtin_amdgcn_ballot_w64(!(top <= most)) != 0) {
+                uint32_t bits = 0;
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        raise_finite(bits, low_of(words[i][e]));
+                        raise_finite(bits, high_of(words[i][e]));
+                    }
+                top = __uint_as_float(bits);
+            }
+            int grow;
+            const float scale = settle(top, old_power, power_at, codes, &grow);
+            // in LDS as rows, from where transposing reads give eight tokens of a channel
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) *(u32x2*)&staged[token_of(i)][8 * piece] = codes_of(words[i], scale);
+            meet();
+            const int r = lane & 15, j = lane >> 4, e = r >> 1;
+            uint32_t keep[2] = {0, 0};                            // the bytes of a word that stay as they are: tokens 16 h + 4 j + i, i = 0 .. 3
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if ((stored >> (16 * (i >> 2) + 4 * j + (i & 3)) & 1) == 0) keep[i >> 2] |= 0xffu << (8 * (i & 3));
+            const uint32_t from = (uint32_t)(uintptr_t)(lptr_t)&staged[16 * (e >> 2) + 4 * j + (e & 3)][8 * (r & 1)];
+            u32x4* const lane_words = (u32x4*)codes + lane;
+#pragma unroll
+            for (int g = 0; g < D / 32; ++g) {
+                const i32x2 y = lds_read_tr8(from + 32 * g), z = lds_read_tr8(from + 32 * g + 16);
+                u32x4 word = {(uint32_t)y[0], (uint32_t)y[1], (uint32_t)z[0], (uint32_t)z[1]};
+                if (stored != kAllTokens) {
+                    const u32x4 old = lane_words[64 * g];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) word[i] = (word[i] & ~keep[i & 1]) | (old[i] & keep[i & 1]);
+                }
+                lane_words[64 * g] = word;
+            }
+            meet();                                               // (the next item's rows go to the same place)
         }
-        meet();                                                   // (the next head's rows go to the same place)
+        if (item + step < items) load(item + step, words);
     }
 }
 
@@ -428,27 +440,30 @@ __device__ __forceinline__ uint32_t within_row(uint32_t x, Op op) {
     return x;
 }
 
-// The new tokens of a step, kMost of a sequence at most: D / 8 lanes take a head, so that several heads share a wavefront and nothing has to cross from token to token
-// but a power, and byte after byte of V goes to its place.  A wavefront has one group of heads.
-template <int D, int kTurn, int kMost>
+// The new tokens of a step: D / 8 lanes take a head, so that several heads share a wavefront, all tokens of a channel are in one lane, and nothing has to cross lanes but
+// a power.  A wavefront has one group of heads.  kSlots 1: one token; 12: nine at most, in three groups of four as V's bytes lie.
+template <int D, int kTurn, int kSlots>
 __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendArgs a) {
     constexpr int kLanes = D / 8, kHeads = 64 / kLanes;           // lanes of a head, heads of a wavefront
-    __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : kMost][kTurn == kAsIs ? 1 : D / 2];
+    __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : kSlots][kTurn == kAsIs ? 1 : D / 2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = lane % kLanes;
     const int place = blockIdx.x / a.head_groups, group = (blockIdx.x - place * a.head_groups) * kWaves + wave;
     const int kv_groups = (a.c.n_kv_heads + kHeads - 1) / kHeads;
     const Piece p = piece_of(a, place);
     if (p.stored == 0) return;
-    const int first = __builtin_ctz(p.stored), count = min(__builtin_popcount(p.stored), kMost);
+    const int first = kSlots == 1 ? __builtin_ctz(p.stored) : __builtin_ctz(p.stored) & ~3;      // token of the first slot
+    const uint32_t present = p.stored >> first & ((1u << kSlots) - 1);
+    auto empty = [&](int i) { return kSlots > 1 && (present >> i & 1) == 0; };
     const bool of_q = group >= kv_groups;
     const int heads = of_q ? a.n_q_heads : a.c.n_kv_heads, wanted_head = (of_q ? group - kv_groups : group) * kHeads + lane / kLanes;
     const bool real = wanted_head < heads;
     const int head = min(wanted_head, max(heads - 1, 0));
-    u32x4 kx[kMost], vx[kMost];
-    int rows[kMost];
+    u32x4 kx[kSlots], vx[kSlots];
+    int rows[kSlots];
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) {
-        rows[i] = __builtin_amdgcn_readlane(p.from, first + min(i, count - 1));
+    for (int i = 0; i < kSlots; ++i) {
+        if (empty(i)) continue;
+        rows[i] = __builtin_amdgcn_readlane(p.from, first + i);
         const int64_t row = max(rows[i], 0);
         if (of_q) {
             if (heads > 0) kx[i] = __builtin_nontemporal_load((const u32x4*)a.q + row * a.q_stride + head * kLanes + piece);
@@ -473,7 +488,8 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
         const int pair = lane % kPairsOf;
         const float freq = pair < a.dims / 2 ? a.freqs[pair] : 0.f;
         const int position = p.from >= 0 ? a.positions[p.from] : 0;
-        for (int i = wave; i < count; i += kWaves) {
+        for (int i = wave; i < kSlots; i += kWaves) {
+            if (empty(i)) continue;
             const f32x2 turn = turn_of(__builtin_amdgcn_readlane(position, first + i), freq);
             if (lane < a.dims / 2) turns[i][pair] = turn;
         }
@@ -481,19 +497,19 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
     }
     if (of_q) {
 #pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-            if (i >= count) break;
+        for (int i = 0; i < kSlots; ++i) {
+            if (empty(i)) continue;
             float x[8];
             turned<kTurn>(kx[i], turns[kTurn == kAsIs ? 0 : i], a.dims, piece, x);
             if (real && rows[i] >= 0) __builtin_nontemporal_store(rounded(x), (u32x4*)a.q_out + ((int64_t)rows[i] * a.n_q_heads + head) * kLanes + piece);
         }
         return;
     }
-    float x[kMost][8];
+    float x[kSlots][8];
     uint32_t ktop = 0, vtop = 0;
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) {
-        if (i >= count) break;
+    for (int i = 0; i < kSlots; ++i) {
+        if (empty(i)) continue;
         turned<kTurn>(kx[i], turns[kTurn == kAsIs ? 0 : i], a.dims, piece, x[i]);
         if (rows[i] < 0) {
 #pragma unroll
@@ -507,8 +523,8 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
     if (special) {
         ktop = vtop = 0;
 #pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-            if (i >= count) break;
+        for (int i = 0; i < kSlots; ++i) {
+            if (empty(i)) continue;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 raise_finite(ktop, x[i][e]);
@@ -536,8 +552,8 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
             down[e] = INFINITY;
             none[e] = false;
 #pragma unroll
-            for (int i = 0; i < kMost; ++i) {
-                if (i >= count) break;
+            for (int i = 0; i < kSlots; ++i) {
+                if (empty(i)) continue;
                 up[e] = fmaxf(up[e], x[i][e]);
                 down[e] = fminf(down[e], x[i][e]);
                 if (special) none[e] |= !(fabsf(x[i][e]) <= __uint_as_float(kNoNumber));
@@ -570,17 +586,46 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
         __builtin_amdgcn_s_waitcnt(0);
     }
     const uint32_t kplace = ((piece >> 3) * 4 + (piece >> 1 & 3)) * 256 + (piece & 1) * 8;
-    const uint32_t vplace = 32 * D + (piece >> 2) * 1024 + (piece & 1) * 128 + (piece >> 1 & 1) * 8;
+    u32x2 v8[kSlots];
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) {
-        if (i >= count) break;
+    for (int i = 0; i < kSlots; ++i) {
+        if (empty(i)) continue;
         const int t = first + i;
-        const u32x2 k8 = codes_of(x[i], kscale), v8 = codes_of(vx[i], vscale);
-        if (!real) continue;
-        *(u32x2*)(codes + (t >> 4) * (16 * D) + kplace + (t & 15) * 16) = k8;
-        uint8_t* to = codes + vplace + (t >> 2 & 3) * 256 + (t >> 4) * 4 + (t & 3);
+        const u32x2 k8 = codes_of(x[i], kscale);
+        v8[i] = codes_of(vx[i], vscale);
+        if (real) *(u32x2*)(codes + (t >> 4) * (16 * D) + kplace + (t & 15) * 16) = k8;
+    }
+    if (!real) return;
+    // four tokens' bytes of a channel lie side by side
+    uint8_t* const vplace = codes + 32 * D + (piece >> 2) * 1024 + (piece & 1) * 128 + (piece >> 1 & 1) * 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) to[16 * e] = (uint8_t)(v8[e >> 2] >> (8 * (e & 3)));
+    for (int i = 0; i < kSlots; i += 4) {
+        const uint32_t four = present >> i & 15;
+        if (four == 0) continue;
+        uint8_t* const to = vplace + ((first + i) >> 2 & 3) * 256 + ((first + i) >> 4) * 4 + (kSlots == 1 ? first & 3 : 0);
+        auto byte = [&](int n, int e) { return v8[n][e >> 2] >> (8 * (e & 3)) & 255; };
+        if constexpr (kSlots == 1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to[16 * e] = (uint8_t)byte(0, e);
+        } else if (four == 15) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) *(uint32_t*)(to + 16 * e) = byte(i, e) | byte(i + 1, e) << 8 | byte(i + 2, e) << 16 | byte(i + 3, e) << 24;
+        } else {
+#pragma unroll
+            for (int n = 0; n < 4; n += 2) {
+                if ((four >> n & 3) == 3) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) *(uint16_t*)(to + 16 * e + n) = (uint16_t)(byte(i + n, e) | byte(i + n + 1, e) << 8);
+                } else {
+#pragma unroll
+                    for (int m = n; m < n + 2; ++m) {
+                        if ((four >> m & 1) == 0) continue;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) to[16 * e + m] = (uint8_t)byte(i + m, e);
+                    }
+                }
+            }
+        }
     }
 }
 
@@ -683,17 +728,19 @@ void launch_append(const AppendArgs& a, int64_t pieces, hipStream_t stream) {
     AppendArgs x = a;
     constexpr int kHeads = 512 / D;                               // (of a wavefront)
     const int groups = (a.c.n_kv_heads + kHeads - 1) / kHeads + (a.n_q_heads + kHeads - 1) / kHeads;
-    if (a.max_new <= 8) {
+    if (a.max_new <= 9) {
         x.head_groups = (groups + kWaves - 1) / kWaves;
         const dim3 blocks((unsigned)(pieces * x.head_groups)), threads(64 * kWaves);
         if (a.max_new == 1) hipLaunchKernelGGL((cache8_append_few_kernel<D, kTurn, 1>), blocks, threads, 0, stream, x);
-        else hipLaunchKernelGGL((cache8_append_few_kernel<D, kTurn, 8>), blocks, threads, 0, stream, x);
+        else hipLaunchKernelGGL((cache8_append_few_kernel<D, kTurn, 12>), blocks, threads, 0, stream, x);
         return;
     }
-    // workgroups of many heads share one reckoning of the turns, but few pieces need all the workgroups they can get
-    const int heads = a.c.n_kv_heads + a.n_q_heads;
-    const int64_t most = (heads + kWaves - 1) / kWaves, want = (2048 + pieces - 1) / pieces;
-    x.head_groups = (int32_t)(want < most ? want : most);
+    // workgroups of many items share one reckoning of the turns and have rows in flight, but few pieces need all the workgroups they can get
+    const int64_t items = 2 * a.c.n_kv_heads + a.n_q_heads, most = (items + kWaves - 1) / kWaves;
+    constexpr int64_t kTwice = 2 * 256 * append_waves<D, kTurn>;  // twice the workgroups that the chip holds
+    int64_t each = pieces * most / kTwice;                        // items of a wavefront
+    if (each < 1) each = 1;
+    x.head_groups = (int32_t)((most + each - 1) / each);
     hipLaunchKernelGGL((cache8_append_kernel<D, kTurn>), dim3((unsigned)(pieces * x.head_groups)), dim3(64 * kWaves), 0, stream, x);
 }
 
