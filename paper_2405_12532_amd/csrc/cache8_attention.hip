@@ -189,7 +189,8 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT>& w, Tile<D>& t, bool mas
     }
 }
 
-template <int D, int NT, int kWaves, bool kListed>
+// kOnce: nobody else reads a block.
+template <int D, int NT, int kWaves, bool kListed, bool kOnce>
 __global__ __launch_bounds__(64 * kWaves, NT == 1 && D == 64 ? 3 : 2) void cache8_attention_kernel(AttendArgs a) {
     constexpr int kRow = D + 4, kCols = 16 * NT;           // floats of a row in LDS; rows of a workgroup
     __shared__ __align__(16) float results[kWaves][kCols][kRow];
@@ -273,10 +274,10 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && D == 64 ? 3 : 2) void cache
         const Page8<D> at(a.c, __builtin_amdgcn_readlane(pages, i & 63));
         const u32x4* from = (const u32x4*)at.codes(head, number);
 #pragma unroll
-        for (int x = 0; x < D / 32; ++x) t.k[x] = NT == 1 ? __builtin_nontemporal_load(from + (uint32_t)(64 * x + lane)) : from[(uint32_t)(64 * x + lane)];
+        for (int x = 0; x < D / 32; ++x) t.k[x] = kOnce ? __builtin_nontemporal_load(from + (uint32_t)(64 * x + lane)) : from[(uint32_t)(64 * x + lane)];
 #pragma unroll
         for (int x = 0; x < D / 32; ++x)
-            t.v[x] = NT == 1 ? __builtin_nontemporal_load(from + (uint32_t)(64 * (D / 32 + x) + lane)) : from[(uint32_t)(64 * (D / 32 + x) + lane)];
+            t.v[x] = kOnce ? __builtin_nontemporal_load(from + (uint32_t)(64 * (D / 32 + x) + lane)) : from[(uint32_t)(64 * (D / 32 + x) + lane)];
         const uint32_t both = (uint32_t)__builtin_amdgcn_readlane((int)powers, i & 63);
         t.ks = scale_of(both & 255);
         t.vs = scale_of(both >> 8);
@@ -340,19 +341,35 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && D == 64 ? 3 : 2) void cache
     }
 }
 
-template <int D, bool kListed>
+template <int D, bool kListed, bool kOnce>
 void launch(const CacheAttention& x, const AttendArgs& a, dim3 blocks, hipStream_t stream) {
     const dim3 threads(64 * x.waves);
-    if (x.col_tiles == 2) hipLaunchKernelGGL((cache8_attention_kernel<D, 2, 4, kListed>), blocks, threads, 0, stream, a);
-    else if (x.waves == 4) hipLaunchKernelGGL((cache8_attention_kernel<D, 1, 4, kListed>), blocks, threads, 0, stream, a);
-    else hipLaunchKernelGGL((cache8_attention_kernel<D, 1, 8, kListed>), blocks, threads, 0, stream, a);
+    if (x.col_tiles == 2) hipLaunchKernelGGL((cache8_attention_kernel<D, 2, 4, kListed, false>), blocks, threads, 0, stream, a);
+    else if (x.waves == 4) hipLaunchKernelGGL((cache8_attention_kernel<D, 1, 4, kListed, kOnce>), blocks, threads, 0, stream, a);
+    else hipLaunchKernelGGL((cache8_attention_kernel<D, 1, 8, kListed, kOnce>), blocks, threads, 0, stream, a);
+}
+
+template <int D>
+void launch(const CacheAttention& x, const AttendArgs& a, dim3 blocks, hipStream_t stream) {
+    if (a.blocks == nullptr) launch<D, false, true>(x, a, blocks, stream);
+    else if (a.n_tokens == 1) launch<D, true, true>(x, a, blocks, stream);
+    else launch<D, true, false>(x, a, blocks, stream);            // (a sequence's tokens choose much the same blocks)
 }
 
 }  // namespace
 
 // n_blocks > 0: lists of so many blocks.
+// What is waited for at the end is the wavefront with the most blocks (8 KB at 128 channels), so few heads are split along the cache until a workgroup of eight wavefronts has
+// every compute unit to itself, and are taken by eight wavefronts unsplit up to one head a unit (two at 64 channels); more heads by four, two workgroups a unit.
+// Splitting takes a launch that joins the parts.  Measured, us (pass with the join; w: wavefronts, s: parts), 128 channels:
+//   heads x tokens   8 x 1000: w8 s1 8.4, w8 s4 7.7, w4 s8 7.4;  32 x 1434: w8 s1 11.4, w8 s4 9.5, w4 s8 8.9;  64 x 1200: w8 s1 10.2, w8 s4 9.9;  64 x 2048: w8 s1 14.3, w8 s4 11.1, w4 s8
+//   11.9;  96 x 1500: w8 s1 12.5, w8 s2 11.3;  128 x 1800: w8 s1 14.2, w8 s2 14.8;  128 x 4000: w8 s1 27.0, w8 s2 25.2;  160 x 1800: w8 s1 15.2, w4 s1 17.9, w4 s4 21.6;  160 x 100 ... 8000:
+//   w8 s1 46.5, w4 s4 46.4;  256 x 2000: w4 s1 23.2, w8 s1 23.6;  480 x 1800: w4 s1 37.0, w8 s1 38.8, w4 s2 42.8;  480 x 300 ... 5000: w4 s1 56.4, w4 s2 60.8;  8 x 65536: w8 s32 26.2, w4 s64 27.3
+//   64 channels: 256 x 2000: w8 s1 12.6, w4 s1 14.6;  480 x 1800: 20.7 either way;  8 x 16384: w4 s64 8.6, w8 s32 8.8
+//   more than 16 rows a head: 64 x 4096: s1 31.8, s4 19.2, s8 22.9;  128 x 2048: s1 26.3, s2 30.7
+//   lists of 64 blocks: 8 heads: w8 s8 8.2, w8 s1 13.0;  64: w8 s4 11.4, w8 s1 14.5;  256: w4 s1 23.9, w8 s1 24.4;  of 16: 2048 heads: w4 s1 45.2, w1 s1 45.3, w2 s1 47.0, w8 s1 57.1
 CacheAttention plan_cache8_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_len, int32_t n_blocks) {
-    constexpr int64_t kShortest = 8, kUnits = 256;
+    constexpr int64_t kUnits = 256;
     CacheAttention x{};
     const int64_t groups = n_blocks > 0 ? (int64_t)n_seqs * n_tokens : n_seqs;
     const int cols = (n_blocks > 0 ? 1 : n_tokens) * (n_q_heads / n_kv_heads);
@@ -361,12 +378,14 @@ CacheAttention plan_cache8_attention(int32_t n_seqs, int32_t n_tokens, int32_t n
     x.col_groups = (tiles + x.col_tiles - 1) / x.col_tiles;
     x.repeats = 1;
     const int64_t units = groups * n_kv_heads * x.col_groups, key_tiles = n_blocks > 0 ? n_blocks : (max_len + 31) / 32;
+    x.waves = x.col_tiles == 1 && units <= (head_dim == 64 ? 2 * kUnits : kUnits - 1) ? 8 : 4;
     int64_t splits = 1;
-    x.waves = x.col_tiles == 1 && units <= kUnits ? 8 : 4;
-    if (units > 0 && key_tiles > 32) splits = (2 * kUnits + units - 1) / units;
+    if (units > 0 && units <= kUnits / 2 && key_tiles > (units <= kUnits * 3 / 8 ? 40 : 72)) splits = kUnits / units;
+    if (units > kUnits / 2 && units < kUnits && key_tiles >= 128 && head_dim == 128) {      // (long enough that all units have to help)
+        x.waves = 4;
+        splits = 2 * kUnits / units;
+    }
     int64_t chunk = (key_tiles + splits - 1) / splits;
-    const int64_t shortest = x.col_tiles * kShortest;
-    if (splits > 1 && chunk < shortest) chunk = shortest;
     chunk = (chunk + x.waves - 1) / x.waves * x.waves;
     if (chunk == 0) chunk = x.waves;
     splits = (key_tiles + chunk - 1) / chunk;
@@ -386,13 +405,8 @@ int launch_cache8_attention(const CacheAttention& x, const CacheView& c, int32_t
     const AttendArgs a{c, (const uint16_t*)q, slots, blocks, split ? parts : out, split ? stats : lse, n_seqs, n_tokens, n_q_heads, n_blocks, x.chunk, x.splits,
                        scale_log2};
     const dim3 grid((unsigned)((int64_t)n_seqs * (listed ? n_tokens : 1) * x.col_groups * c.n_kv_heads), (unsigned)x.splits);
-    if (head_dim == 128) {
-        if (listed) launch<128, true>(x, a, grid, stream);
-        else launch<128, false>(x, a, grid, stream);
-    } else {
-        if (listed) launch<64, true>(x, a, grid, stream);
-        else launch<64, false>(x, a, grid, stream);
-    }
+    if (head_dim == 128) launch<128>(x, a, grid, stream);
+    else launch<64>(x, a, grid, stream);
     const int rc = check_launch();
     if (rc != PYR_OK || !split) return rc;
     return launch_cache_join(c, head_dim, slots, (const float*)parts, stats, n_seqs, n_tokens * n_q_heads, listed ? 0 : x.chunk, x.splits, out, lse, stream);

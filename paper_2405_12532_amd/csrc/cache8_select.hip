@@ -37,20 +37,25 @@ __device__ __forceinline__ uint32_t key_of(float score) {
 
 // A unit: a token of a sequence and a KV head.  What its tokens and blocks are.
 struct Unit {
-    int32_t slot, len, count, low, high, head, row;      // blocks it sees; candidates low .. high - 1; row of q's tokens
+    int32_t slot, len, head, row;                 // as the device has the length; row of q's tokens
+    int32_t count, low, high;                     // blocks it sees; candidates low .. high - 1 (low is n_first where there are some)
 };
 __device__ __forceinline__ Unit unit_of(const SelectArgs& a, int unit) {
     Unit u;
     const int hkv = a.c.n_kv_heads;
     u.row = unit / hkv;
     u.head = unit - u.row * hkv;
-    const int b = u.row / a.n_tokens, token = u.row - b * a.n_tokens;
+    const int b = u.row / a.n_tokens;
     u.slot = cache_slot(a.c, a.slots, b);
-    u.len = u.slot < 0 ? 0 : cache_len(a.c, u.slot);
-    u.count = (max(u.len - a.n_tokens + 1 + token, 0) + 31) >> 5;
+    u.len = a.c.lens[max(u.slot, 0)];
+    return u;
+}
+// The rest, for which the length has to be there.
+__device__ __forceinline__ void see(const SelectArgs& a, Unit& u) {
+    const int token = u.row % a.n_tokens, len = u.slot < 0 ? 0 : min(max(u.len, 0), a.c.max_pages << a.c.shift);
+    u.count = (max(len - a.n_tokens + 1 + token, 0) + 31) >> 5;
     u.low = min(a.n_first, u.count);
     u.high = max(u.low, min(u.count - a.n_recent, a.max_blocks));
-    return u;
 }
 
 // 16 query heads of the group as operands of the products, lane 16 j + t: bytes 16 j .. of head t's.
@@ -105,9 +110,9 @@ struct Queries {
     }
 };
 
-// The page of a block (0 where the table names none of the pool: the attention makes NaN of it).
+// The page of a block, asked for before it is known whether it is there (0 where the table names none of the pool: the attention makes NaN of it).
 __device__ __forceinline__ int page_of(const SelectArgs& a, const int32_t* row_pages, int block) {
-    const int page = row_pages[block >> (a.c.shift - 5)];
+    const int page = row_pages[min(block >> (a.c.shift - 5), a.c.max_pages - 1)];
     return page < 0 || page >= a.c.n_pages ? 0 : page;
 }
 
@@ -156,20 +161,22 @@ __device__ __forceinline__ uint32_t keys_of(const SelectArgs& a, const Unit& u, 
 template <int D>
 __global__ __launch_bounds__(256) void cache8_score_kernel(SelectArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = a.n_q_heads / a.c.n_kv_heads;
-    const Unit u = unit_of(a, blockIdx.x);
-    if (u.high - u.low <= a.n_best) return;
-    const int begin = u.low + (int)blockIdx.y * a.chunk + 64 * wave, end = min(u.high, u.low + ((int)blockIdx.y + 1) * a.chunk);
-    if (begin >= end) return;
-    const int32_t* row_pages = a.c.table + (int64_t)u.slot * a.c.max_pages;
+    Unit u = unit_of(a, blockIdx.x);
+    const int32_t* row_pages = a.c.table + (int64_t)max(u.slot, 0) * a.c.max_pages;
     const uint16_t* q = a.q + ((int64_t)u.row * a.n_q_heads + u.head * g) * D;
     uint32_t* keys = a.keys + (int64_t)blockIdx.x * a.max_blocks;
+    const int begin = (int)min((int64_t)a.n_first + (int64_t)blockIdx.y * a.chunk + 64 * wave, (int64_t)a.max_blocks);      // (as unit_of has it, where there are candidates)
     Queries<D> w;
-    int page = page_of(a, row_pages, min(begin + lane, end - 1));
+    int page = page_of(a, row_pages, begin + lane);
     w.load(q, 0, g, lane);
+    see(a, u);
+    if (u.high - u.low <= a.n_best) return;
+    const int end = (int)min((int64_t)u.high, u.low + ((int64_t)blockIdx.y + 1) * a.chunk);
+    if (begin >= end) return;
     w.round(0, g, lane);
     for (int base = begin; base < end; base += 256) {
         const uint32_t key = keys_of<D>(a, u, w, q, g, base, end, page);
-        if (base + 256 < end) page = page_of(a, row_pages, min(base + 256 + lane, end - 1));
+        if (base + 256 < end) page = page_of(a, row_pages, base + 256 + lane);
         if (base + lane < end) keys[base + lane] = key;
     }
 }
@@ -228,14 +235,15 @@ template <int D, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 4) void cache8_select_kernel(SelectArgs a) {
     __shared__ uint32_t held[kWaves == 1 ? 1 : kWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = a.n_q_heads / a.c.n_kv_heads;
-    const Unit u = unit_of(a, blockIdx.x);
+    Unit u = unit_of(a, blockIdx.x);
     int32_t* out = a.blocks + (int64_t)blockIdx.x * (a.n_first + a.n_recent + a.n_best);
     const int32_t* row_pages = a.c.table + (int64_t)max(u.slot, 0) * a.c.max_pages;
     const uint16_t* q = a.q + ((int64_t)u.row * a.n_q_heads + u.head * g) * D;
-    const int first = u.low + 64 * wave;
+    const int first = min(a.n_first, a.max_blocks) + 64 * wave;      // (as unit_of has it, where there are candidates)
     Queries<D> w;
-    const int page = first < u.high ? page_of(a, row_pages, min(first + lane, u.high - 1)) : 0;
+    const int page = page_of(a, row_pages, first + lane);
     w.load(q, 0, g, lane);
+    see(a, u);
     if (sure_blocks<64 * kWaves>(a, u, out)) return;
     uint32_t keys[kWaves] = {};
     if (first < u.high) {
@@ -263,9 +271,9 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_select_many_kernel(SelectA
     static_assert(kThreads == 1 << kBits && kPer * kWaves == 64, "");
     __shared__ uint32_t counts[kThreads], ends[2][kWaves], sums[kWaves], found[3], parts[2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = a.n_q_heads / a.c.n_kv_heads;
-    const Unit u = unit_of(a, blockIdx.x);
+    Unit u = unit_of(a, blockIdx.x);
     int32_t* out = a.blocks + (int64_t)blockIdx.x * (a.n_first + a.n_recent + a.n_best);
-    const int first = u.low + 64 * wave;
+    const int first = min(a.n_first, a.max_blocks) + 64 * wave;
     uint32_t keys[kPer];                                      // of a pass over the candidates; 0: none
     const uint32_t* from = kScored ? a.keys + (int64_t)blockIdx.x * a.max_blocks : nullptr;
     auto fetch = [&](int base) {
@@ -276,14 +284,16 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_select_many_kernel(SelectA
         }
     };
     if constexpr (kScored) {
+        see(a, u);
         fetch(0);
         if (sure_blocks<kThreads>(a, u, out)) return;
     } else {
         const int32_t* row_pages = a.c.table + (int64_t)max(u.slot, 0) * a.c.max_pages;
         const uint16_t* q = a.q + ((int64_t)u.row * a.n_q_heads + u.head * g) * D;
         Queries<D> w;
-        int page = first < u.high ? page_of(a, row_pages, min(first + lane, u.high - 1)) : 0;
+        int page = page_of(a, row_pages, first + lane);
         w.load(q, 0, g, lane);
+        see(a, u);
         if (sure_blocks<kThreads>(a, u, out)) return;
         w.round(0, g, lane);
 #pragma unroll
@@ -293,7 +303,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_select_many_kernel(SelectA
             if (base < u.high) {
                 keys[i] = keys_of<D>(a, u, w, q, g, base, u.high, page);
                 if (base + lane >= u.high) keys[i] = 0;
-                if (i + 1 < kPer && next < u.high) page = page_of(a, row_pages, min(next + lane, u.high - 1));
+                if (i + 1 < kPer && next < u.high) page = page_of(a, row_pages, next + lane);
             }
         }
     }

@@ -270,11 +270,11 @@ def test_attention_split_along_the_cache(lib, lens, hq, hkv, d, tokens):
 
 
 def test_attention_of_many_rows_by_workgroups_of_four_wavefronts(lib):
-    lens = [37 * (i % 7) for i in range(300)]
+    lens = [37 * (i % 7) for i in range(600)]
     pair = Pair8(lib, lens, 1, 64, 32)
-    qt, q = bf16(pair.rng.normal(size=(300, 1, 3, 64)) * 0.05)
-    assert lib.diag_cache8_attention(pair.cache, 300, 1, 3, 222, 0).waves == 4
-    check_attention(pair, q, range(300), *attend(pair, qt, list(range(300)), 1, 222))
+    qt, q = bf16(pair.rng.normal(size=(600, 1, 3, 64)) * 0.05)
+    assert lib.diag_cache8_attention(pair.cache, 600, 1, 3, 222, 0).waves == 4
+    check_attention(pair, q, range(600), *attend(pair, qt, list(range(600)), 1, 222))
 
 
 @pytest.mark.parametrize("d", [64, 128])
