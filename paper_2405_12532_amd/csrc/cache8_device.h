@@ -61,6 +61,29 @@ __device__ __forceinline__ uint32_t codes8_of(float x0, float x1, float x2, floa
     return __builtin_bit_cast(uint32_t, y);
 }
 
+__device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b) {      // of both halves
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, 0xf, 0xf, false); }
+// op over groups of kLanes lanes (8 or 16), in all of them; over the wavefront.
+template <int kLanes, class Op>
+__device__ __forceinline__ uint32_t within_lanes(uint32_t x, Op op) {
+    x = op(x, dpp<0xb1>(x));              // the neighbour's, the other pair's
+    x = op(x, dpp<0x4e>(x));
+    x = op(x, dpp<0x141>(x));             // (eight lanes mirrored, then sixteen)
+    return kLanes == 16 ? op(x, dpp<0x140>(x)) : x;
+}
+template <class Op>
+__device__ __forceinline__ uint32_t within_wave(uint32_t x, Op op) {
+    x = within_lanes<16>(x, op);
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = op(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return op(b[0], b[1]);
+}
+
 // The power byte of a block whose largest finite magnitude is top: the smallest with top <= 448 * 2^(byte - 127).
 __device__ __forceinline__ int power8_of(float top) {
     const uint32_t bits = __float_as_uint(top);

@@ -6,8 +6,6 @@
 // workgroup takes 32 tokens and some heads: the pairs are worked out once, meet in LDS and turn K and Q of all its heads.
 // A wavefront owns one block (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte.
 // Bound: reading and writing HBM.
-#include <type_traits>
-
 #include "cache8_device.h"
 
 namespace pyr {
@@ -16,22 +14,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr uint32_t kAllTokens = 0xffffffffu;
 
-template <int kCtrl>
-__device__ __forceinline__ float dpp(float x) { return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), kCtrl, 0xf, 0xf, false)); }
-
-// op over the lanes whose number differs from a lane's in bits of `mask` alone (mask: bits from the lowest of D / 8 lanes on, or from 1 on)
-template <int kFrom, class Op>
-__device__ __forceinline__ float across(float x, Op op) {
-    if (kFrom <= 1) x = op(x, dpp<0xb1>(x));
-    if (kFrom <= 2) x = op(x, dpp<0x4e>(x));
-    if (kFrom <= 4) x = op(x, dpp<0x124>(x));       // (what the lane four further holds, inside 16 lanes; then eight)
-    if (kFrom <= 8) x = op(x, dpp<0x128>(x));
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }      // of magnitudes, as bits
 
 typedef __attribute__((address_space(3))) char* lptr_t;
 typedef __attribute__((ext_vector_type(2))) int i32x2;
@@ -73,10 +56,6 @@ struct AppendArgs {
 };
 
 enum { kAsIs, kHalves, kPairs };                                  // channel c turns with c + dims / 2, or 2 c with 2 c + 1
-
-__device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b) {      // of both halves
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
-}
 
 constexpr uint32_t kNoNumber = 0x7f680000u;                       // 464 * 2^119: what lies above has no code
 
@@ -266,7 +245,7 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn>)) void cache8_
     const u32x4 kNoRow = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
     // the power of a block's K or V, whose codes the block held are rounded to it
     auto settle = [&](float top, int old_power, uint8_t* power_at, uint8_t* codes, int* grow) {
-        int power = power8_of(across<1>(top, larger));
+        int power = power8_of(__uint_as_float(within_wave(__float_as_uint(top), larger)));
         *grow = 0;
         if (behind) {
             power = max(power, old_power);
@@ -352,7 +331,7 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn>)) void cache8_
                 }
                 const auto z = __builtin_amdgcn_permlane16_swap(__float_as_uint(y[0]), __float_as_uint(y[1]), false, false);
                 four[e] = __builtin_elementwise_maximum(__uint_as_float(z[0]), __uint_as_float(z[1]));
-                if (kLanes == 8) four[e] = __builtin_elementwise_maximum(four[e], dpp<0x128>(four[e]));
+                if (kLanes == 8) four[e] = __builtin_elementwise_maximum(four[e], __uint_as_float(dpp<0x128>(__float_as_uint(four[e]))));      // (eight lanes further)
             }
             const uint32_t c = codes8_of(four[0], four[1], four[2], four[3], scale);
             const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, false), z = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, true);
@@ -427,17 +406,6 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn>)) void cache8_
         }
         if (item + step < items) load(item + step, words);
     }
-}
-
-// op over the kLanes lanes that hold a row, in all of them
-template <int kLanes, class Op>
-__device__ __forceinline__ uint32_t within_row(uint32_t x, Op op) {
-    auto other = [&](auto ctrl) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xf, 0xf, false); };
-    x = op(x, other(std::integral_constant<int, 0xb1>{}));
-    x = op(x, other(std::integral_constant<int, 0x4e>{}));
-    x = op(x, other(std::integral_constant<int, 0x141>{}));      // (eight lanes mirrored, then sixteen)
-    if (kLanes == 16) x = op(x, other(std::integral_constant<int, 0x140>{}));
-    return x;
 }
 
 // The new tokens of a step: D / 8 lanes take a head, so that several heads share a wavefront, all tokens of a channel are in one lane, and nothing has to cross lanes but
@@ -532,8 +500,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
             }
         }
     }
-    auto larger_bits = [](uint32_t y, uint32_t z) { return max(y, z); };
-    int kp = power8_of(__uint_as_float(within_row<kLanes>(ktop, larger_bits))), vp = power8_of(__uint_as_float(within_row<kLanes>(vtop, larger_bits)));
+    int kp = power8_of(__uint_as_float(within_lanes<kLanes>(ktop, larger))), vp = power8_of(__uint_as_float(within_lanes<kLanes>(vtop, larger)));
     int kgrow = 0, vgrow = 0;
     if (p.behind) {
         const int old_kp = old_powers & 255, old_vp = old_powers >> 8;

@@ -74,36 +74,49 @@ struct Queries {
                 words[s][h] = head + (lane & 15) < g ? *(const u32x4*)(q + (int64_t)(head + (lane & 15)) * D + 64 * s + 16 * (lane >> 4) + 8 * h) : u32x4{};
     }
     __device__ __forceinline__ void round(int head, int g, int lane) {
-        float top = 0.f;
+        uint32_t pair = 0;
 #pragma unroll
         for (int s = 0; s < kHalf; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = fabsf(__uint_as_float(words[s][h][e] << 16)), y = fabsf(__uint_as_float(words[s][h][e] & 0xffff0000u));
-                    top = fmaxf(top, fmaxf(x < INFINITY ? x : 0.f, y < INFINITY ? y : 0.f));
-                }
+                for (int e = 0; e < 4; ++e) pair = max_u16(pair, words[s][h][e] & 0x7fff7fffu);
+        float top = __uint_as_float(max(pair & 0xffff0000u, pair << 16));
+        if (__builtin_amdgcn_ballot_w64(!(top < INFINITY)) != 0) {      // NaN counts as 0, an infinity as what is largest (below); neither as a magnitude
+            top = 0.f;
+#pragma unroll
+            for (int s = 0; s < kHalf; ++s)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t& w = reinterpret_cast<uint32_t*>(&words[s][h])[e];
+                        const float x = __uint_as_float(w << 16), y = __uint_as_float(w & 0xffff0000u);
+                        if (x != x) w &= 0xffff0000u;
+                        if (y != y) w &= 0xffffu;
+                        top = fmaxf(top, fmaxf(fabsf(x) < INFINITY ? fabsf(x) : 0.f, fabsf(y) < INFINITY ? fabsf(y) : 0.f));
+                    }
+        }
         top = max_of_groups(top);
         const uint32_t bits = __float_as_uint(top);
         const int e = min(max((int)(bits >> 23) - 127 - 6 + ((bits & 0x7fffff) > 0x7e0000 ? 1 : 0), -100), 122);
         const float by = __uint_as_float((uint32_t)(127 - e) << 23);
+        // adding 1.5 * 2^23 rounds to a whole number (ties to even) and leaves its byte lowest
+        auto byte_of = [&](float x) { return __float_as_uint(__builtin_amdgcn_fmed3f(x * by, -127.f, 127.f) + 12582912.f); };
 #pragma unroll
         for (int s = 0; s < kHalf; ++s)
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                uint32_t up = 0, down = 0;
+                uint32_t b[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t pair = words[s][w >> 1][2 * (w & 1) + (i >> 1)];
-                    const float x = __uint_as_float(i & 1 ? pair & 0xffff0000u : pair << 16) * by;
-                    const float y = fminf(fmaxf(__builtin_rintf(x), -127.f), 127.f);
-                    const int n = x != x ? 0 : (int)y;
-                    up |= (uint32_t)max(n, 0) << (8 * i);
-                    down |= ((uint32_t)min(n, 0) & 255) << (8 * i);
+                    const uint32_t both = words[s][w >> 1][2 * (w & 1) + (i >> 1)];
+                    b[i] = byte_of(__uint_as_float(i & 1 ? both & 0xffff0000u : both << 16));
                 }
-                whole[s][w] = (int)up;
-                whole[kHalf + s][w] = (int)down;
+                const uint32_t bytes = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
+                const uint32_t below = (bytes >> 7 & 0x01010101u) * 255u;      // of numbers below 0
+                whole[s][w] = (int)(bytes & ~below);
+                whole[kHalf + s][w] = (int)(bytes & below);
             }
 #pragma unroll
         for (int x = 0; x < 4; ++x) power[x] = __shfl(head + (lane & 15) < g ? e : kNone, 4 * (lane >> 4) + x);
@@ -321,11 +334,8 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_select_many_kernel(SelectA
         low = min(low, key);
         high = max(high, key);
     });
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        low = min(low, (uint32_t)__shfl_xor((int)low, d));
-        high = max(high, (uint32_t)__shfl_xor((int)high, d));
-    }
+    low = within_wave(low, [](uint32_t x, uint32_t y) { return min(x, y); });
+    high = within_wave(high, [](uint32_t x, uint32_t y) { return max(x, y); });
     if (lane == 0) {
         ends[0][wave] = low;
         ends[1][wave] = high;
@@ -348,15 +358,11 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_select_many_kernel(SelectA
         __syncthreads();
         // thread i: keys in its part, the i-th from the top, and above
         const uint32_t own = counts[kThreads - 1 - threadIdx.x];
-        uint32_t sum = own;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const uint32_t other = __shfl_up(sum, d);
-            if (lane >= d) sum += other;
-        }
+        uint32_t sum = scan_wave((int)own);
         if (lane == 63) sums[wave] = sum;
         __syncthreads();
-        for (int v = 0; v < wave; ++v) sum += sums[v];
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) sum += v < wave ? sums[v] : 0;
         if (sum >= wanted && sum - own < wanted) {
             found[0] = kThreads - 1 - threadIdx.x;
             found[1] = sum - own;
@@ -386,16 +392,11 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_select_many_kernel(SelectA
         }
         __syncthreads();
         const uint32_t mine = s[lane];
-        uint32_t sum = mine;                                  // (4096 at most in either half)
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const uint32_t other = __shfl_up(sum, d);
-            if (lane >= d) sum += other;
-        }
-        const uint32_t all = (uint32_t)__shfl((int)sum, 63);
+        const uint32_t sum = scan_wave((int)mine);            // (4096 at most in either half)
+        const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const uint32_t before = (uint32_t)__shfl((int)(sum - mine), kWaves * i + wave);
+            const uint32_t before = (uint32_t)__builtin_amdgcn_readlane((int)(sum - mine), kWaves * i + wave);
             const uint64_t equals = __builtin_amdgcn_ballot_w64(keys[i] == limit), aboves = __builtin_amdgcn_ballot_w64(keys[i] > limit);
             const int rank = (int)(before & 0xffff) + __builtin_popcountll(equals & lanes_below());
             const int place = at + (int)(before >> 16) + __builtin_popcountll(aboves & lanes_below()) + min(rank, equal_left);

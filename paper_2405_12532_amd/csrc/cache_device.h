@@ -66,4 +66,16 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
     return e < 1 ? 1 : e > 252 ? 252 : e;
 }
 
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int add_dpp(int x) { return x + __builtin_amdgcn_update_dpp(0, x, kCtrl, kRows, 0xf, false); }
+
+__device__ __forceinline__ int scan_wave(int x) {      // inclusive sum over the lanes
+    int sum = add_dpp<0x111, 0xf>(x);     // from the lane 1 (2, 4, 8) below, inside 16 lanes
+    sum = add_dpp<0x112, 0xf>(sum);
+    sum = add_dpp<0x114, 0xf>(sum);
+    sum = add_dpp<0x118, 0xf>(sum);
+    sum = add_dpp<0x142, 0xa>(sum);       // lane 15's to the second 16, lane 47's to the fourth
+    return add_dpp<0x143, 0xc>(sum);      // lane 31's to the upper half
+}
+
 }  // namespace pyr
