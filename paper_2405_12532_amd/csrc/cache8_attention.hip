@@ -28,11 +28,12 @@ struct AttendArgs {
     const int32_t* blocks;                        // lists [n, tokens, Hkv, n_blocks]
     void* out;                                    // splits == 1: bf16 [n, tokens, Hq, D]; else fp32 [splits, rows, D], not normalised
     float* lse;                                   // splits == 1: [rows] or NULL; else [splits, rows, 4]: reference, sum, sum of the rounded
-    int32_t n_seqs, n_tokens, n_q_heads, n_blocks;
+    int32_t n_seqs, n_tokens, n_blocks;
     int32_t chunk;                                // blocks of a split (the last one takes what is left)
-    int32_t splits;
+    uint16_t n_q_heads, splits;
     float scale;                                  // softmax scale * log2(e)
 };
+static_assert(sizeof(AttendArgs) <= 112, "short arguments");
 
 // What a wavefront holds of a block; token: its first one, -1: no block.
 template <int D>
@@ -402,8 +403,8 @@ int launch_cache8_attention(const CacheAttention& x, const CacheView& c, int32_t
                             float* stats, hipStream_t stream) {
     if (n_seqs == 0) return PYR_OK;
     const bool split = x.splits > 1, listed = blocks != nullptr;
-    const AttendArgs a{c, (const uint16_t*)q, slots, blocks, split ? parts : out, split ? stats : lse, n_seqs, n_tokens, n_q_heads, n_blocks, x.chunk, x.splits,
-                       scale_log2};
+    const AttendArgs a{c, (const uint16_t*)q, slots, blocks, split ? parts : out, split ? stats : lse, n_seqs, n_tokens, n_blocks, x.chunk,
+                       (uint16_t)n_q_heads, (uint16_t)x.splits, scale_log2};
     const dim3 grid((unsigned)((int64_t)n_seqs * (listed ? n_tokens : 1) * x.col_groups * c.n_kv_heads), (unsigned)x.splits);
     if (head_dim == 128) launch<128>(x, a, grid, stream);
     else launch<64>(x, a, grid, stream);

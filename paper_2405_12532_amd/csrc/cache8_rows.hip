@@ -2,8 +2,9 @@
 // Gather(KV, index) keeps of a prompt goes the same way, through its index), tokens of it back to bf16, and pages copied for a fork.
 //
 // A turn by position p takes channels a and b of a pair i to a cos(p f_i) - b sin(p f_i) and b cos(p f_i) + a sin(p f_i).  p f_i is reduced to a
-// quarter of a turn in 64 bits, so that far positions lose nothing; sine and cosine are then Taylor's sums on [-pi/4, pi/4], below 2^-24 off.  A
-// workgroup takes 32 tokens and some heads: the pairs are worked out once, meet in LDS and turn K and Q of all its heads.
+// quarter of a turn in 64 bits, so that far positions lose nothing; sine and cosine are Taylor's sums on [-pi/4, pi/4] in 64 bits too, rounded to 32 (in 32 bits
+// throughout, twice as many numbers next to a border got another code than the exact one).  A workgroup takes 32 tokens and some heads: the pairs are
+// worked out once, meet in LDS and turn K and Q of all its heads.
 // A wavefront owns one block (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte.
 // Bound: reading and writing HBM.
 #include "cache8_device.h"
@@ -32,15 +33,15 @@ __device__ __forceinline__ void meet() {            // (a wavefront's own part o
 __device__ __forceinline__ float low_of(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high_of(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
-// cos and sin of position * freq
+// cos and sin of position * freq, in 64 bits up to their rounding (the sums' next terms are below 2^-28)
 __device__ __forceinline__ f32x2 turn_of(int position, float freq) {
     const double quarters = (double)position * ((double)freq * 0.63661977236758134308);      // of a turn: times 2 / pi
     const double nearest = __builtin_rint(quarters);
-    const float x = (float)(quarters - nearest) * 1.57079632679489661923f, y = x * x;
-    const float s = x * (1.f + y * (-1.f / 6 + y * (1.f / 120 + y * (-1.f / 5040 + y * (1.f / 362880)))));
-    const float c = 1.f + y * (-0.5f + y * (1.f / 24 + y * (-1.f / 720 + y * (1.f / 40320))));
+    const double x = (quarters - nearest) * 1.57079632679489661923, y = x * x;
+    const double s = x * (1. + y * (-1. / 6 + y * (1. / 120 + y * (-1. / 5040 + y * (1. / 362880)))));
+    const double c = 1. + y * (-0.5 + y * (1. / 24 + y * (-1. / 720 + y * (1. / 40320 - y * (1. / 3628800)))));
     const int quadrant = (int)(nearest - 4.0 * __builtin_floor(nearest * 0.25));
-    const float a = quadrant & 1 ? s : c, b = quadrant & 1 ? c : s;
+    const float a = (float)(quadrant & 1 ? s : c), b = (float)(quadrant & 1 ? c : s);
     return f32x2{quadrant == 1 || quadrant == 2 ? -a : a, quadrant >= 2 ? -b : b};
 }
 
