@@ -471,7 +471,8 @@ PYR_API int pyr_cache_attention(const pyr_cache* cache, const void* q, const int
  *   [H][T]  2 d bytes   bounds: the largest [d], the smallest [d], int8
  *   [H][T]  2 bytes     powers of K and of V: 2^(byte - 127)
  *
- * Host checks as above, and PYR_ERR_UNSUPPORTED for pages of 2^31 bytes or more.
+ * Host checks as above, and PYR_ERR_UNSUPPORTED for pages of 2^31 bytes or more and for lists of more than 2^26 blocks; a workgroup takes a sequence's 32
+ * tokens of up to four heads of K, V and Q where rows go in, a token's KV head where blocks are chosen or listed.
  */
 typedef struct pyr_cache8 {
     pyr_cache pool;       /* pages of pyr_cache8_page_bytes() bytes                                  */
@@ -504,7 +505,7 @@ typedef struct pyr_rotation {
  *   q_out              dev bf16 [n_rows, Hq, d], written: the rows of q whose tokens are stored, turned; the others stay as they were
  * Tokens from lens[slots[i]] on (they were not reserved), tokens that have no page and a start of -1 are not stored; a row outside k and v or the list is
  * stored as NaN; nothing else in the pages changes, but for what a larger power does to its block.  Of rows that name the same slot the first is stored.
- * q_out must not overlap k, v or q - but it may be q itself, packed.
+ * q_out must not overlap k, v or q - but it may be q itself, packed, if no row is named twice.  No rows, no list, max_new 0: nothing is done.
  */
 PYR_API int pyr_cache8_append(const pyr_cache8* cache, const void* k, const void* v, int64_t k_stride, int64_t v_stride, int32_t n_rows,
                       const int32_t* row_idx, int32_t n_list, const int32_t* offsets, const int32_t* slots, const int32_t* start, int32_t n, int32_t max_new,
@@ -549,7 +550,7 @@ PYR_API int pyr_cache8_select(const pyr_cache8* cache, const void* q, const int3
  *   max_len            as in pyr_cache_attention; not looked at where there are lists
  *   q, slots, softmax_scale, out, lse, workspace  as in pyr_cache_attention
  * bf16 MFMA products on the cache's exact values (P is rounded to bf16), fp32 accumulation and softmax.  Sums of P V stay in fp32's range as long as V's
- * largest power of two times the sequence's tokens is below 2^105 (a number whose sum leaves it is NaN).
+ * largest power of two times the sequence's tokens is below 2^108 (a number whose sum leaves it is NaN).
  * A row that sees nothing (an empty slot, a skipped row, a list without blocks): zeros in out, -inf in lse.  A K that is NaN makes the rows that see it NaN, a V
  * the channel of those rows; what a row does not see never reaches it.  A page outside the pool among those that it takes: NaN in the sequence's rows, or the list's.
  */

@@ -11,6 +11,8 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 constexpr int64_t kMost = (int64_t)1 << 31;
 constexpr int64_t kMostGroups = (int64_t)1 << 24;                // workgroups of 256 threads: a launch has fewer than 2^32 threads
 
+constexpr int64_t kMostBlocks = (int64_t)1 << 26;               // of a list: no pool has more
+
 int check_layout(const pyr_cache8* cache) {
     if (cache == nullptr) return PYR_ERR_NULL;
     const pyr_cache* c = &cache->pool;
@@ -68,6 +70,7 @@ int check_attention(const pyr_cache8* cache, int32_t n, int32_t n_tokens, int32_
     const int rc = check_rows(cache, n, n_tokens, n_q_heads, max_len);
     if (rc != PYR_OK) return rc;
     if (n_blocks < 0) return PYR_ERR_SHAPE;
+    if (n_blocks > kMostBlocks) return PYR_ERR_UNSUPPORTED;
     const pyr_cache* c = &cache->pool;
     *plan = pyr::plan_cache8_attention(n, n_tokens, n_q_heads, c->n_kv_heads, c->head_dim, within_row(cache, max_len), n_blocks);
     if ((int64_t)n * (n_blocks > 0 ? n_tokens : 1) * plan->col_groups * c->n_kv_heads * plan->waves >= 4 * kMostGroups) return PYR_ERR_UNSUPPORTED;
@@ -173,7 +176,7 @@ int pyr_cache8_select(const pyr_cache8* cache, const void* q, const int32_t* slo
     rc = check_select(cache, n, n_tokens, n_q_heads, max_len, &plan);
     if (rc != PYR_OK) return rc;
     if (n_first < 0 || n_recent < 1 || n_best < 0) return PYR_ERR_SHAPE;
-    if ((int64_t)n_first + n_recent + n_best >= kMost) return PYR_ERR_UNSUPPORTED;
+    if ((int64_t)n_first + n_recent + n_best > kMostBlocks) return PYR_ERR_UNSUPPORTED;
     if (n == 0) return PYR_OK;
     if (!q || !slots || !blocks) return PYR_ERR_NULL;
     if (!aligned16(q)) return PYR_ERR_UNSUPPORTED;

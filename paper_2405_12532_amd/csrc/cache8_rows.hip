@@ -188,10 +188,10 @@ __device__ __forceinline__ Piece piece_of(const AppendArgs& a, int place) {
 }
 
 // Pieces of any length.  A wavefront goes through items: K, V or Q of the piece's block and a head.
+template <int D>
+constexpr int append_waves = D == 64 ? 4 : 2;                     // of a SIMD, as registers allow (128 channels as they are: three spill, 58.7 us for 57.3)
 template <int D, int kTurn>
-constexpr int append_waves = D == 64 ? 4 : kTurn == kAsIs ? 3 : 2;      // of a SIMD, as registers allow
-template <int D, int kTurn>
-__global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn>)) void cache8_append_kernel(AppendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, append_waves<D>) void cache8_append_kernel(AppendArgs a) {
     constexpr int kLanes = D / 8, kTokens = 64 / kLanes, kLoads = 32 / kTokens;      // lanes of a row, rows of a load, loads of a block
     constexpr int kRow = D + 16;                                  // bytes of a token's codes in LDS
     __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : 32][kTurn == kAsIs ? 1 : D / 2];
@@ -671,7 +671,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_load_kernel(LoadArgs a) {
 
 // The page of a parent that is filled in part, as it is.  grid: (n, pieces of a page)
 __global__ __launch_bounds__(256) void cache8_fork_copy_kernel(CacheView c, const int32_t* __restrict__ parents, const int32_t* __restrict__ children,
-                                                               const int32_t* __restrict__ status, uint32_t page_chunks) {
+                                                               const int32_t* __restrict__ status, uint32_t page_chunks, uint32_t piece_chunks) {
     const int state = *status, parent = parents[blockIdx.x], child = children[blockIdx.x];
     if (state != 0 || parent < 0) return;
     const int len = cache_len(c, parent), full = len >> c.shift;
@@ -681,14 +681,16 @@ __global__ __launch_bounds__(256) void cache8_fork_copy_kernel(CacheView c, cons
     const u32x4* from = (const u32x4*)c.pages + (int64_t)src * page_chunks;
     u32x4* to = (u32x4*)c.pages + (int64_t)dst * page_chunks;
     constexpr int kMany = 4;
-    const uint32_t first = blockIdx.y * (256 * kMany) + threadIdx.x;
-    u32x4 x[kMany];
+    const uint32_t end = min(page_chunks, (blockIdx.y + 1) * piece_chunks);
+    for (uint32_t first = blockIdx.y * piece_chunks + threadIdx.x; first < end; first += 256 * kMany) {
+        u32x4 x[kMany];
 #pragma unroll
-    for (int k = 0; k < kMany; ++k)
-        if (first + 256 * k < page_chunks) x[k] = from[first + 256 * k];
+        for (int k = 0; k < kMany; ++k)
+            if (first + 256 * k < end) x[k] = from[first + 256 * k];
 #pragma unroll
-    for (int k = 0; k < kMany; ++k)
-        if (first + 256 * k < page_chunks) to[first + 256 * k] = x[k];
+        for (int k = 0; k < kMany; ++k)
+            if (first + 256 * k < end) to[first + 256 * k] = x[k];
+    }
 }
 
 template <int D, int kTurn>
@@ -705,7 +707,7 @@ void launch_append(const AppendArgs& a, int64_t pieces, hipStream_t stream) {
     }
     // workgroups of many items share one reckoning of the turns and have rows in flight, but few pieces need all the workgroups they can get
     const int64_t items = 2 * a.c.n_kv_heads + a.n_q_heads, most = (items + kWaves - 1) / kWaves;
-    constexpr int64_t kTwice = 2 * 256 * append_waves<D, kTurn>;  // twice the workgroups that the chip holds
+    constexpr int64_t kTwice = 2 * 256 * append_waves<D>;  // twice the workgroups that the chip holds
     int64_t each = pieces * most / kTwice;                        // items of a wavefront
     if (each < 1) each = 1;
     x.head_groups = (int32_t)((most + each - 1) / each);
@@ -748,7 +750,8 @@ int launch_cache8_fork_copy(const CacheView& c, int32_t head_dim, const int32_t*
                             hipStream_t stream) {
     if (n == 0) return PYR_OK;
     const uint32_t chunks = (uint32_t)(cache8_page_bytes(head_dim, c.n_kv_heads, 1 << (c.shift - 5)) / 16);
-    hipLaunchKernelGGL(cache8_fork_copy_kernel, dim3((unsigned)n, (chunks + 1023) / 1024), dim3(256), 0, stream, c, parents, children, status, chunks);
+    const uint32_t piece = chunks <= 1024 * 1024 ? 1024 : chunks / 1024;      // (a thousand pieces at most; 2^31 bytes are 2^27 chunks)
+    hipLaunchKernelGGL(cache8_fork_copy_kernel, dim3((unsigned)n, (chunks + piece - 1) / piece), dim3(256), 0, stream, c, parents, children, status, chunks, piece);
     return check_launch();
 }
 

@@ -170,26 +170,26 @@ __device__ __forceinline__ uint32_t keys_of(const SelectArgs& a, const Unit& u, 
     return key;
 }
 
-// grid: (units, chunks of candidates): keys to memory
+// grid: (units, chunks of candidates), a wavefront each: keys to memory
 template <int D>
-__global__ __launch_bounds__(256) void cache8_score_kernel(SelectArgs a) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = a.n_q_heads / a.c.n_kv_heads;
+__global__ __launch_bounds__(64) void cache8_score_kernel(SelectArgs a) {
+    const int lane = threadIdx.x, g = a.n_q_heads / a.c.n_kv_heads;
     Unit u = unit_of(a, blockIdx.x);
     const int32_t* row_pages = a.c.table + (int64_t)max(u.slot, 0) * a.c.max_pages;
     const uint16_t* q = a.q + ((int64_t)u.row * a.n_q_heads + u.head * g) * D;
     uint32_t* keys = a.keys + (int64_t)blockIdx.x * a.max_blocks;
-    const int begin = (int)min((int64_t)a.n_first + (int64_t)blockIdx.y * a.chunk + 64 * wave, (int64_t)a.max_blocks);      // (as unit_of has it, where there are candidates)
+    const int begin = (int)min((int64_t)a.n_first + (int64_t)blockIdx.y * a.chunk, (int64_t)a.max_blocks);      // (u.low, where there are candidates)
     Queries<D> w;
     int page = page_of(a, row_pages, begin + lane);
     w.load(q, 0, g, lane);
     see(a, u);
     if (u.high - u.low <= a.n_best) return;
-    const int end = (int)min((int64_t)u.high, u.low + ((int64_t)blockIdx.y + 1) * a.chunk);
+    const int end = min(u.high, begin + a.chunk);
     if (begin >= end) return;
     w.round(0, g, lane);
-    for (int base = begin; base < end; base += 256) {
+    for (int base = begin; base < end; base += 64) {
         const uint32_t key = keys_of<D>(a, u, w, q, g, base, end, page);
-        if (base + 256 < end) page = page_of(a, row_pages, base + 256 + lane);
+        if (base + 64 < end) page = page_of(a, row_pages, base + 64 + lane);
         if (base + lane < end) keys[base + lane] = key;
     }
 }
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void cache8_select_kernel(SelectArg
     int32_t* out = a.blocks + (int64_t)blockIdx.x * (a.n_first + a.n_recent + a.n_best);
     const int32_t* row_pages = a.c.table + (int64_t)max(u.slot, 0) * a.c.max_pages;
     const uint16_t* q = a.q + ((int64_t)u.row * a.n_q_heads + u.head * g) * D;
-    const int first = min(a.n_first, a.max_blocks) + 64 * wave;      // (as unit_of has it, where there are candidates)
+    const int first = min(a.n_first, a.max_blocks) + 64 * wave;      // (u.low, where there are candidates)
     Queries<D> w;
     const int page = page_of(a, row_pages, first + lane);
     w.load(q, 0, g, lane);
@@ -428,7 +428,9 @@ CacheSelect plan_cache8_select(int32_t n_seqs, int32_t n_tokens, int32_t n_kv_he
     x.max_blocks = (int32_t)blocks;
     x.chunks = 0;
     if (blocks > kAtOnce || (units < 128 && blocks > kAlone)) {
-        x.chunk = (int32_t)((blocks / 4096 + 256) / 256 * 256);
+        // 64 candidates a wavefront while that leaves the chip room, else as many as keep one reckoning of the queries worth it
+        x.chunk = units * blocks <= 64 * 16384 ? 64 : 256;
+        while ((blocks + x.chunk - 1) / x.chunk > 32768) x.chunk *= 2;
         x.chunks = (int32_t)((blocks + x.chunk - 1) / x.chunk);
         x.key_bytes = (size_t)units * blocks * sizeof(uint32_t);
     }
@@ -441,8 +443,8 @@ int launch_cache8_select(const CacheSelect& x, const CacheView& c, int32_t head_
     const unsigned units = (unsigned)((int64_t)n_seqs * n_tokens * c.n_kv_heads);
     if (x.chunks > 0 && n_best > 0) {
         const dim3 grid(units, (unsigned)x.chunks);
-        if (head_dim == 128) hipLaunchKernelGGL((cache8_score_kernel<128>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((cache8_score_kernel<64>), grid, dim3(256), 0, stream, a);
+        if (head_dim == 128) hipLaunchKernelGGL((cache8_score_kernel<128>), grid, dim3(64), 0, stream, a);
+        else hipLaunchKernelGGL((cache8_score_kernel<64>), grid, dim3(64), 0, stream, a);
         const int rc = check_launch();
         if (rc != PYR_OK) return rc;
     }

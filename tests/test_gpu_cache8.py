@@ -298,6 +298,32 @@ def test_attention_with_large_and_growing_logits(lib, d):
     check_attention(pair, q, [0, 1, 2], *attend(pair, qt, [0, 1, 2], 2, 600, scale=1.0), scale=1.0)
 
 
+@pytest.mark.parametrize("d,hq,tokens", [(128, 8, 1), (64, 8, 3), (128, 24, 2)])
+@pytest.mark.parametrize("lens", [[500, 1, 33], [2000, 64, 7]])
+def test_attention_over_the_largest_and_the_smallest_numbers(lib, d, hq, tokens, lens):
+    """V up to where a sum of its numbers times the weights may still be taken: finite and right; beyond it a number or NaN, never an infinity.  V down to the
+    least: every product keeps to fp32's normal range, as P is not below 2^-20 here."""
+    for power, scale in ((127 + 97, 0.02), (27, 0.02)):
+        pair = Pair8(lib, lens, 2, d, 32, powers=(118, 119))
+        for s, S in enumerate(lens):
+            for c in range(-(-S // 32)):
+                for h in range(2):
+                    pair.o.block(pair.o.table[s, c], h, c)[2][1] = power
+        pair.up()
+        qt, q = bf16(pair.rng.normal(size=(3, tokens, hq, d)) * scale)
+        out, lse = attend(pair, qt, [0, 1, 2], tokens, max(lens))
+        up = 2.0 ** (127 - power)                                                        # (the bounds have an absolute part)
+        reads = {s: (k, v * up) for s, (k, v) in ((s, pair.o.read(s)) for s in range(3))}
+        check_attention(pair, q, [0, 1, 2], out.double() * up, lse, reads=reads)
+    for s, S in enumerate(lens):
+        for c in range(-(-S // 32)):
+            for h in range(2):
+                pair.o.block(pair.o.table[s, c], h, c)[2][1] = 246
+    pair.up()
+    out, _ = attend(pair, qt, [0, 1, 2], tokens, max(lens))
+    assert not torch.isinf(out.float()).any()
+
+
 @pytest.mark.parametrize("d,hq,tokens", [(128, 2, 1), (64, 4, 3), (128, 24, 2)])
 def test_numbers_that_are_none_reach_the_rows_that_see_them_alone(lib, d, hq, tokens):
     """V's: one channel of the rows that see the token, whatever their weights; K's: all of those rows.  Behind the last token every byte is a NaN."""
@@ -364,6 +390,38 @@ def test_select(lib, lens, hq, hkv, d, page, tokens):
         for b, s in enumerate(slots):
             want = pair.o.select(q[b], s if s < len(lens) else -1, first, recent, best, most)
             assert np.array_equal(got[b], want), (b, first, recent, best, most)
+
+
+def test_select_of_more_blocks_than_a_workgroup_holds(lib):
+    """140000 tokens: 4375 blocks, whose keys are looked through in two passes; and the attention over what is chosen."""
+    pair = Pair8(lib, [140000, 50], 1, 64, 1024, powers=(117, 119))
+    qt, q = bf16(pair.rng.normal(size=(2, 1, 2, 64)) * 0.1)
+    for first, recent, best, most in ((1, 2, 5, 140000), (0, 1, 300, 140000), (5, 1, 4100, 140000), (0, 1, 4374, 2 ** 31 - 1), (3, 3, 4000, 135000), (4200, 1, 20, 140000), (9999, 1, 20, 140000)):
+        got = select(pair, qt, [0, 1], 1, most, first, recent, best)
+        for b in (0, 1):
+            assert np.array_equal(got[b].cpu().numpy(), pair.o.select(q[b], b, first, recent, best, most)), (first, recent, best, most, b)
+    blocks = select(pair, qt, [0, 1], 1, 140000, 1, 2, 120)
+    check_attention(pair, q, [0, 1], *attend(pair, qt, [0, 1], 1, 140000, blocks), blocks=blocks.cpu().numpy())
+
+
+@pytest.mark.parametrize("n", [1, 200])
+def test_select_of_thousands_of_ties(lib, n):
+    """Blocks that score alike by the hundred, in one workgroup's lanes and through memory."""
+    pair = Pair8(lib, [64], 1, 64, 64, n_slots=n, max_pages=1100, powers=(115, 116))
+    pair.o.table[:], pair.o.lens[:] = pair.o.table[0, 0], 64 * 1100 - 5                  # (the one page again and again)
+    pair.up()
+    qt, q = bf16(pair.rng.normal(size=(n, 1, 1, 64)))
+    few = pair.o.select(q[0], 0, 0, 1, 1)                                                # which of the page's two blocks scores higher
+    for best in (1, 700, 1100, 1101, 2000):
+        got = select(pair, qt, list(range(n)), 1, 64 * 1100, 0, 1, best).cpu().numpy()
+        even = int(few[0, 0, 0]) % 2 == 0
+        order = list(range(0 if even else 1, 2199, 2)) + list(range(1 if even else 0, 2199, 2))
+        assert got[0, 0, 0, :best + 1].tolist() == sorted(order[:best]) + [2199], best
+        if n > 1:
+            scores = [pair.o._score(q[7, 0, 0], pair.o.block(pair.o.table[0, 0], 0, c)) for c in (0, 1)]
+            even = scores[0] >= scores[1]
+            order = list(range(0 if even else 1, 2199, 2)) + list(range(1 if even else 0, 2199, 2)) if scores[0] != scores[1] else list(range(2199))
+            assert got[7, 0, 0, :best + 1].tolist() == sorted(order[:best]) + [2199], best
 
 
 @pytest.mark.parametrize("n,d", [(1, 64), (40, 128)])

@@ -128,7 +128,7 @@ def test_rows_and_sizes_that_cannot_be():
         return call("pyr_cache8_select", of, q, slots, n, tokens, hq, most, first, recent, best, blocks, ws, size, None)
     assert select(q=None) == NULL and select(slots=None) == NULL and select(blocks=None) == NULL and select(q=0x1008) == UNSUPPORTED
     assert select(tokens=0) == SHAPE and select(most=-1) == SHAPE and select(first=-1) == SHAPE and select(recent=0) == SHAPE and select(best=-1) == SHAPE
-    assert select(hq=6) == UNSUPPORTED and select(n=1 << 23, tokens=2) == UNSUPPORTED and select(first=1 << 30, best=1 << 30) == UNSUPPORTED
+    assert select(hq=6) == UNSUPPORTED and select(n=1 << 23, tokens=2) == UNSUPPORTED and select(first=1 << 30, best=1 << 30) == UNSUPPORTED and select(best=1 << 26) == UNSUPPORTED
     long = ctypes.byref(cache(n_pages=4096, max_pages=1024))
     assert select(of=long, n=1, most=65536, ws=None) == WORKSPACE and select(of=long, n=1, most=65536, size=100) == WORKSPACE and select(of=long, n=1, most=65536, ws=0x180) == WORKSPACE
 
@@ -136,5 +136,5 @@ def test_rows_and_sizes_that_cannot_be():
         return call("pyr_cache8_attention", of, q, 0x2000, n, tokens, hq, most, 0.0, blocks, width, out, None, ws, size, None)
     assert attention(q=None) == NULL and attention(out=None) == NULL and attention(q=0x1008) == UNSUPPORTED
     assert attention(tokens=0) == SHAPE and attention(most=-1) == SHAPE and attention(width=-1) == SHAPE and attention(width=3) == SHAPE
-    assert attention(blocks=0x4000) == SHAPE and attention(hq=6) == UNSUPPORTED and attention(n=1 << 23, tokens=1 << 9) == UNSUPPORTED
+    assert attention(blocks=0x4000) == SHAPE and attention(blocks=0x4000, width=(1 << 26) + 1) == UNSUPPORTED and attention(hq=6) == UNSUPPORTED and attention(n=1 << 23, tokens=1 << 9) == UNSUPPORTED
     assert attention(of=long, n=1, most=65536, ws=None) == WORKSPACE and attention(of=long, n=1, most=65536, size=100) == WORKSPACE
