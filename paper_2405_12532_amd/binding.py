@@ -449,16 +449,24 @@ def cache8_fork(cache, parents, children, n, status, stream=None):
     _check(load().pyr_cache8_fork(ctypes.byref(cache), _ptr(parents), _ptr(children), int(n), _ptr(status), _stream(stream)), "pyr_cache8_fork")
 
 
+# The calls that a step makes for every layer: addresses taken and the status looked at in place, sizes plain ints (ctypes refuses others), which is 0.2 to
+# 0.3 us less of the host's 1.8 to 2.6 in front of a launch.
 def cache8_append(cache, k, v, k_stride, v_stride, n_rows, row_idx, n_list, offsets, slots, start, n, max_new, rotation=None, q=None, q_stride=0,
                   n_q_heads=0, q_out=None, stream=None):
-    _check(load().pyr_cache8_append(ctypes.byref(cache), _ptr(k), _ptr(v), int(k_stride), int(v_stride), int(n_rows), _ptr(row_idx), int(n_list),
-                                    _ptr(offsets), _ptr(slots), _ptr(start), int(n), int(max_new), None if rotation is None else ctypes.byref(rotation),
-                                    _ptr(q), int(q_stride), int(n_q_heads), _ptr(q_out), _stream(stream)), "pyr_cache8_append")
+    status = load().pyr_cache8_append(
+        ctypes.byref(cache), k.data_ptr(), v.data_ptr(), k_stride, v_stride, n_rows, None if row_idx is None else row_idx.data_ptr(), n_list, offsets.data_ptr(),
+        slots.data_ptr(), start.data_ptr(), n, max_new, None if rotation is None else ctypes.byref(rotation), None if q is None else q.data_ptr(), q_stride, n_q_heads,
+        None if q_out is None else q_out.data_ptr(), _stream(stream))
+    if status != 0:
+        raise PyrError(status, "pyr_cache8_append")
 
 
 def cache8_load(cache, slots, first, offsets, n, max_len, k_out, v_out, n_rows, stream=None):
-    _check(load().pyr_cache8_load(ctypes.byref(cache), _ptr(slots), _ptr(first), _ptr(offsets), int(n), int(max_len), _ptr(k_out), _ptr(v_out),
-                                  int(n_rows), _stream(stream)), "pyr_cache8_load")
+    status = load().pyr_cache8_load(
+        ctypes.byref(cache), slots.data_ptr(), None if first is None else first.data_ptr(), offsets.data_ptr(), n, max_len,
+        None if k_out is None else k_out.data_ptr(), None if v_out is None else v_out.data_ptr(), n_rows, _stream(stream))
+    if status != 0:
+        raise PyrError(status, "pyr_cache8_load")
 
 
 def cache8_select_workspace_bytes(cache, n, n_tokens, n_q_heads, max_len) -> int:
@@ -469,8 +477,11 @@ def cache8_select_workspace_bytes(cache, n, n_tokens, n_q_heads, max_len) -> int
 
 
 def cache8_select(cache, q, slots, n, n_tokens, n_q_heads, max_len, n_first, n_recent, n_best, blocks, workspace, workspace_bytes_, stream=None):
-    _check(load().pyr_cache8_select(ctypes.byref(cache), _ptr(q), _ptr(slots), int(n), int(n_tokens), int(n_q_heads), int(max_len), int(n_first),
-                                    int(n_recent), int(n_best), _ptr(blocks), _ptr(workspace), int(workspace_bytes_), _stream(stream)), "pyr_cache8_select")
+    status = load().pyr_cache8_select(
+        ctypes.byref(cache), q.data_ptr(), slots.data_ptr(), n, n_tokens, n_q_heads, max_len, n_first, n_recent, n_best, blocks.data_ptr(),
+        None if workspace is None else workspace.data_ptr(), workspace_bytes_, _stream(stream))
+    if status != 0:
+        raise PyrError(status, "pyr_cache8_select")
 
 
 def cache8_attention_workspace_bytes(cache, n, n_tokens, n_q_heads, max_len, n_blocks) -> int:
@@ -482,9 +493,11 @@ def cache8_attention_workspace_bytes(cache, n, n_tokens, n_q_heads, max_len, n_b
 
 def cache8_attention(cache, q, slots, n, n_tokens, n_q_heads, max_len, softmax_scale, blocks, n_blocks, out, lse, workspace, workspace_bytes_,
                      stream=None):
-    _check(load().pyr_cache8_attention(ctypes.byref(cache), _ptr(q), _ptr(slots), int(n), int(n_tokens), int(n_q_heads), int(max_len), float(softmax_scale),
-                                       _ptr(blocks), int(n_blocks), _ptr(out), _ptr(lse), _ptr(workspace), int(workspace_bytes_), _stream(stream)),
-           "pyr_cache8_attention")
+    status = load().pyr_cache8_attention(
+        ctypes.byref(cache), q.data_ptr(), slots.data_ptr(), n, n_tokens, n_q_heads, max_len, softmax_scale, None if blocks is None else blocks.data_ptr(), n_blocks,
+        out.data_ptr(), None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(), workspace_bytes_, _stream(stream))
+    if status != 0:
+        raise PyrError(status, "pyr_cache8_attention")
 
 
 def diag_cache8_attention(cache, n, n_tokens, n_q_heads, max_len, n_blocks) -> PyrCacheRoute:
