@@ -422,7 +422,12 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
     if (p.stored == 0) return;
     const int first = kSlots == 1 ? __builtin_ctz(p.stored) : __builtin_ctz(p.stored) & ~3;      // token of the first slot
     const uint32_t present = p.stored >> first & ((1u << kSlots) - 1);
-    auto empty = [&](int i) { return kSlots > 1 && (present >> i & 1) == 0; };
+    // four slots at a time are worked through, or none of them; one without a token has what the first one with a token has (which changes no largest and no smallest,
+    // and is not written)
+    const int lead = kSlots == 1 ? 0 : __builtin_ctz(present);
+    auto empty = [&](int g) { return kSlots > 1 && (present >> g & 15) == 0; };
+    auto held = [&](int i) { return kSlots == 1 || (present >> i & 1) != 0; };
+    auto source = [&](int i) { return held(i) ? i : lead; };
     const bool of_q = group >= kv_groups;
     const int heads = of_q ? a.n_q_heads : a.c.n_kv_heads, wanted_head = (of_q ? group - kv_groups : group) * kHeads + lane / kLanes;
     const bool real = wanted_head < heads;
@@ -430,15 +435,18 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
     u32x4 kx[kSlots], vx[kSlots];
     int rows[kSlots];
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i) {
-        if (empty(i)) continue;
-        rows[i] = __builtin_amdgcn_readlane(p.from, first + i);
-        const int64_t row = max(rows[i], 0);
-        if (of_q) {
-            if (heads > 0) kx[i] = __builtin_nontemporal_load((const u32x4*)a.q + row * a.q_stride + head * kLanes + piece);
-        } else {
-            kx[i] = __builtin_nontemporal_load((const u32x4*)a.k + row * a.k_stride + head * kLanes + piece);
-            vx[i] = __builtin_nontemporal_load((const u32x4*)a.v + row * a.v_stride + head * kLanes + piece);
+    for (int g = 0; g < kSlots; g += 4) {
+        if (empty(g)) continue;
+#pragma unroll
+        for (int i = g; i < g + 4 && i < kSlots; ++i) {
+            rows[i] = __builtin_amdgcn_readlane(p.from, first + source(i));
+            const int64_t row = max(rows[i], 0);
+            if (of_q) {
+                if (heads > 0) kx[i] = __builtin_nontemporal_load((const u32x4*)a.q + row * a.q_stride + head * kLanes + piece);
+            } else {
+                kx[i] = __builtin_nontemporal_load((const u32x4*)a.k + row * a.k_stride + head * kLanes + piece);
+                vx[i] = __builtin_nontemporal_load((const u32x4*)a.v + row * a.v_stride + head * kLanes + piece);
+            }
         }
     }
     const Page8<D> at(a.c, p.page);
@@ -457,47 +465,64 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
         const int pair = lane % kPairsOf;
         const float freq = pair < a.dims / 2 ? a.freqs[pair] : 0.f;
         const int position = p.from >= 0 ? a.positions[p.from] : 0;
-        for (int i = wave; i < kSlots; i += kWaves) {
-            if (empty(i)) continue;
-            const f32x2 turn = turn_of(__builtin_amdgcn_readlane(position, first + i), freq);
-            if (lane < a.dims / 2) turns[i][pair] = turn;
+        if constexpr (kSlots == 1) {
+            if (wave == 0) {
+                const f32x2 turn = turn_of(__builtin_amdgcn_readlane(position, first), freq);
+                if (lane < a.dims / 2) turns[0][pair] = turn;
+            }
+        } else {
+            f32x2 turn[kSlots / kWaves];                          // (of tokens that are not there, too: side by side they take no longer)
+#pragma unroll
+            for (int i = 0; i < kSlots / kWaves; ++i) turn[i] = turn_of(__builtin_amdgcn_readlane(position, first + wave + kWaves * i), freq);
+#pragma unroll
+            for (int i = 0; i < kSlots / kWaves; ++i)
+                if (lane < a.dims / 2) turns[wave + kWaves * i][pair] = turn[i];
         }
         __syncthreads();
     }
     if (of_q) {
 #pragma unroll
-        for (int i = 0; i < kSlots; ++i) {
-            if (empty(i)) continue;
-            float x[8];
-            turned<kTurn>(kx[i], turns[kTurn == kAsIs ? 0 : i], a.dims, piece, x);
-            if (real && rows[i] >= 0) __builtin_nontemporal_store(rounded(x), (u32x4*)a.q_out + ((int64_t)rows[i] * a.n_q_heads + head) * kLanes + piece);
+        for (int g = 0; g < kSlots; g += 4) {
+            if (empty(g)) continue;
+#pragma unroll
+            for (int i = g; i < g + 4 && i < kSlots; ++i) {
+                float x[8];
+                turned<kTurn>(kx[i], turns[kTurn == kAsIs ? 0 : source(i)], a.dims, piece, x);
+                if (real && held(i) && rows[i] >= 0) __builtin_nontemporal_store(rounded(x), (u32x4*)a.q_out + ((int64_t)rows[i] * a.n_q_heads + head) * kLanes + piece);
+            }
         }
         return;
     }
     float x[kSlots][8];
     uint32_t ktop = 0, vtop = 0;
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i) {
-        if (empty(i)) continue;
-        turned<kTurn>(kx[i], turns[kTurn == kAsIs ? 0 : i], a.dims, piece, x[i]);
-        if (rows[i] < 0) {
+    for (int g = 0; g < kSlots; g += 4) {
+        if (empty(g)) continue;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = NAN;
-            vx[i] = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+        for (int i = g; i < g + 4 && i < kSlots; ++i) {
+            turned<kTurn>(kx[i], turns[kTurn == kAsIs ? 0 : source(i)], a.dims, piece, x[i]);
+            if (rows[i] < 0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[i][e] = NAN;
+                vx[i] = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+            }
+            raise(ktop, x[i]);
+            raise(vtop, vx[i]);
         }
-        raise(ktop, x[i]);
-        raise(vtop, vx[i]);
     }
     const bool special = __builtin_amdgcn_ballot_w64(ktop > kNoNumber || vtop > kNoNumber) != 0;
     if (special) {
         ktop = vtop = 0;
 #pragma unroll
-        for (int i = 0; i < kSlots; ++i) {
-            if (empty(i)) continue;
+        for (int g = 0; g < kSlots; g += 4) {
+            if (empty(g)) continue;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                raise_finite(ktop, x[i][e]);
-                raise_finite(vtop, e & 1 ? high_of(vx[i][e >> 1]) : low_of(vx[i][e >> 1]));
+            for (int i = g; i < g + 4 && i < kSlots; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    raise_finite(ktop, x[i][e]);
+                    raise_finite(vtop, e & 1 ? high_of(vx[i][e >> 1]) : low_of(vx[i][e >> 1]));
+                }
             }
         }
     }
@@ -519,12 +544,18 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
             up[e] = -INFINITY;
             down[e] = INFINITY;
             none[e] = false;
+        }
 #pragma unroll
-            for (int i = 0; i < kSlots; ++i) {
-                if (empty(i)) continue;
-                up[e] = fmaxf(up[e], x[i][e]);
-                down[e] = fminf(down[e], x[i][e]);
-                if (special) none[e] |= !(fabsf(x[i][e]) <= __uint_as_float(kNoNumber));
+        for (int g = 0; g < kSlots; g += 4) {
+            if (empty(g)) continue;
+#pragma unroll
+            for (int i = g; i < g + 4 && i < kSlots; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    up[e] = fmaxf(up[e], x[i][e]);
+                    down[e] = fminf(down[e], x[i][e]);
+                    if (special) none[e] |= !(fabsf(x[i][e]) <= __uint_as_float(kNoNumber));
+                }
             }
         }
         u32x2 out_up, out_down;
@@ -556,12 +587,15 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
     const uint32_t kplace = ((piece >> 3) * 4 + (piece >> 1 & 3)) * 256 + (piece & 1) * 8;
     u32x2 v8[kSlots];
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i) {
-        if (empty(i)) continue;
-        const int t = first + i;
-        const u32x2 k8 = codes_of(x[i], kscale);
-        v8[i] = codes_of(vx[i], vscale);
-        if (real) *(u32x2*)(codes + (t >> 4) * (16 * D) + kplace + (t & 15) * 16) = k8;
+    for (int g = 0; g < kSlots; g += 4) {
+        if (empty(g)) continue;
+#pragma unroll
+        for (int i = g; i < g + 4 && i < kSlots; ++i) {
+            const int t = first + i;
+            const u32x2 k8 = codes_of(x[i], kscale);
+            v8[i] = codes_of(vx[i], vscale);
+            if (real && held(i)) *(u32x2*)(codes + (t >> 4) * (16 * D) + kplace + (t & 15) * 16) = k8;
+        }
     }
     if (!real) return;
     // four tokens' bytes of a channel lie side by side

@@ -144,28 +144,37 @@ __device__ __forceinline__ uint32_t keys_of(const SelectArgs& a, const Unit& u, 
         for (int i = 0; i < 2 * kHalf; ++i) bounds[s][i] = from[4 * i];
     }
     const int block_power = (int)(*Page8<D>(a.c, page).powers(u.head, block) & 255) - 127;
-    uint32_t key = 0;
+    int of_block[4];
+    float best[4];
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-        const int of_block = __shfl(block_power, 16 * s + t);
-        float best = -INFINITY;
-        for (int first = 0; first < g; first += 16) {
-            if (g > 16) {
-                w.load(q, first, g, lane);
-                w.round(first, g, lane);
-            }
+        of_block[s] = __shfl(block_power, 16 * s + t) + 2;
+        best[s] = -INFINITY;
+    }
+#pragma unroll 1
+    for (int first = 0; first < g; first += 16) {
+        if (g > 16) {
+            w.load(q, first, g, lane);
+            w.round(first, g, lane);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
             i32x4 d = {0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < 2 * kHalf; ++i) d = __builtin_amdgcn_mfma_i32_16x16x64_i8(w.whole[i], bounds[s][i], d, 0, 0, 0);
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-                const int e = min(max(w.power[x] + of_block + 2, -120), 100);
+                const int e = min(max(w.power[x] + of_block[s], -120), 100);
                 const float score = (float)d[x] * __uint_as_float((uint32_t)(127 + e) << 23);
-                best = fmaxf(best, w.power[x] == Queries<D>::kNone ? -INFINITY : score);
+                best[s] = fmaxf(best[s], w.power[x] == Queries<D>::kNone ? -INFINITY : score);
             }
         }
-        best = max_of_groups(best);
-        if (j == s) key = key_of(best);
+    }
+    uint32_t key = 0;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        const uint32_t y = key_of(max_of_groups(best[s]));
+        if (j == s) key = y;
     }
     return key;
 }
@@ -309,16 +318,21 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_select_many_kernel(SelectA
         see(a, u);
         if (sure_blocks<kThreads>(a, u, out)) return;
         w.round(0, g, lane);
-#pragma unroll
+        // (through LDS, so that the code for a block is there once)
+        __shared__ uint32_t held[kPer][kThreads];
+#pragma unroll 1
         for (int i = 0; i < kPer; ++i) {
             const int base = first + kThreads * i, next = base + kThreads;
-            keys[i] = 0;
+            uint32_t key = 0;
             if (base < u.high) {
-                keys[i] = keys_of<D>(a, u, w, q, g, base, u.high, page);
-                if (base + lane >= u.high) keys[i] = 0;
+                key = keys_of<D>(a, u, w, q, g, base, u.high, page);
+                if (base + lane >= u.high) key = 0;
                 if (i + 1 < kPer && next < u.high) page = page_of(a, row_pages, next + lane);
             }
+            held[i][threadIdx.x] = key;
         }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) keys[i] = held[i][threadIdx.x];
     }
     const int passes = kScored ? (u.high - u.low + 4095) / 4096 : 1;
     auto each = [&](auto f) {                                 // over all keys that there are
