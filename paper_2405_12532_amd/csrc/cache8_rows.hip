@@ -102,16 +102,7 @@ __device__ __forceinline__ u32x4 rounded(const float (&x)[8]) {
     return __builtin_bit_cast(u32x4, y);
 }
 
-// The largest magnitudes, as bits: what is no number is above all others.
-__device__ __forceinline__ void raise(uint32_t& top, const float (&x)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-}
-__device__ __forceinline__ void raise(uint32_t& top, u32x4 words) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) top = max(top, max(words[e] << 16 & 0x7fff0000u, words[e] & 0x7fff0000u));
-}
-// The same without what is no number.
+// The largest magnitude, as bits, of what is a number.
 __device__ __forceinline__ void raise_finite(uint32_t& top, float x) {
     const uint32_t bits = __float_as_uint(x) & 0x7fffffffu;
     if (bits < 0x7f800000u) top = max(top, bits);
@@ -129,26 +120,24 @@ __device__ __forceinline__ u32x2 codes_of(u32x4 words, float scale) {
     return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 
-// Bounds of eight channels: of the largest and smallest new numbers, of channels that hold a number without a code, and of what the block held (grown by 2^grow).
-__device__ __forceinline__ void bounds_of(const float (&up)[8], const float (&down)[8], const bool (&none)[8], float scale, bool behind, u32x2 old_up, u32x2 old_down, int grow,
-                                          u32x2& out_up, u32x2& out_down) {
+// Bounds of eight channels: of a token's codes (none: a number without one), and of what the block held (grown by 2^grow).
+__device__ __forceinline__ void bounds_of(u32x2 codes, const bool (&none)[8], bool behind, u32x2 old_up, u32x2 old_down, int grow, u32x2& up, u32x2& down) {
     const float shrink = __uint_as_float((uint32_t)(127 - grow) << 23);
-    out_up = out_down = u32x2{};
+    up = down = u32x2{};
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
-        const uint32_t c = codes8_of(up[e], up[e + 1], down[e], down[e + 1], scale);
-        const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, false), r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, true);
+        const f32x2 y = e & 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes[e >> 2], 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes[e >> 2], 1.f, false);
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
             const int n = e + f;
-            float largest = none[n] ? 127.f : __builtin_ceilf(p[f] * 0.25f), smallest = none[n] ? -127.f : __builtin_floorf(r[f] * 0.25f);
+            float largest = none[n] ? 127.f : __builtin_ceilf(y[f] * 0.25f), smallest = none[n] ? -127.f : __builtin_floorf(y[f] * 0.25f);
             if (behind) {
                 const int o = (int8_t)(old_up[n >> 2] >> (8 * (n & 3))), u = (int8_t)(old_down[n >> 2] >> (8 * (n & 3)));
                 largest = fmaxf(largest, __builtin_ceilf((float)o * shrink));
                 smallest = fminf(smallest, __builtin_floorf((float)u * shrink));
             }
-            out_up[n >> 2] |= ((uint32_t)(int)largest & 255) << (8 * (n & 3));
-            out_down[n >> 2] |= ((uint32_t)(int)smallest & 255) << (8 * (n & 3));
+            up[n >> 2] |= ((uint32_t)(int)largest & 255) << (8 * (n & 3));
+            down[n >> 2] |= ((uint32_t)(int)smallest & 255) << (8 * (n & 3));
         }
     }
 }
@@ -187,12 +176,15 @@ __device__ __forceinline__ Piece piece_of(const AppendArgs& a, int place) {
     return p;
 }
 
-// Pieces of any length.  A wavefront goes through items: K, V or Q of the piece's block and a head.
-template <int D>
-constexpr int append_waves = D == 64 ? 4 : 2;                     // of a SIMD, as registers allow (128 channels as they are: three spill, 58.7 us for 57.3)
-template <int D, int kTurn>
-__global__ __launch_bounds__(64 * kWaves, append_waves<D>) void cache8_append_kernel(AppendArgs a) {
-    constexpr int kLanes = D / 8, kTokens = 64 / kLanes, kLoads = 32 / kTokens;      // lanes of a row, rows of a load, loads of a block
+// Pieces of any length.  A wavefront goes through items: K, V or Q of the piece's block and a head.  kShort: nine tokens at most, which a window of 12 (at 64
+// channels 16) tokens of the block holds.
+template <int D, int kTurn, bool kShort>
+constexpr int append_waves = kShort || D == 64 ? 4 : 2;      // of a SIMD, as registers allow (128 channels as they are: three spill)
+template <int D, int kTurn, bool kShort>
+__global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void cache8_append_kernel(AppendArgs a) {
+    constexpr int kLanes = D / 8, kTokens = 64 / kLanes;          // lanes of a row, rows of a load
+    constexpr bool kEarly = kShort || D == 128;                   // what a block holds is asked for with the rows (at 64 channels longer pieces have no registers for it)
+    constexpr int kWindow = !kShort ? 32 : D == 128 ? 12 : 16, kLoads = kWindow / kTokens;
     constexpr int kRow = D + 16;                                  // bytes of a token's codes in LDS
     __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : 32][kTurn == kAsIs ? 1 : D / 2];
     __shared__ __align__(16) uint8_t all_staged[kWaves][32][kRow];
@@ -207,7 +199,8 @@ __global__ __launch_bounds__(64 * kWaves, append_waves<D>) void cache8_append_ke
     // the row that a lane reads in load i: of a token that is not stored the first one's (what it computes changes no largest and no smallest, and is not
     // written)
     const int first = __builtin_ctz(stored);
-    auto token_of = [&](int i) { return i * kTokens + lane / kLanes; };
+    const int window = kShort ? min(first & ~3, 32 - kWindow) : 0;      // its first token
+    auto token_of = [&](int i) { return window + i * kTokens + lane / kLanes; };
     auto source_of = [&](int i) { return stored >> token_of(i) & 1 ? token_of(i) : first; };
     auto there_of = [&](int i) { return (there >> source_of(i) & 1) != 0; };
     int rows[kLoads];
@@ -281,6 +274,13 @@ __global__ __launch_bounds__(64 * kWaves, append_waves<D>) void cache8_append_ke
             uint8_t* const codes = at.codes(item, block);
             uint8_t* const power_at = (uint8_t*)at.powers(item, block);
             const int old_power = behind ? *power_at : 0;
+            int8_t* const bounds = (int8_t*)at.bounds(item, block) + (lane >> 5) * D + 8 * piece + (lane >> 4 & 1);      // (whose, below)
+            int old_bounds[4] = {};
+            auto look = [&] {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) old_bounds[e] = bounds[2 * e];
+            };
+            if (kEarly && behind) look();
             constexpr bool kExpanded = kTurn != kAsIs;            // in fp32
             float x[kExpanded ? kLoads : 1][8];
             auto number = [&](int i, int e) { return kExpanded ? x[kExpanded ? i : 0][e] : e & 1 ? high_of(words[i][e >> 1]) : low_of(words[i][e >> 1]); };
@@ -290,13 +290,13 @@ __global__ __launch_bounds__(64 * kWaves, append_waves<D>) void cache8_append_ke
 #pragma unroll
             for (int i = 0; i < kLoads; i += 2) {
 #pragma unroll
-                for (int n = i; n < i + 2; ++n) {
+                for (int n = i; n < i + 2 && n < kLoads; ++n) {
                     if (gone && !there_of(n)) words[n] = kNoRow;
                     if (kExpanded) turned<kTurn>(words[n], turns_of(source_of(n)), a.dims, piece, x[kExpanded ? n : 0]);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float y = number(i, e), z = number(i + 1, e);
+                    const float y = number(i, e), z = i + 1 < kLoads ? number(i + 1 < kLoads ? i + 1 : i, e) : y;
                     up[e] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(up[e], y), z);
                     down[e] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(down[e], -y), -z);
                 }
@@ -336,14 +336,14 @@ __global__ __launch_bounds__(64 * kWaves, append_waves<D>) void cache8_append_ke
             }
             const uint32_t c = codes8_of(four[0], four[1], four[2], four[3], scale);
             const f32x2 y = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, false), z = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, 1.f, true);
-            int8_t* const bounds = (int8_t*)at.bounds(item, block) + (lane >> 5) * D + 8 * piece + (lane >> 4 & 1);
+            if (!kEarly && behind) look();
             const float shrink = __uint_as_float((uint32_t)(127 - grow) << 23);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float code = e < 2 ? y[e & 1] : z[e & 1];
                 float bound = code != code ? 127.f : __builtin_ceilf(code * 0.25f);
                 if (behind) {
-                    const float old = (float)bounds[2 * e];
+                    const float old = (float)old_bounds[e];
                     bound = fmaxf(bound, __builtin_ceilf((lane < 32 ? old : -old) * shrink));
                 }
                 if (kLanes == 16 || (lane & 8) == 0) bounds[2 * e] = (int8_t)(int)(lane < 32 ? bound : -bound);
@@ -360,6 +360,12 @@ __global__ __launch_bounds__(64 * kWaves, append_waves<D>) void cache8_append_ke
             uint8_t* const codes = at.codes(item - hkv, block) + 32 * D;
             uint8_t* const power_at = (uint8_t*)at.powers(item - hkv, block) + 1;
             const int old_power = behind ? *power_at : 0;
+            u32x4* const lane_words = (u32x4*)codes + lane;
+            u32x4 old[D / 32] = {};                               // of a block that is written in part
+            if (kEarly && stored != kAllTokens) {
+#pragma unroll
+                for (int g = 0; g < D / 32; ++g) old[g] = lane_words[64 * g];
+            }
             uint32_t pair = 0;
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
@@ -381,6 +387,10 @@ __global__ __launch_bounds__(64 * kWaves, append_waves<D>) void cache8_append_ke
             }
             int grow;
             const float scale = settle(top, old_power, power_at, codes, &grow);
+            if (kEarly ? grow > 0 : stored != kAllTokens) {
+#pragma unroll
+                for (int g = 0; g < D / 32; ++g) old[g] = lane_words[64 * g];
+            }
             // in LDS as rows, from where transposing reads give eight tokens of a channel
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) *(u32x2*)&staged[token_of(i)][8 * piece] = codes_of(words[i], scale);
@@ -391,15 +401,13 @@ __global__ __launch_bounds__(64 * kWaves, append_waves<D>) void cache8_append_ke
             for (int i = 0; i < 8; ++i)
                 if ((stored >> (16 * (i >> 2) + 4 * j + (i & 3)) & 1) == 0) keep[i >> 2] |= 0xffu << (8 * (i & 3));
             const uint32_t from = (uint32_t)(uintptr_t)(lptr_t)&staged[16 * (e >> 2) + 4 * j + (e & 3)][8 * (r & 1)];
-            u32x4* const lane_words = (u32x4*)codes + lane;
 #pragma unroll
             for (int g = 0; g < D / 32; ++g) {
                 const i32x2 y = lds_read_tr8(from + 32 * g), z = lds_read_tr8(from + 32 * g + 16);
                 u32x4 word = {(uint32_t)y[0], (uint32_t)y[1], (uint32_t)z[0], (uint32_t)z[1]};
                 if (stored != kAllTokens) {
-                    const u32x4 old = lane_words[64 * g];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) word[i] = (word[i] & ~keep[i & 1]) | (old[i] & keep[i & 1]);
+                    for (int i = 0; i < 4; ++i) word[i] = (word[i] & ~keep[i & 1]) | (old[g][i] & keep[i & 1]);
                 }
                 lane_words[64 * g] = word;
             }
@@ -409,50 +417,33 @@ __global__ __launch_bounds__(64 * kWaves, append_waves<D>) void cache8_append_ke
     }
 }
 
-// The new tokens of a step: D / 8 lanes take a head, so that several heads share a wavefront, all tokens of a channel are in one lane, and nothing has to cross lanes but
-// a power.  A wavefront has one group of heads.  kSlots 1: one token; 12: nine at most, in three groups of four as V's bytes lie.
-template <int D, int kTurn, int kSlots>
-__global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendArgs a) {
+// A step's new token: D / 8 lanes take a head, so that several heads share a wavefront and nothing has to cross lanes but a power.  A wavefront has one group of heads.
+template <int D, int kTurn>
+__global__ __launch_bounds__(64 * kWaves) void cache8_append_one_kernel(AppendArgs a) {
     constexpr int kLanes = D / 8, kHeads = 64 / kLanes;           // lanes of a head, heads of a wavefront
-    __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : kSlots][kTurn == kAsIs ? 1 : D / 2];
+    __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : D / 2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = lane % kLanes;
     const int place = blockIdx.x / a.head_groups, group = (blockIdx.x - place * a.head_groups) * kWaves + wave;
     const int kv_groups = (a.c.n_kv_heads + kHeads - 1) / kHeads;
     const Piece p = piece_of(a, place);
     if (p.stored == 0) return;
-    const int first = kSlots == 1 ? __builtin_ctz(p.stored) : __builtin_ctz(p.stored) & ~3;      // token of the first slot
-    const uint32_t present = p.stored >> first & ((1u << kSlots) - 1);
-    // four slots at a time are worked through, or none of them; one without a token has what the first one with a token has (which changes no largest and no smallest,
-    // and is not written)
-    const int lead = kSlots == 1 ? 0 : __builtin_ctz(present);
-    auto empty = [&](int g) { return kSlots > 1 && (present >> g & 15) == 0; };
-    auto held = [&](int i) { return kSlots == 1 || (present >> i & 1) != 0; };
-    auto source = [&](int i) { return held(i) ? i : lead; };
+    const int t = __builtin_ctz(p.stored), row = __builtin_amdgcn_readlane(p.from, t);
     const bool of_q = group >= kv_groups;
     const int heads = of_q ? a.n_q_heads : a.c.n_kv_heads, wanted_head = (of_q ? group - kv_groups : group) * kHeads + lane / kLanes;
     const bool real = wanted_head < heads;
     const int head = min(wanted_head, max(heads - 1, 0));
-    u32x4 kx[kSlots], vx[kSlots];
-    int rows[kSlots];
-#pragma unroll
-    for (int g = 0; g < kSlots; g += 4) {
-        if (empty(g)) continue;
-#pragma unroll
-        for (int i = g; i < g + 4 && i < kSlots; ++i) {
-            rows[i] = __builtin_amdgcn_readlane(p.from, first + source(i));
-            const int64_t row = max(rows[i], 0);
-            if (of_q) {
-                if (heads > 0) kx[i] = __builtin_nontemporal_load((const u32x4*)a.q + row * a.q_stride + head * kLanes + piece);
-            } else {
-                kx[i] = __builtin_nontemporal_load((const u32x4*)a.k + row * a.k_stride + head * kLanes + piece);
-                vx[i] = __builtin_nontemporal_load((const u32x4*)a.v + row * a.v_stride + head * kLanes + piece);
-            }
-        }
+    const int64_t at_row = max(row, 0);
+    u32x4 kx = {}, vx = {};
+    if (!of_q) {
+        kx = __builtin_nontemporal_load((const u32x4*)a.k + at_row * a.k_stride + head * kLanes + piece);
+        vx = __builtin_nontemporal_load((const u32x4*)a.v + at_row * a.v_stride + head * kLanes + piece);
+    } else if (heads > 0) {
+        kx = __builtin_nontemporal_load((const u32x4*)a.q + at_row * a.q_stride + head * kLanes + piece);
     }
     const Page8<D> at(a.c, p.page);
     uint8_t* const codes = at.codes(head, p.block);
     uint16_t* const powers = at.powers(head, p.block);
-    u32x2* const bounds = (u32x2*)at.bounds(head, p.block) + piece;
+    u32x2* const bounds = (u32x2*)at.bounds(head, p.block) + piece;      // largest; kLanes further the smallest
     uint32_t old_powers = 0;
     u32x2 old_up = {}, old_down = {};
     if (p.behind && !of_q) {
@@ -461,69 +452,40 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
         old_down = bounds[kLanes];
     }
     if constexpr (kTurn != kAsIs) {
-        constexpr int kPairsOf = D / 2;
-        const int pair = lane % kPairsOf;
-        const float freq = pair < a.dims / 2 ? a.freqs[pair] : 0.f;
-        const int position = p.from >= 0 ? a.positions[p.from] : 0;
-        if constexpr (kSlots == 1) {
-            if (wave == 0) {
-                const f32x2 turn = turn_of(__builtin_amdgcn_readlane(position, first), freq);
-                if (lane < a.dims / 2) turns[0][pair] = turn;
-            }
-        } else {
-            f32x2 turn[kSlots / kWaves];                          // (of tokens that are not there, too: side by side they take no longer)
-#pragma unroll
-            for (int i = 0; i < kSlots / kWaves; ++i) turn[i] = turn_of(__builtin_amdgcn_readlane(position, first + wave + kWaves * i), freq);
-#pragma unroll
-            for (int i = 0; i < kSlots / kWaves; ++i)
-                if (lane < a.dims / 2) turns[wave + kWaves * i][pair] = turn[i];
+        if (wave == 0) {
+            const float freq = lane < a.dims / 2 ? a.freqs[lane] : 0.f;
+            const f32x2 turn = turn_of(row >= 0 ? a.positions[row] : 0, freq);
+            if (lane < a.dims / 2) turns[lane] = turn;
         }
         __syncthreads();
     }
+    float x[8];
+    turned<kTurn>(kx, turns, a.dims, piece, x);
     if (of_q) {
-#pragma unroll
-        for (int g = 0; g < kSlots; g += 4) {
-            if (empty(g)) continue;
-#pragma unroll
-            for (int i = g; i < g + 4 && i < kSlots; ++i) {
-                float x[8];
-                turned<kTurn>(kx[i], turns[kTurn == kAsIs ? 0 : source(i)], a.dims, piece, x);
-                if (real && held(i) && rows[i] >= 0) __builtin_nontemporal_store(rounded(x), (u32x4*)a.q_out + ((int64_t)rows[i] * a.n_q_heads + head) * kLanes + piece);
-            }
-        }
+        if (real && row >= 0) __builtin_nontemporal_store(rounded(x), (u32x4*)a.q_out + (at_row * a.n_q_heads + head) * kLanes + piece);
         return;
     }
-    float x[kSlots][8];
-    uint32_t ktop = 0, vtop = 0;
+    if (row < 0) {
 #pragma unroll
-    for (int g = 0; g < kSlots; g += 4) {
-        if (empty(g)) continue;
-#pragma unroll
-        for (int i = g; i < g + 4 && i < kSlots; ++i) {
-            turned<kTurn>(kx[i], turns[kTurn == kAsIs ? 0 : source(i)], a.dims, piece, x[i]);
-            if (rows[i] < 0) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[i][e] = NAN;
-                vx[i] = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-            }
-            raise(ktop, x[i]);
-            raise(vtop, vx[i]);
-        }
+        for (int e = 0; e < 8; ++e) x[e] = NAN;
+        vx = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
     }
+    uint32_t ktop = 0, vtop = 0;                                  // magnitudes, as bits: what is no number is above all others
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ktop = max(ktop, __float_as_uint(x[e]) & 0x7fffffffu);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) vtop = max_u16(vtop, vx[e] & 0x7fff7fffu);
+    vtop = max(vtop & 0xffff0000u, vtop << 16);
     const bool special = __builtin_amdgcn_ballot_w64(ktop > kNoNumber || vtop > kNoNumber) != 0;
+    bool none[8];                                                 // numbers without a code
+#pragma unroll
+    for (int e = 0; e < 8; ++e) none[e] = special && !(fabsf(x[e]) <= __uint_as_float(kNoNumber));
     if (special) {
         ktop = vtop = 0;
 #pragma unroll
-        for (int g = 0; g < kSlots; g += 4) {
-            if (empty(g)) continue;
-#pragma unroll
-            for (int i = g; i < g + 4 && i < kSlots; ++i) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    raise_finite(ktop, x[i][e]);
-                    raise_finite(vtop, e & 1 ? high_of(vx[i][e >> 1]) : low_of(vx[i][e >> 1]));
-                }
-            }
+        for (int e = 0; e < 8; ++e) {
+            raise_finite(ktop, x[e]);
+            raise_finite(vtop, e & 1 ? high_of(vx[e >> 1]) : low_of(vx[e >> 1]));
         }
     }
     int kp = power8_of(__uint_as_float(within_lanes<kLanes>(ktop, larger))), vp = power8_of(__uint_as_float(within_lanes<kLanes>(vtop, larger)));
@@ -535,36 +497,14 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
         kgrow = min(kp - old_kp, 100);
         vgrow = min(vp - old_vp, 100);
     }
-    const float kscale = scale_of(kp), vscale = scale_of(vp);
-    {
-        float up[8], down[8];
-        bool none[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            up[e] = -INFINITY;
-            down[e] = INFINITY;
-            none[e] = false;
-        }
-#pragma unroll
-        for (int g = 0; g < kSlots; g += 4) {
-            if (empty(g)) continue;
-#pragma unroll
-            for (int i = g; i < g + 4 && i < kSlots; ++i) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    up[e] = fmaxf(up[e], x[i][e]);
-                    down[e] = fminf(down[e], x[i][e]);
-                    if (special) none[e] |= !(fabsf(x[i][e]) <= __uint_as_float(kNoNumber));
-                }
-            }
-        }
-        u32x2 out_up, out_down;
-        bounds_of(up, down, none, kscale, p.behind, old_up, old_down, kgrow, out_up, out_down);
-        if (real) {
-            bounds[0] = out_up;
-            bounds[kLanes] = out_down;
-            if (piece == 0) *powers = (uint16_t)(kp | vp << 8);
-        }
+    const float kscale = scale_of(kp);
+    const u32x2 k8 = codes_of(x, kscale), v8 = codes_of(vx, scale_of(vp));
+    u32x2 up, down;
+    bounds_of(k8, none, p.behind, old_up, old_down, kgrow, up, down);
+    if (real) {
+        bounds[0] = up;
+        bounds[kLanes] = down;
+        if (piece == 0) *powers = (uint16_t)(kp | vp << 8);
     }
     if (__builtin_amdgcn_ballot_w64(real && (kgrow > 0 || vgrow > 0)) != 0) {
         const float kby = __uint_as_float((uint32_t)(127 + kgrow) << 23), vby = __uint_as_float((uint32_t)(127 + vgrow) << 23);
@@ -584,51 +524,11 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_few_kernel(AppendAr
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");    // (the bytes are written again below, by other lanes)
         __builtin_amdgcn_s_waitcnt(0);
     }
-    const uint32_t kplace = ((piece >> 3) * 4 + (piece >> 1 & 3)) * 256 + (piece & 1) * 8;
-    u32x2 v8[kSlots];
-#pragma unroll
-    for (int g = 0; g < kSlots; g += 4) {
-        if (empty(g)) continue;
-#pragma unroll
-        for (int i = g; i < g + 4 && i < kSlots; ++i) {
-            const int t = first + i;
-            const u32x2 k8 = codes_of(x[i], kscale);
-            v8[i] = codes_of(vx[i], vscale);
-            if (real && held(i)) *(u32x2*)(codes + (t >> 4) * (16 * D) + kplace + (t & 15) * 16) = k8;
-        }
-    }
     if (!real) return;
-    // four tokens' bytes of a channel lie side by side
-    uint8_t* const vplace = codes + 32 * D + (piece >> 2) * 1024 + (piece & 1) * 128 + (piece >> 1 & 1) * 8;
+    *(u32x2*)(codes + (t >> 4) * (16 * D) + ((piece >> 3) * 4 + (piece >> 1 & 3)) * 256 + (piece & 1) * 8 + (t & 15) * 16) = k8;
+    uint8_t* const to = codes + 32 * D + (piece >> 2) * 1024 + (t >> 2 & 3) * 256 + (piece & 1) * 128 + (piece >> 1 & 1) * 8 + (t >> 4) * 4 + (t & 3);
 #pragma unroll
-    for (int i = 0; i < kSlots; i += 4) {
-        const uint32_t four = present >> i & 15;
-        if (four == 0) continue;
-        uint8_t* const to = vplace + ((first + i) >> 2 & 3) * 256 + ((first + i) >> 4) * 4 + (kSlots == 1 ? first & 3 : 0);
-        auto byte = [&](int n, int e) { return v8[n][e >> 2] >> (8 * (e & 3)) & 255; };
-        if constexpr (kSlots == 1) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) to[16 * e] = (uint8_t)byte(0, e);
-        } else if (four == 15) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) *(uint32_t*)(to + 16 * e) = byte(i, e) | byte(i + 1, e) << 8 | byte(i + 2, e) << 16 | byte(i + 3, e) << 24;
-        } else {
-#pragma unroll
-            for (int n = 0; n < 4; n += 2) {
-                if ((four >> n & 3) == 3) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) *(uint16_t*)(to + 16 * e + n) = (uint16_t)(byte(i + n, e) | byte(i + n + 1, e) << 8);
-                } else {
-#pragma unroll
-                    for (int m = n; m < n + 2; ++m) {
-                        if ((four >> m & 1) == 0) continue;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) to[16 * e + m] = (uint8_t)byte(i + m, e);
-                    }
-                }
-            }
-        }
-    }
+    for (int e = 0; e < 8; ++e) to[16 * e] = (uint8_t)(v8[e >> 2] >> (8 * (e & 3)));
 }
 
 struct LoadArgs {
@@ -727,25 +627,28 @@ __global__ __launch_bounds__(256) void cache8_fork_copy_kernel(CacheView c, cons
     }
 }
 
-template <int D, int kTurn>
-void launch_append(const AppendArgs& a, int64_t pieces, hipStream_t stream) {
-    AppendArgs x = a;
-    constexpr int kHeads = 512 / D;                               // (of a wavefront)
-    const int groups = (a.c.n_kv_heads + kHeads - 1) / kHeads + (a.n_q_heads + kHeads - 1) / kHeads;
-    if (a.max_new <= 9) {
-        x.head_groups = (groups + kWaves - 1) / kWaves;
-        const dim3 blocks((unsigned)(pieces * x.head_groups)), threads(64 * kWaves);
-        if (a.max_new == 1) hipLaunchKernelGGL((cache8_append_few_kernel<D, kTurn, 1>), blocks, threads, 0, stream, x);
-        else hipLaunchKernelGGL((cache8_append_few_kernel<D, kTurn, 12>), blocks, threads, 0, stream, x);
-        return;
-    }
-    // workgroups of many items share one reckoning of the turns and have rows in flight, but few pieces need all the workgroups they can get
+template <int D, int kTurn, bool kShort>
+void launch_append_items(AppendArgs a, int64_t pieces, hipStream_t stream) {
+    // workgroups of many items share one reckoning of the turns, but few pieces need all the workgroups they can get
     const int64_t items = 2 * a.c.n_kv_heads + a.n_q_heads, most = (items + kWaves - 1) / kWaves;
-    constexpr int64_t kTwice = 2 * 256 * append_waves<D>;  // twice the workgroups that the chip holds
-    int64_t each = pieces * most / kTwice;                        // items of a wavefront
-    if (each < 1) each = 1;
-    x.head_groups = (int32_t)((most + each - 1) / each);
-    hipLaunchKernelGGL((cache8_append_kernel<D, kTurn>), dim3((unsigned)(pieces * x.head_groups)), dim3(64 * kWaves), 0, stream, x);
+    constexpr int64_t kHeld = 256 * append_waves<D, kTurn, kShort>;      // workgroups that the chip holds
+    int64_t each = pieces * most / (2 * kHeld);                   // items of a wavefront
+    if (each < 1) each = kShort && pieces * most > kHeld ? 2 : 1;
+    if (kShort && each > 2) each = 2;                             // (64 x 9 tokens on 40/40 heads: one 20.4 us, five 23.4)
+    a.head_groups = (int32_t)((most + each - 1) / each);
+    hipLaunchKernelGGL((cache8_append_kernel<D, kTurn, kShort>), dim3((unsigned)(pieces * a.head_groups)), dim3(64 * kWaves), 0, stream, a);
+}
+
+template <int D, int kTurn>
+void launch_append(AppendArgs a, int64_t pieces, hipStream_t stream) {
+    if (a.max_new > 9) launch_append_items<D, kTurn, false>(a, pieces, stream);
+    else if (a.max_new > 1) launch_append_items<D, kTurn, true>(a, pieces, stream);
+    else {
+        constexpr int kHeads = 512 / D;                           // (of a wavefront)
+        const int groups = (a.c.n_kv_heads + kHeads - 1) / kHeads + (a.n_q_heads + kHeads - 1) / kHeads;
+        a.head_groups = (groups + kWaves - 1) / kWaves;
+        hipLaunchKernelGGL((cache8_append_one_kernel<D, kTurn>), dim3((unsigned)(pieces * a.head_groups)), dim3(64 * kWaves), 0, stream, a);
+    }
 }
 
 }  // namespace
