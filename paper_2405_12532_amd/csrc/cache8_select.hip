@@ -5,7 +5,8 @@
 // one product of twice the channels.  lo and hi are whole numbers times the block's power, and q is rounded to whole numbers from -127 to 127 times a power
 // of its own, so that the product is one of 8-bit integers (v_mfma_i32_16x16x64_i8) and a score, a whole number below 2^22 times a power of two,
 // is exact in fp32: which blocks are chosen does not depend on the order of a sum.  A block's score is the largest of the group's query heads.
-// Bound: reading the bounds where there are many, the latency of a launch where there are few.
+// Bound: reading the bounds where there are many (64 x 2048 tokens on 32 heads: 9.7 us for 34 MB, 3.6 TB/s with a launch's 2 us in it), the latency of dependent
+// loads where there are few (1 x 2048 on 8 heads of 64: 3.9 us; 1 x 131072 on 8 heads: 5.1 for the scores, of 9.6 MB, 7.0 for the choice, which eight workgroups make).
 #include "cache8_device.h"
 
 namespace pyr {
@@ -422,7 +423,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_select_many_kernel(SelectA
     }
 }
 
-constexpr int kAtOnce = 4096, kAlone = 512;      // candidates whose keys a workgroup holds; that one scores by itself where units are few
+constexpr int kAtOnce = 4096;                    // candidates whose keys a workgroup holds
 
 template <int D>
 void launch(const CacheSelect& x, const SelectArgs& a, unsigned units, hipStream_t stream) {
@@ -441,8 +442,11 @@ CacheSelect plan_cache8_select(int32_t n_seqs, int32_t n_tokens, int32_t n_kv_he
     const int64_t units = (int64_t)n_seqs * n_tokens * n_kv_heads, blocks = (max_len + 31) / 32;
     x.max_blocks = (int32_t)blocks;
     x.chunks = 0;
-    if (blocks > kAtOnce || (units < 128 && blocks > kAlone)) {
-        // 64 candidates a wavefront while that leaves the chip room, else as many as keep one reckoning of the queries worth it
+    // A unit's workgroup scores its blocks by itself unless they are many and the units leave compute units idle.  Measured, us, alone and with a launch for the scores,
+    // units x blocks: 8 x 512 10.2 and 10.0, 8 x 1024 13.8 and 9.6, 64 x 640 12.3 and 12.0, 64 x 4096 38.2 and 23.5, 96 x 768 13.0 and 14.0, 128 x 1024 15.2 and 16.1,
+    // 128 x 2048 23.1 and 21.9, 128 x 4096 39.2 and 33.4, 256 x 1024 18.3 and 21.9, 768 x 640 27.9 and 32.8
+    if (blocks > (units < 96 ? 512 : units < 192 ? 1536 : kAtOnce)) {
+        // 64 candidates a wavefront; 256 (the same time there, 23.7 us for 64 x 4096) where the grid would grow large
         x.chunk = units * blocks <= 64 * 16384 ? 64 : 256;
         while ((blocks + x.chunk - 1) / x.chunk > 32768) x.chunk *= 2;
         x.chunks = (int32_t)((blocks + x.chunk - 1) / x.chunk);

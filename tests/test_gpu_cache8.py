@@ -128,8 +128,8 @@ def test_append_takes_the_first_row_of_a_slot_and_stops_at_its_limits(lib):
 @pytest.mark.parametrize("d,hq,hkv,dims,pairs,far", [(128, 8, 2, 128, 0, 0), (128, 4, 4, 128, 1, 100000), (64, 6, 2, 64, 0, 2 ** 31 - 200), (64, 8, 8, 32, 1, 5000),
                                                      (128, 5, 1, 48, 0, 1000000), (128, 4, 2, 112, 0, 77), (64, 2, 1, 16, 0, -300), (64, 3, 3, 48, 1, 9)])
 def test_append_turns_rows_by_their_positions(lib, d, hq, hkv, dims, pairs, far):
-    """K as the codes say within half a step and what fp32 loses; Q within half a step of bf16; both strided.  An angle is off by 2^-24 in fp32 (and by far * 2^-51 in
-    64 bits), a sine by three roundings more, so that a turned number is by 2^-21 (|a| + |b|) at most."""
+    """K as the codes say within half a step and what fp32 loses; Q within half a step of bf16; both strided.  An angle is off by far * 2^-51 in 64
+    bits, a sine by its rounding to fp32 besides, a product and the sum by theirs, so that a turned number is by 2^-21 (|a| + |b|) at most."""
     lens, start, count = [90, 40, 33, 64], [10, 39, 0, 31], [70, 1, 33, 0]
     pair = Pair8(lib, lens, hkv, d, 32, powers=(113, 114))
     rows = sum(count)

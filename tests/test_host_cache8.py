@@ -64,6 +64,8 @@ def test_sizes():
     assert binding.cache8_attention_workspace_bytes(long, 1, 1, 8, 65536, 4) == 0           # lists of four blocks
     assert binding.cache8_select_workspace_bytes(long, 200, 1, 8, 65536) == 0
     assert binding.cache8_select_workspace_bytes(long, 1, 1, 8, 65536) == 2048 * 4 * 4
+    assert [binding.cache8_select_workspace_bytes(long, 24, 1, 8, 32 * b) for b in (1536, 1537)] == [0, (1537 * 96 * 4 + 255) // 256 * 256]
+    assert [binding.cache8_select_workspace_bytes(long, 23, 1, 8, 32 * b) for b in (512, 513)] == [0, (513 * 92 * 4 + 255) // 256 * 256]
     r = binding.diag_cache8_attention(long, 1, 1, 8, 65536, 0)
     assert r.splits > 1 and r.chunk % r.waves == 0 and r.repeats == 1
     assert call("pyr_diag_cache8_attention", ctypes.byref(long), 1, 1, 8, 100, 0, None) == NULL
