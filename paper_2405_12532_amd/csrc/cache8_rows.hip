@@ -6,10 +6,10 @@
 // throughout, twice as many numbers next to a border got another code than the exact one).  A workgroup takes 32 tokens and some heads: the pairs are
 // worked out once, meet in LDS and turn K and Q of all its heads.
 // A wavefront owns one block (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte.
-// Bound: reading and writing HBM, in part only: the rows that a selection keeps of 8 x 2048 tokens on 32 heads (1433 of each, K and V) go in in 53 us, 287 MB at 5.4 TB/s, vector
-// instructions 32 % of a SIMD's cycles, and come back in 44, 283 MB at 6.4 TB/s; ragged pieces turned with Q (7 x 100 ... 3000 on 32/8 heads of 64) 29.5 us for 110 MB, 3.7 TB/s,
-// where loads, the block's power and stores follow one another in each wavefront and 39 % of the cycles are vector instructions; 64 tokens of a step 7.7 us,
-// latency; back from 64 blocks 9.
+// Bound: reading and writing HBM, in part only: the rows that a selection keeps of 8 x 2048 tokens on 32 heads (1433 of each, K and V) go in in 52 us, 287 MB at 5.5 TB/s, vector
+// instructions 32 % of a SIMD's cycles, and come back in 44, 283 MB at 6.4 TB/s; all of them turned with Q 147 us, 680 MB at 4.6 TB/s, vector instructions 50 %, LDS 31 %; ragged
+// pieces turned with Q (7 x 100 ... 3000 on 32/8 heads of 64) 26 us for 110 MB, 4.2 TB/s, where loads, the block's power and stores follow one another in each
+// wavefront; 64 tokens of a step 7.7 us, latency; back from 64 blocks 9.
 #include "cache8_device.h"
 
 namespace pyr {
@@ -182,7 +182,7 @@ __device__ __forceinline__ Piece piece_of(const AppendArgs& a, int place) {
 // Pieces of any length.  A wavefront goes through items: K, V or Q of the piece's block and a head.  kShort: nine tokens at most, which a window of 12 (at 64
 // channels 16) tokens of the block holds (64 x 9 tokens on 32/8 heads of 128, turned with Q: 10.6 us, with all 32 tokens' places 14.7; 8 x 5 5.7 and 9.5).
 template <int D, int kTurn, bool kShort>
-constexpr int append_waves = kShort || D == 64 ? 4 : 2;      // of a SIMD, as registers allow (128 channels as they are: three spill)
+constexpr int append_waves = kShort || D == 64 ? 4 : kTurn == kAsIs ? 3 : 2;      // of a SIMD, as registers allow
 template <int D, int kTurn, bool kShort>
 __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void cache8_append_kernel(AppendArgs a) {
     constexpr int kLanes = D / 8, kTokens = 64 / kLanes;          // lanes of a row, rows of a load
@@ -209,6 +209,11 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
     int rows[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) rows[i] = max(__shfl(p.from, source_of(i)), 0);
+    // what was worked out from the rows is worked out again (else the compiler keeps all of it for the paths of what is no number)
+    auto afresh = [&](u32x4 (&words)[kLoads]) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) asm volatile("" : "+v"(words[i]));
+    };
     auto load = [&](int item, u32x4 (&words)[kLoads]) {
         const uint16_t* from = item < hkv ? a.k : item < 2 * hkv ? a.v : a.q;
         const int64_t stride = item < hkv ? a.k_stride : item < 2 * hkv ? a.v_stride : a.q_stride;
@@ -310,6 +315,7 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
             for (int e = 1; e < 8; ++e) top = __builtin_elementwise_maximum(top, __builtin_elementwise_maximum(up[e], down[e]));
             if (__builtin_amdgcn_ballot_w64(!(top <= most)) != 0) {      // some have no code: the largest of those that are numbers, and no bounds where they are
                 uint32_t bits = 0;
+                if (!kExpanded) afresh(words);
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
 #pragma unroll
@@ -379,6 +385,7 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
             float top = __uint_as_float(max(pair & 0xffff0000u, pair << 16));
             if (__builtin_amdgcn_ballot_w64(!(top <= most)) != 0) {
                 uint32_t bits = 0;
+                afresh(words);
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i)
 #pragma unroll
@@ -633,12 +640,12 @@ __global__ __launch_bounds__(256) void cache8_fork_copy_kernel(CacheView c, cons
 
 template <int D, int kTurn, bool kShort>
 void launch_append_items(AppendArgs a, int64_t pieces, hipStream_t stream) {
-    // workgroups of many items share one reckoning of the turns, but few pieces need all the workgroups they can get
     const int64_t items = 2 * a.c.n_kv_heads + a.n_q_heads, most = (items + kWaves - 1) / kWaves;
     constexpr int64_t kHeld = 256 * append_waves<D, kTurn, kShort>;      // workgroups that the chip holds
-    int64_t each = pieces * most / (2 * kHeld);                   // items of a wavefront
-    if (each < 1) each = kShort && pieces * most > kHeld ? 2 : 1;
-    if (kShort && each > 2) each = 2;                             // (64 x 9 tokens on 40/40 heads: one 20.4 us, five 23.4)
+    // Items of a wavefront: two share a reckoning of the turns, more of them leave too little in flight, and few pieces need all the workgroups they can get.  Measured,
+    // us, one, two, four: 8 x 2048 tokens on 32/32 heads 185, 145, 149; 7 x 100 ... 3000 on 32/8 68, 51, 50; the same at 64 channels 31, 25.5, 26; 64 x 64 on 32/8 37, 32, 33;
+    // 1 x 800 on 32/32 15.5, 14.1, 17.8; 16 x 200 on 8 heads 6.6, 7.6, 10.8; 64 x 9 on 40/40 20, 18, 21; 2 x 500 on 12/12 heads of 64 6.9, 8.1, 9.4
+    const int64_t each = pieces * most > kHeld ? 2 : 1;
     a.head_groups = (int32_t)((most + each - 1) / each);
     hipLaunchKernelGGL((cache8_append_kernel<D, kTurn, kShort>), dim3((unsigned)(pieces * a.head_groups)), dim3(64 * kWaves), 0, stream, a);
 }
