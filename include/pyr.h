@@ -461,7 +461,8 @@ PYR_API int pyr_cache_attention(const pyr_cache* cache, const void* q, const int
  * less, from 2^-100 to 2^119.  Numbers are rounded to the nearest, ties to the even code; an infinity, a NaN, and what would be rounded to more than
  * 448 * 2^119 is stored as NaN, by itself.  A block that gets tokens behind others keeps its power or takes a larger one, which its older numbers are
  * rounded to (exact, but for those that leave four significant bits: below 2^-6 of a unit).  Storing a block's first token starts it
- * anew: what lay behind the new tokens in it holds nothing then.
+ * anew: what lay behind the new tokens in it holds nothing then.  So a block is filled from its first token on: the power that lies in front of tokens
+ * whose predecessors were never stored counts as theirs, whatever it is (zeroed pages: as the smallest).
  * A block keeps bounds of its K, for pyr_cache8_select: the largest and the smallest number that a channel has held since then, rounded outward to whole
  * multiples of 4 times the power, from -112 to 112; +-127 where one of them was NaN.  When the power grows they are divided and rounded outward.
  *

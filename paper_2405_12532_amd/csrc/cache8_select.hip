@@ -233,7 +233,17 @@ __device__ __forceinline__ void take_alone(const SelectArgs& a, const Unit& u, c
         return n;
     };
     uint32_t prefix = 0;
-    for (int bit = 31; bit >= 0; --bit) {
+    int top = 31;
+    if constexpr (kPer > 1) {                                 // from the highest bit in which two of them differ (8 x 512 blocks 9.4 -> 8.6 us; one key a lane: 3.7 -> 4.2)
+        const uint32_t some = (uint32_t)__builtin_amdgcn_readfirstlane((int)keys[0]);      // a candidate's: there are more than n_best
+        uint32_t differ = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) differ |= keys[i] != 0 ? keys[i] ^ some : 0;
+        differ = within_wave(differ, [](uint32_t x, uint32_t y) { return x | y; });
+        top = 31 - __clz((int)differ);                        // (-1: all alike)
+        prefix = top < 0 ? some : some & ~(0xffffffffu >> (31 - top));
+    }
+    for (int bit = top; bit >= 0; --bit) {
         const uint32_t tried = prefix | 1u << bit;
         const int n = count([&](uint32_t key) { return key >= tried; });
         if (n >= a.n_best) prefix = tried;
