@@ -222,44 +222,84 @@ __device__ __forceinline__ bool sure_blocks(const SelectArgs& a, const Unit& u, 
 
 __device__ __forceinline__ uint64_t lanes_below() { return (1ull << (threadIdx.x & 63)) - 1; }
 
-// The candidates of a unit that a list takes, by one wavefront that holds all keys: candidate low + 64 i + lane is key i of a lane; 0: none (no score's key is 0).
-// The n-th largest key is found bit by bit, from counts of the keys that are at least the prefix with the bit set.
-template <int kPer>
-__device__ __forceinline__ void take_alone(const SelectArgs& a, const Unit& u, const uint32_t (&keys)[kPer], int32_t* out) {
-    auto count = [&](auto test) {
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(test(keys[i])));
-        return n;
-    };
+// The n_best-th largest of one wavefront's keys (0: none; no score's key is 0): all above limit are taken, and of those equal to it equal_left.
+struct Limit {
+    uint32_t limit;
+    int equal_left;
+};
+// One key a lane: bit by bit, from counts of the keys that are at least the prefix with the bit set.
+__device__ __forceinline__ Limit limit_of(const SelectArgs& a, uint32_t key) {
+    auto count = [](bool test) { return __builtin_popcountll(__builtin_amdgcn_ballot_w64(test)); };
     uint32_t prefix = 0;
-    int top = 31;
-    if constexpr (kPer > 1) {                                 // from the highest bit in which two of them differ (8 x 512 blocks 9.4 -> 8.6 us; one key a lane: 3.7 -> 4.2)
-        const uint32_t some = (uint32_t)__builtin_amdgcn_readfirstlane((int)keys[0]);      // a candidate's: there are more than n_best
-        uint32_t differ = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) differ |= keys[i] != 0 ? keys[i] ^ some : 0;
-        differ = within_wave(differ, [](uint32_t x, uint32_t y) { return x | y; });
-        top = 31 - __clz((int)differ);                        // (-1: all alike)
-        prefix = top < 0 ? some : some & ~(0xffffffffu >> (31 - top));
-    }
-    for (int bit = top; bit >= 0; --bit) {
+    for (int bit = 31; bit >= 0; --bit) {
         const uint32_t tried = prefix | 1u << bit;
-        const int n = count([&](uint32_t key) { return key >= tried; });
+        const int n = count(key >= tried);
         if (n >= a.n_best) prefix = tried;
         if (n == a.n_best) break;                             // (the others are below)
     }
-    // in order: all above the n-th largest, and of those equal to it the first
-    int equal_left = a.n_best - count([&](uint32_t key) { return key > prefix; }), at = u.low;
+    return {prefix, a.n_best - count(key > prefix)};
+}
+// Several: from counts of the keys in 256 parts of the range that it lies in (in LDS, the wavefront's own); 8 x 512 blocks 7.7 us, bit by bit 8.6
+template <int kPer>
+__device__ __forceinline__ Limit limit_of(const SelectArgs& a, const uint32_t (&keys)[kPer], uint32_t* counts) {
+    constexpr int kBits = 8;
+    const int lane = threadIdx.x & 63;
+    auto meet = [] {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    uint32_t low = 0xffffffffu, high = 0;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-        const uint64_t equals = __builtin_amdgcn_ballot_w64(keys[i] == prefix), aboves = __builtin_amdgcn_ballot_w64(keys[i] > prefix);
+        low = min(low, keys[i] - 1);                          // (what is none is the largest)
+        high = max(high, keys[i]);
+    }
+    low = within_wave(low, [](uint32_t x, uint32_t y) { return min(x, y); }) + 1;
+    high = within_wave(high, [](uint32_t x, uint32_t y) { return max(x, y); });
+    int wanted = a.n_best;                                    // so many of the keys from low to high, and all above
+    for (int round = 0;; ++round) {
+        const int shift = max(0, 32 - __clz((int)(high - low)) - kBits);
+        *(u32x4*)&counts[4 * lane] = u32x4{};
+        meet();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (keys[i] >= low && keys[i] <= high) atomicAdd(&counts[(keys[i] - low) >> shift], 1u);
+        meet();
+        // lane l: keys in the four parts from 4 (63 - l) on, and above
+        const u32x4 own = *(const u32x4*)&counts[4 * (63 - lane)];
+        const int all = (int)(own[0] + own[1] + own[2] + own[3]), sum = scan_wave(all);
+        const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(sum >= wanted));
+        int above = __builtin_amdgcn_readlane(sum - all, at), n = 0, part = 4;
+#pragma unroll
+        for (int i = 3; i >= 0; --i) {
+            if (above + n >= wanted) break;
+            above += n;
+            n = __builtin_amdgcn_readlane((int)own[i], at);
+            part = i;
+        }
+        low += (uint32_t)(4 * (63 - at) + part) << shift;
+        wanted -= above;
+        if (shift == 0) return {low, wanted};
+        if (n == wanted || round == 3) return {low - 1, 0};   // (32 bits are four rounds at most)
+        high = min(high, low + ((1u << shift) - 1));
+        meet();
+    }
+}
+
+// The candidates of a unit that a list takes, by one wavefront that holds all keys: candidate low + 64 i + lane is key i of a lane.  In order: all above the n-th largest,
+// and of those equal to it the first.
+template <int kPer>
+__device__ __forceinline__ void take_alone(const SelectArgs& a, const Unit& u, const uint32_t (&keys)[kPer], Limit l, int32_t* out) {
+    int at = u.low;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const uint64_t equals = __builtin_amdgcn_ballot_w64(keys[i] == l.limit), aboves = __builtin_amdgcn_ballot_w64(keys[i] > l.limit);
         const int rank = __builtin_popcountll(equals & lanes_below());
-        if (keys[i] > prefix || (keys[i] == prefix && rank < equal_left))
-            out[at + __builtin_popcountll(aboves & lanes_below()) + min(rank, equal_left)] = u.low + 64 * i + (threadIdx.x & 63);
-        const int taken = min(__builtin_popcountll(equals), equal_left);
+        if (keys[i] > l.limit || (keys[i] == l.limit && rank < l.equal_left))
+            out[at + __builtin_popcountll(aboves & lanes_below()) + min(rank, l.equal_left)] = u.low + 64 * i + (threadIdx.x & 63);
+        const int taken = min(__builtin_popcountll(equals), l.equal_left);
         at += __builtin_popcountll(aboves) + taken;
-        equal_left -= taken;
+        l.equal_left -= taken;
     }
 }
 
@@ -267,6 +307,7 @@ __device__ __forceinline__ void take_alone(const SelectArgs& a, const Unit& u, c
 template <int D, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 4) void cache8_select_kernel(SelectArgs a) {
     __shared__ uint32_t held[kWaves == 1 ? 1 : kWaves][64];
+    __shared__ __align__(16) uint32_t counts[kWaves == 1 ? 1 : 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = a.n_q_heads / a.c.n_kv_heads;
     Unit u = unit_of(a, blockIdx.x);
     int32_t* out = a.blocks + (int64_t)blockIdx.x * (a.n_first + a.n_recent + a.n_best);
@@ -290,8 +331,10 @@ __global__ __launch_bounds__(64 * kWaves, 4) void cache8_select_kernel(SelectArg
         if (wave > 0) return;
 #pragma unroll
         for (int i = 1; i < kWaves; ++i) keys[i] = held[i][lane];
+        take_alone<kWaves>(a, u, keys, limit_of<kWaves>(a, keys, counts), out);
+    } else {
+        take_alone<kWaves>(a, u, keys, limit_of(a, keys[0]), out);
     }
-    take_alone<kWaves>(a, u, keys, out);
 }
 
 // For many candidates, 4096 at a time: candidate low + 64 (wave + kWaves i) + lane is key i of a lane.  kScored: their keys are in memory, else they are worked out
@@ -442,6 +485,8 @@ void launch(const CacheSelect& x, const SelectArgs& a, unsigned units, hipStream
     else if (n <= 64) hipLaunchKernelGGL((cache8_select_kernel<D, 1>), dim3(units), dim3(64), 0, stream, a);
     else if (n <= 256) hipLaunchKernelGGL((cache8_select_kernel<D, 4>), dim3(units), dim3(256), 0, stream, a);
     else if (n <= 512) hipLaunchKernelGGL((cache8_select_kernel<D, 8>), dim3(units), dim3(512), 0, stream, a);
+    // (1024 at once of few units: 128 x 1024 blocks 13.4 us, by parts 15.1; 256 x 640 at 64 channels 8.8 and 10.8, but 768 x 640 29.6 and 27.8, 1600 x 750 52 and 43)
+    else if (n <= 1024 && units <= 256) hipLaunchKernelGGL((cache8_select_kernel<D, 16>), dim3(units), dim3(1024), 0, stream, a);
     else hipLaunchKernelGGL((cache8_select_many_kernel<D, 8, false>), dim3(units), dim3(512), 0, stream, a);
 }
 
@@ -453,8 +498,8 @@ CacheSelect plan_cache8_select(int32_t n_seqs, int32_t n_tokens, int32_t n_kv_he
     x.max_blocks = (int32_t)blocks;
     x.chunks = 0;
     // A unit's workgroup scores its blocks by itself unless they are many and the units leave compute units idle.  Measured, us, alone and with a launch for the scores,
-    // units x blocks: 8 x 512 10.2 and 10.0, 8 x 1024 13.8 and 9.6, 64 x 640 12.3 and 12.0, 64 x 4096 38.2 and 23.5, 96 x 768 13.0 and 14.0, 128 x 1024 15.2 and 16.1,
-    // 128 x 2048 23.1 and 21.9, 128 x 4096 39.2 and 33.4, 256 x 1024 18.3 and 21.9, 768 x 640 27.9 and 32.8
+    // units x blocks: 8 x 512 7.7 and 10.0, 8 x 1024 12.9 and 9.6, 64 x 640 10.4 and 11.3, 64 x 1024 13.6 and 12.2, 64 x 4096 38.2 and 23.5, 128 x 1024 13.4 and 14.3,
+    // 128 x 2048 23.1 and 21.9, 128 x 4096 39.2 and 33.4, 256 x 1024 18.5 and 21.9, 768 x 640 27.9 and 32.8
     if (blocks > (units < 96 ? 512 : units < 192 ? 1536 : kAtOnce)) {
         // 64 candidates a wavefront; 256 (the same time there, 23.7 us for 64 x 4096) where the grid would grow large
         x.chunk = units * blocks <= 64 * 16384 ? 64 : 256;

@@ -404,6 +404,17 @@ def test_select_of_more_blocks_than_a_workgroup_holds(lib):
     check_attention(pair, q, [0, 1], *attend(pair, qt, [0, 1], 1, 140000, blocks), blocks=blocks.cpu().numpy())
 
 
+@pytest.mark.parametrize("rows,hkv,d,length", [(48, 2, 64, 20000), (100, 1, 128, 32768), (256, 1, 64, 32760), (257, 1, 64, 20000), (65, 3, 64, 49152), (96, 1, 64, 49200), (30, 1, 64, 16390)])
+def test_select_of_many_rows_and_blocks(lib, rows, hkv, d, length):
+    """One sequence asked for by many rows: blocks scored by sixteen wavefronts, in parts, and through memory."""
+    pair = Pair8(lib, [length], hkv, d, 1024, powers=(116, 118))
+    qt, q = bf16(pair.rng.normal(size=(rows, 1, 2 * hkv, d)) * 2.0 ** pair.rng.integers(-3, 3, (rows, 1, 2 * hkv, 1)))
+    for first, recent, best, most in ((1, 2, 60, length), (0, 1, 1, length), (0, 1, 500, length), (7, 5, length // 32 - 20, 2 ** 31 - 1), (2, 1, 33, length - 100)):
+        got = select(pair, qt, [0] * rows, 1, most, first, recent, best).cpu().numpy()
+        for b in (0, rows // 2, rows - 1):
+            assert np.array_equal(got[b], pair.o.select(q[b], 0, first, recent, best, most)), (b, first, recent, best, most)
+
+
 @pytest.mark.parametrize("n", [1, 200])
 def test_select_of_thousands_of_ties(lib, n):
     """Blocks that score alike by the hundred, in one workgroup's lanes and through memory."""
