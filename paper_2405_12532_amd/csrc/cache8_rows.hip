@@ -7,7 +7,7 @@
 // worked out once, meet in LDS and turn K and Q of all its heads.
 // A wavefront owns one block (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte.
 // Bound: reading and writing HBM, in part only: the rows that a selection keeps of 8 x 2048 tokens on 32 heads (1433 of each, K and V) go in in 52 us, 287 MB at 5.5 TB/s, vector
-// instructions 32 % of a SIMD's cycles, and come back in 44, 283 MB at 6.4 TB/s; all of them turned with Q 147 us, 680 MB at 4.6 TB/s, vector instructions 50 %, LDS 31 %; ragged
+// instructions 32 % of a SIMD's cycles, and come back in 44, 283 MB at 6.4 TB/s; all 2048 turned with Q 142 us, 680 MB at 4.8 TB/s, vector instructions half of the cycles; ragged
 // pieces turned with Q (7 x 100 ... 3000 on 32/8 heads of 64) 26 us for 110 MB, 4.2 TB/s, where loads, the block's power and stores follow one another in each
 // wavefront; 64 tokens of a step 7.7 us, latency; back from 64 blocks 9.
 #include "cache8_device.h"
@@ -59,41 +59,59 @@ struct AppendArgs {
     int32_t n_rows, n_list, max_new, tiles_of_piece, head_groups, n_q_heads, dims;
 };
 
-enum { kAsIs, kHalves, kPairs };                                  // channel c turns with c + dims / 2, or 2 c with 2 c + 1
+enum { kAsIs, kAllHalves, kHalves, kPairs };                      // channel c turns with c + dims / 2 (all channels, some of them), or 2 c with 2 c + 1
+
+// Where the turn of a pair lies among its token's: lanes that turn eight channels each (with their partners, or in pairs) read 16 bytes side by side.  (One behind the
+// other, and partners through LDS: 8 x 2048 rows on 32/32 heads 149.5 us for 144.8, 4 x 4000 on 64/8 127 for 120.)
+template <int D, int kTurn>
+__device__ __forceinline__ int place_of(int pair) {
+    constexpr int kOfLane = kTurn == kPairs ? 4 : 8;
+    return pair / kOfLane * 2 + pair % kOfLane / 2 * (D / kOfLane) + pair % 2;
+}
+template <int D, int kTurn>
+constexpr int turns_of_row = kTurn == kAsIs ? 1 : D == 64 ? 48 : 64;      // (at 64 channels with room between rows, two of which are read at a time)
 
 constexpr uint32_t kNoNumber = 0x7f680000u;                       // 464 * 2^119: what lies above has no code
 
 // Eight channels of a row, turned.  turns: of the row's token; lanes of a row are neighbours.
-template <int kTurn>
+template <int D, int kTurn>
 __device__ __forceinline__ void turned(u32x4 words, const f32x2* turns, int dims, int piece, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[2 * i] = low_of(words[i]);
         x[2 * i + 1] = high_of(words[i]);
     }
-    if constexpr (kTurn == kHalves) {
-        const int half = dims / 16;                               // (lanes)
+    if constexpr (kTurn == kAllHalves || kTurn == kHalves) {
+        const int half = kTurn == kAllHalves ? D / 16 : dims / 16;      // (lanes)
         const int with = piece < half ? half : piece < 2 * half ? -half : 0;
         float y[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t other = (uint32_t)__shfl((int)words[i], (int)(threadIdx.x & 63) + with);
+            uint32_t other;
+            if constexpr (kTurn == kHalves) other = (uint32_t)__shfl((int)words[i], (int)(threadIdx.x & 63) + with);
+            else if constexpr (D == 128) other = dpp<0x128>(words[i]);      // eight lanes further of sixteen
+            else other = dpp<0x1b>(dpp<0x141>(words[i]));      // eight lanes mirrored, then four
             y[2 * i] = low_of(other);
             y[2 * i + 1] = high_of(other);
         }
-        if (with != 0) {
-            const f32x2* turn = turns + 8 * (piece < half ? piece : piece - half);
+        if (kTurn == kAllHalves || with != 0) {
+            const f32x2* at = turns + 2 * (piece < half ? piece : piece - half);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i], turn[i][0], (with > 0 ? -y[i] : y[i]) * turn[i][1]);
+            for (int i = 0; i < 8; i += 2) {
+                const f32x4 two = *(const f32x4*)(at + place_of<D, kTurn>(i));
+                x[i] = __builtin_fmaf(x[i], two[0], (with > 0 ? -y[i] : y[i]) * two[1]);
+                x[i + 1] = __builtin_fmaf(x[i + 1], two[2], (with > 0 ? -y[i + 1] : y[i + 1]) * two[3]);
+            }
         }
     } else if constexpr (kTurn == kPairs) {
         if (piece < dims / 8) {
-            const f32x2* turn = turns + 4 * piece;
+            const f32x2* at = turns + 2 * piece;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float p = x[2 * i], r = x[2 * i + 1];
-                x[2 * i] = __builtin_fmaf(p, turn[i][0], -(r * turn[i][1]));
-                x[2 * i + 1] = __builtin_fmaf(r, turn[i][0], p * turn[i][1]);
+                const f32x4 two = *(const f32x4*)(at + place_of<D, kTurn>(i & 2));
+                const float c = two[2 * (i & 1)], s = two[2 * (i & 1) + 1], p = x[2 * i], r = x[2 * i + 1];
+                x[2 * i] = __builtin_fmaf(p, c, -(r * s));
+                x[2 * i + 1] = __builtin_fmaf(r, c, p * s);
             }
         }
     }
@@ -189,7 +207,7 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
     constexpr bool kEarly = kShort || D == 128;                   // what a block holds is asked for with the rows (at 64 channels longer pieces have no registers for it)
     constexpr int kWindow = !kShort ? 32 : D == 128 ? 12 : 16, kLoads = kWindow / kTokens;
     constexpr int kRow = D + 16;                                  // bytes of a token's codes in LDS
-    __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : 32][kTurn == kAsIs ? 1 : D / 2];
+    __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : 32][turns_of_row<D, kTurn>];
     __shared__ __align__(16) uint8_t all_staged[kWaves][32][kRow];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = lane % kLanes;
     const int place = blockIdx.x / a.head_groups, hkv = a.c.n_kv_heads;
@@ -235,7 +253,7 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
             if ((stored >> t & ((1u << kAtOnce) - 1)) == 0) continue;
             const int mine_t = t + lane / kPairsOf;
             const f32x2 turn = turn_of(__shfl(position, mine_t), freq);
-            if (pair < a.dims / 2) turns[mine_t][pair] = turn;
+            if (pair < a.dims / 2) turns[mine_t][place_of<D, kTurn>(pair)] = turn;
         }
         __syncthreads();
     }
@@ -275,7 +293,7 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 float x[8];
-                turned<kTurn>(words[i], turns_of(source_of(i)), a.dims, piece, x);
+                turned<D, kTurn>(words[i], turns_of(source_of(i)), a.dims, piece, x);
                 if ((stored & there) >> token_of(i) & 1) __builtin_nontemporal_store(rounded(x), to + (int64_t)rows[i] * (a.n_q_heads * kLanes));
             }
         } else if (item < hkv) {                                  // a head of K
@@ -300,7 +318,7 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
 #pragma unroll
                 for (int n = i; n < i + 2 && n < kLoads; ++n) {
                     if (gone && !there_of(n)) words[n] = kNoRow;
-                    if (kExpanded) turned<kTurn>(words[n], turns_of(source_of(n)), a.dims, piece, x[kExpanded ? n : 0]);
+                    if (kExpanded) turned<D, kTurn>(words[n], turns_of(source_of(n)), a.dims, piece, x[kExpanded ? n : 0]);
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -432,7 +450,7 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
 template <int D, int kTurn>
 __global__ __launch_bounds__(64 * kWaves) void cache8_append_one_kernel(AppendArgs a) {
     constexpr int kLanes = D / 8, kHeads = 64 / kLanes;           // lanes of a head, heads of a wavefront
-    __shared__ __align__(16) f32x2 turns[kTurn == kAsIs ? 1 : D / 2];
+    __shared__ __align__(16) f32x2 turns[turns_of_row<D, kTurn>];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = lane % kLanes;
     const int place = blockIdx.x / a.head_groups, group = (blockIdx.x - place * a.head_groups) * kWaves + wave;
     const int kv_groups = (a.c.n_kv_heads + kHeads - 1) / kHeads;
@@ -466,12 +484,12 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_one_kernel(AppendAr
         if (wave == 0) {
             const float freq = lane < a.dims / 2 ? a.freqs[lane] : 0.f;
             const f32x2 turn = turn_of(row >= 0 ? a.positions[row] : 0, freq);
-            if (lane < a.dims / 2) turns[lane] = turn;
+            if (lane < a.dims / 2) turns[place_of<D, kTurn>(lane)] = turn;
         }
         __syncthreads();
     }
     float x[8];
-    turned<kTurn>(kx, turns, a.dims, piece, x);
+    turned<D, kTurn>(kx, turns, a.dims, piece, x);
     if (of_q) {
         if (real && row >= 0) __builtin_nontemporal_store(rounded(x), (u32x4*)a.q_out + (at_row * a.n_q_heads + head) * kLanes + piece);
         return;
@@ -643,7 +661,7 @@ void launch_append_items(AppendArgs a, int64_t pieces, hipStream_t stream) {
     const int64_t items = 2 * a.c.n_kv_heads + a.n_q_heads, most = (items + kWaves - 1) / kWaves;
     constexpr int64_t kHeld = 256 * append_waves<D, kTurn, kShort>;      // workgroups that the chip holds
     // Items of a wavefront: two share a reckoning of the turns, more of them leave too little in flight, and few pieces need all the workgroups they can get.  Measured,
-    // us, one, two, four: 8 x 2048 tokens on 32/32 heads 185, 145, 149; 7 x 100 ... 3000 on 32/8 68, 51, 50; the same at 64 channels 31, 25.5, 26; 64 x 64 on 32/8 37, 32, 33;
+    // us, one, two, four (before the turns lay as above): 8 x 2048 tokens on 32/32 heads 185, 145, 149; 7 x 100 ... 3000 on 32/8 68, 51, 50; the same at 64 channels 31, 25.5, 26; 64 x 64 on 32/8 37, 32, 33;
     // 1 x 800 on 32/32 15.5, 14.1, 17.8; 16 x 200 on 8 heads 6.6, 7.6, 10.8; 64 x 9 on 40/40 20, 18, 21; 2 x 500 on 12/12 heads of 64 6.9, 8.1, 9.4
     const int64_t each = pieces * most > kHeld ? 2 : 1;
     a.head_groups = (int32_t)((most + each - 1) / each);
@@ -670,13 +688,15 @@ int launch_cache8_append(const CacheView& c, int32_t head_dim, const Cache8Rows&
     const AppendArgs a{c, (const uint16_t*)rows.k, (const uint16_t*)rows.v, (const uint16_t*)rows.q, (uint16_t*)rows.q_out, rows.row_idx, offsets, slots, start,
                        rows.positions, rows.freqs, rows.k_stride, rows.v_stride, rows.q_stride, rows.n_rows, rows.n_list, max_new, (int32_t)tiles, 0,
                        rows.n_q_heads, rows.dims};
-    const int turn = rows.dims == 0 ? kAsIs : rows.interleaved ? kPairs : kHalves;
+    const int turn = rows.dims == 0 ? kAsIs : rows.interleaved ? kPairs : rows.dims == head_dim ? kAllHalves : kHalves;
     if (head_dim == 128) {
         if (turn == kAsIs) launch_append<128, kAsIs>(a, n_seqs * tiles, stream);
+        else if (turn == kAllHalves) launch_append<128, kAllHalves>(a, n_seqs * tiles, stream);
         else if (turn == kHalves) launch_append<128, kHalves>(a, n_seqs * tiles, stream);
         else launch_append<128, kPairs>(a, n_seqs * tiles, stream);
     } else {
         if (turn == kAsIs) launch_append<64, kAsIs>(a, n_seqs * tiles, stream);
+        else if (turn == kAllHalves) launch_append<64, kAllHalves>(a, n_seqs * tiles, stream);
         else if (turn == kHalves) launch_append<64, kHalves>(a, n_seqs * tiles, stream);
         else launch_append<64, kPairs>(a, n_seqs * tiles, stream);
     }

@@ -176,6 +176,25 @@ def test_append_turns_rows_by_their_positions(lib, d, hq, hkv, dims, pairs, far)
         assert np.abs(v[mine]).max() <= 7 and (np.abs(gv[span] - v[mine]) <= np.maximum(step, 2.0 ** -9 * 2.0 ** -6 / 2)).all()
 
 
+@pytest.mark.parametrize("d,hq,hkv,dims,pairs", [(128, 8, 2, 128, 0), (128, 5, 5, 128, 1), (64, 6, 2, 64, 0), (64, 24, 3, 64, 1), (64, 8, 8, 32, 1), (128, 5, 1, 48, 0), (64, 2, 1, 16, 0)])
+def test_turns_of_pieces_of_every_size(lib, d, hq, hkv, dims, pairs):
+    """Tokens behind others in a block whose power holds them: one by one, up to nine at a time and all at once leave the same bytes and turn Q alike."""
+    left, out = [], []
+    for sizes in ([1] * 29, [2, 9, 5, 7, 6], [29]):
+        pair = Pair8(lib, [32], hkv, d, 32, powers=(124, 125))
+        qt, _ = bf16(pair.rng.normal(size=(29, hq, d)))
+        kt, _ = bf16(pair.rng.normal(size=(29, hkv, d)))
+        rotation = lib.make_rotation(torch.logspace(0, -3, dims // 2, device="cuda"), torch.arange(900, 929, dtype=torch.int32, device="cuda"), dims, pairs)
+        q_out, at = torch.zeros_like(qt), 0
+        for n in sizes:
+            append(pair, kt, kt, 29, None, [at, at + n], [0], [3 + at], n, rotation, qt, q_out)
+            at += n
+        left.append(pair.pages.clone())
+        out.append(q_out)
+    for i in (0, 1):
+        assert torch.equal(left[i], left[2]) and torch.equal(out[i], out[2]), i
+
+
 def test_queries_turn_in_place_and_of_stored_tokens_alone(lib):
     pair = Pair8(lib, [40, 40], 2, 128, 32)
     qt, q = bf16(pair.rng.normal(size=(30, 4, 128)))
