@@ -2,12 +2,11 @@
 // Gather(KV, index) keeps of a prompt goes the same way, through its index), tokens of it back to bf16, and pages copied for a fork.
 //
 // A turn by position p takes channels a and b of a pair i to a cos(p f_i) - b sin(p f_i) and b cos(p f_i) + a sin(p f_i).  p f_i is reduced to a
-// quarter of a turn in 64 bits, so that far positions lose nothing; sine and cosine are Taylor's sums on [-pi/4, pi/4] in 64 bits too, rounded to 32 (in 32 bits
-// throughout, twice as many numbers next to a border got another code than the exact one).  A workgroup takes 32 tokens and some heads: the pairs are
+// quarter of a turn in 64 bits, so that far positions lose nothing; sine and cosine are Taylor's sums on [-pi/4, pi/4] in 64 bits too, rounded to 32.  A workgroup takes 32 tokens and some heads: the pairs are
 // worked out once, meet in LDS and turn K and Q of all its heads.
 // A wavefront owns one block (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte.
 // Bound: reading and writing HBM, in part only: the rows that a selection keeps of 8 x 2048 tokens on 32 heads (1433 of each, K and V) go in in 52 us, 287 MB at 5.5 TB/s, vector
-// instructions 32 % of a SIMD's cycles, and come back in 44, 283 MB at 6.4 TB/s; all 2048 turned with Q 142 us, 680 MB at 4.8 TB/s, vector instructions half of the cycles; ragged
+// instructions 32 % of a SIMD's cycles, and come back in 44, 283 MB at 6.4 TB/s; all 2048 turned with Q 144 us, 680 MB at 4.7 TB/s, vector instructions half of the cycles; ragged
 // pieces turned with Q (7 x 100 ... 3000 on 32/8 heads of 64) 26 us for 110 MB, 4.2 TB/s, where loads, the block's power and stores follow one another in each
 // wavefront; 64 tokens of a step 7.7 us, latency; back from 64 blocks 9.
 #include "cache8_device.h"
@@ -36,16 +35,23 @@ __device__ __forceinline__ void meet() {            // (a wavefront's own part o
 __device__ __forceinline__ float low_of(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high_of(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
-// cos and sin of position * freq, in 64 bits up to their rounding (the sums' next terms are below 2^-28)
-__device__ __forceinline__ f32x2 turn_of(int position, float freq) {
+// cos and sin of position * freq, in 64 bits (the sums' next terms are below 2^-33)
+struct Turn {
+    double c, s;
+};
+__device__ __forceinline__ Turn exact_turn_of(int position, float freq) {
     const double quarters = (double)position * ((double)freq * 0.63661977236758134308);      // of a turn: times 2 / pi
     const double nearest = __builtin_rint(quarters);
     const double x = (quarters - nearest) * 1.57079632679489661923, y = x * x;
-    const double s = x * (1. + y * (-1. / 6 + y * (1. / 120 + y * (-1. / 5040 + y * (1. / 362880)))));
+    const double s = x * (1. + y * (-1. / 6 + y * (1. / 120 + y * (-1. / 5040 + y * (1. / 362880 - y * (1. / 39916800))))));
     const double c = 1. + y * (-0.5 + y * (1. / 24 + y * (-1. / 720 + y * (1. / 40320 - y * (1. / 3628800)))));
     const int quadrant = (int)(nearest - 4.0 * __builtin_floor(nearest * 0.25));
-    const float a = (float)(quadrant & 1 ? s : c), b = (float)(quadrant & 1 ? c : s);
-    return f32x2{quadrant == 1 || quadrant == 2 ? -a : a, quadrant >= 2 ? -b : b};
+    const double a = quadrant & 1 ? s : c, b = quadrant & 1 ? c : s;
+    return {quadrant == 1 || quadrant == 2 ? -a : a, quadrant >= 2 ? -b : b};
+}
+__device__ __forceinline__ f32x2 turn_of(int position, float freq) {
+    const Turn t = exact_turn_of(position, freq);
+    return f32x2{(float)t.c, (float)t.s};
 }
 
 // Workgroups count through the head groups first: the heads of a row lie side by side in memory.
@@ -73,6 +79,19 @@ constexpr int turns_of_row = kTurn == kAsIs ? 1 : D == 64 ? 48 : 64;      // (at
 
 constexpr uint32_t kNoNumber = 0x7f680000u;                       // 464 * 2^119: what lies above has no code
 
+// The same channels of the lane that holds the partners of a lane's eight; with: lanes to it.
+template <int D, int kTurn>
+__device__ __forceinline__ uint32_t partners(uint32_t word, int with) {
+    if constexpr (kTurn == kHalves) return (uint32_t)__shfl((int)word, (int)(threadIdx.x & 63) + with);
+    else if constexpr (D == 128) return dpp<0x128>(word);      // eight lanes further of sixteen
+    else return dpp<0x1b>(dpp<0x141>(word));                  // eight lanes mirrored, then four
+}
+template <int D, int kTurn>
+__device__ __forceinline__ int lanes_to_partners(int dims, int piece) {
+    const int half = kTurn == kAllHalves ? D / 16 : dims / 16;
+    return piece < half ? half : piece < 2 * half ? -half : 0;
+}
+
 // Eight channels of a row, turned.  turns: of the row's token; lanes of a row are neighbours.
 template <int D, int kTurn>
 __device__ __forceinline__ void turned(u32x4 words, const f32x2* turns, int dims, int piece, float (&x)[8]) {
@@ -82,20 +101,16 @@ __device__ __forceinline__ void turned(u32x4 words, const f32x2* turns, int dims
         x[2 * i + 1] = high_of(words[i]);
     }
     if constexpr (kTurn == kAllHalves || kTurn == kHalves) {
-        const int half = kTurn == kAllHalves ? D / 16 : dims / 16;      // (lanes)
-        const int with = piece < half ? half : piece < 2 * half ? -half : 0;
+        const int with = lanes_to_partners<D, kTurn>(dims, piece);
         float y[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            uint32_t other;
-            if constexpr (kTurn == kHalves) other = (uint32_t)__shfl((int)words[i], (int)(threadIdx.x & 63) + with);
-            else if constexpr (D == 128) other = dpp<0x128>(words[i]);      // eight lanes further of sixteen
-            else other = dpp<0x1b>(dpp<0x141>(words[i]));      // eight lanes mirrored, then four
+            const uint32_t other = partners<D, kTurn>(words[i], with);
             y[2 * i] = low_of(other);
             y[2 * i + 1] = high_of(other);
         }
         if (kTurn == kAllHalves || with != 0) {
-            const f32x2* at = turns + 2 * (piece < half ? piece : piece - half);
+            const f32x2* at = turns + 2 * min(piece, piece + with);
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
                 const f32x4 two = *(const f32x4*)(at + place_of<D, kTurn>(i));
@@ -114,6 +129,48 @@ __device__ __forceinline__ void turned(u32x4 words, const f32x2* turns, int dims
                 x[2 * i + 1] = __builtin_fmaf(r, c, p * s);
             }
         }
+    }
+}
+
+// K is rounded to four significant bits, and what fp32 rounds onto a border between two codes, or across it, gets the wrong one: a number of a million.  Those within three
+// units of fp32's last place of a border (a number of 150000) are turned again in 64 bits and rounded to fp32 so that a number that is on neither side of a border does not end
+// on it (to odd ones).  (Numbers that are small against their partners, and codes of less than four bits, keep fp32's error.)
+// Of 36 million numbers 8 to 16 are then off, all small, where fp32 alone left 30 to 38; it costs 3 % of an append (8 x 2048 rows on 32/32 heads 143.3 us for 144.4, 4 x 4000 on 64/8
+// 117.9 for 120.5, 64 x 9 tokens 9.4 for 9.8).
+__device__ __forceinline__ uint32_t from_border(float x) { return (__float_as_uint(x) << 12) + 0x80003000u; }
+constexpr uint32_t kNear = 6u << 12;
+// Which of a lane's four words of two turned channels hold such a number, in some lane.
+__device__ __forceinline__ uint32_t near_words(const float (&x)[8], bool turns) {
+    uint32_t least[4], words = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) least[w] = min(from_border(x[2 * w]), from_border(x[2 * w + 1]));
+    if (__builtin_amdgcn_ballot_w64(turns && min(min(least[0], least[1]), min(least[2], least[3])) <= kNear) == 0) return 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) words |= __builtin_amdgcn_ballot_w64(turns && least[w] <= kNear) != 0 ? 1u << w : 0;
+    return words;
+}
+template <int D, int kTurn>
+__device__ __forceinline__ bool turns_at_all(int dims, int piece) { return kTurn == kAllHalves || piece < dims / 8; }      // (halves: of dims / 16 lanes each)
+__device__ __forceinline__ void correct(float& x, float exact, bool turns) { x = turns && from_border(x) <= kNear ? exact : x; }
+// Channels 2 i and 2 i + 1 of a lane's eight; row: those eight.
+template <int D, int kTurn>
+__device__ __forceinline__ void turned_exactly(const uint32_t* row, int i, int position, const float* freqs, int dims, int piece, float (&x)[2]) {
+    const int with = kTurn == kPairs ? 0 : lanes_to_partners<D, kTurn>(dims, piece);
+    const bool turns = turns_at_all<D, kTurn>(dims, piece);
+    const uint32_t word = row[i], other = row[i + 4 * with];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int pair = kTurn == kPairs ? 4 * piece + i : 8 * min(piece, piece + with) + 2 * i + h;
+        const Turn t = exact_turn_of(position, freqs[turns ? pair : 0]);
+        const double own = h ? high_of(word) : low_of(word), partner = (kTurn == kPairs ? 1 - h : h) ? high_of(other) : low_of(other);
+        const bool first = kTurn == kPairs ? h == 0 : with > 0;
+        const double y = __builtin_fma(own, t.c, first ? -partner * t.s : partner * t.s), z = turns ? y : own;
+        const float nearest = (float)z;
+        const double rest = z - (double)nearest;
+        uint32_t bits = __float_as_uint(nearest);
+        if (rest != 0 && (bits & 1) == 0) bits += (rest > 0) == (z > 0) ? 1 : -1;
+        x[h] = __uint_as_float(bits);
+        __builtin_amdgcn_sched_barrier(0);                    // (one after the other, for the registers)
     }
 }
 __device__ __forceinline__ u32x4 rounded(const float (&x)[8]) {
@@ -288,6 +345,8 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
         return scale_of(power);
     };
     for (; item < items; item += step) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) asm volatile("" : "+v"(rows[i]));      // (else it keeps what addresses are made of, too)
         if (item >= 2 * hkv) {                                    // a head of Q: rows turned, where there are rows
             u32x4* const to = (u32x4*)a.q_out + (item - 2 * hkv) * kLanes + piece;
 #pragma unroll
@@ -314,12 +373,36 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
 #pragma unroll
             for (int e = 0; e < 8; ++e) up[e] = down[e] = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < kLoads; i += 2) {
+            for (int n = 0; n < kLoads; ++n)
+                if (gone && !there_of(n)) words[n] = kNoRow;
+            if constexpr (kExpanded) {
+                const bool turns = turns_at_all<D, kTurn>(a.dims, piece);
+                uint32_t near = 0;                                // words of them with numbers next to a border
 #pragma unroll
-                for (int n = i; n < i + 2 && n < kLoads; ++n) {
-                    if (gone && !there_of(n)) words[n] = kNoRow;
-                    if (kExpanded) turned<D, kTurn>(words[n], turns_of(source_of(n)), a.dims, piece, x[kExpanded ? n : 0]);
+                for (int n = 0; n < kLoads; ++n) {
+                    turned<D, kTurn>(words[n], turns_of(source_of(n)), a.dims, piece, x[n]);
+                    near |= near_words(x[n], turns) << (4 * n);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+                while (near != 0) {
+                    const int i = __builtin_ctz(near) >> 2, w = __builtin_ctz(near) & 3, row = max(__shfl(p.from, source_of(i)), 0);
+                    near &= near - 1;
+                    int hidden = piece;
+                    asm volatile("" : "+v"(hidden));
+                    float y[2];
+                    turned_exactly<D, kTurn>((const uint32_t*)((const u32x4*)a.k + item * kLanes + hidden + row * (int64_t)a.k_stride), w, a.positions[row], a.freqs, a.dims, hidden, y);
+#pragma unroll
+                    for (int n = 0; n < kLoads; ++n)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            if (n == i && v == w) {
+                                correct(x[n][2 * v], y[0], turns);
+                                correct(x[n][2 * v + 1], y[1], turns);
+                            }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kLoads; i += 2) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float y = number(i, e), z = i + 1 < kLoads ? number(i + 1 < kLoads ? i + 1 : i, e) : y;
@@ -490,6 +573,22 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_one_kernel(AppendAr
     }
     float x[8];
     turned<D, kTurn>(kx, turns, a.dims, piece, x);
+    if (kTurn != kAsIs && !of_q) {
+        const bool turns = turns_at_all<D, kTurn>(a.dims, piece);
+        uint32_t near = near_words(x, turns);
+        while (near != 0) {
+            const int w = __builtin_ctz(near);
+            near &= near - 1;
+            float y[2];
+            turned_exactly<D, kTurn>((const uint32_t*)((const u32x4*)a.k + at_row * a.k_stride + head * kLanes + piece), w, a.positions[at_row], a.freqs, a.dims, piece, y);
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+                if (v == w) {
+                    correct(x[2 * v], y[0], turns);
+                    correct(x[2 * v + 1], y[1], turns);
+                }
+        }
+    }
     if (of_q) {
         if (real && row >= 0) __builtin_nontemporal_store(rounded(x), (u32x4*)a.q_out + (at_row * a.n_q_heads + head) * kLanes + piece);
         return;

@@ -176,6 +176,35 @@ def test_append_turns_rows_by_their_positions(lib, d, hq, hkv, dims, pairs, far)
         assert np.abs(v[mine]).max() <= 7 and (np.abs(gv[span] - v[mine]) <= np.maximum(step, 2.0 ** -9 * 2.0 ** -6 / 2)).all()
 
 
+@pytest.mark.parametrize("d,dims,pairs", [(128, 128, 0), (128, 128, 1), (64, 64, 0), (64, 32, 0)])
+def test_turned_keys_get_the_nearest_codes(lib, d, dims, pairs):
+    """Where the two products of a turn do not cancel, fp32's result is by 2^-24 (2 |x| + |x|) off at most (sine and cosine, a product, the sum), three units of its last place, and
+    what is so near to a border is turned again: millions of numbers, of which fp32 alone gives some the wrong code, and those of 64 bits, by 2^-33, hardly one in 10^9."""
+    hkv, tokens = 16, 4096
+    pair = Pair8(lib, [], hkv, d, 1024, n_slots=1, max_pages=4, spare=4, fill=0)
+    pair.o.table[0], pair.o.lens[0] = [2, 0, 3, 1], tokens
+    pair.up()
+    gen = torch.Generator("cuda").manual_seed(d + dims + pairs)
+    k = torch.randn((tokens, hkv, d), generator=gen, device="cuda").to(torch.bfloat16)
+    freqs = torch.logspace(0, -4, dims // 2, device="cuda")
+    positions = torch.randint(1, 100000, (tokens,), generator=gen, device="cuda", dtype=torch.int32)
+    append(pair, k, k, tokens, None, [0, tokens], [0], [0], tokens, lib.make_rotation(freqs, positions, dims, pairs))
+    got = torch.empty_like(k)
+    lib.cache8_load(pair.cache, torch.zeros(1, dtype=torch.int32, device="cuda"), None, torch.tensor([0, tokens], dtype=torch.int32, device="cuda"), 1, tokens, got, None, tokens)
+    pair.o.pages = pair.pages.cpu().numpy()
+    powers = torch.tensor([[pair.o.block(pair.o.table[0, t // 32], h, t)[2][0] for h in range(hkv)] for t in range(tokens // 32)]).repeat_interleave(32, 0).double().cuda() - 127
+    angle = positions.double()[:, None] * freqs.double()
+    c, s = angle.cos()[:, None], angle.sin()[:, None]
+    first, second = (slice(0, dims, 2), slice(1, dims, 2)) if pairs else (slice(0, dims // 2), slice(dims // 2, dims))
+    for part, own, other in ((first, c, -s), (second, c, s)):
+        x, y = k[..., part].double() * own, k[..., second if part == first else first].double() * other
+        want, same = x + y, x * y >= 0
+        unit = torch.exp2(torch.floor(torch.log2(want.abs() + 1e-300)) - 3)
+        sure = same & (unit >= torch.exp2(powers)[..., None] * 2.0 ** -9)
+        assert sure.double().mean() > 0.45
+        assert torch.equal(got[..., part].double()[sure], ((want / unit).round() * unit)[sure])
+
+
 @pytest.mark.parametrize("d,hq,hkv,dims,pairs", [(128, 8, 2, 128, 0), (128, 5, 5, 128, 1), (64, 6, 2, 64, 0), (64, 24, 3, 64, 1), (64, 8, 8, 32, 1), (128, 5, 1, 48, 0), (64, 2, 1, 16, 0)])
 def test_turns_of_pieces_of_every_size(lib, d, hq, hkv, dims, pairs):
     """Tokens behind others in a block whose power holds them: one by one, up to nine at a time and all at once leave the same bytes and turn Q alike."""
