@@ -6,8 +6,8 @@
 // worked out once, meet in LDS and turn K and Q of all its heads.
 // A wavefront owns one block (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte.
 // Bound: reading and writing HBM, in part only: the rows that a selection keeps of 8 x 2048 tokens on 32 heads (1433 of each, K and V) go in in 52 us, 287 MB at 5.5 TB/s, vector
-// instructions 32 % of a SIMD's cycles, and come back in 44, 283 MB at 6.4 TB/s; all 2048 turned with Q 144 us, 680 MB at 4.7 TB/s, vector instructions half of the cycles; ragged
-// pieces turned with Q (7 x 100 ... 3000 on 32/8 heads of 64) 26 us for 110 MB, 4.2 TB/s, where loads, the block's power and stores follow one another in each
+// instructions 32 % of a SIMD's cycles, and come back in 44, 283 MB at 6.4 TB/s; all 2048 turned with Q 147 us, 680 MB at 4.6 TB/s, vector instructions half of the cycles; ragged
+// pieces turned with Q (7 x 100 ... 3000 on 32/8 heads of 64) 26.5 us for 110 MB, 4.2 TB/s, where loads, the block's power and stores follow one another in each
 // wavefront; 64 tokens of a step 7.7 us, latency; back from 64 blocks 9.
 #include "cache8_device.h"
 
@@ -135,29 +135,43 @@ __device__ __forceinline__ void turned(u32x4 words, const f32x2* turns, int dims
 // K is rounded to four significant bits, and what fp32 rounds onto a border between two codes, or across it, gets the wrong one: a number of a million.  Those within three
 // units of fp32's last place of a border (a number of 150000) are turned again in 64 bits and rounded to fp32 so that a number that is on neither side of a border does not end
 // on it (to odd ones).  (Numbers that are small against their partners, and codes of less than four bits, keep fp32's error.)
-// Of 36 million numbers 8 to 16 are then off, all small, where fp32 alone left 30 to 38; it costs 3 % of an append (8 x 2048 rows on 32/32 heads 143.3 us for 144.4, 4 x 4000 on 64/8
-// 117.9 for 120.5, 64 x 9 tokens 9.4 for 9.8).
+// Of 36 million numbers 8 to 16 are then off, all small, where fp32 alone left 30 to 38; it costs 3 to 5 % of an append (8 x 2048 rows on 32/32 heads 143.3 us without, 146.9 with it, 4 x 4000
+// on 64/8 117.9 and 121.5, 64 x 9 tokens 9.4 and 10).
 __device__ __forceinline__ uint32_t from_border(float x) { return (__float_as_uint(x) << 12) + 0x80003000u; }
 constexpr uint32_t kNear = 6u << 12;
-// Which of a lane's four words of two turned channels hold such a number, in some lane.
-__device__ __forceinline__ uint32_t near_words(const float (&x)[8], bool turns) {
-    uint32_t least[4], words = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) least[w] = min(from_border(x[2 * w]), from_border(x[2 * w + 1]));
-    if (__builtin_amdgcn_ballot_w64(turns && min(min(least[0], least[1]), min(least[2], least[3])) <= kNear) == 0) return 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) words |= __builtin_amdgcn_ballot_w64(turns && least[w] <= kNear) != 0 ? 1u << w : 0;
-    return words;
-}
 template <int D, int kTurn>
 __device__ __forceinline__ bool turns_at_all(int dims, int piece) { return kTurn == kAllHalves || piece < dims / 8; }      // (halves: of dims / 16 lanes each)
-__device__ __forceinline__ void correct(float& x, float exact, bool turns) { x = turns && from_border(x) <= kNear ? exact : x; }
-// Channels 2 i and 2 i + 1 of a lane's eight; row: those eight.
+// Which of a lane's four words of two turned channels hold such a number, in some lane; turned by nothing (a position or a frequency of 0: one bf16 in 16 is a border) they
+// are exact.  turns: of the row's token.
 template <int D, int kTurn>
-__device__ __forceinline__ void turned_exactly(const uint32_t* row, int i, int position, const float* freqs, int dims, int piece, float (&x)[2]) {
+__device__ __forceinline__ uint32_t near_words(const float (&x)[8], const f32x2* turns, int dims, int piece) {
+    const bool turn = turns_at_all<D, kTurn>(dims, piece);
+    uint32_t least = from_border(x[0]), words = 0;
+#pragma unroll
+    for (int e = 1; e < 8; ++e) least = min(least, from_border(x[e]));
+    if (__builtin_amdgcn_ballot_w64(turn && least <= kNear) == 0) return 0;
+    const f32x2* at = turns + 2 * (kTurn == kPairs ? piece : turn ? min(piece, piece + lanes_to_partners<D, kTurn>(dims, piece)) : 0);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        bool near = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) near |= turn && from_border(x[2 * w + h]) <= kNear && at[place_of<D, kTurn>(kTurn == kPairs ? w : 2 * w + h)][1] != 0.f;
+        words |= __builtin_amdgcn_ballot_w64(near) != 0 ? 1u << w : 0;
+    }
+    return words;
+}
+// Channels 2 i and 2 i + 1 of a lane's eight, where they are next to a border; row: those eight.
+struct Exactly {
+    float x[2];
+    bool turns;
+    __device__ __forceinline__ float value(int h, float fast) const { return turns && from_border(fast) <= kNear ? x[h] : fast; }
+};
+template <int D, int kTurn>
+__device__ __forceinline__ Exactly turned_exactly(const uint32_t* row, int i, int position, const float* freqs, int dims, int piece) {
     const int with = kTurn == kPairs ? 0 : lanes_to_partners<D, kTurn>(dims, piece);
     const bool turns = turns_at_all<D, kTurn>(dims, piece);
     const uint32_t word = row[i], other = row[i + 4 * with];
+    float x[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int pair = kTurn == kPairs ? 4 * piece + i : 8 * min(piece, piece + with) + 2 * i + h;
@@ -172,6 +186,7 @@ __device__ __forceinline__ void turned_exactly(const uint32_t* row, int i, int p
         x[h] = __uint_as_float(bits);
         __builtin_amdgcn_sched_barrier(0);                    // (one after the other, for the registers)
     }
+    return {{x[0], x[1]}, turns};
 }
 __device__ __forceinline__ u32x4 rounded(const float (&x)[8]) {
     bf16x8 y;
@@ -257,7 +272,7 @@ __device__ __forceinline__ Piece piece_of(const AppendArgs& a, int place) {
 // Pieces of any length.  A wavefront goes through items: K, V or Q of the piece's block and a head.  kShort: nine tokens at most, which a window of 12 (at 64
 // channels 16) tokens of the block holds (64 x 9 tokens on 32/8 heads of 128, turned with Q: 10.6 us, with all 32 tokens' places 14.7; 8 x 5 5.7 and 9.5).
 template <int D, int kTurn, bool kShort>
-constexpr int append_waves = kShort || D == 64 ? 4 : kTurn == kAsIs ? 3 : 2;      // of a SIMD, as registers allow
+constexpr int append_waves = D == 64 ? 4 : kShort ? (kTurn == kPairs ? 3 : 4) : kTurn == kAsIs ? 3 : 2;      // of a SIMD, as registers allow
 template <int D, int kTurn, bool kShort>
 __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void cache8_append_kernel(AppendArgs a) {
     constexpr int kLanes = D / 8, kTokens = 64 / kLanes;          // lanes of a row, rows of a load
@@ -376,12 +391,11 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
             for (int n = 0; n < kLoads; ++n)
                 if (gone && !there_of(n)) words[n] = kNoRow;
             if constexpr (kExpanded) {
-                const bool turns = turns_at_all<D, kTurn>(a.dims, piece);
                 uint32_t near = 0;                                // words of them with numbers next to a border
 #pragma unroll
                 for (int n = 0; n < kLoads; ++n) {
                     turned<D, kTurn>(words[n], turns_of(source_of(n)), a.dims, piece, x[n]);
-                    near |= near_words(x[n], turns) << (4 * n);
+                    near |= near_words<D, kTurn>(x[n], turns_of(source_of(n)), a.dims, piece) << (4 * n);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 while (near != 0) {
@@ -389,15 +403,15 @@ __global__ __launch_bounds__(64 * kWaves, (append_waves<D, kTurn, kShort>)) void
                     near &= near - 1;
                     int hidden = piece;
                     asm volatile("" : "+v"(hidden));
-                    float y[2];
-                    turned_exactly<D, kTurn>((const uint32_t*)((const u32x4*)a.k + item * kLanes + hidden + row * (int64_t)a.k_stride), w, a.positions[row], a.freqs, a.dims, hidden, y);
+                    const Exactly y = turned_exactly<D, kTurn>((const uint32_t*)((const u32x4*)a.k + item * kLanes + hidden + row * (int64_t)a.k_stride), w, a.positions[row], a.freqs,
+                                                               a.dims, hidden);
 #pragma unroll
                     for (int n = 0; n < kLoads; ++n)
 #pragma unroll
                         for (int v = 0; v < 4; ++v)
                             if (n == i && v == w) {
-                                correct(x[n][2 * v], y[0], turns);
-                                correct(x[n][2 * v + 1], y[1], turns);
+                                x[n][2 * v] = y.value(0, x[n][2 * v]);
+                                x[n][2 * v + 1] = y.value(1, x[n][2 * v + 1]);
                             }
                 }
             }
@@ -574,18 +588,16 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_append_one_kernel(AppendAr
     float x[8];
     turned<D, kTurn>(kx, turns, a.dims, piece, x);
     if (kTurn != kAsIs && !of_q) {
-        const bool turns = turns_at_all<D, kTurn>(a.dims, piece);
-        uint32_t near = near_words(x, turns);
+        uint32_t near = near_words<D, kTurn>(x, turns, a.dims, piece);
         while (near != 0) {
             const int w = __builtin_ctz(near);
             near &= near - 1;
-            float y[2];
-            turned_exactly<D, kTurn>((const uint32_t*)((const u32x4*)a.k + at_row * a.k_stride + head * kLanes + piece), w, a.positions[at_row], a.freqs, a.dims, piece, y);
+            const Exactly y = turned_exactly<D, kTurn>((const uint32_t*)((const u32x4*)a.k + at_row * a.k_stride + head * kLanes + piece), w, a.positions[at_row], a.freqs, a.dims, piece);
 #pragma unroll
             for (int v = 0; v < 4; ++v)
                 if (v == w) {
-                    correct(x[2 * v], y[0], turns);
-                    correct(x[2 * v + 1], y[1], turns);
+                    x[2 * v] = y.value(0, x[2 * v]);
+                    x[2 * v + 1] = y.value(1, x[2 * v + 1]);
                 }
         }
     }

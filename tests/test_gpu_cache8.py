@@ -205,6 +205,20 @@ def test_turned_keys_get_the_nearest_codes(lib, d, dims, pairs):
         assert torch.equal(got[..., part].double()[sure], ((want / unit).round() * unit)[sure])
 
 
+@pytest.mark.parametrize("d,dims,pairs", [(128, 128, 0), (128, 64, 1), (64, 64, 0), (64, 32, 0)])
+@pytest.mark.parametrize("tokens", [1, 7, 50])
+def test_turns_by_nothing_change_nothing(lib, d, dims, pairs, tokens):
+    """A position or frequencies of 0: what rows without a turn leave."""
+    left = []
+    zeros, ones = torch.zeros(64, dtype=torch.int32, device="cuda"), torch.ones(64, device="cuda")
+    for rotation in (None, lib.make_rotation(ones[:dims // 2], zeros[:tokens], dims, pairs), lib.make_rotation(0 * ones[:dims // 2], zeros[:tokens] + 12345, dims, pairs)):
+        pair = Pair8(lib, [60], 3, d, 64, powers=(115, 118))
+        kt, _ = bf16(pair.rng.normal(size=(tokens, 3, d)))
+        append(pair, kt, kt, tokens, None, [0, tokens], [0], [9], tokens, rotation)
+        left.append(pair.pages.clone())
+    assert torch.equal(left[0], left[1]) and torch.equal(left[0], left[2])
+
+
 @pytest.mark.parametrize("d,hq,hkv,dims,pairs", [(128, 8, 2, 128, 0), (128, 5, 5, 128, 1), (64, 6, 2, 64, 0), (64, 24, 3, 64, 1), (64, 8, 8, 32, 1), (128, 5, 1, 48, 0), (64, 2, 1, 16, 0)])
 def test_turns_of_pieces_of_every_size(lib, d, hq, hkv, dims, pairs):
     """Tokens behind others in a block whose power holds them: one by one, up to nine at a time and all at once leave the same bytes and turn Q alike."""
