@@ -550,7 +550,7 @@ PYR_API int pyr_cache8_select(const pyr_cache8* cache, const void* q, const int3
  *                      An entry that is no block which the token sees is left out, one that is there twice counts twice.
  *   max_len            as in pyr_cache_attention; not looked at where there are lists
  *   q, slots, softmax_scale, out, lse, workspace  as in pyr_cache_attention
- * bf16 MFMA products on the cache's exact values (P is rounded to bf16), fp32 accumulation and softmax.  Sums of P V stay in fp32's range as long as V's
+ * bf16 MFMA products on the cache's exact values (P as the sum of two bf16 numbers, sixteen bits), fp32 accumulation and softmax.  Sums of P V stay in fp32's range as long as V's
  * largest power of two times the sequence's tokens is below 2^108 (a number whose sum leaves it is NaN).
  * A row that sees nothing (an empty slot, a skipped row, a list without blocks): zeros in out, -inf in lse.  A K that is NaN makes the rows that see it NaN, a V
  * the channel of those rows; what a row does not see never reaches it.  A page outside the pool among those that it takes: NaN in the sequence's rows, or the list's.

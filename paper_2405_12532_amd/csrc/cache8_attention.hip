@@ -7,8 +7,10 @@
 //   S^T = K Q^T      16 tokens x 16 rows, contracted over 32 channels a step
 //   O^T = V^T P^T    16 channels x 16 rows, contracted over the 32 tokens
 // K and V are converted to bf16 with their power (exactly), and the layout of the block makes every operand what a lane loads or has computed: nothing
-// passes through LDS but the wavefronts' results at the end.  P is rounded to bf16 (up to 2^-8, as in pyr_attention); one more product, of ones
-// and the rounded P, sums what O is divided by, lse comes from the sum before rounding.  P, both sums and O are fp32.
+// passes through LDS but the wavefronts' results at the end.  P goes into the product as two bf16 numbers, the nearest one and the nearest one to what that
+// leaves: sixteen bits, off by 2^-16 at most.  (One alone, off by 2^-8, took outputs from 0.0017 off, rms over rms, which is their own rounding, to 0.0018 to 0.0023.  The second
+// product costs 0 to 3 % where bytes bound, 64 x 2048 on 32 heads 162 us either way; 16 x 2048 on 64/8 heads with nine tokens, bound by instructions, 30 us for 26.5.)  P, its sum
+// and O are fp32.
 // A row's reference is its largest logit when it was last moved, and it is moved when the weights of a block add up to more than 2^12 in a lane.
 // Bound: reading the cache, past the caches: 64 x 2048 tokens on 32 heads of 128 channels in 162 us, 1077 MB at 6.6 TB/s (through the caches 182), vector
 // instructions 22 % of a SIMD's cycles and matrix instructions 10 %; 32 x 307 ... 4915 tokens on 40 heads, four tokens each, 128 us, 6.1 TB/s; lists of 16 blocks, 64 x
@@ -30,7 +32,7 @@ struct AttendArgs {
     const int32_t* slots;
     const int32_t* blocks;                        // lists [n, tokens, Hkv, n_blocks]
     void* out;                                    // splits == 1: bf16 [n, tokens, Hq, D]; else fp32 [splits, rows, D], not normalised
-    float* lse;                                   // splits == 1: [rows] or NULL; else [splits, rows, 4]: reference, sum, sum of the rounded
+    float* lse;                                   // splits == 1: [rows] or NULL; else [splits, rows, 4]: reference, sum, the sum again (what O is divided by)
     int32_t n_seqs, n_tokens, n_blocks;
     int32_t chunk;                                // blocks of a split (the last one takes what is left)
     uint16_t n_q_heads, splits;
@@ -69,7 +71,6 @@ template <int D, int NT>
 struct Rows {
     bf16x8 q[NT][D / 32];                         // operand of step i: lane 16 j + col
     f32x4 o[NT][D / 16];
-    f32x4 weight[NT];                             // sum of the rounded P, in every element
     float m[NT], l[NT];                           // reference; sum of P over the tokens that this lane sees
     int32_t seen[NT];                             // tokens that the row of this lane's column sees
 };
@@ -95,9 +96,6 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT>& w, Tile<D>& t, bool mas
 #pragma unroll
             for (int e = 0; e < 4; ++e) p[n][4 * half + e] = s[n][e];
     }
-    bf16x8 ones;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
     if (masked) {
         const int mine = t.token + 4 * (lane >> 4);
 #pragma unroll
@@ -171,25 +169,36 @@ __device__ __forceinline__ void attend_tile(Rows<D, NT>& w, Tile<D>& t, bool mas
             const float f = __builtin_amdgcn_exp2f(w.m[n] - m);
             w.m[n] = m;
             w.l[n] *= f;
-            w.weight[n] *= f;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) w.o[n][i] *= f;
         }
         weigh();
     }
-    bf16x8 rounded[NT];
+    // What P's nearest bf16 numbers leave, exactly: a product of a pair with -1 and 0 takes one of them off, where a subtraction would need it by itself first.  (In registers:
+    // written as an operand, the instruction takes a constant of -1 for one of fp32, whose upper half is a bf16's.)
+    uint32_t less_first = 0xbf80u, less_second = 0xbf800000u;
+    asm volatile("" : "+s"(less_first), "+s"(less_second));
+    bf16x8 high[NT], low[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         w.l[n] += sum[n];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rounded[n][e] = (__bf16)x[n][e];
-        w.weight[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, rounded[n], w.weight[n], 0, 0, 0);
+        for (int e = 0; e < 8; e += 2) {
+            const bf16x2 y = {(__bf16)x[n][e], (__bf16)x[n][e + 1]};
+            high[n][e] = y[0];
+            high[n][e + 1] = y[1];
+            low[n][e] = (__bf16)__builtin_amdgcn_fdot2_f32_bf16(y, __builtin_bit_cast(bf16x2, less_first), x[n][e], false);
+            low[n][e + 1] = (__bf16)__builtin_amdgcn_fdot2_f32_bf16(y, __builtin_bit_cast(bf16x2, less_second), x[n][e + 1], false);
+        }
     }
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
         const bf16x8 y = values8_of(t.v[i >> 1][2 * (i & 1)], t.v[i >> 1][2 * (i & 1) + 1], t.vs);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) w.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, rounded[n], w.o[n][i], 0, 0, 0);
+        for (int n = 0; n < NT; ++n) {
+            w.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, high[n], w.o[n][i], 0, 0, 0);
+            w.o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, low[n], w.o[n][i], 0, 0, 0);
+        }
     }
 }
 
@@ -198,7 +207,7 @@ template <int D, int NT, int kWaves, bool kListed, bool kOnce>
 __global__ __launch_bounds__(64 * kWaves, NT == 1 && D == 64 ? 3 : 2) void cache8_attention_kernel(AttendArgs a) {
     constexpr int kRow = D + 4, kCols = 16 * NT;           // floats of a row in LDS; rows of a workgroup
     __shared__ __align__(16) float results[kWaves][kCols][kRow];
-    __shared__ __align__(16) float stats[kWaves][kCols][4];      // reference, sum, sum of the rounded
+    __shared__ __align__(8) float stats[kWaves][kCols][2];       // reference, sum
     __shared__ int32_t places[kCols];                      // rows of q and out; -1: none
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = lane >> 4, c = lane & 15;
     const int hkv = a.c.n_kv_heads, g = a.n_q_heads / hkv, cols = kListed ? g : a.n_tokens * g;
@@ -243,7 +252,6 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && D == 64 ? 3 : 2) void cache
         w.seen[n] = min(len - a.n_tokens + 1 + token, len);
         w.m[n] = -FLT_MAX;
         w.l[n] = 0.f;
-        w.weight[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
             w.q[n][i] = row >= 0 ? *(const bf16x8*)(a.q + (int64_t)row * D + 64 * (i >> 1) + 16 * j + 8 * (i & 1)) : bf16x8{};
@@ -307,7 +315,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && D == 64 ? 3 : 2) void cache
     for (int n = 0; n < NT; ++n) {
         const int at = 16 * n + c;
         w.l[n] = bad ? NAN : sum_of_groups(w.l[n]);
-        if (j == 0) *(f32x4*)stats[wave][at] = f32x4{w.m[n], w.l[n], bad ? NAN : w.weight[n][0], 0.f};
+        if (j == 0) *(f32x2*)stats[wave][at] = f32x2{w.m[n], w.l[n]};
         if (first_col + at < cols) {
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) *(f32x4*)&results[wave][at][16 * i + 4 * j] = w.o[n][i];
@@ -319,20 +327,19 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && D == 64 ? 3 : 2) void cache
 #pragma unroll 1
     for (int i = threadIdx.x; i < here * (D / 4); i += 64 * kWaves) {
         const int r = i / (D / 4), c4 = i % (D / 4), row = places[r];
-        float top = stats[0][r][0], sum = 0.f, weight = 0.f;
+        float top = stats[0][r][0], sum = 0.f;
 #pragma unroll
         for (int v = 1; v < kWaves; ++v) top = fmaxf(top, stats[v][r][0]);
         f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < kWaves; ++v) {
-            const f32x4 st = *(const f32x4*)stats[v][r];
+            const f32x2 st = *(const f32x2*)stats[v][r];
             const float f = __builtin_amdgcn_exp2f(st[0] - top);
             sum += f * st[1];
-            weight += f * st[2];
             o += f * *(const f32x4*)&results[v][r][4 * c4];
         }
         if (a.splits == 1) {
-            const float f = weight == 0.f ? 0.f : 1.f / weight;
+            const float f = sum == 0.f ? 0.f : 1.f / sum;
             bf16x4 y;
 #pragma unroll
             for (int x = 0; x < 4; ++x) y[x] = quotient(o[x], f);
@@ -340,7 +347,7 @@ __global__ __launch_bounds__(64 * kWaves, NT == 1 && D == 64 ? 3 : 2) void cache
             if (a.lse != nullptr && c4 == 0) a.lse[row] = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
         } else {
             *(f32x4*)((float*)a.out + (part + row) * D + 4 * c4) = o;
-            if (c4 == 0) *(f32x4*)(a.lse + 4 * (part + row)) = f32x4{top, sum, weight, 0.f};
+            if (c4 == 0) *(f32x4*)(a.lse + 4 * (part + row)) = f32x4{top, sum, sum, 0.f};
         }
     }
 }
