@@ -473,7 +473,7 @@ PYR_API int pyr_cache_attention(const pyr_cache* cache, const void* q, const int
  *   [H][T]  2 bytes     powers of K and of V: 2^(byte - 127)
  *
  * Host checks as above, and PYR_ERR_UNSUPPORTED for pages of 2^31 bytes or more and for lists of more than 2^26 blocks; a workgroup takes a sequence's 32
- * tokens of up to four heads of K, V and Q where rows go in, a token's KV head where blocks are chosen or listed.
+ * tokens of up to four heads of K, V and Q where rows go in, a token's KV head where blocks are chosen or listed (among more than 256 blocks, 2^23 are too many already).
  */
 typedef struct pyr_cache8 {
     pyr_cache pool;       /* pages of pyr_cache8_page_bytes() bytes                                  */

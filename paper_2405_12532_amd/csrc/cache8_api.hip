@@ -9,7 +9,7 @@ constexpr size_t kAlign = 256;
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 constexpr int64_t kMost = (int64_t)1 << 31;
-constexpr int64_t kMostGroups = (int64_t)1 << 24;                // workgroups of 256 threads: a launch has fewer than 2^32 threads
+constexpr int64_t kMostGroups = (int64_t)1 << 24;                // workgroups of four wavefronts: a launch has fewer than 2^32 threads
 
 constexpr int64_t kMostBlocks = (int64_t)1 << 26;               // of a list: no pool has more
 
@@ -84,7 +84,8 @@ int check_select(const pyr_cache8* cache, int32_t n, int32_t n_tokens, int32_t n
     if (rc != PYR_OK) return rc;
     if ((int64_t)n * n_tokens * cache->pool.n_kv_heads >= kMostGroups) return PYR_ERR_UNSUPPORTED;
     *plan = pyr::plan_cache8_select(n, n_tokens, cache->pool.n_kv_heads, within_row(cache, max_len));
-    return (int64_t)n * n_tokens * cache->pool.n_kv_heads * plan->chunks >= kMostGroups ? PYR_ERR_UNSUPPORTED : PYR_OK;
+    const int64_t units = (int64_t)n * n_tokens * cache->pool.n_kv_heads;
+    return units * plan->chunks >= kMostGroups || units * plan->waves >= 4 * kMostGroups ? PYR_ERR_UNSUPPORTED : PYR_OK;
 }
 
 bool workspace_ok(const void* ws, size_t have, size_t need) { return need == 0 || (ws != nullptr && (uintptr_t)ws % kAlign == 0 && have >= need); }

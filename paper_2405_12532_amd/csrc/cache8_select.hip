@@ -480,14 +480,13 @@ constexpr int kAtOnce = 4096;                    // candidates whose keys a work
 
 template <int D>
 void launch(const CacheSelect& x, const SelectArgs& a, unsigned units, hipStream_t stream) {
-    const int n = x.max_blocks;
-    if (x.chunks > 0) hipLaunchKernelGGL((cache8_select_many_kernel<D, 16, true>), dim3(units), dim3(1024), 0, stream, a);
-    else if (n <= 64) hipLaunchKernelGGL((cache8_select_kernel<D, 1>), dim3(units), dim3(64), 0, stream, a);
-    else if (n <= 256) hipLaunchKernelGGL((cache8_select_kernel<D, 4>), dim3(units), dim3(256), 0, stream, a);
-    else if (n <= 512) hipLaunchKernelGGL((cache8_select_kernel<D, 8>), dim3(units), dim3(512), 0, stream, a);
-    // (1024 at once of few units: 128 x 1024 blocks 13.4 us, by parts 15.1; 256 x 640 at 64 channels 8.8 and 10.8, but 768 x 640 29.6 and 27.8, 1600 x 750 52 and 43)
-    else if (n <= 1024 && units <= 256) hipLaunchKernelGGL((cache8_select_kernel<D, 16>), dim3(units), dim3(1024), 0, stream, a);
-    else hipLaunchKernelGGL((cache8_select_many_kernel<D, 8, false>), dim3(units), dim3(512), 0, stream, a);
+    const dim3 threads(64 * x.waves);
+    if (x.chunks > 0) hipLaunchKernelGGL((cache8_select_many_kernel<D, 16, true>), dim3(units), threads, 0, stream, a);
+    else if (x.max_blocks > 64 * x.waves) hipLaunchKernelGGL((cache8_select_many_kernel<D, 8, false>), dim3(units), threads, 0, stream, a);
+    else if (x.waves == 1) hipLaunchKernelGGL((cache8_select_kernel<D, 1>), dim3(units), threads, 0, stream, a);
+    else if (x.waves == 4) hipLaunchKernelGGL((cache8_select_kernel<D, 4>), dim3(units), threads, 0, stream, a);
+    else if (x.waves == 8) hipLaunchKernelGGL((cache8_select_kernel<D, 8>), dim3(units), threads, 0, stream, a);
+    else hipLaunchKernelGGL((cache8_select_kernel<D, 16>), dim3(units), threads, 0, stream, a);
 }
 
 }  // namespace
@@ -497,6 +496,9 @@ CacheSelect plan_cache8_select(int32_t n_seqs, int32_t n_tokens, int32_t n_kv_he
     const int64_t units = (int64_t)n_seqs * n_tokens * n_kv_heads, blocks = (max_len + 31) / 32;
     x.max_blocks = (int32_t)blocks;
     x.chunks = 0;
+    // A wavefront for 64 blocks; more than 512 (1024 of few units) by eight in parts.  Measured, us, 1024 at once and by parts: 128 x 1024 blocks 13.4 and 15.1; 256 x 640 at 64
+    // channels 8.8 and 10.8, but 768 x 640 29.6 and 27.8, 1600 x 750 52 and 43.
+    x.waves = blocks <= 64 ? 1 : blocks <= 256 ? 4 : blocks > 512 && blocks <= 1024 && units <= 256 ? 16 : 8;
     // A unit's workgroup scores its blocks by itself unless they are many and the units leave compute units idle.  Measured, us, alone and with a launch for the scores,
     // units x blocks: 8 x 512 7.7 and 10.0, 8 x 1024 12.9 and 9.6, 64 x 640 10.4 and 11.3, 64 x 1024 13.6 and 12.2, 64 x 4096 38.2 and 23.5, 128 x 1024 13.4 and 14.3,
     // 128 x 2048 23.1 and 21.9, 128 x 4096 39.2 and 33.4, 256 x 1024 18.5 and 21.9, 768 x 640 27.9 and 32.8
@@ -506,6 +508,7 @@ CacheSelect plan_cache8_select(int32_t n_seqs, int32_t n_tokens, int32_t n_kv_he
         while ((blocks + x.chunk - 1) / x.chunk > 32768) x.chunk *= 2;
         x.chunks = (int32_t)((blocks + x.chunk - 1) / x.chunk);
         x.key_bytes = (size_t)units * blocks * sizeof(uint32_t);
+        x.waves = 16;
     }
     return x;
 }

@@ -204,9 +204,10 @@ CacheAttention plan_cache8_attention(int32_t n_seqs, int32_t n_tokens, int32_t n
 int launch_cache8_attention(const CacheAttention& plan, const CacheView& c, int32_t head_dim, const void* q, const int32_t* slots, int32_t n_seqs,
                             int32_t n_tokens, int32_t n_q_heads, const int32_t* blocks, int32_t n_blocks, float scale_log2, void* out, float* lse, void* parts,
                             float* stats, hipStream_t stream);
-// How a choice of blocks is cut up: blocks within max_len; chunks of candidates that a launch of its own scores (0: none), and what their keys take.
+// How a choice of blocks is cut up: blocks within max_len; chunks of candidates that a launch of its own scores (0: none), and what their keys take; wavefronts of a unit's
+// workgroup.
 struct CacheSelect {
-    int32_t max_blocks, chunk, chunks;
+    int32_t max_blocks, chunk, chunks, waves;
     size_t key_bytes;
 };
 CacheSelect plan_cache8_select(int32_t n_seqs, int32_t n_tokens, int32_t n_kv_heads, int64_t max_len);

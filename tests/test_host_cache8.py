@@ -102,6 +102,19 @@ def test_tensors_that_do_not_belong_together():
             binding.make_rotation(*bad)
 
 
+def test_choices_that_one_launch_cannot_make():
+    """A launch has fewer than 2^32 threads: 2^24 workgroups of up to four wavefronts, half of them of eight."""
+    few, many = cache(n_kv_heads=1, max_pages=128), cache(n_kv_heads=1, max_pages=1024)
+    for n, most, fine in (((1 << 24) - 1, 8192, True), (1 << 24, 8192, False), ((1 << 23) - 1, 8192 + 1, True), (1 << 23, 8192 + 1, False), (1 << 23, 16384, False),
+                          ((1 << 23) - 1, 65536, True), (1 << 23, 65536, False), (1 << 23, 2 ** 31 - 1, False)):
+        size, c = ctypes.c_size_t(0), ctypes.byref(many)
+        assert call("pyr_cache8_select_workspace_bytes", c, n, 1, 1, most, ctypes.byref(size)) == (OK if fine else UNSUPPORTED), (n, most)
+        if not fine:
+            assert call("pyr_cache8_select", c, 0x1000, 0x2000, n, 1, 1, most, 1, 1, 1, 0x3000, 0x100, 1 << 62, None) == UNSUPPORTED
+    size = ctypes.c_size_t(0)                                                            # (this one's slots hold 8192 tokens)
+    assert call("pyr_cache8_select_workspace_bytes", ctypes.byref(few), (1 << 24) - 1, 1, 1, 2 ** 31 - 1, ctypes.byref(size)) == OK
+
+
 def test_rows_and_sizes_that_cannot_be():
     c = ctypes.byref(cache())
     assert call("pyr_cache8_fork", c, 0x1000, None, 2, 0x4000, None) == NULL
