@@ -500,8 +500,8 @@ typedef struct pyr_rotation {
  *   k, v               dev bf16 [n_rows, Hkv, d], rows k_stride and v_stride elements apart (a multiple of 8; 0: Hkv * d)
  *   row_idx            dev int32 [n_list] or NULL (then n_list = n_rows)
  *   offsets            dev int32 [n+1];  slots, start  dev int32 [n]
- *   rotation           host, its pointers dev; NULL or dims 0: nothing turns.  Sine and cosine of p f_i are worked out in 64 bits and rounded to fp32, the turn
- *                      itself is fp32, and K is rounded once, to its code (again in 64 bits where fp32 leaves it next to a border between two)
+ *   rotation           host, its pointers dev; NULL or dims 0: nothing turns.  Sine and cosine of p f_i are worked out in 64 bits (by less than 2^-32 off for |p f_i| up to
+ *                      2^47, those of some angle beyond it) and rounded to fp32, the turn itself is fp32, and K is rounded once, to its code (again in 64 bits where fp32 leaves it next to a border between two)
  *   q                  dev bf16 [n_rows, Hq, d], rows q_stride elements apart, or NULL
  *   q_out              dev bf16 [n_rows, Hq, d], written: the rows of q whose tokens are stored, turned; the others stay as they were
  * Tokens from lens[slots[i]] on (they were not reserved), tokens that have no page and a start of -1 are not stored; a row outside k and v or the list is

@@ -1,8 +1,8 @@
 // New rows into the cache held in 8 bits, turned by their positions on the way (Algorithm 1, the new rows of KV = cat(PvC_past, KV); what
 // Gather(KV, index) keeps of a prompt goes the same way, through its index), tokens of it back to bf16, and pages copied for a fork.
 //
-// A turn by position p takes channels a and b of a pair i to a cos(p f_i) - b sin(p f_i) and b cos(p f_i) + a sin(p f_i).  p f_i is reduced to a
-// quarter of a turn in 64 bits, so that far positions lose nothing; sine and cosine are Taylor's sums on [-pi/4, pi/4] in 64 bits too, rounded to 32.  A workgroup takes 32 tokens and some heads: the pairs are
+// A turn by position p takes channels a and b of a pair i to a cos(p f_i) - b sin(p f_i) and b cos(p f_i) + a sin(p f_i).  p f_i, of up to 55 bits, is two
+// numbers of 64 bits, and so is the quarter of a turn that it is reduced by, so that far positions lose nothing; sine and cosine are Taylor's sums on [-pi/4, pi/4] in 64 bits too, rounded to 32.  A workgroup takes 32 tokens and some heads: the pairs are
 // worked out once, meet in LDS and turn K and Q of all its heads.
 // A wavefront owns one block (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte.
 // Bound: reading and writing HBM, in part only: the rows that a selection keeps of 8 x 2048 tokens on 32 heads (1433 of each, K and V) go in in 52 us, 287 MB at 5.5 TB/s, vector
@@ -35,14 +35,16 @@ __device__ __forceinline__ void meet() {            // (a wavefront's own part o
 __device__ __forceinline__ float low_of(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float high_of(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
-// cos and sin of position * freq, in 64 bits (the sums' next terms are below 2^-33)
+// cos and sin of position * freq, in 64 bits (the sums' next terms are below 2^-33), for angles up to 2^47; of larger ones, whose number of quarters is not known to a whole one,
+// those of some angle
 struct Turn {
     double c, s;
 };
 __device__ __forceinline__ Turn exact_turn_of(int position, float freq) {
-    const double quarters = (double)position * ((double)freq * 0.63661977236758134308);      // of a turn: times 2 / pi
-    const double nearest = __builtin_rint(quarters);
-    const double x = (quarters - nearest) * 1.57079632679489661923, y = x * x;
+    const double angle = (double)position * (double)freq, rest = __builtin_fma((double)position, (double)freq, -angle);
+    const double nearest = __builtin_rint(angle * 0.63661977236758134308);      // quarters of a turn: times 2 / pi
+    const double near = __builtin_fma(-nearest, 6.123233995736766e-17, __builtin_fma(-nearest, 1.57079632679489661923, angle)) + rest;      // (pi / 2 in two parts)
+    const double x = __builtin_fmin(__builtin_fmax(near, -1.), 1.), y = x * x;
     const double s = x * (1. + y * (-1. / 6 + y * (1. / 120 + y * (-1. / 5040 + y * (1. / 362880 - y * (1. / 39916800))))));
     const double c = 1. + y * (-0.5 + y * (1. / 24 + y * (-1. / 720 + y * (1. / 40320 - y * (1. / 3628800)))));
     const int quadrant = (int)(nearest - 4.0 * __builtin_floor(nearest * 0.25));

@@ -205,6 +205,49 @@ def test_turned_keys_get_the_nearest_codes(lib, d, dims, pairs):
         assert torch.equal(got[..., part].double()[sure], ((want / unit).round() * unit)[sure])
 
 
+@pytest.mark.parametrize("d,dims,pairs", [(128, 128, 0), (128, 128, 1), (64, 64, 0)])
+@pytest.mark.parametrize("far", [2 ** 21, 2 ** 24, 2 ** 31 - 4096, -2 ** 31])
+def test_turned_keys_get_the_nearest_codes_at_far_positions(lib, d, dims, pairs, far):
+    """As above, where an angle has more bits than a number of 64 bits holds, or its quarters of a turn take most of them: against angles, sines and cosines of 80 bits, in which a
+    position times a frequency (31 and 24 bits) is exact."""
+    hkv, tokens = 16, 4096
+    pair = Pair8(lib, [], hkv, d, 1024, n_slots=1, max_pages=4, spare=4, fill=0)
+    pair.o.table[0], pair.o.lens[0] = [2, 0, 3, 1], tokens
+    pair.up()
+    gen = torch.Generator("cuda").manual_seed(d + dims + pairs)
+    k = torch.randn((tokens, hkv, d), generator=gen, device="cuda").to(torch.bfloat16)
+    freqs = torch.linspace(1, 0.5, dims // 2, device="cuda")
+    positions = torch.arange(far, far + tokens, device="cuda").to(torch.int32)
+    append(pair, k, k, tokens, None, [0, tokens], [0], [0], tokens, lib.make_rotation(freqs, positions, dims, pairs))
+    got = torch.empty_like(k)
+    lib.cache8_load(pair.cache, dev([0]), None, dev([0, tokens]), 1, tokens, got, None, tokens)
+    pair.o.pages = pair.pages.cpu().numpy()
+    powers = torch.tensor([[pair.o.block(pair.o.table[0, t // 32], h, t)[2][0] for h in range(hkv)] for t in range(tokens // 32)]).repeat_interleave(32, 0).double().cuda() - 127
+    angle = positions.cpu().numpy().astype(np.longdouble)[:, None] * freqs.cpu().numpy().astype(np.longdouble)
+    c, s = (torch.from_numpy(f(angle).astype(np.float64)).cuda()[:, None] for f in (np.cos, np.sin))
+    first, second = (slice(0, dims, 2), slice(1, dims, 2)) if pairs else (slice(0, dims // 2), slice(dims // 2, dims))
+    for part, own, other in ((first, c, -s), (second, c, s)):
+        x, y = k[..., part].double() * own, k[..., second if part == first else first].double() * other
+        want, same = x + y, x * y >= 0
+        unit = torch.exp2(torch.floor(torch.log2(want.abs() + 1e-300)) - 3)
+        sure = same & (unit >= torch.exp2(powers)[..., None] * 2.0 ** -9)
+        assert sure.double().mean() > 0.45
+        assert torch.equal(got[..., part].double()[sure], ((want / unit).round() * unit)[sure])
+
+
+def test_angles_that_64_bits_do_not_hold_turn_all_the_same(lib):
+    """Frequencies up to fp32's largest: a turn by some angle, which leaves a pair's length (within half a step of bf16 a number, 2^-8, and 2^-20 besides)."""
+    pair = Pair8(lib, [60], 2, 128, 64)
+    qt, q = bf16(pair.rng.normal(size=(50, 4, 128)))
+    kt, _ = bf16(pair.rng.normal(size=(50, 2, 128)))
+    positions = dev(pair.rng.integers(-2 ** 31, 2 ** 31, 50).astype(np.int32))
+    q_out = torch.empty_like(qt)
+    append(pair, kt, kt, 50, None, [0, 50], [0], [5], 50, lib.make_rotation(torch.logspace(3, 38.5, 64, device="cuda"), positions, 128), qt, q_out)
+    got = q_out.double().cpu().numpy()
+    want = np.hypot(q[..., :64], q[..., 64:])
+    assert (np.abs(np.hypot(got[..., :64], got[..., 64:]) - want) <= (2.0 ** -8 + 2.0 ** -20) * want).all()
+
+
 @pytest.mark.parametrize("d,dims,pairs", [(128, 128, 0), (128, 64, 1), (64, 64, 0), (64, 32, 0)])
 @pytest.mark.parametrize("tokens", [1, 7, 50])
 def test_turns_by_nothing_change_nothing(lib, d, dims, pairs, tokens):
