@@ -41,6 +41,7 @@ class PyrCache8(ctypes.Structure):
 
 class PyrRotation(ctypes.Structure):
     _fields_ = [("freqs", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+    rows = 2 ** 31 - 1       # that have a position; make_rotation knows
 
 
 class PyrCacheRoute(ctypes.Structure):
@@ -429,13 +430,15 @@ def make_cache8(pages, refs, table, lens, page_tokens: int, n_kv_heads: int, hea
 
 
 def make_rotation(freqs, positions, dims: int, interleaved: bool = False) -> PyrRotation:
-    """freqs fp32 [dims / 2], positions int32, one for every row.  It keeps the tensors alive."""
+    """freqs fp32 [dims / 2], positions int32, one for every row: cache8_append refuses more rows than there are.  It keeps the tensors alive."""
     import torch
     if not (freqs.is_contiguous() and positions.is_contiguous()) or freqs.dtype != torch.float32 or positions.dtype != torch.int32 or \
             freqs.numel() < int(dims) // 2 or freqs.device != positions.device:
         raise ValueError("contiguous fp32 frequencies, one for two channels, and int32 positions, on one device")
     rotation = PyrRotation(_ptr(freqs), _ptr(positions), int(dims), int(bool(interleaved)))
     rotation.tensors = (freqs, positions)
+    if rotation.dims != 0:
+        rotation.rows = positions.numel()
     return rotation
 
 
@@ -453,6 +456,8 @@ def cache8_fork(cache, parents, children, n, status, stream=None):
 # 0.3 us less of the host's 1.8 to 2.6 in front of a launch.
 def cache8_append(cache, k, v, k_stride, v_stride, n_rows, row_idx, n_list, offsets, slots, start, n, max_new, rotation=None, q=None, q_stride=0,
                   n_q_heads=0, q_out=None, stream=None):
+    if rotation is not None and rotation.rows < n_rows:
+        raise ValueError(f"{rotation.rows} positions for {n_rows} rows")
     status = load().pyr_cache8_append(
         ctypes.byref(cache), k.data_ptr(), v.data_ptr(), k_stride, v_stride, n_rows, None if row_idx is None else row_idx.data_ptr(), n_list, offsets.data_ptr(),
         slots.data_ptr(), start.data_ptr(), n, max_new, None if rotation is None else ctypes.byref(rotation), None if q is None else q.data_ptr(), q_stride, n_q_heads,

@@ -102,6 +102,28 @@ def test_tensors_that_do_not_belong_together():
             binding.make_rotation(*bad)
 
 
+def test_rows_without_a_position():
+    """A rotation that is kept from a smaller batch: its positions would be read behind their end."""
+    import torch
+
+    class Stream:
+        cuda_stream = None
+    rows, ints, freqs, positions = torch.zeros((9, 4, 128), dtype=torch.bfloat16), torch.zeros(9, dtype=torch.int32), torch.zeros(64), torch.zeros(7, dtype=torch.int32)
+
+    def append(n_rows, rotation):                                                        # (of no sequences: nothing is launched)
+        binding.cache8_append(cache(), rows, rows, 0, 0, n_rows, None, n_rows, ints, ints, ints, 0, 9, rotation, stream=Stream)
+    for pairs in (False, True):
+        rotation = binding.make_rotation(freqs, positions, 128, pairs)
+        append(7, rotation)
+        append(0, rotation)
+        for n_rows in (8, 9):
+            with pytest.raises(ValueError):
+                append(n_rows, rotation)
+    append(9, binding.make_rotation(freqs, positions, 0))                                # nothing turns: none is read
+    append(9, binding.PyrRotation(0x1000, 0x2000, 64, 0))                                # addresses: the caller's to know
+    append(9, None)
+
+
 def test_choices_that_one_launch_cannot_make():
     """A launch has fewer than 2^32 threads: 2^24 workgroups of up to four wavefronts, half of them of eight."""
     few, many = cache(n_kv_heads=1, max_pages=128), cache(n_kv_heads=1, max_pages=1024)
