@@ -30,13 +30,18 @@ class PyrLaunches(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("attention_chunk", "attention_units", "stats_order", "window_order", "sums", "select_split")]
 
 
-class PyrCache(ctypes.Structure):
+class PyrPool(ctypes.Structure):
+    """What handing out and giving back pages takes, of either cache."""
     _fields_ = [(n, ctypes.c_void_p) for n in ("pages", "refs", "table", "lens")] + [(n, ctypes.c_int32) for n in (
         "n_pages", "page_tokens", "n_slots", "max_pages", "n_kv_heads", "head_dim")]
 
 
+class PyrCache(PyrPool):
+    """A cache held in 4 bits: ctypes refuses another pool for it, whose pages lie otherwise."""
+
+
 class PyrCache8(ctypes.Structure):
-    _fields_ = [("pool", PyrCache)]
+    _fields_ = [("pool", PyrPool)]
 
 
 class PyrRotation(ctypes.Structure):
@@ -87,9 +92,9 @@ _SIGNATURES = {
     "pyr_diag_layer": (ctypes.c_int, [ctypes.POINTER(PyrShape), _VP, _I32, _I32, _I32, ctypes.POINTER(_I32)]),
     "pyr_diag_update": (ctypes.c_int, [ctypes.POINTER(PyrShape), _VP, _I32, _I32, _I32, ctypes.POINTER(_I32)]),
     "pyr_cache_page_bytes": (ctypes.c_int, [ctypes.POINTER(PyrCache), ctypes.POINTER(_SZ)]),
-    "pyr_cache_reserve": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _VP, _VP, _VP]),
+    "pyr_cache_reserve": (ctypes.c_int, [ctypes.POINTER(PyrPool), _VP, _VP, _I32, _VP, _VP, _VP]),
     "pyr_cache_fork": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _VP, _VP]),
-    "pyr_cache_release": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _I32, _VP]),
+    "pyr_cache_release": (ctypes.c_int, [ctypes.POINTER(PyrPool), _VP, _I32, _VP]),
     "pyr_cache_compact_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(PyrCache), _I32, ctypes.POINTER(_SZ)]),
     "pyr_cache_compact": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _I32, _VP, _I32, _VP, _VP, _I32, _VP, _VP, _SZ, _VP]),
     "pyr_cache_store": (ctypes.c_int, [ctypes.POINTER(PyrCache), _VP, _VP, _I32, _VP, _I32, _VP, _VP, _VP, _I32, _I32, _VP]),
@@ -423,8 +428,8 @@ def make_cache8(pages, refs, table, lens, page_tokens: int, n_kv_heads: int, hea
             (refs.dim(), table.dim(), lens.dim()) != (1, 2, 1) or lens.shape[0] != table.shape[0] or \
             pages.numel() * pages.element_size() < refs.shape[0] * cache8_page_bytes(page_tokens, n_kv_heads, head_dim):
         raise ValueError("contiguous pages and int32 refs, table and lens of one cache, on one device")
-    cache = PyrCache8(PyrCache(_ptr(pages), _ptr(refs), _ptr(table), _ptr(lens), refs.shape[0], int(page_tokens), table.shape[0], table.shape[1],
-                               int(n_kv_heads), int(head_dim)))
+    cache = PyrCache8(PyrPool(_ptr(pages), _ptr(refs), _ptr(table), _ptr(lens), refs.shape[0], int(page_tokens), table.shape[0], table.shape[1],
+                              int(n_kv_heads), int(head_dim)))
     cache.tensors = (pages, refs, table, lens)
     return cache
 
@@ -443,7 +448,7 @@ def make_rotation(freqs, positions, dims: int, interleaved: bool = False) -> Pyr
 
 
 def cache8_page_bytes(page_tokens: int, n_kv_heads: int, head_dim: int) -> int:
-    out, cache = _SZ(0), PyrCache8(PyrCache(page_tokens=int(page_tokens), n_kv_heads=int(n_kv_heads), head_dim=int(head_dim)))
+    out, cache = _SZ(0), PyrCache8(PyrPool(page_tokens=int(page_tokens), n_kv_heads=int(n_kv_heads), head_dim=int(head_dim)))
     _check(load().pyr_cache8_page_bytes(ctypes.byref(cache), ctypes.byref(out)), "pyr_cache8_page_bytes")
     return int(out.value)
 

@@ -84,6 +84,28 @@ def test_descriptions_do_not_mix():
     binding.cache_release(cache().pool, None, 0, Stream)
 
 
+def test_pages_of_8_bits_are_none_of_4():
+    """What writes or reads numbers of 4 bits refuses the pool of a cache held in 8, before anything is launched; handing out and giving back its pages takes both."""
+    class Stream:
+        cuda_stream = None
+    pool = cache().pool
+    for call_4 in (lambda c: binding.cache_store(c, None, None, 0, None, 0, None, None, None, 0, 0, Stream),
+                   lambda c: binding.cache_load(c, None, None, 0, 0, None, None, 0, Stream),
+                   lambda c: binding.cache_fork(c, None, None, 0, None, Stream),
+                   lambda c: binding.cache_compact(c, None, 0, None, 0, None, None, 0, None, None, 0, Stream),
+                   lambda c: binding.cache_attention(c, None, None, 0, 1, 4, 0, 0.0, None, None, None, 0, Stream),
+                   lambda c: binding.cache_compact_workspace_bytes(c, 1), lambda c: binding.cache_attention_workspace_bytes(c, 1, 1, 4, 64),
+                   lambda c: binding.diag_cache_attention(c, 1, 1, 4, 64)):
+        with pytest.raises(ctypes.ArgumentError):
+            call_4(pool)
+    four = binding.PyrCache(0x10000, 0x20000, 0x30000, 0x40000, 100, 64, 8, 16, 4, 128)
+    for c in (pool, four):
+        binding.cache_release(c, None, 0, Stream)
+        with pytest.raises(binding.PyrError):
+            binding.cache_reserve(c, None, None, 0, None, None, Stream)                  # (no status: refused by the library itself)
+    assert (pool.n_pages, pool.page_tokens, pool.n_kv_heads) == (four.n_pages, four.page_tokens, four.n_kv_heads)
+
+
 def test_tensors_that_do_not_belong_together():
     import torch
     size = binding.cache8_page_bytes(32, 2, 64)
