@@ -536,7 +536,7 @@ PYR_API int pyr_cache8_load(const pyr_cache8* cache, const int32_t* slots, const
  *   n_first, n_best    0 or more;  n_recent  1 or more
  *   blocks             dev int32 [n, n_tokens, Hkv, n_first + n_recent + n_best], written: ascending, -1 behind the last
  *   workspace          dev, >= pyr_cache8_select_workspace_bytes(), 256-byte aligned; not read where that is 0
- * One launch, or two where few long sequences are scored.
+ * One launch, or two: where few rows score many blocks, or any score more than 4096.
  */
 PYR_API int pyr_cache8_select_workspace_bytes(const pyr_cache8* cache, int32_t n, int32_t n_tokens, int32_t n_q_heads, int32_t max_len, size_t* bytes_out);
 PYR_API int pyr_cache8_select(const pyr_cache8* cache, const void* q, const int32_t* slots, int32_t n, int32_t n_tokens, int32_t n_q_heads,

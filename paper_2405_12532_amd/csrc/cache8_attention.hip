@@ -12,10 +12,10 @@
 // product costs 0 to 3 % where bytes bound, 64 x 2048 on 32 heads 162 us either way; 16 x 2048 on 64/8 heads with nine tokens, bound by instructions, 30 us for 26.5.)  P, its sum
 // and O are fp32.
 // A row's reference is its largest logit when it was last moved, and it is moved when the weights of a block add up to more than 2^12 in a lane.
-// Bound: reading the cache, past the caches: 64 x 2048 tokens on 32 heads of 128 channels in 162 us, 1077 MB at 6.6 TB/s (through the caches 182), vector
-// instructions 22 % of a SIMD's cycles and matrix instructions 10 %; 32 x 307 ... 4915 tokens on 40 heads, four tokens each, 128 us, 6.1 TB/s; lists of 16 blocks, 64 x
-// 2048, 47 us for 271 MB, 5.8 TB/s.  Three workgroups a compute unit at 128 channels spill registers (191 us).  One sequence: dependent loads and launches (1 x 16384
-// on 64/8 heads 9.9 us and 3.2 for the join).
+// Bound: reading the cache, past the caches: 64 x 2048 tokens on 32 heads of 128 channels in 162 us, 1077 MB at 6.6 TB/s (through the caches 184), vector
+// instructions 25 % of a SIMD's cycles and matrix instructions 14 %; 32 x 307 ... 4915 tokens on 40 heads, four tokens each, 129 us, 6.1 TB/s; lists of 16 blocks, 64 x
+// 2048, 47.5 us for 271 MB, 5.7 TB/s.  One sequence: dependent loads and launches (1 x 16384 on 64/8 heads 11.8 us a pass; 10.3 and 3.9 for the join in a kernel trace).
+// More than 16 rows a head: instructions too (16 x 2048 on 64/8 heads, nine tokens, vector instructions 47 % of a SIMD's cycles and matrix instructions 32 %).
 #include <float.h>
 #include <math.h>
 
@@ -360,6 +360,8 @@ void launch(const CacheAttention& x, const AttendArgs& a, dim3 blocks, hipStream
     else hipLaunchKernelGGL((cache8_attention_kernel<D, 1, 8, kListed, kOnce>), blocks, threads, 0, stream, a);
 }
 
+// Past the caches or through them, us: 64 x 2048 tokens on 32 heads 163 and 184, on 32/8 44 and 49.5, 64 x 8192 on 64/8 165 and 186.  Where sequences share all their pages, as branches of
+// one prompt do, the other way round, by less: 71 and 62.5, 18.9 and 18.3, 64 and 61 (of four prompts 80 and 65, 20.1 and 19.3, 73 and 67); the host does not know.
 template <int D>
 void launch(const CacheAttention& x, const AttendArgs& a, dim3 blocks, hipStream_t stream) {
     if (a.blocks == nullptr) launch<D, false, true>(x, a, blocks, stream);
@@ -373,12 +375,12 @@ void launch(const CacheAttention& x, const AttendArgs& a, dim3 blocks, hipStream
 // What is waited for at the end is the wavefront with the most blocks (8 KB at 128 channels), so few heads are split along the cache until a workgroup of eight wavefronts has
 // every compute unit to itself, and are taken by eight wavefronts unsplit up to one head a unit (two at 64 channels); more heads by four, two workgroups a unit.
 // Splitting takes a launch that joins the parts.  Measured, us (pass with the join; w: wavefronts, s: parts), 128 channels:
-//   heads x tokens   8 x 1000: w8 s1 8.4, w8 s4 7.7, w4 s8 7.4;  32 x 1434: w8 s1 11.4, w8 s4 9.5, w4 s8 8.9;  64 x 1200: w8 s1 10.2, w8 s4 9.9;  64 x 2048: w8 s1 14.3, w8 s4 11.1, w4 s8
-//   11.9;  96 x 1500: w8 s1 12.5, w8 s2 11.3;  128 x 1800: w8 s1 14.2, w8 s2 14.8;  128 x 4000: w8 s1 27.0, w8 s2 25.2;  160 x 1800: w8 s1 15.2, w4 s1 17.9, w4 s4 21.6;  160 x 100 ... 8000:
-//   w8 s1 46.5, w4 s4 46.4;  256 x 2000: w4 s1 23.2, w8 s1 23.6;  480 x 1800: w4 s1 37.0, w8 s1 38.8, w4 s2 42.8;  480 x 300 ... 5000: w4 s1 56.4, w4 s2 60.8;  8 x 65536: w8 s32 26.2, w4 s64 27.3
-//   64 channels: 256 x 2000: w8 s1 12.6, w4 s1 14.6;  480 x 1800: 20.7 either way;  8 x 16384: w4 s64 8.6, w8 s32 8.8
-//   more than 16 rows a head: 64 x 4096: s1 31.8, s4 19.2, s8 22.9;  128 x 2048: s1 26.3, s2 30.7
-//   lists of 64 blocks: 8 heads: w8 s8 8.2, w8 s1 13.0;  64: w8 s4 11.4, w8 s1 14.5;  256: w4 s1 23.9, w8 s1 24.4;  of 16: 2048 heads: w4 s1 45.2, w1 s1 45.3, w2 s1 47.0, w8 s1 57.1
+//   heads x tokens   8 x 1000: w8 s1 7.3, w8 s4 7.1, w4 s8 6.8;  32 x 1434: w8 s1 11.5, w8 s4 9.6, w4 s8 8.9;  64 x 1200: w8 s1 10.6, w8 s4 10.2;  64 x 2048: w8 s1 14.8, w8 s4 11.6, w4 s8
+//   12.0;  96 x 1500: w8 s1 12.8, w8 s2 11.7;  128 x 1800: w8 s1 14.6, w8 s2 15.2;  128 x 4000: w8 s1 27.3, w8 s2 26.0;  160 x 1800: w8 s1 15.4, w4 s1 17.8, w4 s4 20.6;  160 x 100 ... 8000:
+//   w8 s1 43.3, w4 s4 37.8;  256 x 2000: w4 s1 23.5, w8 s1 23.6;  480 x 1800: w4 s1 37.9, w8 s1 38.5, w4 s2 41.0;  480 x 300 ... 5000: w4 s1 65.2, w4 s2 68.1;  8 x 65536: w8 s32 26.7, w4 s64 27.8
+//   64 channels: 256 x 2000: w8 s1 13.1, w4 s1 14.9;  480 x 1800: 19.9 either way;  8 x 16384: w4 s64 9.3, w8 s32 9.1
+//   24 rows a head: 64 x 4096: s1 35.5, s4 19.5, s8 21.4;  128 x 2048: s1 21.4, s2 19.5 (by the rule s1)
+//   lists of 64 blocks: 8 heads: w8 s8 7.6, w8 s1 10.9;  64: w8 s4 11.6, w8 s1 14.9;  256: w4 s1 24.0, w8 s1 24.6;  of 16: 2048 heads: w4 s1 45.9, w8 s1 57.5
 CacheAttention plan_cache8_attention(int32_t n_seqs, int32_t n_tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int64_t max_len, int32_t n_blocks) {
     constexpr int64_t kUnits = 256;
     CacheAttention x{};

@@ -2,7 +2,7 @@
 //
 // A number is e4m3 (OCP's FP8: four exponent bits, three mantissa bits, up to 448, no infinities, 0x7f and 0xff: not a number) times a power of two,
 // 2^(byte - 127) with a byte from kLeastPower to kMostPower, one for the K and one for the V of a block: 32 tokens of a KV head.  A code keeps four
-// significant bits of every number down to 2^-14 of the block's largest, so that a channel far larger than the others does not cost them theirs, as one
+// significant bits of every number down to 2^-13.8 of the largest that its power was taken for, so that a channel far larger than the others does not cost them theirs, as one
 // step for all of them would; gfx950 converts two codes to bf16 in one instruction, power included, exactly.
 // A block keeps bounds of its K too, the largest and smallest code of every channel in whole units of 4, rounded outward (int8; +-127: not a number).
 //

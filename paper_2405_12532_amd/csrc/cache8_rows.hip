@@ -5,9 +5,9 @@
 // numbers of 64 bits, and so is the quarter of a turn that it is reduced by, so that far positions lose nothing; sine and cosine are Taylor's sums on [-pi/4, pi/4] in 64 bits too, rounded to 32.  A workgroup takes 32 tokens and some heads: the pairs are
 // worked out once, meet in LDS and turn K and Q of all its heads.
 // A wavefront owns one block (32 tokens of one KV head) of the destination, whole or in part, so no two of them write a byte.
-// Bound: reading and writing HBM, in part only: the rows that a selection keeps of 8 x 2048 tokens on 32 heads (1433 of each, K and V) go in in 52 us, 287 MB at 5.5 TB/s, vector
-// instructions 32 % of a SIMD's cycles, and come back in 44, 283 MB at 6.4 TB/s; all 2048 turned with Q 147 us, 680 MB at 4.6 TB/s, vector instructions half of the cycles; ragged
-// pieces turned with Q (7 x 100 ... 3000 on 32/8 heads of 64) 26.5 us for 110 MB, 4.2 TB/s, where loads, the block's power and stores follow one another in each
+// Bound: reading and writing HBM, in part only: the rows that a selection keeps of 8 x 2048 tokens on 32 heads (1433 of each, K and V) go in in 50.8 us, 287 MB at 5.6 TB/s, vector
+// instructions 39 % of a SIMD's cycles, and come back in 44, 283 MB at 6.4 TB/s; all 2048 turned with Q 147 us, 680 MB at 4.6 TB/s, vector instructions 55 % of the cycles; ragged
+// pieces turned with Q (7 x 100 ... 3000 on 32/8 heads of 64) 27 us for 110 MB, 4.1 TB/s, where loads, the block's power and stores follow one another in each
 // wavefront; 64 tokens of a step 7.7 us, latency; back from 64 blocks 9.
 #include "cache8_device.h"
 
@@ -249,7 +249,9 @@ __device__ __forceinline__ Piece piece_of(const AppendArgs& a, int place) {
     const int slot = cache_slot(a.c, a.slots, b);
     const int start = a.start[b], offset = a.offsets[b];
     const int64_t wanted = (int64_t)a.offsets[b + 1] - offset;
-    bool again = false;                                           // an earlier row has the slot: its block may be written by two wavefronts at once
+    // an earlier row has the slot: its block may be written by two wavefronts at once (every workgroup looks at all earlier rows: one token each of 1024 sequences on 32/8 heads turned
+    // with Q 18.9 us, of 4096 on 8/8 heads of 64 33.5)
+    bool again = false;
     for (int i = lane; i < b; i += 64) again |= a.slots[i] == slot;
     if (slot < 0 || start < 0 || wanted <= 0) return p;
     const int64_t token0 = (start & ~31) + 32 * (int64_t)(place - b * a.tiles_of_piece);
@@ -774,8 +776,9 @@ void launch_append_items(AppendArgs a, int64_t pieces, hipStream_t stream) {
     const int64_t items = 2 * a.c.n_kv_heads + a.n_q_heads, most = (items + kWaves - 1) / kWaves;
     constexpr int64_t kHeld = 256 * append_waves<D, kTurn, kShort>;      // workgroups that the chip holds
     // Items of a wavefront: two share a reckoning of the turns, more of them leave too little in flight, and few pieces need all the workgroups they can get.  Measured,
-    // us, one, two, four (before the turns lay as above): 8 x 2048 tokens on 32/32 heads 185, 145, 149; 7 x 100 ... 3000 on 32/8 68, 51, 50; the same at 64 channels 31, 25.5, 26; 64 x 64 on 32/8 37, 32, 33;
-    // 1 x 800 on 32/32 15.5, 14.1, 17.8; 16 x 200 on 8 heads 6.6, 7.6, 10.8; 64 x 9 on 40/40 20, 18, 21; 2 x 500 on 12/12 heads of 64 6.9, 8.1, 9.4
+    // us, one, two, four, turned with Q behind 77 tokens: 8 x 2048 tokens on 32/32 heads 193, 147, 149; 7 x 100 ... 3000 on 32/8 72, 52, 50; the same at 64 channels 35, 28.5, 26.5; 64 x 64 on 32/8 39, 32.6,
+    // 33.5; 1 x 800 on 32/32 18.5, 16.4, 20; 16 x 200 on 8/8 18.4, 16.8, 17.1; 64 x 9 on 40/40 21.5, 19.2, 22, on 32/8 11.5, 10.5, 13.3; 2 x 500 on 12/12 heads of 64 7.9, 8.9, 10.2; 8 x 5 on 32/8
+    // 5.5, 6.6, 8.8; 70 % of 8 x 2048 rows as they are on 32 heads 54.6, 52.7, 54.4
     const int64_t each = pieces * most > kHeld ? 2 : 1;
     a.head_groups = (int32_t)((most + each - 1) / each);
     hipLaunchKernelGGL((cache8_append_kernel<D, kTurn, kShort>), dim3((unsigned)(pieces * a.head_groups)), dim3(64 * kWaves), 0, stream, a);
