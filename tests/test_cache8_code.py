@@ -14,3 +14,9 @@ def test_arguments_and_no_spilled_registers(source, count, most):
     assert len(found) == count
     for arguments, name, scratch, spilled in found:
         assert int(arguments) <= (most if "append" in name else 112) and int(scratch) == 0 and int(spilled) == 0, name
+
+
+def test_products_of_two_take_their_constants_from_registers():
+    """An operand of -1 that is part of the instruction is one of fp32 there, not the pair of bf16 numbers that the source has."""
+    found = re.findall(r"v_dot2c?_f32_bf16\w* v\d+, (.*)", assembly("cache8_attention.hip"))
+    assert found and all(re.match(r"[sv]\d+, ", operands) for operands in found)
